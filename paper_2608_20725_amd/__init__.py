@@ -366,3 +366,10 @@ def conv_im2win_dilated(ws, w, out, N: int, C_i: int, H_i: int, W_i: int, stride
     rc = load_library().conv_im2win_dilated(_ptr(ws), _nbytes(ws), _ptr(w), _ptr(out), N, C_i, H_i, W_i, C_o,
                                             K_h, K_w, stride, dilation, _dtype_code(w.dtype), _stream(stream))
     _check(rc, "conv_im2win_dilated")
+
+
+# The sequence operators (include/im2win_seq.h), same library and conventions.
+from .seq import *  # noqa: E402,F401,F403
+from .seq import __all__ as _seq_names  # noqa: E402
+
+__all__ += _seq_names

@@ -1,0 +1,273 @@
+// What the attention kernels share: operand tiles in LDS, matrix fragments,
+// masks and the score function.
+//
+// All kernels compute score tiles with one token of the *held* side (queries
+// in the forward and dq kernels, keys in the dk/dv kernel) per lane and the
+// tokens of the *streamed* side down the registers.  In the 32x32 layout of
+// the matrix cores lane l holds column l & 31 (its held token) and, with
+// h = l >> 5, rows 8*(r/4) + 4*h + r%4 in registers r = 0 .. 15 (streamed
+// tokens).  So
+//   - a softmax row lies in one lane and its partner l ^ 32: statistics are
+//     per-lane scalars, and rescaling the output is one multiply a register;
+//   - registers 8*ks .. 8*ks+7 are, as they are, the B operand of the second
+//     product over streamed tokens 16*ks .. 16*ks+15 (a product does not
+//     depend on the order in which both operands number the summed index), so
+//     probabilities never leave the registers;
+//   - that product's A operand is the streamed tile transposed, which
+//     ds_read_tr16_b64 reads from its row-major copy.
+// The streamed tiles (64 tokens, or 32 in fp32) are shared by the workgroup's
+// four waves through LDS, in 16-byte chunks permuted within a row (swz) so
+// that both ways of reading spread over the banks.
+#pragma once
+
+#include "mfma16.hpp"
+#include "seq.hpp"
+
+namespace im2win {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+constexpr int kWaves = 4;            // waves a workgroup
+constexpr int kHeld = 32 * kWaves;   // held tokens a workgroup
+constexpr int kDocTile = 64;         // tokens a document-range record covers
+
+// Document ids of a tile of kDocTile tokens: the range of those >= 0 (lo > hi
+// when there are none) and whether the tile holds more than one value.
+struct DocRange {
+    int32_t lo, hi, mixed, pad;
+};
+
+struct AttnArgs {
+    const char *q, *k, *v, *o, *dout;
+    char *out, *dq, *dk, *dv;
+    float *lse;
+    float2 *stat;         // backward: {lse*log2(e) (+inf: no pair), dout.out} [B][H][Lq]
+    uint32_t *norms;      // backward, fp16: bits of the largest |dout_i| and |v_j| [B][H][2]
+    float *part;          // decode: partial outputs; backward: partial strip gradients
+    const float *strip;
+    const int32_t *kv_len, *prefix, *q_doc, *k_doc;
+    const DocRange *q_range, *k_range;  // [B][ceil(L / kDocTile)]
+    // byte strides
+    int64_t q_sb, q_sh, k_sb, k_sh, v_sb, v_sh, o_sb, o_sh, do_sb, do_sh, dq_sb, dq_sh, dk_sb, dk_sh, dv_sb, dv_sh;
+    int32_t q_st, k_st, v_st, o_st, do_st, dq_st, dk_st, dv_st;
+    int32_t B, Lq, Lk, H, Hkv, G, D;
+    int32_t causal, align_end, R;
+    int32_t tiles, splits;
+    float scale, cap;
+};
+
+// fp32 operands beside F16Op and BF16Op: eight 32x32x2 products, the e-th of
+// which takes element e of both fragments.
+struct F32Op {
+    typedef float v8 __attribute__((ext_vector_type(8)));
+    typedef float elem;
+    __device__ static inline f32x16_acc mfma(v8 a, v8 b, f32x16_acc c)
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+        return c;
+    }
+};
+
+template <class Op>
+struct OpInfo {
+    static constexpr int kElt = sizeof(typename Op::elem);
+    static constexpr bool kIs32 = kElt == 4;
+    // all exponent bits set: infinity or NaN
+    static constexpr uint32_t kExp = kIs32 ? 0x7f800000u : 0;
+};
+
+template <class Op>
+__device__ inline uint32_t exp_mask();
+template <>
+__device__ inline uint32_t exp_mask<F16Op>() { return 0x7c007c00u; }
+template <>
+__device__ inline uint32_t exp_mask<BF16Op>() { return 0x7f807f80u; }
+template <>
+__device__ inline uint32_t exp_mask<F32Op>() { return 0x7f800000u; }
+
+// A fragment with its infinities and NaN replaced by zeros; `bad` collects
+// whether there were any.
+template <class Op>
+__device__ inline typename Op::v8 finite(typename Op::v8 f, uint32_t &bad)
+{
+    constexpr int N = OpInfo<Op>::kIs32 ? 8 : 4;
+    typedef uint32_t U __attribute__((ext_vector_type(N)));
+    U u = __builtin_bit_cast(U, f);
+    const uint32_t m = exp_mask<Op>();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if constexpr (OpInfo<Op>::kIs32) {
+            const bool b = (u[i] & m) == m;
+            bad |= b;
+            u[i] = b ? 0u : u[i];
+        } else {
+            // exponent + its lowest bit: carries into the sign place of the
+            // half when all exponent bits are set
+            const uint32_t low = m & (~m + 0x00010001u) & 0x7fff7fffu;  // lowest exponent bit of both halves
+            const uint32_t full = ((u[i] & m) + low) & 0x80008000u;
+            bad |= full;
+            u[i] &= ~((full >> 15) * 0xffffu);
+        }
+    }
+    return __builtin_bit_cast(typename Op::v8, u);
+}
+
+template <class Op>
+__device__ inline typename Op::v8 pack8(const f32x16_acc &a, int first)
+{
+    typename Op::v8 v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        v[e] = (typename Op::elem)a[first + e];
+    return v;
+}
+
+// One streamed tile in LDS: ROWS tokens of DP channels.
+template <class Op, int DP>
+struct Tile {
+    static constexpr int kElt = OpInfo<Op>::kElt;
+    static constexpr int kRowBytes = DP * kElt;
+    static constexpr int kChunks = kRowBytes / 16;
+    static constexpr int kMask = kChunks % 8 == 0 ? 7 : 3;
+
+    // Chunk permutation of a row: any 8 consecutive rows put one chunk into 8
+    // different places (row-wise reads), and two consecutive rows put four
+    // neighbouring chunks into different halves of 128 bytes (transposed reads).
+    __device__ static inline int swz(int row)
+    {
+        return (((row & 1) << 2) | ((row >> 1) & 3)) & kMask;
+    }
+
+    // Elements 16*s + 8*h .. +7 of a row: A or B operand of step s.
+    __device__ static inline typename Op::v8 row_frag(const char *t, int row, int s, int h)
+    {
+        const char *p = t + row * kRowBytes;
+        const int z = swz(row);
+        if constexpr (kElt == 2) {
+            return *(const typename Op::v8 *)(p + (((2 * s + h) ^ z) << 4));
+        } else {
+            typedef float v4 __attribute__((ext_vector_type(4)));
+            const v4 a = *(const v4 *)(p + (((4 * s + 2 * h) ^ z) << 4));
+            const v4 b = *(const v4 *)(p + (((4 * s + 2 * h + 1) ^ z) << 4));
+            return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
+
+    // Channel d = 32*dt + (lane & 31) of the streamed tokens row0 + 4*h +
+    // {0..3, 8..11}: A operand over the transposed tile (row0 a multiple of 16).
+    __device__ static inline typename Op::v8 col_frag(const char *t, int row0, int dt, int lane)
+    {
+        const int h = lane >> 5;
+        if constexpr (kElt == 2) {
+            typedef short s4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s4 lds_s4;
+            // 16 lanes read 4 rows x 16 channels, 8 bytes each; lane a gets
+            // channel a of the four rows
+            const int a = lane & 15;
+            const int row = row0 + 4 * h + (a >> 2);
+            const int c = 4 * dt + 2 * ((lane >> 4) & 1) + ((a & 3) >> 1);
+            const char *p = t + row * kRowBytes + ((c ^ swz(row)) << 4) + (a & 1) * 8;
+            const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)p);
+            const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(p + 8 * kRowBytes));
+            typedef short s8 __attribute__((ext_vector_type(8)));
+            const s8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            return __builtin_bit_cast(typename Op::v8, v);
+        } else {
+            const int d = 32 * dt + (lane & 31);
+            typename Op::v8 v;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int row = row0 + 8 * (e >> 2) + 4 * h + (e & 3);
+                v[e] = *(const float *)(t + row * kRowBytes + (((d >> 2) ^ swz(row)) << 4) + (d & 3) * 4);
+            }
+            return v;
+        }
+    }
+
+    // Four consecutive channels of one token as fp32 (the rare path).
+    __device__ static inline void four(const char *t, int row, int d, float *f)
+    {
+        const char *p = t + row * kRowBytes + (((d * kElt >> 4) ^ swz(row)) << 4) + ((d * kElt) & 15);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            f[e] = (float)((const typename Op::elem *)p)[e];
+    }
+
+    // Copies `valid` tokens (others, and channels from D on, become zeros) of
+    // `rows` to LDS; p points to token 0 of the tile.
+    template <int ROWS>
+    __device__ static inline void stage(char *t, const char *p, int32_t stride, int valid, int D)
+    {
+#pragma unroll
+        for (int i = 0; i < ROWS * kChunks / (64 * kWaves); ++i) {
+            const int id = i * 64 * kWaves + threadIdx.x;
+            const int row = id / kChunks, c = id % kChunks;
+            u32x4 v = {0, 0, 0, 0};
+            if (row < valid && c * 16 < D * kElt)
+                v = *(const u32x4 *)(p + (int64_t)row * stride + c * 16);
+            *(u32x4 *)(t + row * kRowBytes + ((c ^ swz(row)) << 4)) = v;
+        }
+    }
+
+    // Fragments of a held token straight from memory.
+    __device__ static inline void held(typename Op::v8 (&f)[DP / 16], const char *row, bool valid, int h, int D)
+    {
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) {
+            typename Op::v8 z = {};
+            f[s] = z;
+            if (valid && 16 * s + 8 * h < D)
+                f[s] = *(const typename Op::v8 *)(row + (16 * s + 8 * h) * kElt);
+        }
+    }
+};
+
+__device__ inline int wave_min(int v)
+{
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1)
+        v = min(v, __shfl_xor(v, m));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ inline int wave_max(int v)
+{
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1)
+        v = max(v, __shfl_xor(v, m));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+
+// tanh(x) = 1 - 2/(1 + e^2x): absolute error about 1e-7, exact at both ends.
+__device__ inline float fast_tanh(float x)
+{
+    return 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * (2.0f * kLog2e)));
+}
+
+// The number of keys of sequence b, and the position of its query 0.
+__device__ inline int keys_of(const AttnArgs &a, int b)
+{
+    return a.kv_len ? min(max(a.kv_len[b], 0), a.Lk) : a.Lk;
+}
+__device__ inline int first_pos(const AttnArgs &a, int n) { return a.align_end ? n - a.Lq : 0; }
+
+// Work item of this workgroup: `tiles` items per head, consecutive ones on
+// one XCD (workgroup id mod 8), so that a head's streamed side stays in that
+// XCD's L2.  Returns the head's index, *tile the item.
+__device__ inline uint32_t work_item(uint32_t total, uint32_t tiles, uint32_t *tile)
+{
+    const uint32_t x = blockIdx.x % 8, j = blockIdx.x / 8, per = total / 8, rem = total % 8;
+    const uint32_t t = x * per + (x < rem ? x : rem) + j;
+    *tile = t % tiles;
+    return t / tiles;
+}
+
+// Bytes of AttnArgs::part a call may use.
+int64_t attn_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv, int64_t D, int64_t R,
+                        bool backward);
+hipError_t launch_attn_docs(const int32_t *doc, DocRange *out, int64_t B, int64_t L, hipStream_t st);
+hipError_t launch_attn_forward(const AttnArgs &a, int dt, hipStream_t st);
+hipError_t launch_attn_backward(const AttnArgs &a, int dt, float *dstrip, hipStream_t st);
+
+}  // namespace im2win

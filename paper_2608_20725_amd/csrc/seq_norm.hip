@@ -1,0 +1,475 @@
+// Layer norm over the channels of each row, forward and backward.
+//
+// Both are one pass over the rows: a row is held in registers (64 or 256
+// lanes, up to 64 values a lane), so its two sums (mean, then the centred
+// squares: no cancellation) cost no second read, and the backward pass keeps
+// every lane's columns of dweight and dbias in registers over all the rows
+// of its workgroup.  Rows of more values than that go through the looped
+// kernels at the end.  Memory-bound: 2 (3) elements moved a value.
+#include "seq.hpp"
+
+namespace im2win {
+namespace {
+
+constexpr int kThreads = 256;
+
+__device__ inline float wave_sum(float v)
+{
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1)
+        v += __shfl_xor(v, m);
+    return v;
+}
+
+// Sums of a and b over the row's lanes: WAVES = 1, the wave; 4, the workgroup
+// (red: 8 floats, free again on return).
+template <int WAVES>
+__device__ inline void row_sum2(float &a, float &b, float *red)
+{
+    a = wave_sum(a);
+    b = wave_sum(b);
+    if (WAVES == 1)
+        return;
+    const int w = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) {
+        red[w] = a;
+        red[4 + w] = b;
+    }
+    __syncthreads();
+    a = (red[0] + red[1]) + (red[2] + red[3]);
+    b = (red[4] + red[5]) + (red[6] + red[7]);
+    __syncthreads();
+}
+
+// VEC values from p (aligned to VEC elements when VEC > 1) as fp32.
+template <class E, int VEC>
+__device__ inline void load(const typename E::T *p, float *f)
+{
+    typedef typename E::T V __attribute__((ext_vector_type(VEC)));
+    if constexpr (VEC == 1) {
+        f[0] = E::get(*p);
+    } else {
+        const V v = *(const V *)p;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            f[e] = E::get(v[e]);
+    }
+}
+
+template <class E, int VEC>
+__device__ inline void store(typename E::T *p, const float *f)
+{
+    typedef typename E::T V __attribute__((ext_vector_type(VEC)));
+    if constexpr (VEC == 1) {
+        *p = E::put(f[0]);
+    } else {
+        V v;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            v[e] = E::put(f[e]);
+        *(V *)p = v;
+    }
+}
+
+// A row of C <= WAVES*64*NV*VEC values: vector i of a lane starts at column
+// (i*WAVES*64 + lane)*VEC.  C is a multiple of VEC.
+template <class E, class W, int VEC, int NV, int WAVES>
+__global__ __launch_bounds__(kThreads) void norm_fwd(const typename E::T *x,
+                                                     const typename W::T *__restrict__ w,
+                                                     const typename W::T *__restrict__ b, typename E::T *y,
+                                                     float *__restrict__ mean, float *__restrict__ rstd, int64_t rows,
+                                                     int32_t C, int64_t xs, float eps)
+{
+    __shared__ float red[8];
+    constexpr int kRows = 4 / WAVES;
+    const int lane = WAVES == 1 ? (threadIdx.x & 63) : threadIdx.x;
+    const float inv = 1.0f / (float)C;
+    float wv[NV][VEC], bv[NV][VEC];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * WAVES * 64 + lane) * VEC;
+        if (c < C) {
+            load<W, VEC>(w + c, wv[i]);
+            load<W, VEC>(b + c, bv[i]);
+        }
+    }
+    for (int64_t r = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? threadIdx.x >> 6 : 0); r < rows;
+         r += (int64_t)gridDim.x * kRows) {
+        float v[NV][VEC];
+        float s = 0, q = 0, unused = 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * WAVES * 64 + lane) * VEC;
+            if (c < C)
+                load<E, VEC>(x + r * xs + c, v[i]);
+            else
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    v[i][e] = 0;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                s += v[i][e];
+        }
+        row_sum2<WAVES>(s, unused, red);
+        const float mu = s * inv;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const bool in = (i * WAVES * 64 + lane) * VEC < C;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                v[i][e] -= mu;
+                q += in ? v[i][e] * v[i][e] : 0.0f;
+            }
+        }
+        row_sum2<WAVES>(q, unused, red);
+        const float rs = 1.0f / sqrtf(q * inv + eps);
+        if (lane == 0) {
+            mean[r] = mu;
+            rstd[r] = rs;
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * WAVES * 64 + lane) * VEC;
+            if (c < C) {
+                float o[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    o[e] = v[i][e] * rs * wv[i][e] + bv[i][e];
+                store<E, VEC>(y + r * C + c, o);
+            }
+        }
+    }
+}
+
+template <class E, class W, int VEC, int NV, int WAVES>
+__global__ __launch_bounds__(kThreads) void norm_bwd(const typename E::T *__restrict__ dy,
+                                                     const typename E::T *__restrict__ x,
+                                                     const typename W::T *__restrict__ w,
+                                                     const float *__restrict__ mean, const float *__restrict__ rstd,
+                                                     typename E::T *__restrict__ dx, float *__restrict__ part,
+                                                     int64_t rows, int32_t C, int64_t dys, int64_t xs)
+{
+    __shared__ float red[8];
+    extern __shared__ float cols[];  // WAVES = 1: [2][C]
+    constexpr int kRows = 4 / WAVES;
+    const int lane = WAVES == 1 ? (threadIdx.x & 63) : threadIdx.x;
+    const float inv = 1.0f / (float)C;
+    float wv[NV][VEC], aw[NV][VEC], ab[NV][VEC];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * WAVES * 64 + lane) * VEC;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            wv[i][e] = aw[i][e] = ab[i][e] = 0;
+        if (c < C)
+            load<W, VEC>(w + c, wv[i]);
+    }
+    for (int64_t r = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? threadIdx.x >> 6 : 0); r < rows;
+         r += (int64_t)gridDim.x * kRows) {
+        const float mu = mean[r], rs = rstd[r];
+        float g[NV][VEC], h[NV][VEC];
+        float s1 = 0, s2 = 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * WAVES * 64 + lane) * VEC;
+            if (c < C) {
+                load<E, VEC>(dy + r * dys + c, g[i]);
+                load<E, VEC>(x + r * xs + c, h[i]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    g[i][e] = 0, h[i][e] = mu;
+            }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                h[i][e] = (h[i][e] - mu) * rs;
+                aw[i][e] += g[i][e] * h[i][e];
+                ab[i][e] += g[i][e];
+                g[i][e] *= wv[i][e];
+                s1 += g[i][e];
+                s2 += g[i][e] * h[i][e];
+            }
+        }
+        row_sum2<WAVES>(s1, s2, red);
+        s1 *= inv;
+        s2 *= inv;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * WAVES * 64 + lane) * VEC;
+            if (c < C) {
+                float o[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    o[e] = rs * (g[i][e] - s1 - h[i][e] * s2);
+                store<E, VEC>(dx + r * C + c, o);
+            }
+        }
+    }
+    // this workgroup's [2][C] sums: one wave after the other adds its own
+    float *out = part + (int64_t)blockIdx.x * 2 * C;
+    if (WAVES == 1) {
+        for (int k = 0; k < 4; ++k) {
+            if ((int)(threadIdx.x >> 6) == k)
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const int c = (i * 64 + lane) * VEC;
+                    if (c < C)
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) {
+                            cols[c + e] = (k ? cols[c + e] : 0.0f) + aw[i][e];
+                            cols[C + c + e] = (k ? cols[C + c + e] : 0.0f) + ab[i][e];
+                        }
+                }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < 2 * C; c += kThreads)
+            out[c] = cols[c];
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * WAVES * 64 + lane) * VEC;
+            if (c < C)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    out[c + e] = aw[i][e];
+                    out[C + c + e] = ab[i][e];
+                }
+        }
+    }
+}
+
+// Rows of any length, one workgroup a row: every pass reads the row again
+// (from L2).  Rows that fit no register instance only.
+template <class E, class W>
+__global__ __launch_bounds__(kThreads) void norm_fwd_long(const typename E::T *x, const typename W::T *__restrict__ w,
+                                                          const typename W::T *__restrict__ b, typename E::T *y,
+                                                          float *__restrict__ mean, float *__restrict__ rstd,
+                                                          int64_t rows, int32_t C, int64_t xs, float eps)
+{
+    __shared__ float red[8];
+    const float inv = 1.0f / (float)C;
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        float s = 0, q = 0, unused = 0;
+        for (int c = threadIdx.x; c < C; c += kThreads)
+            s += E::get(x[r * xs + c]);
+        row_sum2<4>(s, unused, red);
+        const float mu = s * inv;
+        for (int c = threadIdx.x; c < C; c += kThreads) {
+            const float d = E::get(x[r * xs + c]) - mu;
+            q += d * d;
+        }
+        row_sum2<4>(q, unused, red);
+        const float rs = 1.0f / sqrtf(q * inv + eps);
+        if (threadIdx.x == 0) {
+            mean[r] = mu;
+            rstd[r] = rs;
+        }
+        for (int c = threadIdx.x; c < C; c += kThreads)
+            y[r * C + c] = E::put((E::get(x[r * xs + c]) - mu) * rs * W::get(w[c]) + W::get(b[c]));
+    }
+}
+
+template <class E, class W>
+__global__ __launch_bounds__(kThreads) void norm_bwd_long(const typename E::T *__restrict__ dy,
+                                                          const typename E::T *__restrict__ x,
+                                                          const typename W::T *__restrict__ w,
+                                                          const float *__restrict__ mean,
+                                                          const float *__restrict__ rstd, typename E::T *__restrict__ dx,
+                                                          int64_t rows, int32_t C, int64_t dys, int64_t xs)
+{
+    __shared__ float red[8];
+    const float inv = 1.0f / (float)C;
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        const float mu = mean[r], rs = rstd[r];
+        float s1 = 0, s2 = 0;
+        for (int c = threadIdx.x; c < C; c += kThreads) {
+            const float g = E::get(dy[r * dys + c]) * W::get(w[c]);
+            s1 += g;
+            s2 += g * (E::get(x[r * xs + c]) - mu) * rs;
+        }
+        row_sum2<4>(s1, s2, red);
+        for (int c = threadIdx.x; c < C; c += kThreads) {
+            const float g = E::get(dy[r * dys + c]) * W::get(w[c]), h = (E::get(x[r * xs + c]) - mu) * rs;
+            dx[r * C + c] = E::put(rs * (g - s1 * inv - h * s2 * inv));
+        }
+    }
+}
+
+// dweight and dbias of long rows: a lane sums one column over every
+// gridDim.y-th row.
+template <class E>
+__global__ __launch_bounds__(kThreads) void norm_cols_long(const typename E::T *__restrict__ dy,
+                                                           const typename E::T *__restrict__ x,
+                                                           const float *__restrict__ mean,
+                                                           const float *__restrict__ rstd, float *__restrict__ part,
+                                                           int64_t rows, int32_t C, int64_t dys, int64_t xs)
+{
+    const int c = blockIdx.x * kThreads + threadIdx.x;
+    if (c >= C)
+        return;
+    float aw = 0, ab = 0;
+    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
+        const float g = E::get(dy[r * dys + c]);
+        aw += g * (E::get(x[r * xs + c]) - mean[r]) * rstd[r];
+        ab += g;
+    }
+    float *out = part + (int64_t)blockIdx.y * 2 * C;
+    out[c] = aw;
+    out[C + c] = ab;
+}
+
+// Sums the partial rows: 32 columns a workgroup, each by 32 lanes that take
+// every 32nd partial row, joined in a fixed order.
+template <class W>
+__global__ __launch_bounds__(1024) void norm_reduce(const float *__restrict__ part, typename W::T *__restrict__ dw,
+                                                    typename W::T *__restrict__ db, int32_t n, int32_t C)
+{
+    __shared__ float s[32][33];
+    const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + cx;
+    float a = 0;
+    if (c < 2 * (int64_t)C)
+        for (int64_t r = ry; r < n; r += 32)
+            a += part[r * 2 * C + c];
+    s[ry][cx] = a;
+    __syncthreads();
+    if (ry == 0 && c < 2 * (int64_t)C) {
+        a = 0;
+#pragma unroll
+        for (int k = 0; k < 32; ++k)
+            a += s[k][cx];
+        if (c < C)
+            dw[c] = W::put(a);
+        else
+            db[c - C] = W::put(a);
+    }
+}
+
+struct Args {
+    const void *dy, *x, *w, *b;
+    void *y;  // y or dx
+    float *mean, *rstd;
+    float *part;
+    int64_t rows, C, dys, xs;
+    float eps;
+    hipStream_t st;
+};
+
+template <class E, class W, int VEC, int NV, int WAVES>
+void run(const Args &a, bool bwd)
+{
+    typedef typename E::T T;
+    typedef typename W::T U;
+    const int64_t rows_wg = 4 / WAVES;
+    if (!bwd) {
+        const int64_t want = (a.rows + rows_wg - 1) / rows_wg;
+        const int64_t grid = want < 4096 ? want : 4096;
+        norm_fwd<E, W, VEC, NV, WAVES><<<(uint32_t)grid, kThreads, 0, a.st>>>(
+            (const T *)a.x, (const U *)a.w, (const U *)a.b, (T *)a.y, a.mean, a.rstd, a.rows, (int32_t)a.C, a.xs,
+            a.eps);
+    } else {
+        const size_t lds = WAVES == 1 ? (size_t)a.C * 8 : 0;
+        norm_bwd<E, W, VEC, NV, WAVES><<<(uint32_t)norm_partial_rows(a.rows, a.C), kThreads, lds, a.st>>>(
+            (const T *)a.dy, (const T *)a.x, (const U *)a.w, a.mean, a.rstd, (T *)a.y, a.part, a.rows, (int32_t)a.C,
+            a.dys, a.xs);
+    }
+}
+
+// The smallest instance that holds a row of C values read VEC at a time;
+// false when none does.
+template <class E, class W, int VEC>
+bool run_held(const Args &a, bool bwd)
+{
+    const int64_t n = (a.C + VEC - 1) / VEC;  // vectors in a row
+    constexpr int kMost = VEC == 1 ? 32 : 32 / VEC;  // vectors a lane of a 1-wave row
+    if (n <= 64)
+        run<E, W, VEC, 1, 1>(a, bwd);
+    else if (n <= 128)
+        run<E, W, VEC, 2, 1>(a, bwd);
+    else if (n <= 256)
+        run<E, W, VEC, 4, 1>(a, bwd);
+    else if (kMost >= 8 && n <= 512)
+        run<E, W, VEC, kMost >= 8 ? 8 : 1, 1>(a, bwd);
+    else if (kMost >= 16 && n <= 1024)
+        run<E, W, VEC, kMost >= 16 ? 16 : 1, 1>(a, bwd);
+    else if (n <= 512)
+        run<E, W, VEC, 2, 4>(a, bwd);
+    else if (n <= 1024)
+        run<E, W, VEC, 4, 4>(a, bwd);
+    else if (VEC <= 4 && n <= 2048)
+        run<E, W, VEC, VEC <= 4 ? 8 : 1, 4>(a, bwd);
+    else if (VEC == 1 && n <= 8192)
+        run<E, W, VEC, VEC == 1 ? 32 : 1, 4>(a, bwd);
+    else
+        return false;
+    return true;
+}
+
+template <class E, class W>
+void run_typed(const Args &a, bool bwd, void *dw, void *db)
+{
+    typedef typename E::T T;
+    typedef typename W::T U;
+    constexpr int VEC = 16 / sizeof(T);
+    // 16-byte loads where every row and the parameters allow them
+    const uintptr_t p = (uintptr_t)a.x | (uintptr_t)a.y | (uintptr_t)a.w | (uintptr_t)a.b | (uintptr_t)a.dy;
+    const bool vec = (p & 15) == 0 && a.C % VEC == 0 && a.xs % VEC == 0 && a.dys % VEC == 0;
+    const int32_t C = (int32_t)a.C;
+    const int64_t grid = a.rows < 8192 ? a.rows : 8192;
+    if (!(vec ? run_held<E, W, VEC>(a, bwd) : run_held<E, W, 1>(a, bwd))) {
+        if (!bwd) {
+            norm_fwd_long<E, W><<<(uint32_t)grid, kThreads, 0, a.st>>>((const T *)a.x, (const U *)a.w, (const U *)a.b,
+                                                                       (T *)a.y, a.mean, a.rstd, a.rows, C, a.xs,
+                                                                       a.eps);
+        } else {
+            norm_bwd_long<E, W><<<(uint32_t)grid, kThreads, 0, a.st>>>((const T *)a.dy, (const T *)a.x,
+                                                                       (const U *)a.w, a.mean, a.rstd, (T *)a.y,
+                                                                       a.rows, C, a.dys, a.xs);
+            const dim3 g((uint32_t)((a.C + kThreads - 1) / kThreads), (uint32_t)norm_partial_rows(a.rows, a.C));
+            norm_cols_long<E><<<g, kThreads, 0, a.st>>>((const T *)a.dy, (const T *)a.x, a.mean, a.rstd, a.part, a.rows,
+                                                        C, a.dys, a.xs);
+        }
+    }
+    if (bwd)
+        norm_reduce<W><<<(uint32_t)((2 * a.C + 31) / 32), 1024, 0, a.st>>>(
+            a.part, (U *)dw, (U *)db, (int32_t)norm_partial_rows(a.rows, a.C), C);
+}
+
+hipError_t run_any(const Args &a, bool bwd, int dt, int wdt, void *dw, void *db)
+{
+    if (dt == IM2WIN_F32)
+        run_typed<EltF32, EltF32>(a, bwd, dw, db);
+    else if (dt == IM2WIN_F16)
+        wdt == IM2WIN_F32 ? run_typed<EltF16, EltF32>(a, bwd, dw, db) : run_typed<EltF16, EltF16>(a, bwd, dw, db);
+    else
+        wdt == IM2WIN_F32 ? run_typed<EltBF16, EltF32>(a, bwd, dw, db) : run_typed<EltBF16, EltBF16>(a, bwd, dw, db);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t norm_partial_rows(int64_t rows, int64_t C)
+{
+    (void)C;
+    // enough workgroups to fill 256 CUs, and at least 32 rows for each
+    const int64_t n = (rows + 31) / 32;
+    return n < 1 ? 1 : n > 1024 ? 1024 : n;
+}
+
+hipError_t launch_norm_forward(const void *x, const void *w, const void *b, void *y, float *mean, float *rstd,
+                               int64_t rows, int64_t C, int64_t x_stride, float eps, int dt, int wdt, hipStream_t st)
+{
+    const Args a{nullptr, x, w, b, y, mean, rstd, nullptr, rows, C, 0, x_stride, eps, st};
+    return run_any(a, false, dt, wdt, nullptr, nullptr);
+}
+
+hipError_t launch_norm_backward(const void *dy, const void *x, const void *w, const float *mean, const float *rstd,
+                                void *dx, void *dw, void *db, float *part, int64_t rows, int64_t C, int64_t dy_stride,
+                                int64_t x_stride, int dt, int wdt, hipStream_t st)
+{
+    const Args a{dy,   x,    w, nullptr, dx,        const_cast<float *>(mean), const_cast<float *>(rstd),
+                 part, rows, C, dy_stride, x_stride, 0.0f,                      st};
+    return run_any(a, true, dt, wdt, dw, db);
+}
+
+}  // namespace im2win
