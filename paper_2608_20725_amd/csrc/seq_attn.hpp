@@ -52,7 +52,7 @@ struct AttnArgs {
     int32_t q_st, k_st, v_st, o_st, do_st, dq_st, dk_st, dv_st;
     int32_t B, Lq, Lk, H, Hkv, G, D;
     int32_t causal, align_end, R;
-    int32_t tiles, splits;
+    int32_t tiles, splits, chunk;  // held tiles of a head; decode: key chunks, keys in each
     float scale, cap;
 };
 
@@ -195,6 +195,24 @@ struct Tile {
             f[e] = (float)((const typename Op::elem *)p)[e];
     }
 
+    // Starts the copy of a tile to LDS by wave `wave` of NW: `valid` tokens from
+    // p on (the others, and channels from D on, become zeros).  The loads
+    // write LDS in lane order, so the chunk permutation is applied to the
+    // addresses.
+    template <int ROWS, int NW>
+    __device__ static inline void dma(char *t, const char *p, int32_t stride, int valid, int D, int wave, int lane)
+    {
+        typedef __attribute__((address_space(3))) void *lds_ptr;
+        const __amdgpu_buffer_rsrc_t rs = make_rsrc(p, kMaxRecords);
+#pragma unroll
+        for (int i = 0; i < ROWS * kChunks / (64 * NW); ++i) {
+            const int id = (wave + NW * i) * 64 + lane;
+            const int row = id / kChunks, c = (id % kChunks) ^ swz(row);
+            const uint32_t off = row < valid && c * 16 < D * kElt ? (uint32_t)(row * stride + c * 16) : kOOB;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(t + (wave + NW * i) * 1024), 16, off, 0, 0, 0);
+        }
+    }
+
     // Copies `valid` tokens (others, and channels from D on, become zeros) of
     // `rows` to LDS; p points to token 0 of the tile.
     template <int ROWS>
@@ -245,6 +263,215 @@ __device__ inline float fast_tanh(float x)
     return 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * (2.0f * kLog2e)));
 }
 
+// Both lanes of a pair (l, l ^ 32) get the larger of their values.
+__device__ inline float pair_max(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// Row of register r of a 32x32 result, + 4*h.
+__device__ constexpr int reg_row(int r) { return 8 * (r >> 2) + (r & 3); }
+
+// How products q.k become scores (in units of ln 2): c2*tanh(x*c1) when
+// capped, x*c1 else, plus the bias.
+struct ScoreArgs {
+    float c1, c2;
+    bool cap;
+};
+__device__ inline ScoreArgs score_args(const AttnArgs &a)
+{
+    return ScoreArgs{a.cap > 0 ? a.scale / a.cap : a.scale * kLog2e, a.cap * kLog2e, a.cap > 0};
+}
+
+// A query's running softmax: output sums, maximum (of the pair), sum (of this
+// lane's keys), both times 2^kShift.
+template <class Op, int DP>
+struct RowState {
+    // fp16 keeps 5 exponent bits: its probabilities are multiplied by 2^14, so
+    // that those of long rows stay normal numbers.  The maximum is raised only
+    // when a score passes it by kSlack, so they stay below 2^15.
+    static constexpr bool kIs16 = __is_same(Op, F16Op);
+    static constexpr float kShift = kIs16 ? 14.0f : 0.0f;
+    static constexpr float kSlack = kIs16 ? 1.0f : 8.0f;
+    f32x16_acc o[DP / 32];
+    float m, l;
+
+    __device__ inline void clear()
+    {
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                o[t][r] = 0;
+        m = -INFINITY;
+        l = 0;
+    }
+    __device__ inline void rescale(float f)
+    {
+        l *= f;
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                o[t][r] *= f;
+    }
+};
+
+// What the queries of a wave and one tile of keys have to do with each other
+// (uniform but for lim, doc and far).
+struct TilePairs {
+    int k0;            // first key
+    bool partial;      // some pairs are left out
+    bool docs_differ;  // .. by documents
+    bool near;         // the bias differs within the tile
+    float far;         // the bias where it does not
+    int lim, doc;      // this lane's query: keys below lim, its document
+    const int *kdoc;   // documents of the tile's keys
+};
+
+// One tile of 32*SUB keys: s = K q, the softmax's update, o += V^T p.
+// near(t, r): bias of key 32*t + reg_row(r) + 4*h of the tile.
+template <class Op, int DP, int SUB, class Near>
+__device__ inline void attend(const char *tk, const char *tv, const typename Op::v8 (&q)[DP / 16], RowState<Op, DP> &st,
+                              const ScoreArgs &sc, const TilePairs &tp, int lane, Near near)
+{
+    typedef Tile<Op, DP> T;
+    typedef RowState<Op, DP> S;
+    const int h = lane >> 5;
+    f32x16_acc s[SUB];
+#pragma unroll
+    for (int t = 0; t < SUB; ++t) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            s[t][r] = 0;
+#pragma unroll
+        for (int x = 0; x < DP / 16; ++x)
+            s[t] = Op::mfma(T::row_frag(tk, 32 * t + (lane & 31), x, h), q[x], s[t]);
+    }
+    float mul = sc.c1, add = tp.far;
+    if (sc.cap || tp.near || tp.partial || !(sc.c1 > 0)) {
+        // scores one by one; else the maximum is taken of the products and
+        // one fused multiply-add scales a score and subtracts the maximum
+        if (sc.cap) {
+#pragma unroll
+            for (int t = 0; t < SUB; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    s[t][r] = fmaf(sc.c2, fast_tanh(s[t][r] * sc.c1), tp.far);
+        } else {
+#pragma unroll
+            for (int t = 0; t < SUB; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    s[t][r] = fmaf(s[t][r], sc.c1, tp.far);
+        }
+        if (tp.near)
+#pragma unroll
+            for (int t = 0; t < SUB; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    s[t][r] += near(t, r);
+        if (tp.partial) {
+            const int last = tp.lim - tp.k0 - 4 * h;
+#pragma unroll
+            for (int t = 0; t < SUB; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    s[t][r] = 32 * t + reg_row(r) < last ? s[t][r] : -INFINITY;
+            if (tp.docs_differ)
+#pragma unroll
+                for (int t = 0; t < SUB; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        s[t][r] = tp.kdoc[32 * t + reg_row(r) + 4 * h] == tp.doc ? s[t][r] : -INFINITY;
+        }
+        mul = 1.0f;
+        add = 0.0f;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int t = 0; t < SUB; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            top = fmaxf(top, s[t][r]);
+    top = pair_max(fmaf(top, mul, add));
+    if (__any(top > st.m + S::kSlack)) {
+        // each row by its own scores alone: what a row gives does not depend
+        // on the rows beside it
+        const bool up = top > st.m + S::kSlack;
+        st.rescale(up ? __builtin_amdgcn_exp2f(st.m - top) : 1.0f);
+        st.m = up ? top : st.m;
+    }
+    const float sub = add - (st.m == -INFINITY ? 0.0f : st.m) + S::kShift;
+#pragma unroll
+    for (int t = 0; t < SUB; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], mul, sub));
+            st.l += s[t][r];
+        }
+    uint32_t bad = 0;
+#pragma unroll
+    for (int t = 0; t < SUB; ++t)
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            const typename Op::v8 p = pack8<Op>(s[t], 8 * ks);
+#pragma unroll
+            for (int dt = 0; dt < DP / 32; ++dt) {
+                typename Op::v8 v = T::col_frag(tv, 32 * t + 16 * ks, dt, lane);
+                if (tp.partial)  // a value of a left-out pair times its zero must stay zero
+                    v = finite<Op>(v, bad);
+                st.o[dt] = Op::mfma(v, p, st.o[dt]);
+            }
+        }
+    if (tp.partial && __any(bad)) {
+        // values that are not finite reach the queries that see them
+        for (int kk = 0; kk < 32 * SUB; ++kk) {
+            if (tp.k0 + kk >= tp.lim || (tp.docs_differ && tp.kdoc[kk] != tp.doc))
+                continue;
+#pragma unroll
+            for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    float f[4];
+                    T::four(tv, kk, 32 * dt + 8 * g + 4 * h, f);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        st.o[dt][4 * g + e] += fabsf(f[e]) < INFINITY ? 0.0f : f[e];
+                }
+        }
+    }
+}
+
+// Writes a held token's result times f: channels down the registers of its
+// lane pair.
+template <class Op, int DP>
+__device__ inline void store_row(char *p, const f32x16_acc (&g)[DP / 32], float f, int h, int D)
+{
+#pragma unroll
+    for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int d = 32 * dt + 8 * q + 4 * h;
+            if (d < D) {
+                typedef typename Op::elem V __attribute__((ext_vector_type(4)));
+                V v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[e] = (typename Op::elem)(g[dt][4 * q + e] * f);
+                *(V *)(p + d * sizeof(typename Op::elem)) = v;
+            }
+        }
+}
+
+template <int N>
+__device__ inline void wait_loads()
+{
+    // s_waitcnt vmcnt(N), expcnt and lgkmcnt left alone
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+
 // The number of keys of sequence b, and the position of its query 0.
 __device__ inline int keys_of(const AttnArgs &a, int b)
 {
@@ -266,8 +493,12 @@ __device__ inline uint32_t work_item(uint32_t total, uint32_t tiles, uint32_t *t
 // Bytes of AttnArgs::part a call may use.
 int64_t attn_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv, int64_t D, int64_t R,
                         bool backward);
+// Few query rows: the kernel that splits the keys (seq_attn_decode.hip).
+bool attn_few_rows(int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv);
+int64_t attn_decode_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv, int64_t D);
 hipError_t launch_attn_docs(const int32_t *doc, DocRange *out, int64_t B, int64_t L, hipStream_t st);
 hipError_t launch_attn_forward(const AttnArgs &a, int dt, hipStream_t st);
+hipError_t launch_attn_decode(const AttnArgs &a, int dt, hipStream_t st);
 hipError_t launch_attn_backward(const AttnArgs &a, int dt, float *dstrip, hipStream_t st);
 
 }  // namespace im2win

@@ -315,3 +315,55 @@ def test_graph():
         torch.cuda.synchronize()
         for a, b in zip(want, held):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("shape", [(1, 1, 5000, 8, 2, 64), (3, 1, 1025, 32, 1, 128), (2, 3, 700, 8, 1, 96), (2, 8, 333, 4, 1, 32),
+                                   (70, 1, 300, 8, 8, 40), (1, 32, 2111, 1, 1, 128)], ids=str)
+def test_few_rows_long_cache(shape, dtype):
+    """Single tokens (and a few) over caches that several workgroups split."""
+    B, Lq, Lk, H, Hk, D = shape
+    x, bias = draw(*shape, dtype, seed=Lk, R=50)
+    g = torch.Generator().manual_seed(3)
+    lens = torch.randint(0, Lk + 1, (B,), generator=g).to(torch.int32)
+    lens[0] = Lk
+    run(x, None, {}, backward=False)
+    run(x, bias, {"causal": True, "align_end": True, "kv_len": lens, "cap": 20.0}, backward=False)
+    doc = torch.randint(-1, 3, (B, Lk), generator=g).to(torch.int32)
+    run(x, bias, {"align_end": True, "kv_len": lens, "q_doc": doc[:, -Lq:].contiguous(), "k_doc": doc}, backward=False)
+    pre = torch.randint(0, Lk, (B,), generator=g).to(torch.int32)
+    run(x, bias, {"causal": True, "prefix": pre}, backward=False)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+def test_few_rows_masked_places(dtype):
+    """What a cache holds beyond its length, and in other documents, does not
+    reach the result."""
+    B, Lk = 3, 900
+    x, bias = draw(B, 2, Lk, 4, 2, 64, dtype, R=10)
+    lens = torch.tensor([900, 0, 415], dtype=torch.int32)
+    doc = torch.zeros((B, Lk), dtype=torch.int32)
+    doc[:, 100:150] = 2
+    o = {"kv_len": lens.cuda(), "k_doc": doc.cuda(), "q_doc": torch.zeros((B, 2), dtype=torch.int32, device="cuda")}
+    gone = (doc != 0) | (torch.arange(Lk)[None] >= lens[:, None])
+    res = []
+    for value in (0.0, math.nan, math.inf):
+        k, v = x["k"].clone(), x["v"].clone()
+        k[gone] = value
+        v[gone] = value
+        res.append(pkg.seq_attention_forward(x["q"].cuda(), k.cuda(), v.cuda(), bias=bias.cuda(), **o))
+    for other in res[1:]:
+        for a, b in zip(res[0], other):
+            assert not torch.isnan(b).any() and torch.equal(a, b)
+    assert (res[0][0][1] == 0).all() and (res[0][1][1] == -math.inf).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+def test_rows_do_not_depend_on_their_batch(dtype):
+    """A sequence gives the same bits alone and among others (one chunking)."""
+    x, _ = draw(9, 200, 200, 4, 2, 64, dtype)
+    q, k, v = (x[n].cuda() for n in "qkv")
+    whole = pkg.seq_attention_forward(q, k, v, causal=True)
+    for b in (0, 4, 8):
+        one = pkg.seq_attention_forward(q[b:b + 1], k[b:b + 1], v[b:b + 1], causal=True)
+        assert torch.equal(one[0][0], whole[0][b]) and torch.equal(one[1][0], whole[1][b])
