@@ -168,7 +168,7 @@ Sizes sizes_of(const seq_attention_t *a, bool backward)
         s.k_range = pad256(a->B * ((a->Lk + kDocTile - 1) / kDocTile) * (int64_t)sizeof(DocRange));
     }
     if (backward) {
-        s.stat = pad256(a->B * a->H * a->Lq * 8);
+        s.stat = pad256(a->B * a->H * ((a->Lq + 63) / 64 * 64) * 8);
         s.norms = pad256(a->B * a->H * 8);
     }
     s.part = pad256(attn_part_bytes(a->dt, a->B, a->Lq, a->Lk, a->H, a->Hkv, a->D, a->R, backward));
@@ -198,7 +198,7 @@ AttnArgs make_args(const seq_attention_t *a)
 int place(AttnArgs *r, const seq_attention_t *a, const Sizes &s, void *ws, hipStream_t st)
 {
     char *p = (char *)ws;
-    r->stat = (float2 *)p, p += s.stat;
+    r->stat = (float *)p, p += s.stat;
     r->norms = (uint32_t *)p, p += s.norms;
     DocRange *qr = (DocRange *)p;
     p += s.q_range;

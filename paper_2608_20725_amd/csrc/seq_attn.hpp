@@ -41,7 +41,7 @@ struct AttnArgs {
     const char *q, *k, *v, *o, *dout;
     char *out, *dq, *dk, *dv;
     float *lse;
-    float2 *stat;         // backward: {lse*log2(e) (+inf: no pair), dout.out} [B][H][Lq]
+    float *stat;          // backward: [B][H][2][Lq rounded up to 64] lse*log2(e) less p_shift (+inf: no pair), dout.out
     uint32_t *norms;      // backward, fp16: bits of the largest |dout_i| and |v_j| [B][H][2]
     float *part;          // decode: partial outputs; backward: partial strip gradients
     const float *strip;
@@ -213,22 +213,6 @@ struct Tile {
         }
     }
 
-    // Copies `valid` tokens (others, and channels from D on, become zeros) of
-    // `rows` to LDS; p points to token 0 of the tile.
-    template <int ROWS>
-    __device__ static inline void stage(char *t, const char *p, int32_t stride, int valid, int D)
-    {
-#pragma unroll
-        for (int i = 0; i < ROWS * kChunks / (64 * kWaves); ++i) {
-            const int id = i * 64 * kWaves + threadIdx.x;
-            const int row = id / kChunks, c = id % kChunks;
-            u32x4 v = {0, 0, 0, 0};
-            if (row < valid && c * 16 < D * kElt)
-                v = *(const u32x4 *)(p + (int64_t)row * stride + c * 16);
-            *(u32x4 *)(t + row * kRowBytes + ((c ^ swz(row)) << 4)) = v;
-        }
-    }
-
     // Fragments of a held token straight from memory.
     __device__ static inline void held(typename Op::v8 (&f)[DP / 16], const char *row, bool valid, int h, int D)
     {
@@ -241,6 +225,15 @@ struct Tile {
         }
     }
 };
+
+// Starts the copy of 64 words to LDS by one wave; those from `valid` on become
+// zeros.
+__device__ inline void dma_words(void *t, const void *p, int valid, int lane)
+{
+    typedef __attribute__((address_space(3))) void *lds_ptr;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(p, kMaxRecords), (lds_ptr)t, 4,
+                                             lane < valid ? (uint32_t)lane * 4 : kOOB, 0, 0, 0);
+}
 
 __device__ inline int wave_min(int v)
 {
@@ -470,6 +463,39 @@ __device__ inline void wait_loads()
 {
     // s_waitcnt vmcnt(N), expcnt and lgkmcnt left alone
     __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+
+// The streamed tiles that hold a document of the workgroup's tokens: one bit
+// a tile in `bits` (LDS), 64 tiles a word, `tiles` in all.  Every wave takes
+// part; the caller's next barrier publishes them.
+__device__ inline void mark_tiles(uint64_t *bits, const DocRange *ranges, int tiles, int tokens, int lo, int hi,
+                                  int wave, int lane)
+{
+    for (int t0 = wave * 64; t0 < tiles; t0 += 64 * kWaves) {
+        bool meet = false;
+        if (t0 + lane < tiles) {
+            const DocRange r = ranges[(t0 + lane) * tokens / kDocTile];
+            meet = r.lo <= hi && r.hi >= lo;
+        }
+        const uint64_t w = __ballot(meet);
+        if (lane == 0)
+            bits[t0 >> 6] = w;
+    }
+}
+
+// The first marked tile from t on.
+__device__ inline int next_tile(const uint64_t *bits, int t, int tiles)
+{
+    while (t < tiles) {
+        const uint64_t w = bits[t >> 6] >> (t & 63);
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)w), hi = __builtin_amdgcn_readfirstlane((uint32_t)(w >> 32));
+        if (lo)
+            return t + __builtin_ctz(lo);
+        if (hi)
+            return t + 32 + __builtin_ctz(hi);
+        t = (t | 63) + 1;
+    }
+    return tiles;
 }
 
 // The number of keys of sequence b, and the position of its query 0.

@@ -19,6 +19,15 @@ namespace {
 
 constexpr int kThreads = 64 * kWaves;
 
+// Rows of statistics a head has: whole tiles.
+__host__ __device__ inline int stat_rows(int Lq) { return (Lq + 63) / 64 * 64; }
+
+// Floats of attn_dq's strip and its gradients in LDS (even: 8-byte words follow).
+__host__ __device__ inline int strip_floats(int R, int want_strip)
+{
+    return R ? ((2 * R + 1) * (want_strip ? 1 + 2 * kWaves : 1) + 1) / 2 * 2 : 0;
+}
+
 template <class Op>
 constexpr float p_shift() { return 0.0f; }
 template <>
@@ -62,46 +71,59 @@ __device__ inline float sum16(float v)
     return v;
 }
 
-// Raises *to to the largest finite value of v over the workgroup.
+// Raises *to to the largest of v over the workgroup.
 __device__ inline void raise(uint32_t *to, float v)
 {
-    v = v < INFINITY ? v : 0.0f;
+    __shared__ float w[kWaves];
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1)
         v = fmaxf(v, __shfl_xor(v, m));
     if ((threadIdx.x & 63) == 0)
-        atomicMax(to, __float_as_uint(v));  // a maximum: the same in any order
+        w[threadIdx.x >> 6] = v;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        atomicMax(to, __float_as_uint(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]))));  // the same in any order
 }
 
-// 16 lanes a row: {lse*log2(e), dout.out} and, fp16, the largest |dout|.
+constexpr int kStatRows = 64;  // rows a workgroup, 16 lanes each
+
+// {lse*log2(e) - p_shift, dout.out} and, fp16, the largest |dout| (finite ones
+// of queries that see something).
 template <class Op>
 __global__ __launch_bounds__(kThreads) void row_stats(AttnArgs a)
 {
     const uint32_t bh = blockIdx.x / a.tiles, t = blockIdx.x - bh * a.tiles;
-    const int b = bh / a.H, hq = bh - b * a.H;
-    const int i = t * (kThreads / 16) + (threadIdx.x >> 4), d = (threadIdx.x & 15) * 8;
-    float f[8], g[8], dot = 0, sq = 0;
-    if (i < a.Lq && d < a.D) {
-        load8<Op>(a.dout + b * a.do_sb + hq * a.do_sh + (int64_t)i * a.do_st + d * sizeof(typename Op::elem), f);
-        load8<Op>(a.o + b * a.o_sb + hq * a.o_sh + (int64_t)i * a.o_st + d * sizeof(typename Op::elem), g);
+    const int b = bh / a.H, hq = bh - b * a.H, d = (threadIdx.x & 15) * 8;
+    const int Lp = stat_rows(a.Lq);
+    float *const stat = a.stat + (int64_t)bh * 2 * Lp;
+    float most = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            dot += f[e] * g[e];
-            sq += f[e] * f[e];
+    for (int k = 0; k < kStatRows / 16; ++k) {
+        const int i = t * kStatRows + k * 16 + (threadIdx.x >> 4);
+        float f[8], g[8], dot = 0, sq = 0;
+        if (i < a.Lq && d < a.D) {
+            load8<Op>(a.dout + b * a.do_sb + hq * a.do_sh + (int64_t)i * a.do_st + d * sizeof(typename Op::elem), f);
+            load8<Op>(a.o + b * a.o_sb + hq * a.o_sh + (int64_t)i * a.o_st + d * sizeof(typename Op::elem), g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                dot += f[e] * g[e];
+                sq += f[e] * f[e];
+            }
+        }
+        dot = sum16(dot);
+        const float l = i < a.Lq ? a.lse[(int64_t)bh * a.Lq + i] : -INFINITY;
+        const bool some = l != -INFINITY;
+        if (d == 0) {
+            stat[i] = some ? l * kLog2e - p_shift<Op>() : INFINITY;
+            stat[Lp + i] = i < a.Lq ? dot : 0.0f;
+        }
+        if constexpr (p_shift<Op>() > 0) {
+            sq = sum16(sq);
+            most = fmaxf(most, some && sq < INFINITY ? sq : 0.0f);
         }
     }
-    dot = sum16(dot);
-    sq = sum16(sq);
-    bool some = false;
-    if (i < a.Lq) {
-        const int64_t at = (int64_t)bh * a.Lq + i;
-        const float l = a.lse[at];
-        some = l != -INFINITY;
-        if (d == 0)
-            a.stat[at] = make_float2(some ? l * kLog2e : INFINITY, dot);
-    }
     if constexpr (p_shift<Op>() > 0)
-        raise(a.norms + ((int64_t)b * a.Hkv + hq / a.G) * 2, some ? sqrtf(sq) : 0.0f);
+        raise(a.norms + ((int64_t)b * a.Hkv + hq / a.G) * 2, sqrtf(most));
 }
 
 // fp16: the largest |v_j| of each key/value head.
@@ -109,36 +131,43 @@ template <class Op>
 __global__ __launch_bounds__(kThreads) void value_norms(AttnArgs a)
 {
     const uint32_t bh = blockIdx.x / a.tiles, t = blockIdx.x - bh * a.tiles;
-    const int b = bh / a.Hkv, hk = bh - b * a.Hkv;
-    const int j = t * (kThreads / 16) + (threadIdx.x >> 4), d = (threadIdx.x & 15) * 8;
-    float f[8], sq = 0;
-    const bool in = j < keys_of(a, b) && (!a.k_doc || a.k_doc[(int64_t)b * a.Lk + j] >= 0);
-    if (in && d < a.D) {
-        load8<Op>(a.v + b * a.v_sb + hk * a.v_sh + (int64_t)j * a.v_st + d * sizeof(typename Op::elem), f);
+    const int b = bh / a.Hkv, hk = bh - b * a.Hkv, d = (threadIdx.x & 15) * 8, n = keys_of(a, b);
+    float most = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            sq += f[e] * f[e];
+    for (int k = 0; k < kStatRows / 16; ++k) {
+        const int j = t * kStatRows + k * 16 + (threadIdx.x >> 4);
+        float f[8], sq = 0;
+        if (j < n && d < a.D && (!a.k_doc || a.k_doc[(int64_t)b * a.Lk + j] >= 0)) {
+            load8<Op>(a.v + b * a.v_sb + hk * a.v_sh + (int64_t)j * a.v_st + d * sizeof(typename Op::elem), f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                sq += f[e] * f[e];
+        }
+        sq = sum16(sq);
+        most = fmaxf(most, sq < INFINITY ? sq : 0.0f);
     }
-    raise(a.norms + ((int64_t)b * a.Hkv + hk) * 2 + 1, sqrtf(sum16(sq)));
+    raise(a.norms + ((int64_t)b * a.Hkv + hk) * 2 + 1, sqrtf(most));
 }
 
 // ---- what both kernels do with a 32 x 32 tile of scores ----
 
-// Scores (times log2 e) of products q.k, without the bias; slope: 1 - tanh^2
-// where they are capped.
-__device__ inline void to_scores(f32x16_acc &s, f32x16_acc &slope, const ScoreArgs &c)
+// Exponents of the probabilities (base 2), without the bias: the scores of
+// the products in s less lse(r), the row statistic of register r; slope:
+// 1 - tanh^2 where scores are capped.
+template <class Lse>
+__device__ inline void to_scores(f32x16_acc &s, f32x16_acc &slope, const ScoreArgs &c, Lse lse)
 {
     if (c.cap) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const float t = fast_tanh(s[r] * c.c1);
             slope[r] = 1.0f - t * t;
-            s[r] = c.c2 * t;
+            s[r] = fmaf(c.c2, t, -lse(r));
         }
     } else {
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-            s[r] *= c.c1;
+            s[r] = fmaf(s[r], c.c1, -lse(r));
     }
 }
 
@@ -152,21 +181,24 @@ struct Bwd {
 
 // ---- dk, dv: a key per lane ----
 template <class Op, int DP>
-__global__ __launch_bounds__(kThreads) void attn_dkdv(AttnArgs a)
+__global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 128 ? 2 : 1)) void attn_dkdv(AttnArgs a)
 {
     typedef Bwd<Op, DP> W;
     typedef Tile<Op, DP> T;
-    extern __shared__ __align__(16) char lds[];
-    char *const tq = lds, *const tdo = lds + W::kTileBytes;
-    float *const strip = (float *)(lds + 2 * W::kTileBytes);
-    __shared__ float s_lse[W::kRows], s_delta[W::kRows];
-    __shared__ int s_doc[W::kRows];
+    // two slots of a tile of q and dout, and of their rows' statistics; each
+    // an array of its own: the compiler can tell that reading one does not
+    // wait for the loads that land in the other
+    __shared__ __align__(16) char slot0[2 * W::kTileBytes];
+    __shared__ __align__(16) char slot1[2 * W::kTileBytes];
+    __shared__ __align__(16) float rows0[192];  // 64 of lse, delta, documents
+    __shared__ __align__(16) float rows1[192];
     __shared__ int shared_first[kWaves], shared_lo[kWaves], shared_hi[kWaves];
+    extern __shared__ __align__(16) float strip[];  // 2R+1, times log2(e); documents: a bit for each query tile
 
     uint32_t kt;
     const uint32_t bh = work_item((uint32_t)(a.B * a.Hkv) * a.tiles, a.tiles, &kt);
     const int b = bh / a.Hkv, hk = bh - b * a.Hkv;
-    const int lane = threadIdx.x & 63, h = lane >> 5, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int j = kt * kHeld + wave * 32 + (lane & 31);  // this lane's key
     const bool in = j < a.Lk;
     const int n = keys_of(a, b), off = first_pos(a, n);
@@ -199,6 +231,14 @@ __global__ __launch_bounds__(kThreads) void attn_dkdv(AttnArgs a)
         wg_lo = min(wg_lo, shared_lo[w]);
         wg_hi = max(wg_hi, shared_hi[w]);
     }
+    const int t_first = __builtin_amdgcn_readfirstlane(wg_first) / W::kRows;
+    const int tiles = (a.Lq + W::kRows - 1) / W::kRows;
+    const DocRange *const ranges = a.k_doc ? a.q_range + (int64_t)b * ((a.Lq + kDocTile - 1) / kDocTile) : nullptr;
+    uint64_t *const bits = (uint64_t *)(strip + (a.R ? 2 * a.R + 2 : 0));
+    if (a.k_doc) {
+        mark_tiles(bits, ranges, tiles, W::kRows, wg_lo, wg_hi, wave, lane);
+        __syncthreads();
+    }
 
     const bool held = in && j < n;
     typename Op::v8 kf[DP / 16], vf[DP / 16];
@@ -213,42 +253,38 @@ __global__ __launch_bounds__(kThreads) void attn_dkdv(AttnArgs a)
 
     const ScoreArgs sc = score_args(a);
     const float dss = ds_scale<Op>(a, b, hk);
-    const float f = dss * exp2f(-p_shift<Op>());  // dS*dss = P' * (f*dP - f*delta)
+    const float f = dss * exp2f(-p_shift<Op>());  // dS*dss = P' * f*(dP - delta)
+    const int Lp = stat_rows(a.Lq);
 
     for (int g = 0; g < a.G; ++g) {
         const int hq = hk * a.G + g;
-        if (a.R) {
-            __syncthreads();
-            for (int t = threadIdx.x; t < 2 * a.R + 1; t += kThreads)
-                strip[t] = a.strip[(int64_t)hq * (2 * a.R + 1) + t] * kLog2e;
-        }
-        const char *qp = a.q + b * a.q_sb + hq * a.q_sh, *dop = a.dout + b * a.do_sb + hq * a.do_sh;
-        const float2 *stat = a.stat + ((int64_t)b * a.H + hq) * a.Lq;
-        for (int q0 = wg_first / W::kRows * W::kRows; q0 < a.Lq; q0 += W::kRows) {
+        const char *const qp = a.q + b * a.q_sb + hq * a.q_sh, *const dop = a.dout + b * a.do_sb + hq * a.do_sh;
+        const float *const stat = a.stat + ((int64_t)b * a.H + hq) * 2 * Lp;
+        auto issue = [&](char *slot, float *rows, int t) {
+            const int q0 = t * W::kRows;
+            T::template dma<W::kRows, kWaves>(slot, qp + (int64_t)q0 * a.q_st, a.q_st, a.Lq - q0, a.D, wave, lane);
+            T::template dma<W::kRows, kWaves>(slot + W::kTileBytes, dop + (int64_t)q0 * a.do_st, a.do_st, a.Lq - q0, a.D,
+                                              wave, lane);
+            if (wave < 2)  // statistics have whole tiles of rows
+                dma_words(rows + 64 * wave, stat + wave * Lp + q0, W::kRows, lane);
+            else if (wave == 2 && a.k_doc)
+                dma_words(rows + 128, a.q_doc + (int64_t)b * a.Lq + q0, a.Lq - q0, lane);
+        };
+        auto after = [&](int t) { return a.k_doc ? next_tile(bits, t, tiles) : t; };
+        auto step = [&](char *slot, float *rows, char *other, float *other_rows, int x) {
+            wait_loads<0>();
+            ring_barrier();
+            const int next = after(x + 1), q0 = x * W::kRows;
+            if (next < tiles)
+                issue(other, other_rows, next);
             DocRange dr = {0, 0, 0, 0};
-            if (a.k_doc) {
-                dr = a.q_range[(int64_t)b * ((a.Lq + kDocTile - 1) / kDocTile) + q0 / kDocTile];
-                if (!(dr.lo <= wg_hi && dr.hi >= wg_lo))
-                    continue;
-            }
-            __syncthreads();
-            T::template stage<W::kRows>(tq, qp + (int64_t)q0 * a.q_st, a.q_st, a.Lq - q0, a.D);
-            T::template stage<W::kRows>(tdo, dop + (int64_t)q0 * a.do_st, a.do_st, a.Lq - q0, a.D);
-            if (threadIdx.x < W::kRows) {
-                const int i = q0 + threadIdx.x;
-                float2 v = make_float2(INFINITY, 0);
-                if (i < a.Lq)
-                    v = stat[i];
-                s_lse[threadIdx.x] = v.x - p_shift<Op>();
-                s_delta[threadIdx.x] = v.y * f;
-                if (a.k_doc)
-                    s_doc[threadIdx.x] = i < a.Lq ? a.q_doc[(int64_t)b * a.Lq + i] : -1;
-            }
-            __syncthreads();
+            if (a.k_doc)
+                dr = ranges[q0 / kDocTile];
             if (q0 + W::kRows <= least || (a.k_doc && !(dr.lo <= dhi && dr.hi >= dlo)))
-                continue;
+                return next;
             const bool docs_differ = a.k_doc && (dr.mixed || dlo != dhi || dr.lo != dlo);
             const bool partial = q0 < most || docs_differ;
+            const char *const tq = slot, *const tdo = slot + W::kTileBytes;
 #pragma unroll
             for (int t = 0; t < W::kSub; ++t) {
                 f32x16_acc s, dp, slope;
@@ -260,7 +296,7 @@ __global__ __launch_bounds__(kThreads) void attn_dkdv(AttnArgs a)
                     s = Op::mfma(T::row_frag(tq, 32 * t + (lane & 31), st, h), kf[st], s);
                     dp = Op::mfma(T::row_frag(tdo, 32 * t + (lane & 31), st, h), vf[st], dp);
                 }
-                to_scores(s, slope, sc);
+                to_scores(s, slope, sc, [&](int r) { return rows[32 * t + reg_row(r) + 4 * h]; });
                 const int i0 = q0 + 32 * t;
                 if (a.R) {
                     const int dmin = jlo - (i0 + 31 + off), dmax = jhi - (i0 + off);
@@ -276,23 +312,29 @@ __global__ __launch_bounds__(kThreads) void attn_dkdv(AttnArgs a)
                             s[r] += strip[min(max(d0 - reg_row(r), -a.R), a.R) + a.R];
                     }
                 }
-                bool out[16];
-                const int lim = first == INT32_MAX ? INT32_MAX : first - i0 - 4 * h;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    out[r] = partial && (reg_row(r) < lim || (docs_differ && s_doc[32 * t + reg_row(r) + 4 * h] != doc));
-                    const float delta = s_delta[32 * t + reg_row(r) + 4 * h];
-                    float p = __builtin_amdgcn_exp2f(s[r] - s_lse[32 * t + reg_row(r) + 4 * h]);
-                    float ds = p * (dp[r] * f - delta);
-                    if (sc.cap)
-                        ds *= slope[r];
-                    if (partial) {
-                        p += 0.0f * delta;  // a dout that is not finite reaches dv through p
-                        p = out[r] ? 0.0f : p;
-                        ds = out[r] ? 0.0f : ds;
+                    const int row = 32 * t + reg_row(r) + 4 * h;
+                    s[r] = __builtin_amdgcn_exp2f(s[r]);
+                    float d = dp[r] - rows[64 + row];
+                    if constexpr (p_shift<Op>() > 0)
+                        d *= f;
+                    dp[r] = s[r] * d;
+                }
+                if (sc.cap)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        dp[r] *= slope[r];
+                if (partial) {
+                    const int lim = first == INT32_MAX ? INT32_MAX : first - i0 - 4 * h;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int row = 32 * t + reg_row(r) + 4 * h;
+                        const bool out = reg_row(r) < lim || (docs_differ && __float_as_int(rows[128 + row]) != doc);
+                        // a dout that is not finite reaches dv through p
+                        s[r] = out ? 0.0f : s[r] + 0.0f * rows[64 + row];
+                        dp[r] = out ? 0.0f : dp[r];
                     }
-                    s[r] = p;
-                    dp[r] = ds;
                 }
                 uint32_t bad = 0;
 #pragma unroll
@@ -300,17 +342,33 @@ __global__ __launch_bounds__(kThreads) void attn_dkdv(AttnArgs a)
                     const typename Op::v8 p = pack8<Op>(s, 8 * ks), ds = pack8<Op>(dp, 8 * ks);
 #pragma unroll
                     for (int dt = 0; dt < DP / 32; ++dt) {
-                        typename Op::v8 x = T::col_frag(tdo, 32 * t + 16 * ks, dt, lane);
-                        typename Op::v8 y = T::col_frag(tq, 32 * t + 16 * ks, dt, lane);
+                        typename Op::v8 x1 = T::col_frag(tdo, 32 * t + 16 * ks, dt, lane);
+                        typename Op::v8 y1 = T::col_frag(tq, 32 * t + 16 * ks, dt, lane);
                         if (partial) {  // a left-out pair's zero times infinity or NaN must stay zero
-                            x = finite<Op>(x, bad);
-                            y = finite<Op>(y, bad);
+                            x1 = finite<Op>(x1, bad);
+                            y1 = finite<Op>(y1, bad);
                         }
-                        dv[dt] = Op::mfma(x, p, dv[dt]);
-                        dk[dt] = Op::mfma(y, ds, dk[dt]);
+                        dv[dt] = Op::mfma(x1, p, dv[dt]);
+                        dk[dt] = Op::mfma(y1, ds, dk[dt]);
                     }
                 }
             }
+            return next;
+        };
+        __syncthreads();  // the head before this one has read its tiles and strip
+        int t = after(t_first);
+        if (t < tiles)
+            issue(slot0, rows0, t);
+        if (a.R) {
+            for (int x = threadIdx.x; x < 2 * a.R + 1; x += kThreads)
+                strip[x] = a.strip[(int64_t)hq * (2 * a.R + 1) + x] * kLog2e;
+            ring_barrier();
+        }
+        while (t < tiles) {
+            t = step(slot0, rows0, slot1, rows1, t);
+            if (t >= tiles)
+                break;
+            t = step(slot1, rows1, slot0, rows0, t);
         }
     }
     if (!in)
@@ -321,39 +379,42 @@ __global__ __launch_bounds__(kThreads) void attn_dkdv(AttnArgs a)
 
 // ---- dq (and the strip's gradient): a query per lane ----
 template <class Op, int DP>
-__global__ __launch_bounds__(kThreads) void attn_dq(AttnArgs a, int want_strip)
+__global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 256 ? 2 : 1)) void attn_dq(AttnArgs a, int want_strip)
 {
     typedef Bwd<Op, DP> W;
     typedef Tile<Op, DP> T;
-    extern __shared__ __align__(16) char lds[];
-    char *const tk = lds, *const tv = lds + W::kTileBytes;
-    float *const strip = (float *)(lds + 2 * W::kTileBytes);
+    __shared__ __align__(16) char slot0[2 * W::kTileBytes];
+    __shared__ __align__(16) char slot1[2 * W::kTileBytes];
+    __shared__ int kdoc0[64], kdoc1[64];
+    // [1 or 1 + 2*kWaves][2R+1]: the strip times log2(e), its gradients; documents: a bit for each key tile
+    extern __shared__ __align__(16) float strip[];
     const int width = 2 * a.R + 1;
-    __shared__ int kdoc[W::kRows];
     __shared__ int shared_most[kWaves], shared_lo[kWaves], shared_hi[kWaves];
 
     uint32_t qt;
     const uint32_t bh = work_item((uint32_t)(a.B * a.H) * a.tiles, a.tiles, &qt);
     qt = a.tiles - 1 - qt;
     const int b = bh / a.H, hq = bh - b * a.H, hk = hq / a.G;
-    const int lane = threadIdx.x & 63, h = lane >> 5, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = qt * kHeld + wave * 32 + (lane & 31);
     const bool live = i < a.Lq;
     const int n = keys_of(a, b);
     const int pos = i + first_pos(a, n);
-    int lim = n, doc = 0;
+    int lim = n, doc = -1;
     if (a.causal)
-        lim = min(n, max(pos + 1, a.prefix ? a.prefix[b] : 0));
+        lim = max(0, min(n, max(pos + 1, a.prefix ? a.prefix[b] : 0)));
     if (a.q_doc) {
-        doc = live ? a.q_doc[(int64_t)b * a.Lq + i] : -1;
+        if (live)
+            doc = a.q_doc[(int64_t)b * a.Lq + i];
         if (doc < 0)
             lim = 0;
     }
-    if (!live || lim < 0)
-        lim = 0;
-    const int most = wave_max(lim), least = wave_min(lim);
+    // a lane without a query holds zeros and an lse of infinity: it adds
+    // nothing, masked or not
+    const int most = wave_max(live ? lim : 0), least = wave_min(live ? lim : INT32_MAX);
     const int plo = wave_min(pos), phi = wave_max(pos);
-    const int dlo = wave_min(lim > 0 ? doc : INT32_MAX), dhi = wave_max(lim > 0 ? doc : -1);
+    const bool seen = live && lim > 0;
+    const int dlo = wave_min(seen ? doc : INT32_MAX), dhi = wave_max(seen ? doc : -1);
     // each half wave has a strip of gradients of its own: the 32 lanes that
     // add in one instruction hold 32 different distances, so nothing is
     // summed in an order that could change
@@ -384,11 +445,11 @@ __global__ __launch_bounds__(kThreads) void attn_dq(AttnArgs a, int want_strip)
     typename Op::v8 qf[DP / 16], dof[DP / 16];
     T::held(qf, a.q + b * a.q_sb + hq * a.q_sh + (int64_t)i * a.q_st, live, h, a.D);
     T::held(dof, a.dout + b * a.do_sb + hq * a.do_sh + (int64_t)i * a.do_st, live, h, a.D);
-    float2 st = make_float2(INFINITY, 0);
-    if (live)
-        st = a.stat[((int64_t)b * a.H + hq) * a.Lq + i];
+    const int Lp = stat_rows(a.Lq);
+    const float *const stat = a.stat + ((int64_t)b * a.H + hq) * 2 * Lp;
+    const float lse = live ? stat[i] : INFINITY, row_delta = live ? stat[Lp + i] : 0.0f;
     const float dss = ds_scale<Op>(a, b, hk);
-    const float lse = st.x - p_shift<Op>(), delta = st.y * dss * exp2f(-p_shift<Op>());
+    const float delta = row_delta * dss * exp2f(-p_shift<Op>());
     // The matrix cores' 16-bit products come out low by 1 % of an ulp in the
     // mean (measured: -9e-9 at |dP| of 8), which sums over the thousands of
     // pairs of a bucket.  Every second query holds -dout, so that what the
@@ -407,21 +468,34 @@ __global__ __launch_bounds__(kThreads) void attn_dq(AttnArgs a, int want_strip)
     const char *kp = a.k + b * a.k_sb + hk * a.k_sh, *vp = a.v + b * a.v_sb + hk * a.v_sh;
     const ScoreArgs sc = score_args(a);
 
-    for (int k0 = 0; k0 < wg_most; k0 += W::kRows) {
+    const int tiles = (__builtin_amdgcn_readfirstlane(wg_most) + W::kRows - 1) / W::kRows;
+    const DocRange *const ranges = a.q_doc ? a.k_range + (int64_t)b * ((a.Lk + kDocTile - 1) / kDocTile) : nullptr;
+    uint64_t *const bits = (uint64_t *)(strip + strip_floats(a.R, want_strip));
+    if (a.q_doc) {
+        mark_tiles(bits, ranges, tiles, W::kRows, wg_lo, wg_hi, wave, lane);
+        __syncthreads();
+    }
+    auto issue = [&](char *slot, int *ids, int t) {
+        const int k0 = t * W::kRows;
+        T::template dma<W::kRows, kWaves>(slot, kp + (int64_t)k0 * a.k_st, a.k_st, n - k0, a.D, wave, lane);
+        T::template dma<W::kRows, kWaves>(slot + W::kTileBytes, vp + (int64_t)k0 * a.v_st, a.v_st, n - k0, a.D, wave,
+                                          lane);
+        if (a.q_doc && wave == 0)
+            dma_words(ids, a.k_doc + (int64_t)b * a.Lk + k0, n - k0, lane);
+    };
+    auto after = [&](int t) { return a.q_doc ? next_tile(bits, t, tiles) : t; };
+    auto step = [&](char *slot, int *kdoc, char *other, int *other_ids, int at) {
+        wait_loads<0>();
+        ring_barrier();
+        const int next = after(at + 1), k0 = at * W::kRows;
+        if (next < tiles)
+            issue(other, other_ids, next);
         DocRange dr = {0, 0, 0, 0};
-        if (a.q_doc) {
-            dr = a.k_range[(int64_t)b * ((a.Lk + kDocTile - 1) / kDocTile) + k0 / kDocTile];
-            if (!(dr.lo <= wg_hi && dr.hi >= wg_lo))
-                continue;
-        }
-        __syncthreads();
-        T::template stage<W::kRows>(tk, kp + (int64_t)k0 * a.k_st, a.k_st, n - k0, a.D);
-        T::template stage<W::kRows>(tv, vp + (int64_t)k0 * a.v_st, a.v_st, n - k0, a.D);
-        if (a.q_doc && threadIdx.x < W::kRows)
-            kdoc[threadIdx.x] = k0 + (int)threadIdx.x < n ? a.k_doc[(int64_t)b * a.Lk + k0 + threadIdx.x] : -1;
-        __syncthreads();
+        if (a.q_doc)
+            dr = ranges[k0 / kDocTile];
+        const char *const tk = slot, *const tv = slot + W::kTileBytes;
         if (k0 >= most || (a.q_doc && !(dr.lo <= dhi && dr.hi >= dlo)))
-            continue;
+            return next;
         const bool docs_differ = a.q_doc && (dr.mixed || dlo != dhi || dr.lo != dlo);
         const bool partial = k0 + W::kRows > least || docs_differ;
 #pragma unroll
@@ -435,7 +509,7 @@ __global__ __launch_bounds__(kThreads) void attn_dq(AttnArgs a, int want_strip)
                 s = Op::mfma(T::row_frag(tk, 32 * t + (lane & 31), x, h), qf[x], s);
                 dp = Op::mfma(T::row_frag(tv, 32 * t + (lane & 31), x, h), dof[x], dp);
             }
-            to_scores(s, slope, sc);
+            to_scores(s, slope, sc, [&](int) { return lse; });
             const int j0 = k0 + 32 * t, d0 = j0 + 4 * h - pos;
             const bool far = a.R && (j0 + 31 - plo <= -a.R || j0 - phi >= a.R);
             if (a.R) {
@@ -453,8 +527,8 @@ __global__ __launch_bounds__(kThreads) void attn_dq(AttnArgs a, int want_strip)
             const int last = lim - j0 - 4 * h;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const float p = __builtin_amdgcn_exp2f(s[r] - lse);
-                float ds = p * (dp[r] * f - delta);
+                const float p = __builtin_amdgcn_exp2f(s[r]);
+                float ds = p * fmaf(dp[r], f, -delta);
                 if (partial)
                     ds = reg_row(r) >= last || (docs_differ && kdoc[32 * t + reg_row(r) + 4 * h] != doc) ? 0.0f : ds;
                 dp[r] = ds;
@@ -497,6 +571,16 @@ __global__ __launch_bounds__(kThreads) void attn_dq(AttnArgs a, int want_strip)
                 }
             }
         }
+        return next;
+    };
+    int t = after(0);
+    if (t < tiles)
+        issue(slot0, kdoc0, t);
+    while (t < tiles) {
+        t = step(slot0, kdoc0, slot1, kdoc1, t);
+        if (t >= tiles)
+            break;
+        t = step(slot1, kdoc1, slot0, kdoc0, t);
     }
     if (live)
         store_row<Op, DP>(a.dq + b * a.dq_sb + hq * a.dq_sh + (int64_t)i * a.dq_st, dq, a.scale / dss, h, a.D);
@@ -553,31 +637,33 @@ hipError_t run(const AttnArgs &a, float *dstrip, hipStream_t st)
         if (words)
             clear_words<<<(uint32_t)((words + kThreads - 1) / kThreads < 256 ? (words + kThreads - 1) / kThreads : 256),
                           kThreads, 0, st>>>(a.norms, words);
-        b.tiles = (a.Lk + kThreads / 16 - 1) / (kThreads / 16);
+        b.tiles = (a.Lk + kStatRows - 1) / kStatRows;
         if (a.B * b.tiles)
             value_norms<Op><<<(uint32_t)(a.B * a.Hkv) * b.tiles, kThreads, 0, st>>>(b);
     }
-    b.tiles = (a.Lq + kThreads / 16 - 1) / (kThreads / 16);
+    b.tiles = stat_rows(a.Lq) / kStatRows;
     if (a.B * b.tiles)
         row_stats<Op><<<(uint32_t)(a.B * a.H) * b.tiles, kThreads, 0, st>>>(b);
     if ((e = hipGetLastError()) != hipSuccess)
         return e;
 
-    constexpr size_t kMost = 2 * W::kTileBytes + (2 * SEQ_BIAS_RANGE + 1) * 4;
-    if ((e = hipFuncSetAttribute((const void *)attn_dkdv<Op, DP>, hipFuncAttributeMaxDynamicSharedMemorySize, kMost)) !=
-            hipSuccess ||
-        (e = hipFuncSetAttribute((const void *)attn_dq<Op, DP>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                 kMost + 2 * kWaves * (2 * SEQ_BIAS_RANGE + 1) * 4)) != hipSuccess)
+    // LDS beside the tiles: strips and a bit for each streamed tile
+    const size_t bits_k = a.q_doc ? (a.Lk + 64 * W::kRows - 1) / (64 * W::kRows) * 8 : 0;
+    const size_t bits_q = a.q_doc ? (a.Lq + 64 * W::kRows - 1) / (64 * W::kRows) * 8 : 0;
+    const size_t lds_kv = (a.R ? (2 * a.R + 2) * 4 : 0) + bits_q;
+    const size_t lds_q = strip_floats(a.R, dstrip != nullptr) * 4 + bits_k;
+    if (lds_kv && (e = hipFuncSetAttribute((const void *)attn_dkdv<Op, DP>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                           16 << 10)) != hipSuccess)
+        return e;
+    if (lds_q && (e = hipFuncSetAttribute((const void *)attn_dq<Op, DP>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                          84 << 10)) != hipSuccess)
         return e;
     b.tiles = (a.Lk + kHeld - 1) / kHeld;
     if (a.B * b.tiles)
-        attn_dkdv<Op, DP><<<(uint32_t)(a.B * a.Hkv) * b.tiles, kThreads, 2 * W::kTileBytes + (a.R ? width * 4 : 0), st>>>(
-            b);
+        attn_dkdv<Op, DP><<<(uint32_t)(a.B * a.Hkv) * b.tiles, kThreads, lds_kv, st>>>(b);
     b.tiles = (a.Lq + kHeld - 1) / kHeld;
     if (a.B * b.tiles)
-        attn_dq<Op, DP><<<(uint32_t)(a.B * a.H) * b.tiles, kThreads,
-                          2 * W::kTileBytes + (a.R ? width * 4 * (dstrip ? 1 + 2 * kWaves : 1) : 0), st>>>(
-            b, dstrip != nullptr);
+        attn_dq<Op, DP><<<(uint32_t)(a.B * a.H) * b.tiles, kThreads, lds_q, st>>>(b, dstrip != nullptr);
     if (dstrip)
         strip_reduce<<<dim3((uint32_t)((width + 63) / 64), (uint32_t)a.H), kThreads, 0, st>>>(a.part, dstrip,
                                                                                            a.B * b.tiles, width);

@@ -16,22 +16,6 @@ struct Fwd {
     static constexpr int kTileBytes = kKeys * T::kRowBytes;
 };
 
-// The next key tile from t on that holds a document of the workgroup's
-// queries: one bit a tile in `bits`, 64 tiles a word, `tiles` in all.
-__device__ inline int next_tile(const uint64_t *bits, int t, int tiles)
-{
-    while (t < tiles) {
-        const uint64_t w = bits[t >> 6] >> (t & 63);
-        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)w), hi = __builtin_amdgcn_readfirstlane((uint32_t)(w >> 32));
-        if (lo)
-            return t + __builtin_ctz(lo);
-        if (hi)
-            return t + 32 + __builtin_ctz(hi);
-        t = (t | 63) + 1;
-    }
-    return tiles;
-}
-
 template <class Op, int DP>
 __global__ __launch_bounds__(64 * kWaves, (OpInfo<Op>::kIs32 && DP == 128 ? 1 : 2)) void attn_fwd(AttnArgs a)
 {
@@ -41,7 +25,7 @@ __global__ __launch_bounds__(64 * kWaves, (OpInfo<Op>::kIs32 && DP == 128 ? 1 : 
     // one does not wait for the loads that land in the other
     __shared__ __align__(16) char slot0[2 * F::kTileBytes];
     __shared__ __align__(16) char slot1[2 * F::kTileBytes];
-    __shared__ int kdoc[2][F::kKeys];
+    __shared__ int kdoc0[64], kdoc1[64];  // 64: a wave's words
     __shared__ int shared_most[kWaves], shared_lo[kWaves], shared_hi[kWaves];
     extern __shared__ __align__(16) float strip[];  // 2R+1, times log2(e); documents: a bit for each key tile
 
@@ -91,16 +75,7 @@ __global__ __launch_bounds__(64 * kWaves, (OpInfo<Op>::kIs32 && DP == 128 ? 1 : 
     const DocRange *const ranges = a.q_doc ? a.k_range + (int64_t)b * ((a.Lk + kDocTile - 1) / kDocTile) : nullptr;
     uint64_t *const bits = (uint64_t *)(strip + (a.R ? 2 * a.R + 2 : 0));
     if (a.q_doc) {
-        for (int t0 = wave * 64; t0 < tiles; t0 += 64 * kWaves) {
-            bool meet = false;
-            if (t0 + lane < tiles) {
-                const DocRange r = ranges[(t0 + lane) * F::kKeys / kDocTile];
-                meet = r.lo <= wg_hi && r.hi >= wg_lo;
-            }
-            const uint64_t w = __ballot(meet);
-            if (lane == 0)
-                bits[t0 >> 6] = w;
-        }
+        mark_tiles(bits, ranges, tiles, F::kKeys, wg_lo, wg_hi, wave, lane);
         __syncthreads();
     }
 
@@ -111,26 +86,23 @@ __global__ __launch_bounds__(64 * kWaves, (OpInfo<Op>::kIs32 && DP == 128 ? 1 : 
     RowState<Op, DP> st;
     st.clear();
 
-    int kd = -1;  // the document of key threadIdx.x of the tile under way
-    auto issue = [&](char *slot, int t) {
+    auto issue = [&](char *slot, int *doc_ids, int t) {
         const int k0 = t * F::kKeys;
         T::template dma<F::kKeys, kWaves>(slot, kp + (int64_t)k0 * a.k_st, a.k_st, n - k0, a.D, wave, lane);
         T::template dma<F::kKeys, kWaves>(slot + F::kTileBytes, vp + (int64_t)k0 * a.v_st, a.v_st, n - k0, a.D, wave,
                                           lane);
-        if (a.q_doc && threadIdx.x < F::kKeys)
-            kd = k0 + (int)threadIdx.x < n ? a.k_doc[(int64_t)b * a.Lk + k0 + threadIdx.x] : -1;
+        if (a.q_doc && wave == 0)
+            dma_words(doc_ids, a.k_doc + (int64_t)b * a.Lk + k0, n - k0, lane);
     };
     auto after = [&](int t) { return a.q_doc ? next_tile(bits, t, tiles) : t; };
     // tile t in `slot` (its loads under way); starts the loads of the next
     // one into `other` and returns it
-    auto step = [&](char *slot, char *other, int *doc_ids, int t) {
+    auto step = [&](char *slot, int *doc_ids, char *other, int *other_ids, int t) {
         wait_loads<0>();
-        if (a.q_doc && threadIdx.x < F::kKeys)
-            doc_ids[threadIdx.x] = kd;
         ring_barrier();  // everyone's loads have landed, and `other` has been read
         const int next = after(t + 1), k0 = t * F::kKeys;
         if (next < tiles)
-            issue(other, next);
+            issue(other, other_ids, next);
         DocRange dr = {0, 0, 0, 0};
         if (a.q_doc)
             dr = ranges[k0 / kDocTile];
@@ -160,12 +132,12 @@ __global__ __launch_bounds__(64 * kWaves, (OpInfo<Op>::kIs32 && DP == 128 ? 1 : 
 
     int t = after(0);
     if (t < tiles)
-        issue(slot0, t);
+        issue(slot0, kdoc0, t);
     while (t < tiles) {
-        t = step(slot0, slot1, kdoc[0], t);
+        t = step(slot0, kdoc0, slot1, kdoc1, t);
         if (t >= tiles)
             break;
-        t = step(slot1, slot0, kdoc[1], t);
+        t = step(slot1, kdoc1, slot0, kdoc0, t);
     }
 
     float l = st.l;
