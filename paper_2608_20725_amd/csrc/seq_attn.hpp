@@ -318,13 +318,15 @@ struct TilePairs {
     bool partial;      // some pairs are left out
     bool docs_differ;  // .. by documents
     bool near;         // the bias differs within the tile
+    bool inner;        // .. and no distance of the tile is beyond the strip
     float far;         // the bias where it does not
     int lim, doc;      // this lane's query: keys below lim, its document
     const int *kdoc;   // documents of the tile's keys
 };
 
 // One tile of 32*SUB keys: s = K q, the softmax's update, o += V^T p.
-// near(t, r): bias of key 32*t + reg_row(r) + 4*h of the tile.
+// near(x, clamp): bias of key x + 4*h of the tile, its distance clamped to the
+// strip if `clamp`.
 template <class Op, int DP, int SUB, class Near>
 __device__ inline void attend(const char *tk, const char *tv, const typename Op::v8 (&q)[DP / 16], RowState<Op, DP> &st,
                               const ScoreArgs &sc, const TilePairs &tp, int lane, Near near)
@@ -359,12 +361,21 @@ __device__ inline void attend(const char *tk, const char *tv, const typename Op:
                 for (int r = 0; r < 16; ++r)
                     s[t][r] = fmaf(s[t][r], sc.c1, tp.far);
         }
-        if (tp.near)
+        if (tp.near) {
+            if (tp.inner) {
 #pragma unroll
-            for (int t = 0; t < SUB; ++t)
+                for (int t = 0; t < SUB; ++t)
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    s[t][r] += near(t, r);
+                    for (int r = 0; r < 16; ++r)
+                        s[t][r] += near(32 * t + reg_row(r), false);
+            } else {
+#pragma unroll
+                for (int t = 0; t < SUB; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        s[t][r] += near(32 * t + reg_row(r), true);
+            }
+        }
         if (tp.partial) {
             const int last = tp.lim - tp.k0 - 4 * h;
 #pragma unroll
@@ -505,15 +516,39 @@ __device__ inline int keys_of(const AttnArgs &a, int b)
 }
 __device__ inline int first_pos(const AttnArgs &a, int n) { return a.align_end ? n - a.Lq : 0; }
 
-// Work item of this workgroup: `tiles` items per head, consecutive ones on
-// one XCD (workgroup id mod 8), so that a head's streamed side stays in that
-// XCD's L2.  Returns the head's index, *tile the item.
-__device__ inline uint32_t work_item(uint32_t total, uint32_t tiles, uint32_t *tile)
+// What a workgroup works on: tile `tile` of key/value head `kv` (of B*Hkv) and
+// of its query head `g`.  Workgroups go to the 8 XCDs in turn (id mod 8).
+//   uneven = false: runs of consecutive ids (head by head) on one XCD, so that
+//     the streamed side of a head stays in that XCD's L2.
+//   uneven = true (causal masks, whose tiles differ in work): tile 0 of every
+//     head first, then tile 1, .., so that the caller can start the longest
+//     ones first; heads that share keys still fall on one XCD where the number
+//     of key/value heads is a multiple of 8.
+struct Work {
+    uint32_t kv, g, tile;
+};
+__device__ inline Work work_item(uint32_t heads, uint32_t G, uint32_t tiles, bool uneven, uint32_t id)
 {
-    const uint32_t x = blockIdx.x % 8, j = blockIdx.x / 8, per = total / 8, rem = total % 8;
+    Work w;
+    const uint32_t all = heads * G;
+    if (uneven) {
+        const uint32_t r = id % all;
+        w.tile = id / all;
+        if (heads % 8 == 0) {
+            w.g = r / 8 % G;
+            w.kv = r % 8 + 8 * (r / (8 * G));
+        } else {
+            w.kv = r / G;
+            w.g = r % G;
+        }
+        return w;
+    }
+    const uint32_t total = all * tiles, x = id % 8, j = id / 8, per = total / 8, rem = total % 8;
     const uint32_t t = x * per + (x < rem ? x : rem) + j;
-    *tile = t % tiles;
-    return t / tiles;
+    w.tile = t % tiles;
+    w.kv = t / tiles / G;
+    w.g = t / tiles % G;
+    return w;
 }
 
 // Bytes of AttnArgs::part a call may use.

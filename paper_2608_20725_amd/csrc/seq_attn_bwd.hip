@@ -22,6 +22,27 @@ constexpr int kThreads = 64 * kWaves;
 // Rows of statistics a head has: whole tiles.
 __host__ __device__ inline int stat_rows(int Lq) { return (Lq + 63) / 64 * 64; }
 
+// Floats of the partial strip gradients: one strip for each of attn_dq's
+// workgroups.
+int64_t strip_part_floats(int64_t B, int64_t Lq, int64_t H, int64_t R)
+{
+    return R ? (B * H * ((Lq + kHeld - 1) / kHeld) * (2 * R + 1) + 3) / 4 * 4 : 0;
+}
+
+// Workgroups that share the queries of one key tile: with few key/value heads
+// and short rows there are fewer key tiles than the 256 CUs can work on, and
+// causal masks need about two of them a CU to even out.
+int32_t dkdv_splits(int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv)
+{
+    const int64_t groups = B * Hkv * ((Lk + kHeld - 1) / kHeld), work = (H / Hkv) * ((Lq + 63) / 64);
+    if (groups <= 0 || groups >= 512)
+        return 1;
+    int64_t s = (512 + groups - 1) / groups;
+    if (s > work / 4)  // at least four tiles each
+        s = work / 4;
+    return s < 1 ? 1 : (int32_t)s;
+}
+
 // Floats of attn_dq's strip and its gradients in LDS (even: 8-byte words follow).
 __host__ __device__ inline int strip_floats(int R, int want_strip)
 {
@@ -195,9 +216,9 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 128 ? 2 : 1)) v
     __shared__ int shared_first[kWaves], shared_lo[kWaves], shared_hi[kWaves];
     extern __shared__ __align__(16) float strip[];  // 2R+1, times log2(e); documents: a bit for each query tile
 
-    uint32_t kt;
-    const uint32_t bh = work_item((uint32_t)(a.B * a.Hkv) * a.tiles, a.tiles, &kt);
-    const int b = bh / a.Hkv, hk = bh - b * a.Hkv;
+    // `splits` workgroups share the (head, query tile) pairs of a key tile
+    const Work work = work_item(a.B * a.Hkv, a.splits, a.tiles, a.causal, blockIdx.x);
+    const int kt = work.tile, b = work.kv / a.Hkv, hk = work.kv - b * a.Hkv;  // early keys: long columns of causal masks
     const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int j = kt * kHeld + wave * 32 + (lane & 31);  // this lane's key
     const bool in = j < a.Lk;
@@ -256,8 +277,13 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 128 ? 2 : 1)) v
     const float f = dss * exp2f(-p_shift<Op>());  // dS*dss = P' * f*(dP - delta)
     const int Lp = stat_rows(a.Lq);
 
-    for (int g = 0; g < a.G; ++g) {
-        const int hq = hk * a.G + g;
+    // this workgroup's pairs u of head u / span and tile t_first + u % span
+    const int span = max(tiles - t_first, 0);
+    const int u_end = (int)((int64_t)span * a.G * (work.g + 1) / a.splits);
+    for (int u = (int)((int64_t)span * a.G * work.g / a.splits); u < u_end;) {
+        const int g = u / span, hq = hk * a.G + g;
+        const int t_begin = t_first + (u - g * span), t_end = min(tiles, t_begin + (u_end - u));
+        u += t_end - t_begin;
         const char *const qp = a.q + b * a.q_sb + hq * a.q_sh, *const dop = a.dout + b * a.do_sb + hq * a.do_sh;
         const float *const stat = a.stat + ((int64_t)b * a.H + hq) * 2 * Lp;
         auto issue = [&](char *slot, float *rows, int t) {
@@ -270,12 +296,12 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 128 ? 2 : 1)) v
             else if (wave == 2 && a.k_doc)
                 dma_words(rows + 128, a.q_doc + (int64_t)b * a.Lq + q0, a.Lq - q0, lane);
         };
-        auto after = [&](int t) { return a.k_doc ? next_tile(bits, t, tiles) : t; };
+        auto after = [&](int t) { return a.k_doc ? next_tile(bits, t, t_end) : t; };
         auto step = [&](char *slot, float *rows, char *other, float *other_rows, int x) {
             wait_loads<0>();
             ring_barrier();
             const int next = after(x + 1), q0 = x * W::kRows;
-            if (next < tiles)
+            if (next < t_end)
                 issue(other, other_rows, next);
             DocRange dr = {0, 0, 0, 0};
             if (a.k_doc)
@@ -305,6 +331,11 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 128 ? 2 : 1)) v
 #pragma unroll
                         for (int r = 0; r < 16; ++r)
                             s[r] += far;
+                    } else if (dmin >= -a.R && dmax <= a.R) {
+                        const float *const at = strip + (j - (i0 + 4 * h + off) + a.R);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            s[r] += at[-reg_row(r)];
                     } else {
                         const int d0 = j - (i0 + 4 * h + off);
 #pragma unroll
@@ -356,29 +387,79 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 128 ? 2 : 1)) v
             return next;
         };
         __syncthreads();  // the head before this one has read its tiles and strip
-        int t = after(t_first);
-        if (t < tiles)
+        int t = after(t_begin);
+        if (t < t_end)
             issue(slot0, rows0, t);
         if (a.R) {
             for (int x = threadIdx.x; x < 2 * a.R + 1; x += kThreads)
                 strip[x] = a.strip[(int64_t)hq * (2 * a.R + 1) + x] * kLog2e;
             ring_barrier();
         }
-        while (t < tiles) {
+        while (t < t_end) {
             t = step(slot0, rows0, slot1, rows1, t);
-            if (t >= tiles)
+            if (t >= t_end)
                 break;
             t = step(slot1, rows1, slot0, rows0, t);
         }
     }
     if (!in)
         return;
+    if (a.splits > 1) {  // sums as they are; dkdv_join adds the splits
+        float *const part = a.part + (((int64_t)work.g * a.B * a.Hkv + work.kv) * a.Lk + j) * 2 * a.D;
+        store_row<F32Op, DP>((char *)part, dk, a.scale / dss, h, a.D);
+        store_row<F32Op, DP>((char *)(part + a.D), dv, exp2f(-p_shift<Op>()), h, a.D);
+        return;
+    }
     store_row<Op, DP>(a.dk + b * a.dk_sb + hk * a.dk_sh + (int64_t)j * a.dk_st, dk, a.scale / dss, h, a.D);
     store_row<Op, DP>(a.dv + b * a.dv_sb + hk * a.dv_sh + (int64_t)j * a.dv_st, dv, exp2f(-p_shift<Op>()), h, a.D);
 }
 
 // ---- dq (and the strip's gradient): a query per lane ----
-template <class Op, int DP>
+
+// Sums of a 32x32 tile along its diagonals.  Lane i of 16 (one query each)
+// holds rows k = reg_row(r) (the lane half's 4*h apart), on diagonal k - i.
+// Moving row k = 16*c + n down by n lanes puts diagonal 16*c - i into lane i,
+// and what leaves the 16 lanes at the bottom re-enters at the top on diagonal
+// 16*(c+1) - i: two adds an element whose operand moves on the way.
+// sum[x] of lane i: diagonal 16*x - i.
+template <int N>
+__device__ inline void move_add(float v, float &here, float &next)
+{
+    if constexpr (N == 0) {
+        here += v;
+    } else {
+        // row_shl:N and row_shr:(16-N); lanes without a source take 0
+        here += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x100 + N, 0xf, 0xf, true));
+        next += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x110 + 16 - N, 0xf, 0xf, true));
+    }
+}
+
+__device__ inline void diagonal_sums(const f32x16_acc &v, f32x4_acc &sum)
+{
+    float a = 0, b = 0, c = 0;
+    move_add<0>(v[0], a, b);
+    move_add<1>(v[1], a, b);
+    move_add<2>(v[2], a, b);
+    move_add<3>(v[3], a, b);
+    move_add<8>(v[4], a, b);
+    move_add<9>(v[5], a, b);
+    move_add<10>(v[6], a, b);
+    move_add<11>(v[7], a, b);
+    move_add<0>(v[8], b, c);
+    move_add<1>(v[9], b, c);
+    move_add<2>(v[10], b, c);
+    move_add<3>(v[11], b, c);
+    move_add<8>(v[12], b, c);
+    move_add<9>(v[13], b, c);
+    move_add<10>(v[14], b, c);
+    move_add<11>(v[15], b, c);
+    sum[0] = a;
+    sum[1] = b;
+    sum[2] = c;
+}
+
+// BIAS = false (no strip) leaves the registers of its paths to the rest.
+template <class Op, int DP, bool BIAS>
 __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 256 ? 2 : 1)) void attn_dq(AttnArgs a, int want_strip)
 {
     typedef Bwd<Op, DP> W;
@@ -391,10 +472,9 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 256 ? 2 : 1)) v
     const int width = 2 * a.R + 1;
     __shared__ int shared_most[kWaves], shared_lo[kWaves], shared_hi[kWaves];
 
-    uint32_t qt;
-    const uint32_t bh = work_item((uint32_t)(a.B * a.H) * a.tiles, a.tiles, &qt);
-    qt = a.tiles - 1 - qt;
-    const int b = bh / a.H, hq = bh - b * a.H, hk = hq / a.G;
+    const Work work = work_item(a.B * a.Hkv, a.G, a.tiles, a.causal, blockIdx.x);
+    const int qt = a.tiles - 1 - work.tile;  // long rows of causal masks first
+    const int b = work.kv / a.Hkv, hk = work.kv - b * a.Hkv, hq = hk * a.G + work.g;
     const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = qt * kHeld + wave * 32 + (lane & 31);
     const bool live = i < a.Lq;
@@ -420,7 +500,7 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 256 ? 2 : 1)) v
     // summed in an order that could change
     float *const grad = strip + width * (1 + 2 * wave + h);
     float far_lo = 0, far_hi = 0;
-    if (a.R)
+    if (BIAS)
         for (int t = threadIdx.x; t < width; t += kThreads) {
             strip[t] = a.strip[(int64_t)hq * width + t] * kLog2e;
             if (want_strip)
@@ -511,13 +591,17 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 256 ? 2 : 1)) v
             }
             to_scores(s, slope, sc, [&](int) { return lse; });
             const int j0 = k0 + 32 * t, d0 = j0 + 4 * h - pos;
-            const bool far = a.R && (j0 + 31 - plo <= -a.R || j0 - phi >= a.R);
-            if (a.R) {
+            const bool far = BIAS && (j0 + 31 - plo <= -a.R || j0 - phi >= a.R);
+            if (BIAS) {
                 if (far) {
                     const float v = strip[j0 - phi >= a.R ? 2 * a.R : 0];
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
                         s[r] += v;
+                } else if (j0 - phi >= -a.R && j0 + 31 - plo <= a.R) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        s[r] += strip[d0 + a.R + reg_row(r)];
                 } else {
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
@@ -533,7 +617,7 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 256 ? 2 : 1)) v
                     ds = reg_row(r) >= last || (docs_differ && kdoc[32 * t + reg_row(r) + 4 * h] != doc) ? 0.0f : ds;
                 dp[r] = ds;
             }
-            if (want_strip) {
+            if (BIAS && want_strip) {
                 if (far) {
                     float v = 0;
 #pragma unroll
@@ -544,13 +628,16 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 256 ? 2 : 1)) v
                     else
                         far_lo += v;
                 } else {
+                    f32x4_acc sum;
+                    diagonal_sums(dp, sum);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int d = d0 + reg_row(r);
-                        far_lo += d <= -a.R ? dp[r] : 0.0f;
-                        far_hi += d >= a.R ? dp[r] : 0.0f;
+                    for (int x = 0; x < 3; ++x) {
+                        const int d = j0 + 4 * h + 16 * x - pos;
+                        far_lo += d <= -a.R ? sum[x] : 0.0f;
+                        far_hi += d >= a.R ? sum[x] : 0.0f;
                         if (d > -a.R && d < a.R)
-                            __hip_atomic_fetch_add(grad + d + a.R, dp[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+                            __hip_atomic_fetch_add(grad + d + a.R, sum[x], __ATOMIC_RELAXED,
+                                                   __HIP_MEMORY_SCOPE_WAVEFRONT);
                     }
                 }
             }
@@ -584,7 +671,7 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 256 ? 2 : 1)) v
     }
     if (live)
         store_row<Op, DP>(a.dq + b * a.dq_sb + hq * a.dq_sh + (int64_t)i * a.dq_st, dq, a.scale / dss, h, a.D);
-    if (!want_strip)
+    if (!BIAS || !want_strip)
         return;
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) {
@@ -605,6 +692,30 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 256 ? 2 : 1)) v
             v += strip[w * width + t];
         out[t] = v / dss;
     }
+}
+
+// dk and dv of a key: the sum of the splits, four channels a lane.
+template <class Op>
+__global__ __launch_bounds__(kThreads) void dkdv_join(AttnArgs a)
+{
+    const int per = a.D / 2;  // lanes a key
+    const int64_t keys = (int64_t)a.B * a.Hkv * a.Lk, id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int64_t key = id / per;
+    if (key >= keys)
+        return;
+    const int d = (int)(id - key * per) * 4;
+    typedef float v4 __attribute__((ext_vector_type(4)));
+    v4 v = {0, 0, 0, 0};
+    for (int s = 0; s < a.splits; ++s)
+        v += *(const v4 *)(a.part + (s * keys + key) * 2 * a.D + d);
+    const int64_t kv = key / a.Lk, j = key - kv * a.Lk, b = kv / a.Hkv, hk = kv - b * a.Hkv;
+    char *const p = d < a.D ? a.dk + b * a.dk_sb + hk * a.dk_sh + j * a.dk_st : a.dv + b * a.dv_sb + hk * a.dv_sh + j * a.dv_st;
+    typedef typename Op::elem V __attribute__((ext_vector_type(4)));
+    V o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        o[e] = (typename Op::elem)v[e];
+    *(V *)(p + (d < a.D ? d : d - a.D) * sizeof(typename Op::elem)) = o;
 }
 
 // dstrip[h][x]: the sum of `n` partial strips, 64 entries a workgroup, each
@@ -655,15 +766,24 @@ hipError_t run(const AttnArgs &a, float *dstrip, hipStream_t st)
     if (lds_kv && (e = hipFuncSetAttribute((const void *)attn_dkdv<Op, DP>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                            16 << 10)) != hipSuccess)
         return e;
-    if (lds_q && (e = hipFuncSetAttribute((const void *)attn_dq<Op, DP>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                          84 << 10)) != hipSuccess)
+    if (lds_q && (e = hipFuncSetAttribute(
+                      a.R ? (const void *)attn_dq<Op, DP, true> : (const void *)attn_dq<Op, DP, false>,
+                      hipFuncAttributeMaxDynamicSharedMemorySize, 84 << 10)) != hipSuccess)
         return e;
     b.tiles = (a.Lk + kHeld - 1) / kHeld;
-    if (a.B * b.tiles)
-        attn_dkdv<Op, DP><<<(uint32_t)(a.B * a.Hkv) * b.tiles, kThreads, lds_kv, st>>>(b);
+    if (a.B * b.tiles) {
+        b.splits = dkdv_splits(a.B, a.Lq, a.Lk, a.H, a.Hkv);
+        b.part = a.part + (dstrip ? strip_part_floats(a.B, a.Lq, a.H, a.R) : 0);
+        attn_dkdv<Op, DP><<<(uint32_t)(a.B * a.Hkv) * b.tiles * b.splits, kThreads, lds_kv, st>>>(b);
+        const int64_t lanes = (int64_t)a.B * a.Hkv * a.Lk * (a.D / 2);
+        if (b.splits > 1)
+            dkdv_join<Op><<<(uint32_t)((lanes + kThreads - 1) / kThreads), kThreads, 0, st>>>(b);
+        b.part = a.part;
+    }
     b.tiles = (a.Lq + kHeld - 1) / kHeld;
     if (a.B * b.tiles)
-        attn_dq<Op, DP><<<(uint32_t)(a.B * a.H) * b.tiles, kThreads, lds_q, st>>>(b, dstrip != nullptr);
+        (a.R ? attn_dq<Op, DP, true> : attn_dq<Op, DP, false>)<<<(uint32_t)(a.B * a.H) * b.tiles, kThreads, lds_q, st>>>(
+            b, dstrip != nullptr);
     if (dstrip)
         strip_reduce<<<dim3((uint32_t)((width + 63) / 64), (uint32_t)a.H), kThreads, 0, st>>>(a.part, dstrip,
                                                                                            a.B * b.tiles, width);
@@ -686,9 +806,8 @@ int64_t attn_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, in
 {
     if (!backward)
         return attn_few_rows(B, Lq, Lk, H, Hkv) ? attn_decode_part_bytes(dt, B, Lq, Lk, H, Hkv, D) : 0;
-    if (R == 0)
-        return 0;
-    return B * H * ((Lq + kHeld - 1) / kHeld) * (2 * R + 1) * 4;
+    const int64_t splits = dkdv_splits(B, Lq, Lk, H, Hkv);
+    return (strip_part_floats(B, Lq, H, R) + (splits > 1 ? splits * B * Hkv * Lk * 2 * D : 0)) * 4;
 }
 
 hipError_t launch_attn_backward(const AttnArgs &a, int dt, float *dstrip, hipStream_t st)

@@ -99,7 +99,7 @@ __global__ __launch_bounds__(64 * (Dec<Op, DP>::kNW)) void attn_decode(AttnArgs 
         tp.lim = live ? lim : INT32_MAX;
         tp.doc = doc;
         tp.kdoc = a.k_doc + (int64_t)b * a.Lk + k0;
-        tp.near = false;
+        tp.near = tp.inner = false;
         tp.far = 0;
         if (a.R) {
             const bool left = k0 + F::kKeys - 1 - plo <= -a.R, right = k0 - phi >= a.R;
@@ -108,8 +108,8 @@ __global__ __launch_bounds__(64 * (Dec<Op, DP>::kNW)) void attn_decode(AttnArgs 
         }
         const int d0 = k0 + 4 * h - pos;
         if (!skip)
-            attend<Op, DP, 1>(slot, slot + F::kTileBytes, q, st, sc, tp, lane, [&](int, int r) {
-                return strip[min(max(d0 + reg_row(r), -a.R), a.R) + a.R] * kLog2e;
+            attend<Op, DP, 1>(slot, slot + F::kTileBytes, q, st, sc, tp, lane, [&](int x, bool) {
+                return strip[min(max(d0 + x, -a.R), a.R) + a.R] * kLog2e;
             });
         // the slot is read before the next loads are started into it
         __builtin_amdgcn_s_waitcnt(0xC07F);

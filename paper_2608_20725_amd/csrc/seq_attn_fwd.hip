@@ -29,10 +29,9 @@ __global__ __launch_bounds__(64 * kWaves, (OpInfo<Op>::kIs32 && DP == 128 ? 1 : 
     __shared__ int shared_most[kWaves], shared_lo[kWaves], shared_hi[kWaves];
     extern __shared__ __align__(16) float strip[];  // 2R+1, times log2(e); documents: a bit for each key tile
 
-    uint32_t qt;
-    const uint32_t bh = work_item((uint32_t)(a.B * a.H) * a.tiles, a.tiles, &qt);
-    qt = a.tiles - 1 - qt;  // long rows of causal masks first
-    const int b = bh / a.H, hq = bh - b * a.H, hk = hq / a.G;
+    const Work work = work_item(a.B * a.Hkv, a.G, a.tiles, a.causal, blockIdx.x);
+    const int qt = a.tiles - 1 - work.tile;  // long rows of causal masks first
+    const int b = work.kv / a.Hkv, hk = work.kv - b * a.Hkv, hq = hk * a.G + work.g;
     const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = qt * kHeld + wave * 32 + (lane & 31);  // this lane's query
     const bool live = i < a.Lq;
@@ -115,17 +114,18 @@ __global__ __launch_bounds__(64 * kWaves, (OpInfo<Op>::kIs32 && DP == 128 ? 1 : 
         tp.lim = live ? lim : INT32_MAX;
         tp.doc = doc;
         tp.kdoc = doc_ids;
-        tp.near = false;
+        tp.near = tp.inner = false;
         tp.far = 0;
         if (a.R) {
             const bool left = k0 + F::kKeys - 1 - plo <= -a.R, right = k0 - phi >= a.R;
             tp.near = !left && !right;
+            tp.inner = k0 - phi >= -a.R && k0 + F::kKeys - 1 - plo <= a.R;
             if (!tp.near)
                 tp.far = strip[right ? 2 * a.R : 0];
         }
         const int d0 = k0 + 4 * h - pos;
-        attend<Op, DP, F::kSub>(slot, slot + F::kTileBytes, q, st, sc, tp, lane, [&](int x, int r) {
-            return strip[min(max(d0 + 32 * x + reg_row(r), -a.R), a.R) + a.R];
+        attend<Op, DP, F::kSub>(slot, slot + F::kTileBytes, q, st, sc, tp, lane, [&](int x, bool clamp) {
+            return strip[(clamp ? min(max(d0 + x, -a.R), a.R) : d0 + x) + a.R];
         });
         return next;
     };
