@@ -151,48 +151,71 @@ struct Tile {
             return (row >> 1) & 7;
     }
 
-    // Elements 16*s + 8*h .. +7 of a row: A or B operand of step s.
-    __device__ static inline typename Op::v8 row_frag(const char *t, int row, int s, int h)
+    // Offset of lane `lane` for row_frag: its row (lane & 31) and the place of
+    // its first chunk.  Chunks that differ only in bits below kXor bytes lie
+    // at offsets that differ in the same bits, the others further on.
+    static constexpr int kXor = kElt == 2 ? (kChunks % 16 == 0 ? 256 : kChunks == 8 ? 128 : 64) : kChunks % 16 == 0 ? 256 : 128;
+    __device__ static inline uint32_t row_offset(int lane)
     {
-        const char *p = t + row * kRowBytes;
-        const int z = swz(row);
+        const int row = lane & 31, first = (lane >> 5) * (kElt / 2);
+        return row * kRowBytes + ((first ^ swz(row)) << 4);
+    }
+    __device__ static inline const char *place(const char *t, uint32_t off, int bytes)
+    {
+        return t + ((off ^ (bytes % kXor)) + bytes / kXor * kXor);
+    }
+
+    // Elements 16*s + 8*h .. +7 of row 32*sub + (lane & 31): A or B operand of
+    // step s; `off` = row_offset.
+    __device__ static inline typename Op::v8 row_frag(const char *t, uint32_t off, int sub, int s)
+    {
+        t += 32 * sub * kRowBytes;
         if constexpr (kElt == 2) {
-            return *(const typename Op::v8 *)(p + (((2 * s + h) ^ z) << 4));
+            return *(const typename Op::v8 *)place(t, off, 32 * s);
         } else {
             typedef float v4 __attribute__((ext_vector_type(4)));
-            const v4 a = *(const v4 *)(p + (((4 * s + 2 * h) ^ z) << 4));
-            const v4 b = *(const v4 *)(p + (((4 * s + 2 * h + 1) ^ z) << 4));
+            const v4 a = *(const v4 *)place(t, off, 64 * s), b = *(const v4 *)place(t, off, 64 * s + 16);
             return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
         }
     }
 
-    // Channel d = 32*dt + (lane & 31) of the streamed tokens row0 + 4*h +
-    // {0..3, 8..11}: A operand over the transposed tile (row0 a multiple of 16).
-    __device__ static inline typename Op::v8 col_frag(const char *t, int row0, int dt, int lane)
+    // Offset of a lane for col_frag.  16 bits: 16 lanes read 4 rows x 16
+    // channels, 8 bytes each, of which lane a receives channel a of the four
+    // rows.  fp32: a lane reads its channel of row 4*h.
+    __device__ static inline uint32_t col_offset(int lane)
     {
         const int h = lane >> 5;
         if constexpr (kElt == 2) {
+            const int a = lane & 15, row = 4 * h + (a >> 2), c = 2 * ((lane >> 4) & 1) + ((a & 3) >> 1);
+            return row * kRowBytes + ((c ^ swz(row)) << 4) + (a & 1) * 8;
+        } else {
+            const int d = lane & 31;
+            return 4 * h * kRowBytes + (((d >> 2) ^ swz(4 * h)) << 4) + (d & 3) * 4;
+        }
+    }
+
+    // Channel d = 32*dt + (lane & 31) of the streamed tokens row0 + 4*h +
+    // {0..3, 8..11}: A operand over the transposed tile (row0 a multiple of
+    // 16); `off` = col_offset.
+    __device__ static inline typename Op::v8 col_frag(const char *t, uint32_t off, int row0, int dt)
+    {
+        t += row0 * kRowBytes;
+        if constexpr (kElt == 2) {
             typedef short s4 __attribute__((ext_vector_type(4)));
             typedef __attribute__((address_space(3))) s4 lds_s4;
-            // 16 lanes read 4 rows x 16 channels, 8 bytes each; lane a gets
-            // channel a of the four rows
-            const int a = lane & 15;
-            const int row = row0 + 4 * h + (a >> 2);
-            const int c = 4 * dt + 2 * ((lane >> 4) & 1) + ((a & 3) >> 1);
-            const char *const p = t + row * kRowBytes + (a & 1) * 8;
-            const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(p + ((c ^ swz(row)) << 4)));
+            // 8 rows on, bit 1 of the chunk permutation differs
+            const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)place(t, off, 64 * dt));
             const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lds_s4 *)(p + 8 * kRowBytes + ((c ^ swz(row + 8)) << 4)));
+                (lds_s4 *)(place(t, off ^ 32, 64 * dt) + 8 * kRowBytes));
             typedef short s8 __attribute__((ext_vector_type(8)));
             const s8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
             return __builtin_bit_cast(typename Op::v8, v);
         } else {
-            const int d = 32 * dt + (lane & 31);
             typename Op::v8 v;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int row = row0 + 8 * (e >> 2) + 4 * h + (e & 3);
-                v[e] = *(const float *)(t + row * kRowBytes + (((d >> 2) ^ swz(row)) << 4) + (d & 3) * 4);
+                const int row = 8 * (e >> 2) + (e & 3);  // + 4*h: its bits of the permutation are in `off`
+                v[e] = *(const float *)(place(t, off ^ (swz(row) << 4), 128 * dt) + row * kRowBytes);
             }
             return v;
         }
@@ -336,44 +359,86 @@ struct TilePairs {
     const int *kdoc;   // documents of the tile's keys
 };
 
+// Runs use(i, fragments of step i) for N steps of G fragments from LDS.
+// AHEAD: each step's fragments are read while the step before it runs on the
+// matrix cores, and buf[0] holds step 0 on entry.  Left to itself the compiler
+// reads every fragment right before its product and waits for it, which costs
+// a kernel of one wave a SIMD 12 % (the dk/dv kernel, D = 128); where two or
+// more waves share a SIMD they fill each other's waits, and the registers are
+// worth more.
+template <class Op, bool AHEAD, int N, int G, class Load, class Use>
+__device__ inline void pipeline(typename Op::v8 (&buf)[2][G], Load load, Use use)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if constexpr (AHEAD) {
+            if (i + 1 < N)
+                load(i + 1, buf[(i + 1) & 1]);
+            __builtin_amdgcn_sched_barrier(0);
+            use(i, buf[i & 1]);
+        } else {
+            load(i, buf[0]);
+            use(i, buf[0]);
+        }
+    }
+}
+
+// Keeps what follows from x inside the loop it stands in: the fragments'
+// addresses cost one xor each, and as loop constants a register each.
+__device__ inline uint32_t opaque(uint32_t x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// Which scores a kernel instance handles: products alone, capped ones, or
+// whatever the arguments say (a bias; fp32).  The first two leave out the
+// branches and registers of the rest.
+enum Feat { kPlain = 0, kCapped = 1, kAny = 2 };
+
 // One tile of 32*SUB keys: s = K q, the softmax's update, o += V^T p.
 // near(x, clamp): bias of key x + 4*h of the tile, its distance clamped to the
 // strip if `clamp`.
-template <class Op, int DP, int SUB, class Near>
+template <class Op, int DP, int SUB, int FEAT, class Near>
 __device__ inline void attend(const char *tk, const char *tv, const typename Op::v8 (&q)[DP / 16], RowState<Op, DP> &st,
                               const ScoreArgs &sc, const TilePairs &tp, int lane, Near near)
 {
     typedef Tile<Op, DP> T;
     typedef RowState<Op, DP> S;
+    typedef typename Op::v8 V8;
     const int h = lane >> 5;
+    const uint32_t roff = opaque(T::row_offset(lane)), coff = opaque(T::col_offset(lane));
+    const bool cap = FEAT == kAny ? sc.cap : FEAT == kCapped;
     f32x16_acc s[SUB];
 #pragma unroll
-    for (int t = 0; t < SUB; ++t) {
+    for (int t = 0; t < SUB; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
             s[t][r] = 0;
 #pragma unroll
-        for (int x = 0; x < DP / 16; ++x)
-            s[t] = Op::mfma(T::row_frag(tk, 32 * t + (lane & 31), x, h), q[x], s[t]);
-    }
-    float mul = sc.c1, add = tp.far;
-    if (sc.cap || tp.near || tp.partial || !(sc.c1 > 0)) {
+    for (int x = 0; x < DP / 16; ++x)
+#pragma unroll
+        for (int t = 0; t < SUB; ++t)
+            s[t] = Op::mfma(T::row_frag(tk, roff, t, x), q[x], s[t]);
+
+    float mul = sc.c1, add = FEAT == kAny ? tp.far : 0.0f;
+    if (cap || (FEAT == kAny && tp.near) || tp.partial || !(sc.c1 > 0)) {
         // scores one by one; else the maximum is taken of the products and
         // one fused multiply-add scales a score and subtracts the maximum
-        if (sc.cap) {
+        if (cap) {
 #pragma unroll
             for (int t = 0; t < SUB; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    s[t][r] = fmaf(sc.c2, fast_tanh(s[t][r] * sc.c1), tp.far);
+                    s[t][r] = fmaf(sc.c2, fast_tanh(s[t][r] * sc.c1), add);
         } else {
 #pragma unroll
             for (int t = 0; t < SUB; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    s[t][r] = fmaf(s[t][r], sc.c1, tp.far);
+                    s[t][r] = fmaf(s[t][r], sc.c1, add);
         }
-        if (tp.near) {
+        if (FEAT == kAny && tp.near) {
             if (tp.inner) {
 #pragma unroll
                 for (int t = 0; t < SUB; ++t)
@@ -405,12 +470,17 @@ __device__ inline void attend(const char *tk, const char *tv, const typename Op:
         mul = 1.0f;
         add = 0.0f;
     }
-    float top = s[0][0];
+    // four maxima and sums at a time: no chain of 32 dependent operations
+    float m4[4], l4[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+        m4[x] = s[0][x];
 #pragma unroll
     for (int t = 0; t < SUB; ++t)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-            top = fmaxf(top, s[t][r]);
+        for (int r = t ? 0 : 4; r < 16; ++r)
+            m4[r & 3] = fmaxf(m4[r & 3], s[t][r]);
+    float top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
     top = pair_max(fmaf(top, mul, add));
     if (__any(top > st.m + S::kSlack)) {
         // each row by its own scores alone: what a row gives does not depend
@@ -425,23 +495,30 @@ __device__ inline void attend(const char *tk, const char *tv, const typename Op:
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], mul, sub));
-            st.l += s[t][r];
+            l4[r & 3] = t == 0 && r < 4 ? s[t][r] : l4[r & 3] + s[t][r];
         }
+    st.l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+
+    if (!tp.partial) {
+#pragma unroll
+        for (int i = 0; i < 2 * SUB; ++i) {
+            const V8 p = pack8<Op>(s[i >> 1], 8 * (i & 1));
+#pragma unroll
+            for (int dt = 0; dt < DP / 32; ++dt)
+                st.o[dt] = Op::mfma(T::col_frag(tv, coff, 16 * i, dt), p, st.o[dt]);
+        }
+        return;
+    }
+    // a value of a left-out pair times its zero must stay zero
     uint32_t bad = 0;
 #pragma unroll
-    for (int t = 0; t < SUB; ++t)
+    for (int i = 0; i < 2 * SUB; ++i) {
+        const V8 p = pack8<Op>(s[i >> 1], 8 * (i & 1));
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            const typename Op::v8 p = pack8<Op>(s[t], 8 * ks);
-#pragma unroll
-            for (int dt = 0; dt < DP / 32; ++dt) {
-                typename Op::v8 v = T::col_frag(tv, 32 * t + 16 * ks, dt, lane);
-                if (tp.partial)  // a value of a left-out pair times its zero must stay zero
-                    v = finite<Op>(v, bad);
-                st.o[dt] = Op::mfma(v, p, st.o[dt]);
-            }
-        }
-    if (tp.partial && __any(bad)) {
+        for (int dt = 0; dt < DP / 32; ++dt)
+            st.o[dt] = Op::mfma(finite<Op>(T::col_frag(tv, coff, 16 * i, dt), bad), p, st.o[dt]);
+    }
+    if (__any(bad)) {
         // values that are not finite reach the queries that see them
         for (int kk = 0; kk < 32 * SUB; ++kk) {
             if (tp.k0 + kk >= tp.lim || (tp.docs_differ && tp.kdoc[kk] != tp.doc))

@@ -175,10 +175,10 @@ __global__ __launch_bounds__(kThreads) void value_norms(AttnArgs a)
 // Exponents of the probabilities (base 2), without the bias: the scores of
 // the products in s less lse(r), the row statistic of register r; slope:
 // 1 - tanh^2 where scores are capped.
-template <class Lse>
+template <int FEAT, class Lse>
 __device__ inline void to_scores(f32x16_acc &s, f32x16_acc &slope, const ScoreArgs &c, Lse lse)
 {
-    if (c.cap) {
+    if (FEAT == kAny ? c.cap : FEAT == kCapped) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const float t = fast_tanh(s[r] * c.c1);
@@ -198,14 +198,19 @@ struct Bwd {
     static constexpr int kRows = OpInfo<Op>::kIs32 ? 32 : 64;  // streamed tokens a tile
     static constexpr int kSub = kRows / 32;
     static constexpr int kTileBytes = kRows * T::kRowBytes;
+    // waves a SIMD to fit in, and whether the dk/dv kernel, alone on its SIMD
+    // with more than 256 registers, reads fragments ahead
+    static constexpr int kOccKV = T::kRowBytes <= 128 ? 2 : 1, kOccQ = T::kRowBytes <= 256 ? 2 : 1;
+    static constexpr bool kAhead = kOccKV == 1 && !OpInfo<Op>::kIs32;
 };
 
 // ---- dk, dv: a key per lane ----
-template <class Op, int DP>
-__global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 128 ? 2 : 1)) void attn_dkdv(AttnArgs a)
+template <class Op, int DP, int FEAT>
+__global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccKV)) void attn_dkdv(AttnArgs a)
 {
     typedef Bwd<Op, DP> W;
     typedef Tile<Op, DP> T;
+    typedef typename Op::v8 V8;
     // two slots of a tile of q and dout, and of their rows' statistics; each
     // an array of its own: the compiler can tell that reading one does not
     // wait for the loads that land in the other
@@ -311,20 +316,46 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 128 ? 2 : 1)) v
             const bool docs_differ = a.k_doc && (dr.mixed || dlo != dhi || dr.lo != dlo);
             const bool partial = q0 < most || docs_differ;
             const char *const tq = slot, *const tdo = slot + W::kTileBytes;
+            const uint32_t roff = opaque(T::row_offset(lane)), coff = opaque(T::col_offset(lane));
 #pragma unroll
             for (int t = 0; t < W::kSub; ++t) {
                 f32x16_acc s, dp, slope;
+                const float *const lse = rows + 32 * t + 4 * h, *const delta = lse + 64;  // of row reg_row(r)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     s[r] = dp[r] = 0;
+                {
+                    V8 buf[2][4];  // two steps of 16 channels, q and dout
+                    auto load = [&](int i, V8(&f)[4]) {
 #pragma unroll
-                for (int st = 0; st < DP / 16; ++st) {
-                    s = Op::mfma(T::row_frag(tq, 32 * t + (lane & 31), st, h), kf[st], s);
-                    dp = Op::mfma(T::row_frag(tdo, 32 * t + (lane & 31), st, h), vf[st], dp);
+                        for (int x = 0; x < 2; ++x) {
+                            f[2 * x] = T::row_frag(tq, roff, t, 2 * i + x);
+                            f[2 * x + 1] = T::row_frag(tdo, roff, t, 2 * i + x);
+                        }
+                    };
+                    if constexpr (W::kAhead)
+                        load(0, buf[0]);
+                    pipeline<Op, W::kAhead, DP / 32, 4>(buf, load, [&](int i, const V8(&f)[4]) {
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            s = Op::mfma(f[2 * x], kf[2 * i + x], s);
+                            dp = Op::mfma(f[2 * x + 1], vf[2 * i + x], dp);
+                        }
+                    });
                 }
-                to_scores(s, slope, sc, [&](int r) { return rows[32 * t + reg_row(r) + 4 * h]; });
+                // 16 rows and 32 channels of dout and q a step
+                V8 cbuf[2][2];
+                auto cload = [&](int i, V8(&c)[2]) {
+                    c[0] = T::col_frag(tdo, coff, 32 * t + 16 * (i / (DP / 32)), i % (DP / 32));
+                    c[1] = T::col_frag(tq, coff, 32 * t + 16 * (i / (DP / 32)), i % (DP / 32));
+                };
+                if constexpr (W::kAhead) {
+                    cload(0, cbuf[0]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                to_scores<FEAT>(s, slope, sc, [&](int r) { return lse[reg_row(r)]; });
                 const int i0 = q0 + 32 * t;
-                if (a.R) {
+                if (FEAT == kAny && a.R) {
                     const int dmin = jlo - (i0 + 31 + off), dmax = jhi - (i0 + off);
                     if (dmax <= -a.R || dmin >= a.R) {
                         const float far = strip[dmin >= a.R ? 2 * a.R : 0];
@@ -345,44 +376,50 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 128 ? 2 : 1)) v
                 }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int row = 32 * t + reg_row(r) + 4 * h;
                     s[r] = __builtin_amdgcn_exp2f(s[r]);
-                    float d = dp[r] - rows[64 + row];
+                    float d = dp[r] - delta[reg_row(r)];
                     if constexpr (p_shift<Op>() > 0)
                         d *= f;
                     dp[r] = s[r] * d;
                 }
-                if (sc.cap)
+                if (FEAT == kAny ? sc.cap : FEAT == kCapped)
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
                         dp[r] *= slope[r];
-                if (partial) {
-                    const int lim = first == INT32_MAX ? INT32_MAX : first - i0 - 4 * h;
+                if (!partial) {
+                    V8 p, ds;
+                    pipeline<Op, W::kAhead, 2 * (DP / 32), 2>(cbuf, cload, [&](int i, const V8(&c)[2]) {
+                        constexpr int N = DP / 32;
+                        if (i % N == 0) {
+                            p = pack8<Op>(s, 8 * (i / N));
+                            ds = pack8<Op>(dp, 8 * (i / N));
+                        }
+                        dv[i % N] = Op::mfma(c[0], p, dv[i % N]);
+                        dk[i % N] = Op::mfma(c[1], ds, dk[i % N]);
+                    });
+                    continue;
+                }
+                const int lim = first == INT32_MAX ? INT32_MAX : first - i0 - 4 * h;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int row = 32 * t + reg_row(r) + 4 * h;
-                        const bool out = reg_row(r) < lim || (docs_differ && __float_as_int(rows[128 + row]) != doc);
-                        // a dout that is not finite reaches dv through p
-                        s[r] = out ? 0.0f : s[r] + 0.0f * rows[64 + row];
-                        dp[r] = out ? 0.0f : dp[r];
-                    }
+                for (int r = 0; r < 16; ++r) {
+                    const bool out = reg_row(r) < lim ||
+                                     (docs_differ && __float_as_int(rows[128 + 32 * t + reg_row(r) + 4 * h]) != doc);
+                    // a dout that is not finite reaches dv through p
+                    s[r] = out ? 0.0f : s[r] + 0.0f * delta[reg_row(r)];
+                    dp[r] = out ? 0.0f : dp[r];
                 }
                 uint32_t bad = 0;
-#pragma unroll
-                for (int ks = 0; ks < 2; ++ks) {
-                    const typename Op::v8 p = pack8<Op>(s, 8 * ks), ds = pack8<Op>(dp, 8 * ks);
-#pragma unroll
-                    for (int dt = 0; dt < DP / 32; ++dt) {
-                        typename Op::v8 x1 = T::col_frag(tdo, 32 * t + 16 * ks, dt, lane);
-                        typename Op::v8 y1 = T::col_frag(tq, 32 * t + 16 * ks, dt, lane);
-                        if (partial) {  // a left-out pair's zero times infinity or NaN must stay zero
-                            x1 = finite<Op>(x1, bad);
-                            y1 = finite<Op>(y1, bad);
-                        }
-                        dv[dt] = Op::mfma(x1, p, dv[dt]);
-                        dk[dt] = Op::mfma(y1, ds, dk[dt]);
+                V8 p, ds;
+                pipeline<Op, W::kAhead, 2 * (DP / 32), 2>(cbuf, cload, [&](int i, const V8(&c)[2]) {
+                    constexpr int N = DP / 32;
+                    if (i % N == 0) {
+                        p = pack8<Op>(s, 8 * (i / N));
+                        ds = pack8<Op>(dp, 8 * (i / N));
                     }
-                }
+                    // a left-out pair's zero times infinity or NaN must stay zero
+                    dv[i % N] = Op::mfma(finite<Op>(c[0], bad), p, dv[i % N]);
+                    dk[i % N] = Op::mfma(finite<Op>(c[1], bad), ds, dk[i % N]);
+                });
             }
             return next;
         };
@@ -390,7 +427,7 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 128 ? 2 : 1)) v
         int t = after(t_begin);
         if (t < t_end)
             issue(slot0, rows0, t);
-        if (a.R) {
+        if (FEAT == kAny && a.R) {
             for (int x = threadIdx.x; x < 2 * a.R + 1; x += kThreads)
                 strip[x] = a.strip[(int64_t)hq * (2 * a.R + 1) + x] * kLog2e;
             ring_barrier();
@@ -458,12 +495,12 @@ __device__ inline void diagonal_sums(const f32x16_acc &v, f32x4_acc &sum)
     sum[2] = c;
 }
 
-// BIAS = false (no strip) leaves the registers of its paths to the rest.
-template <class Op, int DP, bool BIAS>
-__global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 256 ? 2 : 1)) void attn_dq(AttnArgs a, int want_strip)
+template <class Op, int DP, int FEAT>
+__global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccQ)) void attn_dq(AttnArgs a, int want_strip)
 {
     typedef Bwd<Op, DP> W;
     typedef Tile<Op, DP> T;
+    typedef typename Op::v8 V8;
     __shared__ __align__(16) char slot0[2 * W::kTileBytes];
     __shared__ __align__(16) char slot1[2 * W::kTileBytes];
     __shared__ int kdoc0[64], kdoc1[64];
@@ -500,7 +537,7 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 256 ? 2 : 1)) v
     // summed in an order that could change
     float *const grad = strip + width * (1 + 2 * wave + h);
     float far_lo = 0, far_hi = 0;
-    if (BIAS)
+    if (FEAT == kAny && a.R)
         for (int t = threadIdx.x; t < width; t += kThreads) {
             strip[t] = a.strip[(int64_t)hq * width + t] * kLog2e;
             if (want_strip)
@@ -574,6 +611,7 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 256 ? 2 : 1)) v
         if (a.q_doc)
             dr = ranges[k0 / kDocTile];
         const char *const tk = slot, *const tv = slot + W::kTileBytes;
+        const uint32_t roff = opaque(T::row_offset(lane)), coff = opaque(T::col_offset(lane));
         if (k0 >= most || (a.q_doc && !(dr.lo <= dhi && dr.hi >= dlo)))
             return next;
         const bool docs_differ = a.q_doc && (dr.mixed || dlo != dhi || dr.lo != dlo);
@@ -584,15 +622,33 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 256 ? 2 : 1)) v
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 s[r] = dp[r] = 0;
+            {
+                V8 buf[2][4];  // two steps of 16 channels, k and v
+                auto load = [&](int i, V8(&c)[4]) {
 #pragma unroll
-            for (int x = 0; x < DP / 16; ++x) {
-                s = Op::mfma(T::row_frag(tk, 32 * t + (lane & 31), x, h), qf[x], s);
-                dp = Op::mfma(T::row_frag(tv, 32 * t + (lane & 31), x, h), dof[x], dp);
+                    for (int x = 0; x < 2; ++x) {
+                        c[2 * x] = T::row_frag(tk, roff, t, 2 * i + x);
+                        c[2 * x + 1] = T::row_frag(tv, roff, t, 2 * i + x);
+                    }
+                };
+                pipeline<Op, false, DP / 32, 4>(buf, load, [&](int i, const V8(&c)[4]) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        s = Op::mfma(c[2 * x], qf[2 * i + x], s);
+                        dp = Op::mfma(c[2 * x + 1], dof[2 * i + x], dp);
+                    }
+                });
             }
-            to_scores(s, slope, sc, [&](int) { return lse; });
+            V8 cbuf[2][DP / 32];  // 16 keys, all channels
+            auto cload = [&](int i, V8(&c)[DP / 32]) {
+#pragma unroll
+                for (int dt = 0; dt < DP / 32; ++dt)
+                    c[dt] = T::col_frag(tk, coff, 32 * t + 16 * i, dt);
+            };
+            to_scores<FEAT>(s, slope, sc, [&](int) { return lse; });
             const int j0 = k0 + 32 * t, d0 = j0 + 4 * h - pos;
-            const bool far = BIAS && (j0 + 31 - plo <= -a.R || j0 - phi >= a.R);
-            if (BIAS) {
+            const bool far = FEAT == kAny && a.R && (j0 + 31 - plo <= -a.R || j0 - phi >= a.R);
+            if (FEAT == kAny && a.R) {
                 if (far) {
                     const float v = strip[j0 - phi >= a.R ? 2 * a.R : 0];
 #pragma unroll
@@ -617,7 +673,7 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 256 ? 2 : 1)) v
                     ds = reg_row(r) >= last || (docs_differ && kdoc[32 * t + reg_row(r) + 4 * h] != doc) ? 0.0f : ds;
                 dp[r] = ds;
             }
-            if (BIAS && want_strip) {
+            if (FEAT == kAny && want_strip) {
                 if (far) {
                     float v = 0;
 #pragma unroll
@@ -641,22 +697,26 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 256 ? 2 : 1)) v
                     }
                 }
             }
-            if (sc.cap)
+            if (FEAT == kAny ? sc.cap : FEAT == kCapped)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     dp[r] *= slope[r];
-            uint32_t bad = 0;
+            if (!partial) {
+                pipeline<Op, false, 2, DP / 32>(cbuf, cload, [&](int i, const V8(&c)[DP / 32]) {
+                    const V8 ds = pack8<Op>(dp, 8 * i);
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                const typename Op::v8 ds = pack8<Op>(dp, 8 * ks);
-#pragma unroll
-                for (int dt = 0; dt < DP / 32; ++dt) {
-                    typename Op::v8 x = T::col_frag(tk, 32 * t + 16 * ks, dt, lane);
-                    if (partial)
-                        x = finite<Op>(x, bad);
-                    dq[dt] = Op::mfma(x, ds, dq[dt]);
-                }
+                    for (int dt = 0; dt < DP / 32; ++dt)
+                        dq[dt] = Op::mfma(c[dt], ds, dq[dt]);
+                });
+                continue;
             }
+            uint32_t bad = 0;
+            pipeline<Op, false, 2, DP / 32>(cbuf, cload, [&](int i, const V8(&c)[DP / 32]) {
+                const V8 ds = pack8<Op>(dp, 8 * i);
+#pragma unroll
+                for (int dt = 0; dt < DP / 32; ++dt)
+                    dq[dt] = Op::mfma(finite<Op>(c[dt], bad), ds, dq[dt]);
+            });
         }
         return next;
     };
@@ -671,7 +731,7 @@ __global__ __launch_bounds__(kThreads, (DP * OpInfo<Op>::kElt <= 256 ? 2 : 1)) v
     }
     if (live)
         store_row<Op, DP>(a.dq + b * a.dq_sb + hq * a.dq_sh + (int64_t)i * a.dq_st, dq, a.scale / dss, h, a.D);
-    if (!BIAS || !want_strip)
+    if (FEAT != kAny || !want_strip)
         return;
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) {
@@ -736,7 +796,7 @@ __global__ __launch_bounds__(kThreads) void strip_reduce(const float *__restrict
             (s[0][threadIdx.x] + s[1][threadIdx.x]) + (s[2][threadIdx.x] + s[3][threadIdx.x]);
 }
 
-template <class Op, int DP>
+template <class Op, int DP, int FEAT>
 hipError_t run(const AttnArgs &a, float *dstrip, hipStream_t st)
 {
     typedef Bwd<Op, DP> W;
@@ -763,18 +823,17 @@ hipError_t run(const AttnArgs &a, float *dstrip, hipStream_t st)
     const size_t bits_q = a.q_doc ? (a.Lq + 64 * W::kRows - 1) / (64 * W::kRows) * 8 : 0;
     const size_t lds_kv = (a.R ? (2 * a.R + 2) * 4 : 0) + bits_q;
     const size_t lds_q = strip_floats(a.R, dstrip != nullptr) * 4 + bits_k;
-    if (lds_kv && (e = hipFuncSetAttribute((const void *)attn_dkdv<Op, DP>, hipFuncAttributeMaxDynamicSharedMemorySize,
+    if (lds_kv && (e = hipFuncSetAttribute((const void *)attn_dkdv<Op, DP, FEAT>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                            16 << 10)) != hipSuccess)
         return e;
-    if (lds_q && (e = hipFuncSetAttribute(
-                      a.R ? (const void *)attn_dq<Op, DP, true> : (const void *)attn_dq<Op, DP, false>,
-                      hipFuncAttributeMaxDynamicSharedMemorySize, 84 << 10)) != hipSuccess)
+    if (lds_q && (e = hipFuncSetAttribute((const void *)attn_dq<Op, DP, FEAT>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                          84 << 10)) != hipSuccess)
         return e;
     b.tiles = (a.Lk + kHeld - 1) / kHeld;
     if (a.B * b.tiles) {
         b.splits = dkdv_splits(a.B, a.Lq, a.Lk, a.H, a.Hkv);
         b.part = a.part + (dstrip ? strip_part_floats(a.B, a.Lq, a.H, a.R) : 0);
-        attn_dkdv<Op, DP><<<(uint32_t)(a.B * a.Hkv) * b.tiles * b.splits, kThreads, lds_kv, st>>>(b);
+        attn_dkdv<Op, DP, FEAT><<<(uint32_t)(a.B * a.Hkv) * b.tiles * b.splits, kThreads, lds_kv, st>>>(b);
         const int64_t lanes = (int64_t)a.B * a.Hkv * a.Lk * (a.D / 2);
         if (b.splits > 1)
             dkdv_join<Op><<<(uint32_t)((lanes + kThreads - 1) / kThreads), kThreads, 0, st>>>(b);
@@ -782,7 +841,7 @@ hipError_t run(const AttnArgs &a, float *dstrip, hipStream_t st)
     }
     b.tiles = (a.Lq + kHeld - 1) / kHeld;
     if (a.B * b.tiles)
-        (a.R ? attn_dq<Op, DP, true> : attn_dq<Op, DP, false>)<<<(uint32_t)(a.B * a.H) * b.tiles, kThreads, lds_q, st>>>(
+        attn_dq<Op, DP, FEAT><<<(uint32_t)(a.B * a.H) * b.tiles, kThreads, lds_q, st>>>(
             b, dstrip != nullptr);
     if (dstrip)
         strip_reduce<<<dim3((uint32_t)((width + 63) / 64), (uint32_t)a.H), kThreads, 0, st>>>(a.part, dstrip,
@@ -790,13 +849,23 @@ hipError_t run(const AttnArgs &a, float *dstrip, hipStream_t st)
     return hipGetLastError();
 }
 
+template <class Op, int DP>
+hipError_t run_feat(const AttnArgs &a, float *dstrip, hipStream_t st)
+{
+    if constexpr (!OpInfo<Op>::kIs32) {
+        if (!a.R)
+            return a.cap > 0 ? run<Op, DP, kCapped>(a, dstrip, st) : run<Op, DP, kPlain>(a, dstrip, st);
+    }
+    return run<Op, DP, kAny>(a, dstrip, st);
+}
+
 template <class Op>
 hipError_t run_dim(const AttnArgs &a, float *dstrip, hipStream_t st)
 {
-    return a.D <= 32 ? run<Op, 32>(a, dstrip, st)
-         : a.D <= 64 ? run<Op, 64>(a, dstrip, st)
-         : a.D <= 96 ? run<Op, 96>(a, dstrip, st)
-                     : run<Op, 128>(a, dstrip, st);
+    return a.D <= 32 ? run_feat<Op, 32>(a, dstrip, st)
+         : a.D <= 64 ? run_feat<Op, 64>(a, dstrip, st)
+         : a.D <= 96 ? run_feat<Op, 96>(a, dstrip, st)
+                     : run_feat<Op, 128>(a, dstrip, st);
 }
 
 }  // namespace

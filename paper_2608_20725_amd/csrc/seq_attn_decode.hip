@@ -108,7 +108,7 @@ __global__ __launch_bounds__(64 * (Dec<Op, DP>::kNW)) void attn_decode(AttnArgs 
         }
         const int d0 = k0 + 4 * h - pos;
         if (!skip)
-            attend<Op, DP, 1>(slot, slot + F::kTileBytes, q, st, sc, tp, lane, [&](int x, bool) {
+            attend<Op, DP, 1, kAny>(slot, slot + F::kTileBytes, q, st, sc, tp, lane, [&](int x, bool) {
                 return strip[min(max(d0 + x, -a.R), a.R) + a.R] * kLog2e;
             });
         // the slot is read before the next loads are started into it

@@ -14,10 +14,11 @@ struct Fwd {
     static constexpr int kSub = OpInfo<Op>::kIs32 ? 1 : 2;
     static constexpr int kKeys = 32 * kSub;  // keys a tile
     static constexpr int kTileBytes = kKeys * T::kRowBytes;
+    static constexpr int kOcc = T::kRowBytes <= 128 ? 3 : T::kRowBytes <= 256 ? 2 : 1;  // waves a SIMD to fit in
 };
 
-template <class Op, int DP>
-__global__ __launch_bounds__(64 * kWaves, (OpInfo<Op>::kIs32 && DP == 128 ? 1 : 2)) void attn_fwd(AttnArgs a)
+template <class Op, int DP, int FEAT>
+__global__ __launch_bounds__(64 * kWaves, (Fwd<Op, DP>::kOcc)) void attn_fwd(AttnArgs a)
 {
     typedef Fwd<Op, DP> F;
     typedef Tile<Op, DP> T;
@@ -58,7 +59,7 @@ __global__ __launch_bounds__(64 * kWaves, (OpInfo<Op>::kIs32 && DP == 128 ? 1 : 
         shared_lo[wave] = dlo;
         shared_hi[wave] = dhi;
     }
-    if (a.R)
+    if (FEAT == kAny && a.R)
         for (int t = threadIdx.x; t < 2 * a.R + 1; t += 64 * kWaves)
             strip[t] = a.strip[(int64_t)hq * (2 * a.R + 1) + t] * kLog2e;
     __syncthreads();
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(64 * kWaves, (OpInfo<Op>::kIs32 && DP == 128 ? 1 : 
         tp.kdoc = doc_ids;
         tp.near = tp.inner = false;
         tp.far = 0;
-        if (a.R) {
+        if (FEAT == kAny && a.R) {
             const bool left = k0 + F::kKeys - 1 - plo <= -a.R, right = k0 - phi >= a.R;
             tp.near = !left && !right;
             tp.inner = k0 - phi >= -a.R && k0 + F::kKeys - 1 - plo <= a.R;
@@ -124,7 +125,7 @@ __global__ __launch_bounds__(64 * kWaves, (OpInfo<Op>::kIs32 && DP == 128 ? 1 : 
                 tp.far = strip[right ? 2 * a.R : 0];
         }
         const int d0 = k0 + 4 * h - pos;
-        attend<Op, DP, F::kSub>(slot, slot + F::kTileBytes, q, st, sc, tp, lane, [&](int x, bool clamp) {
+        attend<Op, DP, F::kSub, FEAT>(slot, slot + F::kTileBytes, q, st, sc, tp, lane, [&](int x, bool clamp) {
             return strip[(clamp ? min(max(d0 + x, -a.R), a.R) : d0 + x) + a.R];
         });
         return next;
@@ -163,30 +164,40 @@ __global__ __launch_bounds__(64) void doc_ranges(const int32_t *__restrict__ doc
         out[blockIdx.x] = DocRange{lo, hi, least != hi, 0};
 }
 
-template <class Op, int DP>
+template <class Op, int DP, int FEAT>
 hipError_t run(const AttnArgs &a, hipStream_t st)
 {
     typedef Fwd<Op, DP> F;
     const size_t lds = (a.R ? (2 * a.R + 2) * 4 : 0) + (a.q_doc ? (a.Lk + 64 * F::kKeys - 1) / (64 * F::kKeys) * 8 : 0);
     if (lds) {
-        const hipError_t e = hipFuncSetAttribute((const void *)attn_fwd<Op, DP>, hipFuncAttributeMaxDynamicSharedMemorySize,
+        const hipError_t e = hipFuncSetAttribute((const void *)attn_fwd<Op, DP, FEAT>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                                  16 << 10);
         if (e != hipSuccess)
             return e;
     }
     AttnArgs b = a;
     b.tiles = (a.Lq + kHeld - 1) / kHeld;
-    attn_fwd<Op, DP><<<(uint32_t)(a.B * a.H) * b.tiles, 64 * kWaves, lds, st>>>(b);
+    attn_fwd<Op, DP, FEAT><<<(uint32_t)(a.B * a.H) * b.tiles, 64 * kWaves, lds, st>>>(b);
     return hipGetLastError();
+}
+
+template <class Op, int DP>
+hipError_t run_feat(const AttnArgs &a, hipStream_t st)
+{
+    if constexpr (!OpInfo<Op>::kIs32) {
+        if (!a.R)
+            return a.cap > 0 ? run<Op, DP, kCapped>(a, st) : run<Op, DP, kPlain>(a, st);
+    }
+    return run<Op, DP, kAny>(a, st);
 }
 
 template <class Op>
 hipError_t run_dim(const AttnArgs &a, hipStream_t st)
 {
-    return a.D <= 32 ? run<Op, 32>(a, st)
-         : a.D <= 64 ? run<Op, 64>(a, st)
-         : a.D <= 96 ? run<Op, 96>(a, st)
-                     : run<Op, 128>(a, st);
+    return a.D <= 32 ? run_feat<Op, 32>(a, st)
+         : a.D <= 64 ? run_feat<Op, 64>(a, st)
+         : a.D <= 96 ? run_feat<Op, 96>(a, st)
+                     : run_feat<Op, 128>(a, st);
 }
 
 }  // namespace
