@@ -124,6 +124,13 @@ __device__ inline typename Op::v8 pack8(const f32x16_acc &a, int first)
     return v;
 }
 
+template <class Op>
+__device__ inline void pack16(const f32x16_acc &a, typename Op::v8 (&v)[2])
+{
+    v[0] = pack8<Op>(a, 0);
+    v[1] = pack8<Op>(a, 8);
+}
+
 // One streamed tile in LDS: ROWS tokens of DP channels.
 template <class Op, int DP>
 struct Tile {
@@ -361,11 +368,11 @@ struct TilePairs {
 
 // Runs use(i, fragments of step i) for N steps of G fragments from LDS.
 // AHEAD: each step's fragments are read while the step before it runs on the
-// matrix cores, and buf[0] holds step 0 on entry.  Left to itself the compiler
-// reads every fragment right before its product and waits for it, which costs
-// a kernel of one wave a SIMD 12 % (the dk/dv kernel, D = 128); where two or
-// more waves share a SIMD they fill each other's waits, and the registers are
-// worth more.
+// matrix cores, and buf[0] holds step 0 on entry.  Left to itself the compiler reads every fragment right before
+// its product and waits for it, which costs a kernel of one wave a SIMD 12 %
+// (the dk/dv kernel, D = 128); where two or more waves share a SIMD they fill
+// each other's waits, and the registers are worth more (8192 tokens forward,
+// D = 128: spills, 2.2 times the time).
 template <class Op, bool AHEAD, int N, int G, class Load, class Use>
 __device__ inline void pipeline(typename Op::v8 (&buf)[2][G], Load load, Use use)
 {
@@ -375,11 +382,10 @@ __device__ inline void pipeline(typename Op::v8 (&buf)[2][G], Load load, Use use
             if (i + 1 < N)
                 load(i + 1, buf[(i + 1) & 1]);
             __builtin_amdgcn_sched_barrier(0);
-            use(i, buf[i & 1]);
         } else {
-            load(i, buf[0]);
-            use(i, buf[0]);
+            load(i, buf[i & 1]);
         }
+        use(i, buf[i & 1]);
     }
 }
 

@@ -317,42 +317,33 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccKV)) void attn_dkdv(Att
             const bool partial = q0 < most || docs_differ;
             const char *const tq = slot, *const tdo = slot + W::kTileBytes;
             const uint32_t roff = opaque(T::row_offset(lane)), coff = opaque(T::col_offset(lane));
-#pragma unroll
-            for (int t = 0; t < W::kSub; ++t) {
-                f32x16_acc s, dp, slope;
-                const float *const lse = rows + 32 * t + 4 * h, *const delta = lse + 64;  // of row reg_row(r)
+            // products of 32 rows and this wave's keys: s = q k, dp = dout v
+            auto scores = [&](int t, f32x16_acc &s, f32x16_acc &dp) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     s[r] = dp[r] = 0;
-                {
-                    V8 buf[2][4];  // two steps of 16 channels, q and dout
-                    auto load = [&](int i, V8(&f)[4]) {
+                V8 buf[2][4];  // two steps of 16 channels, q and dout
+                auto load = [&](int i, V8(&c)[4]) {
 #pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            f[2 * x] = T::row_frag(tq, roff, t, 2 * i + x);
-                            f[2 * x + 1] = T::row_frag(tdo, roff, t, 2 * i + x);
-                        }
-                    };
-                    if constexpr (W::kAhead)
-                        load(0, buf[0]);
-                    pipeline<Op, W::kAhead, DP / 32, 4>(buf, load, [&](int i, const V8(&f)[4]) {
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            s = Op::mfma(f[2 * x], kf[2 * i + x], s);
-                            dp = Op::mfma(f[2 * x + 1], vf[2 * i + x], dp);
-                        }
-                    });
-                }
-                // 16 rows and 32 channels of dout and q a step
-                V8 cbuf[2][2];
-                auto cload = [&](int i, V8(&c)[2]) {
-                    c[0] = T::col_frag(tdo, coff, 32 * t + 16 * (i / (DP / 32)), i % (DP / 32));
-                    c[1] = T::col_frag(tq, coff, 32 * t + 16 * (i / (DP / 32)), i % (DP / 32));
+                    for (int x = 0; x < 2; ++x) {
+                        c[2 * x] = T::row_frag(tq, roff, t, 2 * i + x);
+                        c[2 * x + 1] = T::row_frag(tdo, roff, t, 2 * i + x);
+                    }
                 };
-                if constexpr (W::kAhead) {
-                    cload(0, cbuf[0]);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                if constexpr (W::kAhead)
+                    load(0, buf[0]);
+                pipeline<Op, W::kAhead, DP / 32, 4>(buf, load, [&](int i, const V8(&c)[4]) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        s = Op::mfma(c[2 * x], kf[2 * i + x], s);
+                        dp = Op::mfma(c[2 * x + 1], vf[2 * i + x], dp);
+                    }
+                });
+            };
+            // their probabilities and score gradients, in place
+            auto gradients = [&](int t, f32x16_acc &s, f32x16_acc &dp) {
+                const float *const lse = rows + 32 * t + 4 * h, *const delta = lse + 64;  // of row reg_row(r)
+                f32x16_acc slope;
                 to_scores<FEAT>(s, slope, sc, [&](int r) { return lse[reg_row(r)]; });
                 const int i0 = q0 + 32 * t;
                 if (FEAT == kAny && a.R) {
@@ -386,40 +377,53 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccKV)) void attn_dkdv(Att
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
                         dp[r] *= slope[r];
-                if (!partial) {
-                    V8 p, ds;
-                    pipeline<Op, W::kAhead, 2 * (DP / 32), 2>(cbuf, cload, [&](int i, const V8(&c)[2]) {
-                        constexpr int N = DP / 32;
-                        if (i % N == 0) {
-                            p = pack8<Op>(s, 8 * (i / N));
-                            ds = pack8<Op>(dp, 8 * (i / N));
-                        }
-                        dv[i % N] = Op::mfma(c[0], p, dv[i % N]);
-                        dk[i % N] = Op::mfma(c[1], ds, dk[i % N]);
+            };
+            // dv += dout^T p, dk += q^T ds: 16 rows and 32 channels a step
+            constexpr int N = DP / 32;
+            auto columns = [&](int t, int i, V8(&c)[2]) {
+                c[0] = T::col_frag(tdo, coff, 32 * t + 16 * (i / N), i % N);
+                c[1] = T::col_frag(tq, coff, 32 * t + 16 * (i / N), i % N);
+            };
+            auto sums = [&](int t, const V8(&p)[2], const V8(&ds)[2], V8(&buf)[2][2], auto each) {
+                pipeline<Op, W::kAhead, 2 * N, 2>(
+                    buf, [&](int i, V8(&c)[2]) { columns(t, i, c); },
+                    [&](int i, const V8(&c)[2]) {
+                        dv[i % N] = Op::mfma(each(c[0]), p[i / N], dv[i % N]);
+                        dk[i % N] = Op::mfma(each(c[1]), ds[i / N], dk[i % N]);
                     });
-                    continue;
-                }
-                const int lim = first == INT32_MAX ? INT32_MAX : first - i0 - 4 * h;
+            };
+            auto same = [](V8 c) { return c; };
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const bool out = reg_row(r) < lim ||
-                                     (docs_differ && __float_as_int(rows[128 + 32 * t + reg_row(r) + 4 * h]) != doc);
-                    // a dout that is not finite reaches dv through p
-                    s[r] = out ? 0.0f : s[r] + 0.0f * delta[reg_row(r)];
-                    dp[r] = out ? 0.0f : dp[r];
+            for (int t = 0; t < W::kSub; ++t) {
+                f32x16_acc s, dp;
+                V8 p[2], ds[2], cbuf[2][2];
+                scores(t, s, dp);
+                if constexpr (W::kAhead) {  // these travel while the exponentials are taken
+                    columns(t, 0, cbuf[0]);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                uint32_t bad = 0;
-                V8 p, ds;
-                pipeline<Op, W::kAhead, 2 * (DP / 32), 2>(cbuf, cload, [&](int i, const V8(&c)[2]) {
-                    constexpr int N = DP / 32;
-                    if (i % N == 0) {
-                        p = pack8<Op>(s, 8 * (i / N));
-                        ds = pack8<Op>(dp, 8 * (i / N));
+                gradients(t, s, dp);
+                if (partial) {
+                    const int lim = first == INT32_MAX ? INT32_MAX : first - (q0 + 32 * t) - 4 * h;
+                    const float *const at = rows + 32 * t + 4 * h;  // + 64: delta, + 128: document
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const bool out =
+                            reg_row(r) < lim || (docs_differ && __float_as_int(at[128 + reg_row(r)]) != doc);
+                        // a dout that is not finite reaches dv through p
+                        s[r] = out ? 0.0f : s[r] + 0.0f * at[64 + reg_row(r)];
+                        dp[r] = out ? 0.0f : dp[r];
                     }
+                }
+                pack16<Op>(s, p);
+                pack16<Op>(dp, ds);
+                if (partial) {
                     // a left-out pair's zero times infinity or NaN must stay zero
-                    dv[i % N] = Op::mfma(finite<Op>(c[0], bad), p, dv[i % N]);
-                    dk[i % N] = Op::mfma(finite<Op>(c[1], bad), ds, dk[i % N]);
-                });
+                    uint32_t bad = 0;
+                    sums(t, p, ds, cbuf, [&](V8 c) { return finite<Op>(c, bad); });
+                } else {
+                    sums(t, p, ds, cbuf, same);
+                }
             }
             return next;
         };
