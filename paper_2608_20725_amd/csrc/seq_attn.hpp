@@ -292,12 +292,6 @@ __device__ inline int wave_max(int v)
     return __builtin_amdgcn_readfirstlane(v);
 }
 
-// tanh(x) = 1 - 2/(1 + e^2x): absolute error about 1e-7, exact at both ends.
-__device__ inline float fast_tanh(float x)
-{
-    return 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * (2.0f * kLog2e)));
-}
-
 // Both lanes of a pair (l, l ^ 32) get the larger of their values.
 __device__ inline float pair_max(float v)
 {
@@ -308,16 +302,18 @@ __device__ inline float pair_max(float v)
 // Row of register r of a 32x32 result, + 4*h.
 __device__ constexpr int reg_row(int r) { return 8 * (r >> 2) + (r & 3); }
 
-// How products q.k become scores (in units of ln 2): c2*tanh(x*c1) when
-// capped, x*c1 else, plus the bias.
+// How products q.k become scores in units of ln 2: x*c1, or capped,
+// c2*tanh(x*scale/cap) = c2 - 2*c2*r with r = 1/(1 + e^(2*x*scale/cap)) =
+// half(x*c1).  tanh's slope 1 - tanh^2 is 4*(r - r^2).
 struct ScoreArgs {
     float c1, c2;
     bool cap;
 };
 __device__ inline ScoreArgs score_args(const AttnArgs &a)
 {
-    return ScoreArgs{a.cap > 0 ? a.scale / a.cap : a.scale * kLog2e, a.cap * kLog2e, a.cap > 0};
+    return ScoreArgs{a.cap > 0 ? a.scale / a.cap * (2.0f * kLog2e) : a.scale * kLog2e, a.cap * kLog2e, a.cap > 0};
 }
+__device__ inline float half(float y) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y)); }
 
 // A query's running softmax: output sums, maximum (of the pair), sum (of this
 // lane's keys), both times 2^kShift.
@@ -427,54 +423,55 @@ __device__ inline void attend(const char *tk, const char *tv, const typename Op:
         for (int t = 0; t < SUB; ++t)
             s[t] = Op::mfma(T::row_frag(tk, roff, t, x), q[x], s[t]);
 
+    // A score is s*mul + add (mul > 0): the maximum is taken of s, and one
+    // fused multiply-add scales a score and subtracts the maximum.
     float mul = sc.c1, add = FEAT == kAny ? tp.far : 0.0f;
-    if (cap || (FEAT == kAny && tp.near) || tp.partial || !(sc.c1 > 0)) {
-        // scores one by one; else the maximum is taken of the products and
-        // one fused multiply-add scales a score and subtracts the maximum
-        if (cap) {
+    if (cap) {
+#pragma unroll
+        for (int t = 0; t < SUB; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[t][r] = -half(s[t][r] * sc.c1);
+        mul = 2.0f * sc.c2;
+        add += sc.c2;
+    }
+    if ((FEAT == kAny && tp.near) || !(sc.c1 > 0)) {
+#pragma unroll
+        for (int t = 0; t < SUB; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[t][r] = fmaf(s[t][r], mul, add);
+        mul = 1.0f;
+        add = 0.0f;
+    }
+    if (FEAT == kAny && tp.near) {
+        if (tp.inner) {
 #pragma unroll
             for (int t = 0; t < SUB; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    s[t][r] = fmaf(sc.c2, fast_tanh(s[t][r] * sc.c1), add);
+                    s[t][r] += near(32 * t + reg_row(r), false);
         } else {
 #pragma unroll
             for (int t = 0; t < SUB; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    s[t][r] = fmaf(s[t][r], sc.c1, add);
+                    s[t][r] += near(32 * t + reg_row(r), true);
         }
-        if (FEAT == kAny && tp.near) {
-            if (tp.inner) {
+    }
+    if (tp.partial) {
+        const int last = tp.lim - tp.k0 - 4 * h;
 #pragma unroll
-                for (int t = 0; t < SUB; ++t)
+        for (int t = 0; t < SUB; ++t)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        s[t][r] += near(32 * t + reg_row(r), false);
-            } else {
-#pragma unroll
-                for (int t = 0; t < SUB; ++t)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        s[t][r] += near(32 * t + reg_row(r), true);
-            }
-        }
-        if (tp.partial) {
-            const int last = tp.lim - tp.k0 - 4 * h;
+            for (int r = 0; r < 16; ++r)
+                s[t][r] = 32 * t + reg_row(r) < last ? s[t][r] : -INFINITY;
+        if (tp.docs_differ)
 #pragma unroll
             for (int t = 0; t < SUB; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    s[t][r] = 32 * t + reg_row(r) < last ? s[t][r] : -INFINITY;
-            if (tp.docs_differ)
-#pragma unroll
-                for (int t = 0; t < SUB; ++t)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        s[t][r] = tp.kdoc[32 * t + reg_row(r) + 4 * h] == tp.doc ? s[t][r] : -INFINITY;
-        }
-        mul = 1.0f;
-        add = 0.0f;
+                    s[t][r] = tp.kdoc[32 * t + reg_row(r) + 4 * h] == tp.doc ? s[t][r] : -INFINITY;
     }
     // four maxima and sums at a time: no chain of 32 dependent operations
     float m4[4], l4[4];

@@ -173,17 +173,18 @@ __global__ __launch_bounds__(kThreads) void value_norms(AttnArgs a)
 // ---- what both kernels do with a 32 x 32 tile of scores ----
 
 // Exponents of the probabilities (base 2), without the bias: the scores of
-// the products in s less lse(r), the row statistic of register r; slope:
-// 1 - tanh^2 where scores are capped.
+// the products in s less lse(r), the row statistic of register r; slope: a
+// quarter of 1 - tanh^2 where scores are capped (slope_scale has the rest).
+__device__ inline float slope_scale(const AttnArgs &a) { return a.cap > 0 ? 4.0f * a.scale : a.scale; }
 template <int FEAT, class Lse>
 __device__ inline void to_scores(f32x16_acc &s, f32x16_acc &slope, const ScoreArgs &c, Lse lse)
 {
     if (FEAT == kAny ? c.cap : FEAT == kCapped) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            const float t = fast_tanh(s[r] * c.c1);
-            slope[r] = 1.0f - t * t;
-            s[r] = fmaf(c.c2, t, -lse(r));
+            const float t = half(s[r] * c.c1);
+            slope[r] = fmaf(-t, t, t);
+            s[r] = fmaf(-2.0f * c.c2, t, c.c2 - lse(r));
         }
     } else {
 #pragma unroll
@@ -447,11 +448,11 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccKV)) void attn_dkdv(Att
         return;
     if (a.splits > 1) {  // sums as they are; dkdv_join adds the splits
         float *const part = a.part + (((int64_t)work.g * a.B * a.Hkv + work.kv) * a.Lk + j) * 2 * a.D;
-        store_row<F32Op, DP>((char *)part, dk, a.scale / dss, h, a.D);
+        store_row<F32Op, DP>((char *)part, dk, slope_scale(a) / dss, h, a.D);
         store_row<F32Op, DP>((char *)(part + a.D), dv, exp2f(-p_shift<Op>()), h, a.D);
         return;
     }
-    store_row<Op, DP>(a.dk + b * a.dk_sb + hk * a.dk_sh + (int64_t)j * a.dk_st, dk, a.scale / dss, h, a.D);
+    store_row<Op, DP>(a.dk + b * a.dk_sb + hk * a.dk_sh + (int64_t)j * a.dk_st, dk, slope_scale(a) / dss, h, a.D);
     store_row<Op, DP>(a.dv + b * a.dv_sb + hk * a.dv_sh + (int64_t)j * a.dv_st, dv, exp2f(-p_shift<Op>()), h, a.D);
 }
 
@@ -734,7 +735,7 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccQ)) void attn_dq(AttnAr
         t = step(slot1, kdoc1, slot0, kdoc0, t);
     }
     if (live)
-        store_row<Op, DP>(a.dq + b * a.dq_sb + hq * a.dq_sh + (int64_t)i * a.dq_st, dq, a.scale / dss, h, a.D);
+        store_row<Op, DP>(a.dq + b * a.dq_sb + hq * a.dq_sh + (int64_t)i * a.dq_st, dq, slope_scale(a) / dss, h, a.D);
     if (FEAT != kAny || !want_strip)
         return;
 #pragma unroll
