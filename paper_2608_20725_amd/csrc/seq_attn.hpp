@@ -52,7 +52,7 @@ struct AttnArgs {
     int32_t q_st, k_st, v_st, o_st, do_st, dq_st, dk_st, dv_st;
     int32_t B, Lq, Lk, H, Hkv, G, D;
     int32_t causal, align_end, R;
-    int32_t tiles, splits, chunk;  // held tiles of a head; decode: key chunks, keys in each
+    int32_t tiles, splits, chunk;  // held tiles of a head; workgroups that share one; decode: keys of each
     float scale, cap;
 };
 
@@ -646,6 +646,13 @@ __device__ inline Work work_item(uint32_t heads, uint32_t G, uint32_t tiles, boo
 // Bytes of AttnArgs::part a call may use.
 int64_t attn_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv, int64_t D, int64_t R,
                         bool backward);
+int64_t attn_forward_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv, int64_t D);
+
+// Parts of a row that several workgroups computed: its D output sums, maximum
+// and sum, at part[((split*B*Hkv + kv)*Lq*G + query*G + g)*part_floats].
+__host__ __device__ inline int64_t part_floats(int64_t D) { return D + 4; }  // D + 2, in 16-byte pieces
+void launch_attn_join(const AttnArgs &a, int dt, hipStream_t st);
+
 // Few query rows: the kernel that splits the keys (seq_attn_decode.hip).
 bool attn_few_rows(int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv);
 int64_t attn_decode_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv, int64_t D);

@@ -879,7 +879,7 @@ int64_t attn_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, in
                         bool backward)
 {
     if (!backward)
-        return attn_few_rows(B, Lq, Lk, H, Hkv) ? attn_decode_part_bytes(dt, B, Lq, Lk, H, Hkv, D) : 0;
+        return attn_forward_part_bytes(dt, B, Lq, Lk, H, Hkv, D);
     const int64_t splits = dkdv_splits(B, Lq, Lk, H, Hkv);
     return (strip_part_floats(B, Lq, H, R) + (splits > 1 ? splits * B * Hkv * Lk * 2 * D : 0)) * 4;
 }

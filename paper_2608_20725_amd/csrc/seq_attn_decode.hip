@@ -22,9 +22,6 @@ struct Dec {
     static constexpr int kLoads = 2 * kTileBytes / 1024;  // of a wave, a tile
 };
 
-// Floats a chunk leaves for one row: D outputs, maximum, sum.
-__device__ __host__ inline int64_t part_floats(int64_t D) { return D + 2; }
-
 template <class Op, int DP>
 __global__ __launch_bounds__(64 * (Dec<Op, DP>::kNW)) void attn_decode(AttnArgs a)
 {
@@ -185,42 +182,52 @@ __global__ __launch_bounds__(64 * (Dec<Op, DP>::kNW)) void attn_decode(AttnArgs 
     }
 }
 
-// Joins the chunks of one row: a wave a row, a lane one or two channels.
+// Joins the parts of each row: 32 lanes a row, four channels a lane.
 template <class Op>
-__global__ __launch_bounds__(64) void attn_join(AttnArgs a)
+__global__ __launch_bounds__(256) void attn_join(AttnArgs a)
 {
-    const int rows = a.Lq * a.G, heads = a.B * a.Hkv;
-    const int bh = blockIdx.x / rows, row = blockIdx.x - bh * rows, b = bh / a.Hkv, hk = bh - b * a.Hkv;
-    const int i = row / a.G, hq = hk * a.G + row - i * a.G, lane = threadIdx.x;
+    const int rows = a.Lq * a.G, heads = a.B * a.Hkv, lane = threadIdx.x & 31, d = lane * 4;
+    const int64_t id = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);  // (sequence, key/value head, row)
+    const bool in = id < (int64_t)heads * rows;
+    const int bh = in ? (int)(id / rows) : 0, row = in ? (int)(id - (int64_t)bh * rows) : 0;
+    const int b = bh / a.Hkv, hk = bh - b * a.Hkv, i = row / a.G, hq = hk * a.G + row - i * a.G;
     const int64_t step = (int64_t)heads * rows * part_floats(a.D);
     const float *const p = a.part + ((int64_t)bh * rows + row) * part_floats(a.D);
-    const int chunks = min(a.splits, (keys_of(a, b) + a.chunk - 1) / a.chunk);
-    // lanes take the chunks' maxima and sums in turn
+    const int parts = a.chunk ? min(a.splits, (keys_of(a, b) + a.chunk - 1) / a.chunk) : a.splits;
+    // lanes take the parts' maxima in turn
     float m = -INFINITY;
-    for (int c = lane; c < chunks; c += 64)
+    for (int c = lane; c < parts; c += 32)
         m = fmaxf(m, p[c * step + a.D]);
 #pragma unroll
-    for (int x = 32; x >= 1; x >>= 1)
+    for (int x = 16; x >= 1; x >>= 1)
         m = fmaxf(m, __shfl_xor(m, x));
-    const float base = m == -INFINITY ? 0.0f : m;
-    float l = 0, v0 = 0, v1 = 0;
-    const bool two = lane + 64 < a.D, one = lane < a.D;
-    for (int c = 0; c < chunks; ++c) {
-        const float f = __builtin_amdgcn_exp2f(p[c * step + a.D] - base);
-        l += f * p[c * step + a.D + 1];
-        v0 += one ? f * p[c * step + lane] : 0.0f;
-        v1 += two ? f * p[c * step + lane + 64] : 0.0f;
-    }
     const bool none = m == -INFINITY;
+    const float base = none ? 0.0f : m;
+    typedef float v4 __attribute__((ext_vector_type(4)));
+    v4 v = {0, 0, 0, 0};
+    float l = 0;
+#pragma unroll 4
+    for (int c = 0; c < parts; ++c) {
+        const float *const q = p + c * step;
+        const float f = __builtin_amdgcn_exp2f(q[a.D] - base);
+        l += f * q[a.D + 1];
+        if (d < a.D)
+            v += *(const v4 *)(q + d) * f;
+    }
+    if (!in)
+        return;
     const float inv = none ? 0.0f : 1.0f / l;
     if (lane == 0)
         a.lse[((int64_t)b * a.H + hq) * a.Lq + i] =
             none ? -INFINITY : (m - RowState<Op, 32>::kShift + __log2f(l)) * kLn2;
-    typename Op::elem *const out = (typename Op::elem *)(a.out + b * a.o_sb + hq * a.o_sh + (int64_t)i * a.o_st);
-    if (one)
-        out[lane] = (typename Op::elem)(none ? 0.0f : v0 * inv);
-    if (two)
-        out[lane + 64] = (typename Op::elem)(none ? 0.0f : v1 * inv);
+    if (d < a.D) {
+        typedef typename Op::elem V __attribute__((ext_vector_type(4)));
+        V o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            o[e] = (typename Op::elem)(none ? 0.0f : v[e] * inv);
+        *(V *)(a.out + b * a.o_sb + hq * a.o_sh + (int64_t)i * a.o_st + d * sizeof(typename Op::elem)) = o;
+    }
 }
 
 struct Split {
@@ -254,8 +261,6 @@ template <class Op, int DP>
 void run(const AttnArgs &a, hipStream_t st)
 {
     attn_decode<Op, DP><<<(uint32_t)(a.B * a.Hkv) * a.tiles * a.splits, 64 * Dec<Op, DP>::kNW, 0, st>>>(a);
-    if (a.splits > 1)
-        attn_join<Op><<<(uint32_t)(a.B * a.H) * a.Lq, 64, 0, st>>>(a);
 }
 
 template <class Op>
@@ -278,12 +283,25 @@ int64_t attn_decode_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_
     return s.splits > 1 ? s.splits * B * H * Lq * part_floats(D) * 4 : 0;
 }
 
+void launch_attn_join(const AttnArgs &a, int dt, hipStream_t st)
+{
+    const uint32_t grid = (uint32_t)(((int64_t)a.B * a.H * a.Lq + 7) / 8);
+    if (dt == IM2WIN_F32)
+        attn_join<F32Op><<<grid, 256, 0, st>>>(a);
+    else if (dt == IM2WIN_F16)
+        attn_join<F16Op><<<grid, 256, 0, st>>>(a);
+    else
+        attn_join<BF16Op><<<grid, 256, 0, st>>>(a);
+}
+
 hipError_t launch_attn_decode(const AttnArgs &a, int dt, hipStream_t st)
 {
     AttnArgs b = a;
     const Split s = split_of(dt, a.B, a.Lq, a.Lk, a.Hkv, a.G, a.D);
     b.tiles = s.tiles, b.chunk = s.chunk, b.splits = s.splits;
     dt == IM2WIN_F32 ? run_dim<F32Op>(b, st) : dt == IM2WIN_F16 ? run_dim<F16Op>(b, st) : run_dim<BF16Op>(b, st);
+    if (b.splits > 1)
+        launch_attn_join(b, dt, st);
     return hipGetLastError();
 }
 

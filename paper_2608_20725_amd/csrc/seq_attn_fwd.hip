@@ -30,9 +30,11 @@ __global__ __launch_bounds__(64 * kWaves, (Fwd<Op, DP>::kOcc)) void attn_fwd(Att
     __shared__ int shared_most[kWaves], shared_lo[kWaves], shared_hi[kWaves];
     extern __shared__ __align__(16) float strip[];  // 2R+1, times log2(e); documents: a bit for each key tile
 
-    const Work work = work_item(a.B * a.Hkv, a.G, a.tiles, a.causal, blockIdx.x);
+    // `splits` workgroups share the keys of a query tile
+    const Work work = work_item(a.B * a.Hkv, a.G * a.splits, a.tiles, a.causal, blockIdx.x);
     const int qt = a.tiles - 1 - work.tile;  // long rows of causal masks first
-    const int b = work.kv / a.Hkv, hk = work.kv - b * a.Hkv, hq = hk * a.G + work.g;
+    const int g = work.g % a.G, split = work.g / a.G;
+    const int b = work.kv / a.Hkv, hk = work.kv - b * a.Hkv, hq = hk * a.G + g;
     const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = qt * kHeld + wave * 32 + (lane & 31);  // this lane's query
     const bool live = i < a.Lq;
@@ -71,7 +73,8 @@ __global__ __launch_bounds__(64 * kWaves, (Fwd<Op, DP>::kOcc)) void attn_fwd(Att
         wg_hi = max(wg_hi, shared_hi[w]);
     }
     wg_most = __builtin_amdgcn_readfirstlane(wg_most);
-    const int tiles = (wg_most + F::kKeys - 1) / F::kKeys;
+    const int all_tiles = (wg_most + F::kKeys - 1) / F::kKeys;
+    const int tiles = (int)((int64_t)all_tiles * (split + 1) / a.splits);  // the first tile not this workgroup's
     const DocRange *const ranges = a.q_doc ? a.k_range + (int64_t)b * ((a.Lk + kDocTile - 1) / kDocTile) : nullptr;
     uint64_t *const bits = (uint64_t *)(strip + (a.R ? 2 * a.R + 2 : 0));
     if (a.q_doc) {
@@ -131,7 +134,7 @@ __global__ __launch_bounds__(64 * kWaves, (Fwd<Op, DP>::kOcc)) void attn_fwd(Att
         return next;
     };
 
-    int t = after(0);
+    int t = after((int)((int64_t)all_tiles * split / a.splits));
     if (t < tiles)
         issue(slot0, kdoc0, t);
     while (t < tiles) {
@@ -145,6 +148,15 @@ __global__ __launch_bounds__(64 * kWaves, (Fwd<Op, DP>::kOcc)) void attn_fwd(Att
     l += __shfl_xor(l, 32);
     if (!live)
         return;
+    if (a.splits > 1) {  // sums as they are; attn_join joins the splits
+        float *const part = a.part + (((int64_t)split * a.B * a.Hkv + work.kv) * a.Lq * a.G + (int64_t)i * a.G + g) * part_floats(a.D);
+        store_row<F32Op, DP>((char *)part, st.o, 1.0f, h, a.D);
+        if (h == 0) {
+            part[a.D] = st.m;
+            part[a.D + 1] = l;
+        }
+        return;
+    }
     const bool none = st.m == -INFINITY;
     const float inv = none ? 0.0f : 1.0f / l;
     if (h == 0)
@@ -164,6 +176,23 @@ __global__ __launch_bounds__(64) void doc_ranges(const int32_t *__restrict__ doc
         out[blockIdx.x] = DocRange{lo, hi, least != hi, 0};
 }
 
+// Workgroups that share the keys of one query tile, where there are fewer than
+// 512 query tiles (two for each of 256 CUs) and the keys are many enough to
+// pay for writing and joining the parts; at least 256 keys each.  Measured,
+// one workgroup against split: fp16 64 tiles of 1024 keys 21 -> 19 us, bf16 64
+// tiles of 4096 keys 102 -> 42, 256 tiles of 4096 110 -> 98; not split, 128
+// tiles of 512 keys 19 (26 split), 256 tiles of 2048 42 (49); fp32 144 tiles of
+// 1001 keys 121 -> 70, 168 tiles of 784 71 -> 63.
+int32_t forward_splits(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H)
+{
+    const int64_t groups = B * H * ((Lq + kHeld - 1) / kHeld);
+    const int64_t enough = dt == IM2WIN_F32 ? 512 : groups < 256 ? 1024 : 4096;
+    if (groups <= 0 || groups >= 512 || Lk < enough)
+        return 1;
+    const int64_t s = (512 + groups - 1) / groups;
+    return (int32_t)(s < Lk / 256 ? s : Lk / 256);
+}
+
 template <class Op, int DP, int FEAT>
 hipError_t run(const AttnArgs &a, hipStream_t st)
 {
@@ -177,7 +206,12 @@ hipError_t run(const AttnArgs &a, hipStream_t st)
     }
     AttnArgs b = a;
     b.tiles = (a.Lq + kHeld - 1) / kHeld;
-    attn_fwd<Op, DP, FEAT><<<(uint32_t)(a.B * a.H) * b.tiles, 64 * kWaves, lds, st>>>(b);
+    constexpr int dt = __is_same(Op, F32Op) ? IM2WIN_F32 : __is_same(Op, F16Op) ? IM2WIN_F16 : IM2WIN_BF16;
+    b.splits = forward_splits(dt, a.B, a.Lq, a.Lk, a.H);
+    b.chunk = 0;
+    attn_fwd<Op, DP, FEAT><<<(uint32_t)(a.B * a.H) * b.tiles * b.splits, 64 * kWaves, lds, st>>>(b);
+    if (b.splits > 1)
+        launch_attn_join(b, dt, st);
     return hipGetLastError();
 }
 
@@ -209,6 +243,14 @@ hipError_t launch_attn_docs(const int32_t *doc, DocRange *out, int64_t B, int64_
         return hipSuccess;
     doc_ranges<<<(uint32_t)(B * tiles), 64, 0, st>>>(doc, out, (int32_t)L, (int32_t)tiles);
     return hipGetLastError();
+}
+
+int64_t attn_forward_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv, int64_t D)
+{
+    if (attn_few_rows(B, Lq, Lk, H, Hkv))
+        return attn_decode_part_bytes(dt, B, Lq, Lk, H, Hkv, D);
+    const int32_t splits = forward_splits(dt, B, Lq, Lk, H);
+    return splits > 1 ? splits * B * H * Lq * part_floats(D) * 4 : 0;
 }
 
 hipError_t launch_attn_forward(const AttnArgs &a, int dt, hipStream_t st)
