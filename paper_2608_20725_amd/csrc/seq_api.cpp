@@ -24,14 +24,51 @@ struct Buf {
     int64_t bytes;
 };
 
-int check_extents(const Buf *b, int n)
-{
-    for (int i = 0; i < n; ++i)
-        if (b[i].bytes > 0)
-            if (const int rc = check_extent(b[i].p, b[i].bytes))
-                return rc;
-    return IM2WIN_OK;
-}
+// Checks that buffers lie in one device allocation each.  The allocations that
+// a call has met are kept for its other buffers: asking the runtime takes 0.2
+// us a buffer, and an allocator serves many tensors from one allocation.
+class Extents {
+public:
+    int check(const Buf *b, int n)
+    {
+        for (int i = 0; i < n; ++i)
+            if (b[i].bytes > 0)
+                if (const int rc = one(b[i]))
+                    return rc;
+        return IM2WIN_OK;
+    }
+
+private:
+    static constexpr int kMost = 8;
+    uintptr_t base_[kMost];
+    uint64_t size_[kMost];
+    int n_ = 0;
+
+    static bool inside(const Buf &b, uintptr_t base, uint64_t size)
+    {
+        const uintptr_t q = (uintptr_t)b.p;
+        return q >= base && (uint64_t)(q - base) + (uint64_t)b.bytes <= size;
+    }
+    int one(const Buf &b)
+    {
+        for (int i = 0; i < n_; ++i)
+            if (inside(b, base_[i], size_[i]))
+                return IM2WIN_OK;
+        hipDeviceptr_t base = nullptr;
+        size_t size = 0;
+        if (hipMemGetAddressRange(&base, &size, (hipDeviceptr_t)b.p) != hipSuccess) {
+            (void)hipGetLastError();  // leave no sticky error behind for the caller
+            return IM2WIN_EBUFFER;
+        }
+        if (!inside(b, (uintptr_t)base, size))
+            return IM2WIN_EBUFFER;
+        if (n_ < kMost) {
+            base_[n_] = (uintptr_t)base;
+            size_[n_++] = size;
+        }
+        return IM2WIN_OK;
+    }
+};
 
 bool meet(const Buf &a, const Buf &b) { return a.bytes > 0 && b.bytes > 0 && overlaps(a.p, a.bytes, b.p, b.bytes); }
 
@@ -237,7 +274,8 @@ int seq_layer_norm_forward(const void *x, const void *weight, const void *bias, 
     const Buf in[3] = {{x, ((rows - 1) * x_stride + C) * e}, {weight, C * we}, {bias, C * we}};
     const Buf out[3] = {{y, rows * C * e}, {mean, rows * 4}, {rstd, rows * 4}};
     int rc;
-    if ((rc = check_extents(in, 3)) || (rc = check_extents(out, 3)))
+    Extents ext;
+    if ((rc = ext.check(in, 3)) || (rc = ext.check(out, 3)))
         return rc;
     for (int o = 0; o < 3; ++o) {
         for (int i = 0; i < 3; ++i)
@@ -288,7 +326,8 @@ int seq_layer_norm_backward(const void *dy, const void *x, const void *weight, c
                        {rstd, rows * 4}};
     const Buf out[4] = {{dx, rows * C * e}, {dweight, C * we}, {dbias, C * we}, {ws, ws_bytes}};
     int rc;
-    if ((rc = check_extents(in, 5)) || (rc = check_extents(out, 4)))
+    Extents ext;
+    if ((rc = ext.check(in, 5)) || (rc = ext.check(out, 4)))
         return rc;
     for (int o = 0; o < 4; ++o) {
         for (int i = 0; i < 5; ++i)
@@ -343,7 +382,7 @@ int seq_rel_bias_forward(const void *table, float *strip, int64_t H, int64_t buc
     if (!aligned(table, elt(dt)) || !aligned(strip, 4))
         return IM2WIN_EALIGN;
     const Buf b[2] = {{table, buckets * H * elt(dt)}, {strip, H * (2 * R + 1) * 4}};
-    if ((rc = check_extents(b, 2)))
+    if ((rc = Extents().check(b, 2)))
         return rc;
     if (meet(b[0], b[1]))
         return IM2WIN_EOVERLAP;
@@ -366,7 +405,7 @@ int seq_rel_bias_backward(const float *dstrip, void *dtable, int64_t n, int64_t 
     if (!aligned(dstrip, 4) || !aligned(dtable, elt(dt)))
         return IM2WIN_EALIGN;
     const Buf b[2] = {{dstrip, n * H * (2 * R + 1) * 4}, {dtable, buckets * H * elt(dt)}};
-    if ((rc = check_extents(b, 2)))
+    if ((rc = Extents().check(b, 2)))
         return rc;
     if (meet(b[0], b[1]))
         return IM2WIN_EOVERLAP;
@@ -432,17 +471,18 @@ static int attention(const seq_attention_t *a, const void *dout, const void *q, 
                           {a->q_doc, a->q_doc ? a->B * a->Lq * 4 : 0},
                           {a->k_doc, a->k_doc ? a->B * a->Lk * 4 : 0}};
     const Buf flat[3] = {{lse, lse_bytes}, {dstrip, backward && dstrip ? strip_bytes : 0}, {ws, ws_bytes}};
+    Extents ext;
     for (int i = 0; i < n_in; ++i) {
         const Buf b{ins[i]->p, ins[i]->bytes()};
-        if ((rc = check_extents(&b, 1)))
+        if ((rc = ext.check(&b, 1)))
             return rc;
     }
     for (int i = 0; i < n_out; ++i) {
         const Buf b{outs[i]->p, outs[i]->bytes()};
-        if ((rc = check_extents(&b, 1)))
+        if ((rc = ext.check(&b, 1)))
             return rc;
     }
-    if ((rc = check_extents(small, 5)) || (rc = check_extents(flat, 3)))
+    if ((rc = ext.check(small, 5)) || (rc = ext.check(flat, 3)))
         return rc;
     if (late)
         return late;

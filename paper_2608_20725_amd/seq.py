@@ -14,8 +14,9 @@ fallback.
 from __future__ import annotations
 
 import ctypes
+import struct
 
-from . import F32, _check, _dtype_code, _i64, _nbytes, _stream, _vp, load_library, Im2winError
+from . import _check, _dtype_code, _i64, _nbytes, _stream, _vp, load_library, Im2winError
 
 __all__ = ["seq_layer_norm_workspace_bytes", "seq_layer_norm_forward", "seq_layer_norm_backward", "seq_rel_bias_bucket",
            "seq_rel_bias_forward", "seq_rel_bias_backward", "seq_attention_workspace_bytes", "seq_attention_forward",
@@ -25,13 +26,10 @@ _lib = None
 _int = ctypes.c_int
 
 
-class _Attention(ctypes.Structure):
-    """seq_attention_t"""
-    _fields_ = [("dt", _int), ("causal", _int), ("align_end", _int), ("scale", ctypes.c_float), ("cap", ctypes.c_float),
-                ("B", _i64), ("Lq", _i64), ("Lk", _i64), ("H", _i64), ("Hkv", _i64), ("D", _i64),
-                ("q_stride", _i64 * 3), ("k_stride", _i64 * 3), ("v_stride", _i64 * 3), ("out_stride", _i64 * 3),
-                ("dout_stride", _i64 * 3), ("dq_stride", _i64 * 3), ("dk_stride", _i64 * 3), ("dv_stride", _i64 * 3),
-                ("R", _i64), ("strip", _vp), ("kv_len", _vp), ("prefix", _vp), ("q_doc", _vp), ("k_doc", _vp)]
+# seq_attention_t: dt, causal, align_end, scale, cap; B, Lq, Lk, H, Hkv, D; eight operands' strides (q, k, v, out, dout,
+# dq, dk, dv); R, strip, kv_len, prefix, q_doc, k_doc.  One pack takes 1 us, a ctypes structure set field by field 6.
+_PACK = struct.Struct("@3i2f4x6q24qq5P")
+_NO_STRIDES = (0, 0, 0)
 
 
 def _library():
@@ -51,11 +49,11 @@ def _library():
         lib.seq_rel_bias_bucket.restype = _i64
         lib.seq_rel_bias_bucket.argtypes = [_i64] * 3 + [_int]
         lib.seq_attention_workspace_bytes.restype = _i64
-        lib.seq_attention_workspace_bytes.argtypes = [ctypes.POINTER(_Attention), _int]
+        lib.seq_attention_workspace_bytes.argtypes = [ctypes.c_char_p, _int]
         lib.seq_attention_forward.restype = _int
-        lib.seq_attention_forward.argtypes = [ctypes.POINTER(_Attention)] + [_vp] * 6 + [_i64, _vp]
+        lib.seq_attention_forward.argtypes = [ctypes.c_char_p] + [_vp] * 6 + [_i64, _vp]
         lib.seq_attention_backward.restype = _int
-        lib.seq_attention_backward.argtypes = [ctypes.POINTER(_Attention)] + [_vp] * 11 + [_i64, _vp]
+        lib.seq_attention_backward.argtypes = [ctypes.c_char_p] + [_vp] * 11 + [_i64, _vp]
         _lib = lib
     return _lib
 
@@ -196,50 +194,67 @@ def seq_rel_bias_backward(dstrip, buckets: int, two_sided: bool = True, dtype=No
 
 
 def _strides(t, what):
-    if t.stride(3) != 1 and t.shape[3] > 1:
+    """Strides of the sequence, token and head dimensions."""
+    st = t.stride()
+    if st[3] != 1 and t.shape[3] > 1:
         raise ValueError("%s must be dense in its last dimension" % what)
-    return (_i64 * 3)(t.stride(0), t.stride(1), t.stride(2))
+    return st[:3]
 
 
-def _describe(q, k, v, scale, cap, causal, align_end, bias, kv_len, prefix, q_doc, k_doc):
-    """The description of a call and what its pointers refer to."""
+def _dense(shape):
+    return (shape[1] * shape[2] * shape[3], shape[2] * shape[3], shape[3])
+
+
+def _ints(name, t, shape, device):
     import torch
-    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+    if t.shape != shape or t.dtype != torch.int32 or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 tensor of shape %s" % (name, shape))
+    if t.device != device:
+        raise ValueError("all tensors must be on %s" % device)
+    return t.data_ptr()
+
+
+def _describe(q, k, v, strides, scale, cap, causal, align_end, bias, kv_len, prefix, q_doc, k_doc):
+    """The packed description of a call; ``strides``: of out, dout, dq, dk, dv."""
+    qs, ks = q.shape, k.shape
+    if len(qs) != 4 or len(ks) != 4:
         raise ValueError("q must be [B][Lq][H][D], k and v [B][Lk][Hkv][D]")
-    B, Lq, H, D = q.shape
-    if k.shape != v.shape or k.shape[0] != B or k.shape[3] != D:
+    B, Lq, H, D = qs
+    _, Lk, Hkv, _ = ks
+    if v.shape != ks or ks[0] != B or ks[3] != D:
         raise ValueError("k and v must have one shape, with the batch and channels of q")
     if k.dtype != q.dtype or v.dtype != q.dtype:
         raise TypeError("q, k and v must have one type")
-    Lk, Hkv = k.shape[1], k.shape[2]
-    _same_device(q, k, v, bias, kv_len, prefix, q_doc, k_doc)
-    a = _Attention()
-    a.dt = _dtype_code(q.dtype)
-    a.causal, a.align_end = int(bool(causal)), int(bool(align_end))
-    a.scale, a.cap = D ** -0.5 if scale is None else scale, cap
-    a.B, a.Lq, a.Lk, a.H, a.Hkv, a.D = B, Lq, Lk, H, Hkv, D
-    a.q_stride, a.k_stride, a.v_stride = _strides(q, "q"), _strides(k, "k"), _strides(v, "v")
+    device = q.device
+    if k.device != device or v.device != device:
+        raise ValueError("all tensors must be on %s" % device)
+    R = strip = lens = pre = qd = kd = 0
     if bias is not None:
+        import torch
         if bias.dim() != 2 or bias.shape[0] != H or bias.shape[1] % 2 == 0 or bias.shape[1] < 3 \
                 or bias.dtype != torch.float32 or not bias.is_contiguous():
             raise ValueError("bias must be a contiguous fp32 [H][2R+1] strip")
-        a.R, a.strip = bias.shape[1] // 2, bias.data_ptr()
-    for name, t, shape in (("kv_len", kv_len, (B,)), ("prefix", prefix, (B,)), ("q_doc", q_doc, (B, Lq)),
-                           ("k_doc", k_doc, (B, Lk))):
-        if t is None:
-            continue
-        if tuple(t.shape) != shape or t.dtype != torch.int32 or not t.is_contiguous():
-            raise ValueError("%s must be a contiguous int32 tensor of shape %s" % (name, shape))
-        setattr(a, name, t.data_ptr())
-    if (q_doc is None) != (k_doc is None):
-        raise ValueError("q_doc and k_doc go together")
-    if prefix is not None and not causal:
-        raise ValueError("prefix needs causal")
-    return a
+        if bias.device != device:
+            raise ValueError("all tensors must be on %s" % device)
+        R, strip = bias.shape[1] // 2, bias.data_ptr()
+    if kv_len is not None:
+        lens = _ints("kv_len", kv_len, (B,), device)
+    if prefix is not None:
+        if not causal:
+            raise ValueError("prefix needs causal")
+        pre = _ints("prefix", prefix, (B,), device)
+    if q_doc is not None or k_doc is not None:
+        if q_doc is None or k_doc is None:
+            raise ValueError("q_doc and k_doc go together")
+        qd, kd = _ints("q_doc", q_doc, (B, Lq), device), _ints("k_doc", k_doc, (B, Lk), device)
+    so, sdo, sdq, sdk, sdv = strides
+    return _PACK.pack(_dtype_code(q.dtype), 1 if causal else 0, 1 if align_end else 0, D ** -0.5 if scale is None else scale,
+                      cap, B, Lq, Lk, H, Hkv, D, *_strides(q, "q"), *_strides(k, "k"), *_strides(v, "v"), *so, *sdo, *sdq,
+                      *sdk, *sdv, R, strip, lens, pre, qd, kd)
 
 
 def _attention_ws(a, backward, ws, device):
-    n = _library().seq_attention_workspace_bytes(ctypes.byref(a), backward)
+    n = _library().seq_attention_workspace_bytes(a, backward)
     if n < 0:
         raise Im2winError(int(n), "seq_attention_workspace_bytes")
     if ws is None and n:
@@ -254,17 +269,12 @@ def seq_attention_workspace_bytes(q, k, v, backward: bool = False, **options) ->
     opts = dict(scale=None, cap=0.0, causal=False, align_end=False, bias=None, kv_len=None, prefix=None, q_doc=None,
                 k_doc=None)
     opts.update(options)
-    a = _describe(q, k, v, **opts)
-    a.out_stride = a.dout_stride = a.dq_stride = _dense(q.shape)
-    a.dk_stride = a.dv_stride = _dense(k.shape)
-    n = _library().seq_attention_workspace_bytes(ctypes.byref(a), 1 if backward else 0)
+    like_q, like_k = _dense(q.shape), _dense(k.shape)
+    a = _describe(q, k, v, (like_q, like_q, like_q, like_k, like_k), **opts)
+    n = _library().seq_attention_workspace_bytes(a, 1 if backward else 0)
     if n < 0:
         raise Im2winError(int(n), "seq_attention_workspace_bytes")
     return int(n)
-
-
-def _dense(shape):
-    return (_i64 * 3)(shape[1] * shape[2] * shape[3], shape[2] * shape[3], shape[3])
 
 
 def _like(t, shape, dtype, what):
@@ -285,19 +295,26 @@ def seq_attention_forward(q, k, v, scale=None, cap: float = 0.0, causal: bool = 
     q_doc, k_doc  [B][Lq], [B][Lk] int32: pairs need equal ids, negative ids see and are seen by nothing
     """
     import torch
-    a = _describe(q, k, v, scale, cap, causal, align_end, bias, kv_len, prefix, q_doc, k_doc)
+    device = q.device
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _like(out, q.shape, q.dtype, "out")
-    _same_device(q, out, ws)
-    a.out_stride = _strides(out, "out")
-    lse = torch.empty((a.B, a.H, a.Lq), dtype=torch.float32, device=q.device)
-    ws = _attention_ws(a, 0, ws, q.device)
-    _check(_library().seq_attention_forward(ctypes.byref(a), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
-                                            lse.data_ptr(), None if ws is None else ws.data_ptr(),
-                                            0 if ws is None else _nbytes(ws), _on(stream, out, lse, ws)),
-           "seq_attention_forward")
+        out = torch.empty(q.shape, dtype=q.dtype, device=device)
+    else:
+        _like(out, q.shape, q.dtype, "out")
+        _same_device(q, out)
+    a = _describe(q, k, v, (_strides(out, "out"), _NO_STRIDES, _NO_STRIDES, _NO_STRIDES, _NO_STRIDES), scale, cap, causal,
+                  align_end, bias, kv_len, prefix, q_doc, k_doc)
+    lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=device)
+    ws = _attention_ws(a, 0, ws, device)
+    _check(_library().seq_attention_forward(a, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
+                                            *_workspace(q, ws), _on(stream, out, lse, ws)), "seq_attention_forward")
     return out, lse
+
+
+def _workspace(like, ws):
+    if ws is None:
+        return None, 0
+    _same_device(like, ws)
+    return ws.data_ptr(), _nbytes(ws)
 
 
 def seq_attention_backward(dout, q, k, v, out, lse, scale=None, cap: float = 0.0, causal: bool = False,
@@ -308,26 +325,25 @@ def seq_attention_backward(dout, q, k, v, out, lse, scale=None, cap: float = 0.0
     dk and dv are written to the tensors given, of any strides with a dense
     last dimension (columns of one packed tensor, for example)."""
     import torch
-    a = _describe(q, k, v, scale, cap, causal, align_end, bias, kv_len, prefix, q_doc, k_doc)
     _like(dout, q.shape, q.dtype, "dout")
     _like(out, q.shape, q.dtype, "out")
-    _like(lse, (a.B, a.H, a.Lq), torch.float32, "lse")
+    _like(lse, (q.shape[0], q.shape[2], q.shape[1]), torch.float32, "lse")
     if not lse.is_contiguous():
         raise ValueError("lse must be contiguous")
-    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
-    dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dk is None else dk
-    dv = torch.empty(v.shape, dtype=q.dtype, device=q.device) if dv is None else dv
+    device = q.device
+    dq = torch.empty(q.shape, dtype=q.dtype, device=device) if dq is None else dq
+    dk = torch.empty(k.shape, dtype=q.dtype, device=device) if dk is None else dk
+    dv = torch.empty(v.shape, dtype=q.dtype, device=device) if dv is None else dv
     _like(dq, q.shape, q.dtype, "dq")
     _like(dk, k.shape, q.dtype, "dk")
     _like(dv, v.shape, q.dtype, "dv")
-    _same_device(q, dout, out, lse, dq, dk, dv, ws)
-    a.out_stride, a.dout_stride = _strides(out, "out"), _strides(dout, "dout")
-    a.dq_stride, a.dk_stride, a.dv_stride = _strides(dq, "dq"), _strides(dk, "dk"), _strides(dv, "dv")
-    dstrip = None if bias is None else torch.empty(bias.shape, dtype=torch.float32, device=q.device)
-    ws = _attention_ws(a, 1, ws, q.device)
-    _check(_library().seq_attention_backward(ctypes.byref(a), dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                             out.data_ptr(), lse.data_ptr(), dq.data_ptr(), dk.data_ptr(),
-                                             dv.data_ptr(), None if dstrip is None else dstrip.data_ptr(),
-                                             None if ws is None else ws.data_ptr(), 0 if ws is None else _nbytes(ws),
+    _same_device(q, dout, out, lse, dq, dk, dv)
+    a = _describe(q, k, v, (_strides(out, "out"), _strides(dout, "dout"), _strides(dq, "dq"), _strides(dk, "dk"),
+                            _strides(dv, "dv")), scale, cap, causal, align_end, bias, kv_len, prefix, q_doc, k_doc)
+    dstrip = None if bias is None else torch.empty(bias.shape, dtype=torch.float32, device=device)
+    ws = _attention_ws(a, 1, ws, device)
+    _check(_library().seq_attention_backward(a, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+                                             lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+                                             None if dstrip is None else dstrip.data_ptr(), *_workspace(q, ws),
                                              _on(stream, dq, dk, dv, dstrip, ws)), "seq_attention_backward")
     return dq, dk, dv, dstrip
