@@ -224,9 +224,13 @@ AttnArgs make_args(const seq_attention_t *a)
     r.o_sb = a->out_stride[0] * e, r.o_st = (int32_t)(a->out_stride[1] * e), r.o_sh = a->out_stride[2] * e;
     r.B = (int32_t)a->B, r.Lq = (int32_t)a->Lq, r.Lk = (int32_t)a->Lk;
     r.H = (int32_t)a->H, r.Hkv = (int32_t)a->Hkv, r.G = (int32_t)(a->H / a->Hkv), r.D = (int32_t)a->D;
-    r.causal = a->causal != 0, r.align_end = a->align_end != 0, r.R = (int32_t)a->R;
+    r.causal = a->causal != 0, r.align_end = a->align_end != 0;
     r.scale = a->scale, r.cap = a->cap;
-    r.strip = a->strip, r.kv_len = a->kv_len, r.prefix = a->causal ? a->prefix : nullptr;
+    if (a->R) {
+        r.R = (int32_t)attn_range(a->R, a->Lq, a->Lk), r.strip_step = (int32_t)(2 * a->R + 1);
+        r.strip = a->strip + (a->R - r.R);
+    }
+    r.kv_len = a->kv_len, r.prefix = a->causal ? a->prefix : nullptr;
     r.q_doc = a->q_doc, r.k_doc = a->k_doc;
     return r;
 }

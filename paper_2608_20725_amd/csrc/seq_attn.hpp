@@ -43,15 +43,16 @@ struct AttnArgs {
     float *lse;
     float *stat;          // backward: [B][H][2][Lq rounded up to 64] lse*log2(e) less p_shift (+inf: no pair), dout.out
     uint32_t *norms;      // backward, fp16: bits of the largest |dout_i| and |v_j| [B][H][2]
-    float *part;          // decode: partial outputs; backward: partial strip gradients
-    const float *strip;
+    float *part;          // sums of rows that several workgroups share
+    float *strip_part;    // backward: the strip's gradients of every workgroup
+    const float *strip;   // its middle 2R+1 entries; heads strip_step apart
     const int32_t *kv_len, *prefix, *q_doc, *k_doc;
     const DocRange *q_range, *k_range;  // [B][ceil(L / kDocTile)]
     // byte strides
     int64_t q_sb, q_sh, k_sb, k_sh, v_sb, v_sh, o_sb, o_sh, do_sb, do_sh, dq_sb, dq_sh, dk_sb, dk_sh, dv_sb, dv_sh;
     int32_t q_st, k_st, v_st, o_st, do_st, dq_st, dk_st, dv_st;
     int32_t B, Lq, Lk, H, Hkv, G, D;
-    int32_t causal, align_end, R;
+    int32_t causal, align_end, R, strip_step;
     int32_t tiles, splits, chunk;  // held tiles of a head; workgroups that share one; decode: keys of each
     float scale, cap;
 };
@@ -646,6 +647,14 @@ __device__ inline Work work_item(uint32_t heads, uint32_t G, uint32_t tiles, boo
 // Bytes of AttnArgs::part a call may use.
 int64_t attn_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv, int64_t D, int64_t R,
                         bool backward);
+// Distances that occur lie within the longer side, so only that much of a
+// strip's range is worth its LDS and its partial gradients.
+inline int64_t attn_range(int64_t R, int64_t Lq, int64_t Lk)
+{
+    const int64_t most = Lq > Lk ? Lq : Lk;
+    return R < most ? R : most > 0 ? most : 1;
+}
+
 int64_t attn_forward_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv, int64_t D);
 
 // Parts of a row that several workgroups computed: its D output sums, maximum

@@ -22,11 +22,29 @@ constexpr int kThreads = 64 * kWaves;
 // Rows of statistics a head has: whole tiles.
 __host__ __device__ inline int stat_rows(int Lq) { return (Lq + 63) / 64 * 64; }
 
-// Floats of the partial strip gradients: one strip for each of attn_dq's
-// workgroups.
-int64_t strip_part_floats(int64_t B, int64_t Lq, int64_t H, int64_t R)
+// Workgroups that share the keys of one query tile in attn_dq, as in the
+// forward pass; a key costs more here, so shorter rows are worth it.
+int32_t dq_splits(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H)
 {
-    return R ? (B * H * ((Lq + kHeld - 1) / kHeld) * (2 * R + 1) + 3) / 4 * 4 : 0;
+    const int64_t groups = B * H * ((Lq + kHeld - 1) / kHeld);
+    const int64_t least = dt == IM2WIN_F32 ? 128 : 256, enough = groups < 256 ? 2 * least : 8 * least;
+    if (groups <= 0 || groups >= 512 || Lk < enough)
+        return 1;
+    const int64_t s = (512 + groups - 1) / groups;
+    return (int32_t)(s < Lk / least ? s : Lk / least);
+}
+
+// Floats of the partial strip gradients: one strip for each of attn_dq's
+// workgroups.  R here is what is left of the range (attn_range).
+int64_t strip_part_floats(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t R)
+{
+    const int64_t n = dq_splits(dt, B, Lq, Lk, H) * ((Lq + kHeld - 1) / kHeld);
+    return R ? (B * H * n * (2 * R + 1) + 3) / 4 * 4 : 0;
+}
+int64_t dq_part_floats(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t D)
+{
+    const int64_t s = dq_splits(dt, B, Lq, Lk, H);
+    return s > 1 ? s * B * H * Lq * D : 0;
 }
 
 // Workgroups that share the queries of one key tile: with few key/value heads
@@ -41,6 +59,12 @@ int32_t dkdv_splits(int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv)
     if (s > work / 4)  // at least four tiles each
         s = work / 4;
     return s < 1 ? 1 : (int32_t)s;
+}
+
+int64_t dkdv_part_floats(int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv, int64_t D)
+{
+    const int64_t s = dkdv_splits(B, Lq, Lk, H, Hkv);
+    return s > 1 ? s * B * Hkv * Lk * 2 * D : 0;
 }
 
 // Floats of attn_dq's strip and its gradients in LDS (even: 8-byte words follow).
@@ -434,7 +458,7 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccKV)) void attn_dkdv(Att
             issue(slot0, rows0, t);
         if (FEAT == kAny && a.R) {
             for (int x = threadIdx.x; x < 2 * a.R + 1; x += kThreads)
-                strip[x] = a.strip[(int64_t)hq * (2 * a.R + 1) + x] * kLog2e;
+                strip[x] = a.strip[hq * a.strip_step + x] * kLog2e;
             ring_barrier();
         }
         while (t < t_end) {
@@ -514,9 +538,11 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccQ)) void attn_dq(AttnAr
     const int width = 2 * a.R + 1;
     __shared__ int shared_most[kWaves], shared_lo[kWaves], shared_hi[kWaves];
 
-    const Work work = work_item(a.B * a.Hkv, a.G, a.tiles, a.causal, blockIdx.x);
+    // `splits` workgroups share the keys of a query tile
+    const Work work = work_item(a.B * a.Hkv, a.G * a.splits, a.tiles, a.causal, blockIdx.x);
     const int qt = a.tiles - 1 - work.tile;  // long rows of causal masks first
-    const int b = work.kv / a.Hkv, hk = work.kv - b * a.Hkv, hq = hk * a.G + work.g;
+    const int split = work.g / a.G;
+    const int b = work.kv / a.Hkv, hk = work.kv - b * a.Hkv, hq = hk * a.G + work.g % a.G;
     const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = qt * kHeld + wave * 32 + (lane & 31);
     const bool live = i < a.Lq;
@@ -544,7 +570,7 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccQ)) void attn_dq(AttnAr
     float far_lo = 0, far_hi = 0;
     if (FEAT == kAny && a.R)
         for (int t = threadIdx.x; t < width; t += kThreads) {
-            strip[t] = a.strip[(int64_t)hq * width + t] * kLog2e;
+            strip[t] = a.strip[hq * a.strip_step + t] * kLog2e;
             if (want_strip)
 #pragma unroll
                 for (int w = 1; w <= 2 * kWaves; ++w)
@@ -590,7 +616,8 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccQ)) void attn_dq(AttnAr
     const char *kp = a.k + b * a.k_sb + hk * a.k_sh, *vp = a.v + b * a.v_sb + hk * a.v_sh;
     const ScoreArgs sc = score_args(a);
 
-    const int tiles = (__builtin_amdgcn_readfirstlane(wg_most) + W::kRows - 1) / W::kRows;
+    const int all_tiles = (__builtin_amdgcn_readfirstlane(wg_most) + W::kRows - 1) / W::kRows;
+    const int tiles = (int)((int64_t)all_tiles * (split + 1) / a.splits);  // the first tile not this workgroup's
     const DocRange *const ranges = a.q_doc ? a.k_range + (int64_t)b * ((a.Lk + kDocTile - 1) / kDocTile) : nullptr;
     uint64_t *const bits = (uint64_t *)(strip + strip_floats(a.R, want_strip));
     if (a.q_doc) {
@@ -725,7 +752,7 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccQ)) void attn_dq(AttnAr
         }
         return next;
     };
-    int t = after(0);
+    int t = after((int)((int64_t)all_tiles * split / a.splits));
     if (t < tiles)
         issue(slot0, kdoc0, t);
     while (t < tiles) {
@@ -734,7 +761,10 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccQ)) void attn_dq(AttnAr
             break;
         t = step(slot1, kdoc1, slot0, kdoc0, t);
     }
-    if (live)
+    if (live && a.splits > 1)  // sums as they are; dq_join adds the splits
+        store_row<F32Op, DP>((char *)(a.part + (((int64_t)split * a.B * a.H + (int64_t)b * a.H + hq) * a.Lq + i) * a.D), dq,
+                             slope_scale(a) / dss, h, a.D);
+    else if (live)
         store_row<Op, DP>(a.dq + b * a.dq_sb + hq * a.dq_sh + (int64_t)i * a.dq_st, dq, slope_scale(a) / dss, h, a.D);
     if (FEAT != kAny || !want_strip)
         return;
@@ -749,7 +779,7 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccQ)) void attn_dq(AttnAr
         strip[width * (1 + 2 * wave) + 2 * a.R] = far_hi;
     }
     __syncthreads();
-    float *out = a.part + (((int64_t)hq * a.B + b) * a.tiles + qt) * width;
+    float *out = a.strip_part + ((((int64_t)hq * a.B + b) * a.splits + split) * a.tiles + qt) * width;
     for (int t = threadIdx.x; t < width; t += kThreads) {
         float v = 0;
 #pragma unroll
@@ -783,21 +813,47 @@ __global__ __launch_bounds__(kThreads) void dkdv_join(AttnArgs a)
     *(V *)(p + (d < a.D ? d : d - a.D) * sizeof(typename Op::elem)) = o;
 }
 
-// dstrip[h][x]: the sum of `n` partial strips, 64 entries a workgroup, each
-// by four lanes that take every fourth strip.
+// dq of a query: the sum of the splits, four channels a lane.
+template <class Op>
+__global__ __launch_bounds__(kThreads) void dq_join(AttnArgs a)
+{
+    const int per = a.D / 4;  // lanes a query
+    const int64_t rows = (int64_t)a.B * a.H * a.Lq, id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int64_t row = id / per;
+    if (row >= rows)
+        return;
+    const int d = (int)(id - row * per) * 4;
+    typedef float v4 __attribute__((ext_vector_type(4)));
+    v4 v = {0, 0, 0, 0};
+    for (int s = 0; s < a.splits; ++s)
+        v += *(const v4 *)(a.part + (s * rows + row) * a.D + d);
+    const int64_t bh = row / a.Lq, i = row - bh * a.Lq, b = bh / a.H, hq = bh - b * a.H;
+    typedef typename Op::elem V __attribute__((ext_vector_type(4)));
+    V o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        o[e] = (typename Op::elem)v[e];
+    *(V *)(a.dq + b * a.dq_sb + hq * a.dq_sh + i * a.dq_st + d * sizeof(typename Op::elem)) = o;
+}
+
+// dstrip[h][x]: the sum of `n` partial strips, which hold the `width` middle
+// entries of the `full` that a strip has (the others have no pair), 64 entries
+// a workgroup, each by four lanes that take every fourth strip.
 __global__ __launch_bounds__(kThreads) void strip_reduce(const float *__restrict__ part, float *__restrict__ dstrip,
-                                                         int32_t n, int32_t width)
+                                                         int32_t n, int32_t width, int32_t full)
 {
     __shared__ float s[4][64];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6, h = blockIdx.y;
+    const int x = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6, h = blockIdx.y;
+    const int c = x - (full - width) / 2;
     float v = 0;
-    if (c < width)
+    if (c >= 0 && c < width)
+#pragma unroll 4
         for (int r = k; r < n; r += 4)
             v += part[((int64_t)h * n + r) * width + c];
     s[k][threadIdx.x & 63] = v;
     __syncthreads();
-    if (k == 0 && c < width)
-        dstrip[(int64_t)h * width + c] =
+    if (k == 0 && x < full)
+        dstrip[(int64_t)h * full + x] =
             (s[0][threadIdx.x] + s[1][threadIdx.x]) + (s[2][threadIdx.x] + s[3][threadIdx.x]);
 }
 
@@ -805,6 +861,7 @@ template <class Op, int DP, int FEAT>
 hipError_t run(const AttnArgs &a, float *dstrip, hipStream_t st)
 {
     typedef Bwd<Op, DP> W;
+    constexpr int dt = __is_same(Op, F32Op) ? IM2WIN_F32 : __is_same(Op, F16Op) ? IM2WIN_F16 : IM2WIN_BF16;
     const int width = 2 * a.R + 1;
     AttnArgs b = a;
     hipError_t e;
@@ -837,20 +894,24 @@ hipError_t run(const AttnArgs &a, float *dstrip, hipStream_t st)
     b.tiles = (a.Lk + kHeld - 1) / kHeld;
     if (a.B * b.tiles) {
         b.splits = dkdv_splits(a.B, a.Lq, a.Lk, a.H, a.Hkv);
-        b.part = a.part + (dstrip ? strip_part_floats(a.B, a.Lq, a.H, a.R) : 0);
         attn_dkdv<Op, DP, FEAT><<<(uint32_t)(a.B * a.Hkv) * b.tiles * b.splits, kThreads, lds_kv, st>>>(b);
         const int64_t lanes = (int64_t)a.B * a.Hkv * a.Lk * (a.D / 2);
         if (b.splits > 1)
             dkdv_join<Op><<<(uint32_t)((lanes + kThreads - 1) / kThreads), kThreads, 0, st>>>(b);
-        b.part = a.part;
     }
     b.tiles = (a.Lq + kHeld - 1) / kHeld;
-    if (a.B * b.tiles)
-        attn_dq<Op, DP, FEAT><<<(uint32_t)(a.B * a.H) * b.tiles, kThreads, lds_q, st>>>(
-            b, dstrip != nullptr);
+    b.splits = dq_splits(dt, a.B, a.Lq, a.Lk, a.H);
+    b.part = a.part + dkdv_part_floats(a.B, a.Lq, a.Lk, a.H, a.Hkv, a.D);
+    b.strip_part = b.part + dq_part_floats(dt, a.B, a.Lq, a.Lk, a.H, a.D);
+    if (a.B * b.tiles) {
+        attn_dq<Op, DP, FEAT><<<(uint32_t)(a.B * a.H) * b.tiles * b.splits, kThreads, lds_q, st>>>(b, dstrip != nullptr);
+        const int64_t lanes = (int64_t)a.B * a.H * a.Lq * (a.D / 4);
+        if (b.splits > 1)
+            dq_join<Op><<<(uint32_t)((lanes + kThreads - 1) / kThreads), kThreads, 0, st>>>(b);
+    }
     if (dstrip)
-        strip_reduce<<<dim3((uint32_t)((width + 63) / 64), (uint32_t)a.H), kThreads, 0, st>>>(a.part, dstrip,
-                                                                                           a.B * b.tiles, width);
+        strip_reduce<<<dim3((uint32_t)((a.strip_step + 63) / 64), (uint32_t)a.H), kThreads, 0, st>>>(
+            b.strip_part, dstrip, a.B * b.tiles * b.splits, width, a.strip_step);
     return hipGetLastError();
 }
 
@@ -880,8 +941,8 @@ int64_t attn_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, in
 {
     if (!backward)
         return attn_forward_part_bytes(dt, B, Lq, Lk, H, Hkv, D);
-    const int64_t splits = dkdv_splits(B, Lq, Lk, H, Hkv);
-    return (strip_part_floats(B, Lq, H, R) + (splits > 1 ? splits * B * Hkv * Lk * 2 * D : 0)) * 4;
+    return (dkdv_part_floats(B, Lq, Lk, H, Hkv, D) + dq_part_floats(dt, B, Lq, Lk, H, D) +
+            strip_part_floats(dt, B, Lq, Lk, H, attn_range(R, Lq, Lk))) * 4;
 }
 
 hipError_t launch_attn_backward(const AttnArgs &a, int dt, float *dstrip, hipStream_t st)

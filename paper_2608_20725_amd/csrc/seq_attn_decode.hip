@@ -56,7 +56,7 @@ __global__ __launch_bounds__(64 * (Dec<Op, DP>::kNW)) void attn_decode(AttnArgs 
     const bool seen = live && lim > 0;
     const int dlo = wave_min(seen ? doc : INT32_MAX), dhi = wave_max(seen ? doc : -1);
     const DocRange *const ranges = a.q_doc ? a.k_range + (int64_t)b * ((a.Lk + kDocTile - 1) / kDocTile) : nullptr;
-    const float *const strip = a.strip + (live ? (int64_t)hq * (2 * a.R + 1) : 0);
+    const float *const strip = a.strip + (live ? hq * a.strip_step : 0);
     float far_l = 0, far_r = 0;
     if (a.R) {
         far_l = strip[0] * kLog2e;

@@ -63,7 +63,7 @@ __global__ __launch_bounds__(64 * kWaves, (Fwd<Op, DP>::kOcc)) void attn_fwd(Att
     }
     if (FEAT == kAny && a.R)
         for (int t = threadIdx.x; t < 2 * a.R + 1; t += 64 * kWaves)
-            strip[t] = a.strip[(int64_t)hq * (2 * a.R + 1) + t] * kLog2e;
+            strip[t] = a.strip[hq * a.strip_step + t] * kLog2e;
     __syncthreads();
     int wg_most = 0, wg_lo = INT32_MAX, wg_hi = -1;
 #pragma unroll
