@@ -1,11 +1,11 @@
 // Layer norm over the channels of each row, forward and backward.
 //
-// Both are one pass over the rows: a row is held in registers (64 or 256
-// lanes, up to 64 values a lane), so its two sums (mean, then the centred
-// squares: no cancellation) cost no second read, and the backward pass keeps
-// every lane's columns of dweight and dbias in registers over all the rows
-// of its workgroup.  Rows of more values than that go through the looped
-// kernels at the end.  Memory-bound: 2 (3) elements moved a value.
+// Both are one pass over the rows: a row is held in the registers of 8 to 1024
+// lanes, so its two sums (mean, then the centred squares: no cancellation)
+// cost no second read, and the backward pass keeps every lane's columns of
+// dweight and dbias in registers over all the rows of its workgroup.  Rows
+// that fit no register instance go through the looped kernels at the end.
+// Memory-bound: 2 (3) elements moved a value.
 #include "seq.hpp"
 
 namespace im2win {
@@ -13,115 +13,121 @@ namespace {
 
 constexpr int kThreads = 256;
 
-__device__ inline float wave_sum(float v)
-{
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1)
-        v += __shfl_xor(v, m);
-    return v;
-}
+// Threads of a workgroup whose rows take LPR lanes each.
+template <int LPR>
+constexpr int threads() { return LPR < 256 ? 256 : LPR; }
 
-// Sums of a and b over the row's lanes: WAVES = 1, the wave; 4, the workgroup
-// (red: 8 floats, free again on return).
-template <int WAVES>
+// Sums of a and b over the row's LPR lanes (red: 2*LPR/64 floats where a row
+// takes more than a wave, free again on return).
+template <int LPR>
 __device__ inline void row_sum2(float &a, float &b, float *red)
 {
-    a = wave_sum(a);
-    b = wave_sum(b);
-    if (WAVES == 1)
-        return;
-    const int w = threadIdx.x >> 6;
-    if ((threadIdx.x & 63) == 0) {
-        red[w] = a;
-        red[4 + w] = b;
+#pragma unroll
+    for (int m = (LPR < 64 ? LPR : 64) / 2; m >= 1; m >>= 1) {
+        a += __shfl_xor(a, m);
+        b += __shfl_xor(b, m);
     }
-    __syncthreads();
-    a = (red[0] + red[1]) + (red[2] + red[3]);
-    b = (red[4] + red[5]) + (red[6] + red[7]);
-    __syncthreads();
+    if constexpr (LPR > 64) {
+        constexpr int N = LPR / 64;
+        const int w = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) {
+            red[w] = a;
+            red[N + w] = b;
+        }
+        __syncthreads();
+        a = b = 0;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            a += red[k];
+            b += red[N + k];
+        }
+        __syncthreads();
+    }
 }
 
-// VEC values from p (aligned to VEC elements when VEC > 1) as fp32.
+// n of VEC values from p as fp32 (n <= 0: none), the others zero.  Rows of odd
+// length or stride start anywhere: the vectors are loaded and stored with
+// their element's alignment, which is the same instruction for aligned
+// addresses and hardly slower for others (5673 rows of 5112 fp16 channels
+// forward: 31 us both dense and 5115 apart; element by element 90 us).
 template <class E, int VEC>
-__device__ inline void load(const typename E::T *p, float *f)
+__device__ inline void load(const typename E::T *p, int n, float *f)
 {
-    typedef typename E::T V __attribute__((ext_vector_type(VEC)));
-    if constexpr (VEC == 1) {
-        f[0] = E::get(*p);
-    } else {
+    typedef typename E::T V __attribute__((ext_vector_type(VEC), aligned(sizeof(typename E::T))));
+    if (n >= VEC) {
         const V v = *(const V *)p;
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
             f[e] = E::get(v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            f[e] = e < n ? E::get(p[e]) : 0.0f;
     }
 }
 
 template <class E, int VEC>
-__device__ inline void store(typename E::T *p, const float *f)
+__device__ inline void store(typename E::T *p, int n, const float *f)
 {
-    typedef typename E::T V __attribute__((ext_vector_type(VEC)));
-    if constexpr (VEC == 1) {
-        *p = E::put(f[0]);
-    } else {
+    typedef typename E::T V __attribute__((ext_vector_type(VEC), aligned(sizeof(typename E::T))));
+    if (n >= VEC) {
         V v;
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
             v[e] = E::put(f[e]);
         *(V *)p = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (e < n)
+                p[e] = E::put(f[e]);
     }
 }
 
-// A row of C <= WAVES*64*NV*VEC values: vector i of a lane starts at column
-// (i*WAVES*64 + lane)*VEC.  C is a multiple of VEC.
-template <class E, class W, int VEC, int NV, int WAVES>
-__global__ __launch_bounds__(kThreads) void norm_fwd(const typename E::T *x,
+// A row of C <= LPR*NV*VEC values: vector i of a lane starts at column
+// (i*LPR + lane)*VEC.
+template <class E, class W, int VEC, int NV, int LPR>
+__global__ __launch_bounds__((threads<LPR>())) void norm_fwd(const typename E::T *x,
                                                      const typename W::T *__restrict__ w,
                                                      const typename W::T *__restrict__ b, typename E::T *y,
                                                      float *__restrict__ mean, float *__restrict__ rstd, int64_t rows,
                                                      int32_t C, int64_t xs, float eps)
 {
-    __shared__ float red[8];
-    constexpr int kRows = 4 / WAVES;
-    const int lane = WAVES == 1 ? (threadIdx.x & 63) : threadIdx.x;
+    __shared__ float red[LPR > 64 ? LPR / 32 : 1];
+    constexpr int kRows = threads<LPR>() / LPR;
+    const int lane = threadIdx.x % LPR;
     const float inv = 1.0f / (float)C;
     float wv[NV][VEC], bv[NV][VEC];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (i * WAVES * 64 + lane) * VEC;
-        if (c < C) {
-            load<W, VEC>(w + c, wv[i]);
-            load<W, VEC>(b + c, bv[i]);
-        }
+        const int c = (i * LPR + lane) * VEC;
+        load<W, VEC>(w + c, C - c, wv[i]);
+        load<W, VEC>(b + c, C - c, bv[i]);
     }
-    for (int64_t r = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? threadIdx.x >> 6 : 0); r < rows;
+    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / LPR; r < rows;
          r += (int64_t)gridDim.x * kRows) {
         float v[NV][VEC];
         float s = 0, q = 0, unused = 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (i * WAVES * 64 + lane) * VEC;
-            if (c < C)
-                load<E, VEC>(x + r * xs + c, v[i]);
-            else
-#pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    v[i][e] = 0;
+            const int c = (i * LPR + lane) * VEC;
+            load<E, VEC>(x + r * xs + c, C - c, v[i]);
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
                 s += v[i][e];
         }
-        row_sum2<WAVES>(s, unused, red);
+        row_sum2<LPR>(s, unused, red);
         const float mu = s * inv;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const bool in = (i * WAVES * 64 + lane) * VEC < C;
+            const int left = C - (i * LPR + lane) * VEC;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 v[i][e] -= mu;
-                q += in ? v[i][e] * v[i][e] : 0.0f;
+                q += e < left ? v[i][e] * v[i][e] : 0.0f;
             }
         }
-        row_sum2<WAVES>(q, unused, red);
+        row_sum2<LPR>(q, unused, red);
         const float rs = 1.0f / sqrtf(q * inv + eps);
         if (lane == 0) {
             mean[r] = mu;
@@ -129,57 +135,49 @@ __global__ __launch_bounds__(kThreads) void norm_fwd(const typename E::T *x,
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (i * WAVES * 64 + lane) * VEC;
-            if (c < C) {
-                float o[VEC];
+            const int c = (i * LPR + lane) * VEC;
+            float o[VEC];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    o[e] = v[i][e] * rs * wv[i][e] + bv[i][e];
-                store<E, VEC>(y + r * C + c, o);
-            }
+            for (int e = 0; e < VEC; ++e)
+                o[e] = v[i][e] * rs * wv[i][e] + bv[i][e];
+            store<E, VEC>(y + r * C + c, C - c, o);
         }
     }
 }
 
-template <class E, class W, int VEC, int NV, int WAVES>
-__global__ __launch_bounds__(kThreads) void norm_bwd(const typename E::T *__restrict__ dy,
+template <class E, class W, int VEC, int NV, int LPR>
+__global__ __launch_bounds__((threads<LPR>())) void norm_bwd(const typename E::T *__restrict__ dy,
                                                      const typename E::T *__restrict__ x,
                                                      const typename W::T *__restrict__ w,
                                                      const float *__restrict__ mean, const float *__restrict__ rstd,
                                                      typename E::T *__restrict__ dx, float *__restrict__ part,
                                                      int64_t rows, int32_t C, int64_t dys, int64_t xs)
 {
-    __shared__ float red[8];
-    extern __shared__ float cols[];  // WAVES = 1: [2][C]
-    constexpr int kRows = 4 / WAVES;
-    const int lane = WAVES == 1 ? (threadIdx.x & 63) : threadIdx.x;
+    __shared__ float red[LPR > 64 ? LPR / 32 : 1];
+    extern __shared__ float cols[];  // more than one row at a time: [2][C]
+    constexpr int kRows = threads<LPR>() / LPR;
+    const int lane = threadIdx.x % LPR;
     const float inv = 1.0f / (float)C;
     float wv[NV][VEC], aw[NV][VEC], ab[NV][VEC];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (i * WAVES * 64 + lane) * VEC;
+        const int c = (i * LPR + lane) * VEC;
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
-            wv[i][e] = aw[i][e] = ab[i][e] = 0;
-        if (c < C)
-            load<W, VEC>(w + c, wv[i]);
+            aw[i][e] = ab[i][e] = 0;
+        load<W, VEC>(w + c, C - c, wv[i]);
     }
-    for (int64_t r = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? threadIdx.x >> 6 : 0); r < rows;
+    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / LPR; r < rows;
          r += (int64_t)gridDim.x * kRows) {
         const float mu = mean[r], rs = rstd[r];
         float g[NV][VEC], h[NV][VEC];
         float s1 = 0, s2 = 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (i * WAVES * 64 + lane) * VEC;
-            if (c < C) {
-                load<E, VEC>(dy + r * dys + c, g[i]);
-                load<E, VEC>(x + r * xs + c, h[i]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    g[i][e] = 0, h[i][e] = mu;
-            }
+            const int c = (i * LPR + lane) * VEC;
+            // beyond the row dy is 0, and with it everything that is summed
+            load<E, VEC>(dy + r * dys + c, C - c, g[i]);
+            load<E, VEC>(x + r * xs + c, C - c, h[i]);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 h[i][e] = (h[i][e] - mu) * rs;
@@ -190,47 +188,45 @@ __global__ __launch_bounds__(kThreads) void norm_bwd(const typename E::T *__rest
                 s2 += g[i][e] * h[i][e];
             }
         }
-        row_sum2<WAVES>(s1, s2, red);
+        row_sum2<LPR>(s1, s2, red);
         s1 *= inv;
         s2 *= inv;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (i * WAVES * 64 + lane) * VEC;
-            if (c < C) {
-                float o[VEC];
+            const int c = (i * LPR + lane) * VEC;
+            float o[VEC];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    o[e] = rs * (g[i][e] - s1 - h[i][e] * s2);
-                store<E, VEC>(dx + r * C + c, o);
-            }
+            for (int e = 0; e < VEC; ++e)
+                o[e] = rs * (g[i][e] - s1 - h[i][e] * s2);
+            store<E, VEC>(dx + r * C + c, C - c, o);
         }
     }
-    // this workgroup's [2][C] sums: one wave after the other adds its own
+    // this workgroup's [2][C] sums: one row's lanes after the other add theirs
     float *out = part + (int64_t)blockIdx.x * 2 * C;
-    if (WAVES == 1) {
-        for (int k = 0; k < 4; ++k) {
-            if ((int)(threadIdx.x >> 6) == k)
+    if constexpr (kRows > 1) {
+        for (int k = 0; k < kRows; ++k) {
+            if ((int)(threadIdx.x / LPR) == k)
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
-                    const int c = (i * 64 + lane) * VEC;
-                    if (c < C)
+                    const int c = (i * LPR + lane) * VEC;
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e) {
+                    for (int e = 0; e < VEC; ++e)
+                        if (c + e < C) {
                             cols[c + e] = (k ? cols[c + e] : 0.0f) + aw[i][e];
                             cols[C + c + e] = (k ? cols[C + c + e] : 0.0f) + ab[i][e];
                         }
                 }
             __syncthreads();
         }
-        for (int c = threadIdx.x; c < 2 * C; c += kThreads)
+        for (int c = threadIdx.x; c < 2 * C; c += threads<LPR>())
             out[c] = cols[c];
     } else {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (i * WAVES * 64 + lane) * VEC;
-            if (c < C)
+            const int c = (i * LPR + lane) * VEC;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
+            for (int e = 0; e < VEC; ++e)
+                if (c + e < C) {
                     out[c + e] = aw[i][e];
                     out[C + c + e] = ab[i][e];
                 }
@@ -252,13 +248,13 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_long(const typename E::T *x
         float s = 0, q = 0, unused = 0;
         for (int c = threadIdx.x; c < C; c += kThreads)
             s += E::get(x[r * xs + c]);
-        row_sum2<4>(s, unused, red);
+        row_sum2<256>(s, unused, red);
         const float mu = s * inv;
         for (int c = threadIdx.x; c < C; c += kThreads) {
             const float d = E::get(x[r * xs + c]) - mu;
             q += d * d;
         }
-        row_sum2<4>(q, unused, red);
+        row_sum2<256>(q, unused, red);
         const float rs = 1.0f / sqrtf(q * inv + eps);
         if (threadIdx.x == 0) {
             mean[r] = mu;
@@ -287,7 +283,7 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_long(const typename E::T *_
             s1 += g;
             s2 += g * (E::get(x[r * xs + c]) - mu) * rs;
         }
-        row_sum2<4>(s1, s2, red);
+        row_sum2<256>(s1, s2, red);
         for (int c = threadIdx.x; c < C; c += kThreads) {
             const float g = E::get(dy[r * dys + c]) * W::get(w[c]), h = (E::get(x[r * xs + c]) - mu) * rs;
             dx[r * C + c] = E::put(rs * (g - s1 * inv - h * s2 * inv));
@@ -355,51 +351,53 @@ struct Args {
     hipStream_t st;
 };
 
-template <class E, class W, int VEC, int NV, int WAVES>
+template <class E, class W, int VEC, int NV, int LPR>
 void run(const Args &a, bool bwd)
 {
     typedef typename E::T T;
     typedef typename W::T U;
-    const int64_t rows_wg = 4 / WAVES;
+    const int64_t rows_wg = threads<LPR>() / LPR;
     if (!bwd) {
         const int64_t want = (a.rows + rows_wg - 1) / rows_wg;
         const int64_t grid = want < 4096 ? want : 4096;
-        norm_fwd<E, W, VEC, NV, WAVES><<<(uint32_t)grid, kThreads, 0, a.st>>>(
+        norm_fwd<E, W, VEC, NV, LPR><<<(uint32_t)grid, threads<LPR>(), 0, a.st>>>(
             (const T *)a.x, (const U *)a.w, (const U *)a.b, (T *)a.y, a.mean, a.rstd, a.rows, (int32_t)a.C, a.xs,
             a.eps);
     } else {
-        const size_t lds = WAVES == 1 ? (size_t)a.C * 8 : 0;
-        norm_bwd<E, W, VEC, NV, WAVES><<<(uint32_t)norm_partial_rows(a.rows, a.C), kThreads, lds, a.st>>>(
+        const size_t lds = rows_wg > 1 ? (size_t)a.C * 8 : 0;
+        norm_bwd<E, W, VEC, NV, LPR><<<(uint32_t)norm_partial_rows(a.rows, a.C), threads<LPR>(), lds, a.st>>>(
             (const T *)a.dy, (const T *)a.x, (const U *)a.w, a.mean, a.rstd, (T *)a.y, a.part, a.rows, (int32_t)a.C,
             a.dys, a.xs);
     }
 }
 
-// The smallest instance that holds a row of C values read VEC at a time;
-// false when none does.
+// The smallest instance that holds a row of C values; false when none does.
+// Rows shorter than a wave's 64 vectors share the wave; long ones take up to
+// 16 waves before a lane holds more than two vectors.
 template <class E, class W, int VEC>
 bool run_held(const Args &a, bool bwd)
 {
     const int64_t n = (a.C + VEC - 1) / VEC;  // vectors in a row
-    constexpr int kMost = VEC == 1 ? 32 : 32 / VEC;  // vectors a lane of a 1-wave row
-    if (n <= 64)
-        run<E, W, VEC, 1, 1>(a, bwd);
+    if (n <= 8)
+        run<E, W, VEC, 1, 8>(a, bwd);
+    else if (n <= 16)
+        run<E, W, VEC, 1, 16>(a, bwd);
+    else if (n <= 32)
+        run<E, W, VEC, 1, 32>(a, bwd);
+    else if (n <= 64)
+        run<E, W, VEC, 1, 64>(a, bwd);
     else if (n <= 128)
-        run<E, W, VEC, 2, 1>(a, bwd);
+        run<E, W, VEC, 2, 64>(a, bwd);
     else if (n <= 256)
-        run<E, W, VEC, 4, 1>(a, bwd);
-    else if (kMost >= 8 && n <= 512)
-        run<E, W, VEC, kMost >= 8 ? 8 : 1, 1>(a, bwd);
-    else if (kMost >= 16 && n <= 1024)
-        run<E, W, VEC, kMost >= 16 ? 16 : 1, 1>(a, bwd);
+        run<E, W, VEC, 4, 64>(a, bwd);
     else if (n <= 512)
-        run<E, W, VEC, 2, 4>(a, bwd);
+        bwd ? run<E, W, VEC, 1, 512>(a, bwd) : run<E, W, VEC, 2, 256>(a, bwd);
     else if (n <= 1024)
-        run<E, W, VEC, 4, 4>(a, bwd);
-    else if (VEC <= 4 && n <= 2048)
-        run<E, W, VEC, VEC <= 4 ? 8 : 1, 4>(a, bwd);
-    else if (VEC == 1 && n <= 8192)
-        run<E, W, VEC, VEC == 1 ? 32 : 1, 4>(a, bwd);
+        bwd ? run<E, W, VEC, 2, 512>(a, bwd) : run<E, W, VEC, 4, 256>(a, bwd);
+    else if (n <= 2048)
+        run<E, W, VEC, 2, 1024>(a, bwd);
+    else if (n <= 4096)
+        run<E, W, VEC, 4, 1024>(a, bwd);
     else
         return false;
     return true;
@@ -410,13 +408,9 @@ void run_typed(const Args &a, bool bwd, void *dw, void *db)
 {
     typedef typename E::T T;
     typedef typename W::T U;
-    constexpr int VEC = 16 / sizeof(T);
-    // 16-byte loads where every row and the parameters allow them
-    const uintptr_t p = (uintptr_t)a.x | (uintptr_t)a.y | (uintptr_t)a.w | (uintptr_t)a.b | (uintptr_t)a.dy;
-    const bool vec = (p & 15) == 0 && a.C % VEC == 0 && a.xs % VEC == 0 && a.dys % VEC == 0;
     const int32_t C = (int32_t)a.C;
     const int64_t grid = a.rows < 8192 ? a.rows : 8192;
-    if (!(vec ? run_held<E, W, VEC>(a, bwd) : run_held<E, W, 1>(a, bwd))) {
+    if (!run_held<E, W, 16 / sizeof(T)>(a, bwd)) {
         if (!bwd) {
             norm_fwd_long<E, W><<<(uint32_t)grid, kThreads, 0, a.st>>>((const T *)a.x, (const U *)a.w, (const U *)a.b,
                                                                        (T *)a.y, a.mean, a.rstd, a.rows, C, a.xs,
@@ -450,9 +444,10 @@ hipError_t run_any(const Args &a, bool bwd, int dt, int wdt, void *dw, void *db)
 
 int64_t norm_partial_rows(int64_t rows, int64_t C)
 {
-    (void)C;
-    // enough workgroups to fill 256 CUs, and at least 32 rows for each
-    const int64_t n = (rows + 31) / 32;
+    // enough workgroups to fill 256 CUs; a workgroup takes one row at a time,
+    // or four of the short ones, and with many rows at least 32
+    const int64_t least = (rows + 31) / 32, step = C <= 1024 ? (rows + 3) / 4 : rows;
+    const int64_t n = least > 256 ? least : step < 256 ? step : 256;
     return n < 1 ? 1 : n > 1024 ? 1024 : n;
 }
 
