@@ -76,7 +76,10 @@ def _rows(x, what):
     if x.dim() == 0:
         raise ValueError("%s must have a channel dimension" % what)
     C = x.shape[-1]
-    flat = x if x.dim() == 2 else x.view(-1, C)  # view refuses what has no single row stride
+    try:
+        flat = x if x.dim() == 2 else x.view(-1, C)
+    except RuntimeError:
+        raise ValueError("%s must have evenly spaced rows (one stride over its leading dimensions)" % what) from None
     if C > 1 and flat.stride(1) != 1:
         raise ValueError("%s must be dense in its last dimension" % what)
     return flat.shape[0], C, flat.stride(0) if flat.shape[0] > 1 else C
@@ -196,6 +199,8 @@ def seq_rel_bias_backward(dstrip, buckets: int, two_sided: bool = True, dtype=No
 def _strides(t, what):
     """Strides of the sequence, token and head dimensions."""
     st = t.stride()
+    if len(st) != 4:
+        raise ValueError("%s must have four dimensions" % what)
     if st[3] != 1 and t.shape[3] > 1:
         raise ValueError("%s must be dense in its last dimension" % what)
     return st[:3]
