@@ -304,17 +304,61 @@ __device__ inline float pair_max(float v)
 __device__ constexpr int reg_row(int r) { return 8 * (r >> 2) + (r & 3); }
 
 // How products q.k become scores in units of ln 2: x*c1, or capped,
-// c2*tanh(x*scale/cap) = c2 - 2*c2*r with r = 1/(1 + e^(2*x*scale/cap)) =
-// half(x*c1).  tanh's slope 1 - tanh^2 is 4*(r - r^2).
+// c2*tanh(x*c1).
 struct ScoreArgs {
     float c1, c2;
     bool cap;
 };
 __device__ inline ScoreArgs score_args(const AttnArgs &a)
 {
-    return ScoreArgs{a.cap > 0 ? a.scale / a.cap * (2.0f * kLog2e) : a.scale * kLog2e, a.cap * kLog2e, a.cap > 0};
+    return ScoreArgs{a.cap > 0 ? a.scale / a.cap : a.scale * kLog2e, a.cap * kLog2e, a.cap > 0};
 }
-__device__ inline float half(float y) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y)); }
+
+// tanh(u) for |u| < 1/4: its Taylor series to u^9 (the next term is below 9e-9
+// of the value).  1 - 2/(1 + e^2u), which serves the rest, is off by 6e-8
+// whatever u is: with scores far below the cap, as most are, that would be an
+// error of 1e-5 in the exponent (cap 50).
+constexpr float kSmallTanh = 0.25f;
+__device__ inline float small_tanh(float u)
+{
+    const float w = u * u;
+    float p = fmaf(w, 62.0f / 2835.0f, -17.0f / 315.0f);
+    p = fmaf(w, p, 2.0f / 15.0f);
+    p = fmaf(w, p, -1.0f / 3.0f);
+    return fmaf(u * w, p, u);
+}
+
+// s = tanh(s*c1) of N tiles.  Where all arguments of the wave are small the
+// exponential and the reciprocal are left out; which of the two forms a value
+// takes depends on itself alone.
+template <int N>
+__device__ inline void tanh_scores(f32x16_acc (&s)[N], float c1)
+{
+    float m[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[t][r] *= c1;
+            m[r & 3] = fmaxf(m[r & 3], fabsf(s[t][r]));
+        }
+    if (!__any(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) >= kSmallTanh)) {
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[t][r] = small_tanh(s[t][r]);
+    } else {
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float u = s[t][r];
+                const float big = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * (2.0f * kLog2e)));
+                s[t][r] = fabsf(u) < kSmallTanh ? small_tanh(u) : big;
+            }
+    }
+}
 
 // A query's running softmax: output sums, maximum (of the pair), sum (of this
 // lane's keys), both times 2^kShift.
@@ -328,6 +372,10 @@ struct RowState {
     static constexpr float kSlack = kIs16 ? 1.0f : 8.0f;
     f32x16_acc o[DP / 32];
     float m, l;
+
+    // ln of the sum of exponentials, from a row's maximum and (whole) sum: the
+    // shift is taken off the sum, not off the large logarithm.
+    __device__ static inline float lse(float m, float l) { return (m + __log2f(l * (kIs16 ? 0x1p-14f : 1.0f))) * kLn2; }
 
     __device__ inline void clear()
     {
@@ -428,15 +476,10 @@ __device__ inline void attend(const char *tk, const char *tv, const typename Op:
     // fused multiply-add scales a score and subtracts the maximum.
     float mul = sc.c1, add = FEAT == kAny ? tp.far : 0.0f;
     if (cap) {
-#pragma unroll
-        for (int t = 0; t < SUB; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                s[t][r] = -half(s[t][r] * sc.c1);
-        mul = 2.0f * sc.c2;
-        add += sc.c2;
+        tanh_scores(s, sc.c1);
+        mul = sc.c2;
     }
-    if ((FEAT == kAny && tp.near) || !(sc.c1 > 0)) {
+    if ((FEAT == kAny && tp.near) || !(mul > 0)) {
 #pragma unroll
         for (int t = 0; t < SUB; ++t)
 #pragma unroll

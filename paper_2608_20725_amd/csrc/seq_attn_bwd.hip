@@ -197,18 +197,18 @@ __global__ __launch_bounds__(kThreads) void value_norms(AttnArgs a)
 // ---- what both kernels do with a 32 x 32 tile of scores ----
 
 // Exponents of the probabilities (base 2), without the bias: the scores of
-// the products in s less lse(r), the row statistic of register r; slope: a
-// quarter of 1 - tanh^2 where scores are capped (slope_scale has the rest).
-__device__ inline float slope_scale(const AttnArgs &a) { return a.cap > 0 ? 4.0f * a.scale : a.scale; }
+// the products in s less lse(r), the row statistic of register r; slope:
+// 1 - tanh^2 where scores are capped.
 template <int FEAT, class Lse>
 __device__ inline void to_scores(f32x16_acc &s, f32x16_acc &slope, const ScoreArgs &c, Lse lse)
 {
     if (FEAT == kAny ? c.cap : FEAT == kCapped) {
+        f32x16_acc t[1] = {s};
+        tanh_scores(t, c.c1);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            const float t = half(s[r] * c.c1);
-            slope[r] = fmaf(-t, t, t);
-            s[r] = fmaf(-2.0f * c.c2, t, c.c2 - lse(r));
+            slope[r] = fmaf(-t[0][r], t[0][r], 1.0f);
+            s[r] = fmaf(c.c2, t[0][r], -lse(r));
         }
     } else {
 #pragma unroll
@@ -472,11 +472,11 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccKV)) void attn_dkdv(Att
         return;
     if (a.splits > 1) {  // sums as they are; dkdv_join adds the splits
         float *const part = a.part + (((int64_t)work.g * a.B * a.Hkv + work.kv) * a.Lk + j) * 2 * a.D;
-        store_row<F32Op, DP>((char *)part, dk, slope_scale(a) / dss, h, a.D);
+        store_row<F32Op, DP>((char *)part, dk, a.scale / dss, h, a.D);
         store_row<F32Op, DP>((char *)(part + a.D), dv, exp2f(-p_shift<Op>()), h, a.D);
         return;
     }
-    store_row<Op, DP>(a.dk + b * a.dk_sb + hk * a.dk_sh + (int64_t)j * a.dk_st, dk, slope_scale(a) / dss, h, a.D);
+    store_row<Op, DP>(a.dk + b * a.dk_sb + hk * a.dk_sh + (int64_t)j * a.dk_st, dk, a.scale / dss, h, a.D);
     store_row<Op, DP>(a.dv + b * a.dv_sb + hk * a.dv_sh + (int64_t)j * a.dv_st, dv, exp2f(-p_shift<Op>()), h, a.D);
 }
 
@@ -763,9 +763,9 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccQ)) void attn_dq(AttnAr
     }
     if (live && a.splits > 1)  // sums as they are; dq_join adds the splits
         store_row<F32Op, DP>((char *)(a.part + (((int64_t)split * a.B * a.H + (int64_t)b * a.H + hq) * a.Lq + i) * a.D), dq,
-                             slope_scale(a) / dss, h, a.D);
+                             a.scale / dss, h, a.D);
     else if (live)
-        store_row<Op, DP>(a.dq + b * a.dq_sb + hq * a.dq_sh + (int64_t)i * a.dq_st, dq, slope_scale(a) / dss, h, a.D);
+        store_row<Op, DP>(a.dq + b * a.dq_sb + hq * a.dq_sh + (int64_t)i * a.dq_st, dq, a.scale / dss, h, a.D);
     if (FEAT != kAny || !want_strip)
         return;
 #pragma unroll

@@ -156,7 +156,7 @@ __global__ __launch_bounds__(64 * (Dec<Op, DP>::kNW)) void attn_decode(AttnArgs 
             part[a.D + 1] = sum;
         }
     } else if (live && wave == 0 && h == 0) {
-        a.lse[out_row] = none ? -INFINITY : (m - st.kShift + __log2f(sum)) * kLn2;
+        a.lse[out_row] = none ? -INFINITY : st.lse(m, sum);
     }
     // a wave takes every NW-th row, a lane its channels
     for (int c = wave; c < 32 && rt * 32 + c < rows; c += NW) {
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(256) void attn_join(AttnArgs a)
     const float inv = none ? 0.0f : 1.0f / l;
     if (lane == 0)
         a.lse[((int64_t)b * a.H + hq) * a.Lq + i] =
-            none ? -INFINITY : (m - RowState<Op, 32>::kShift + __log2f(l)) * kLn2;
+            none ? -INFINITY : RowState<Op, 32>::lse(m, l);
     if (d < a.D) {
         typedef typename Op::elem V __attribute__((ext_vector_type(4)));
         V o;

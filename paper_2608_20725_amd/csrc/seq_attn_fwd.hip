@@ -160,7 +160,7 @@ __global__ __launch_bounds__(64 * kWaves, (Fwd<Op, DP>::kOcc)) void attn_fwd(Att
     const bool none = st.m == -INFINITY;
     const float inv = none ? 0.0f : 1.0f / l;
     if (h == 0)
-        a.lse[((int64_t)b * a.H + hq) * a.Lq + i] = none ? -INFINITY : (st.m - st.kShift + __log2f(l)) * kLn2;
+        a.lse[((int64_t)b * a.H + hq) * a.Lq + i] = none ? -INFINITY : st.lse(st.m, l);
     store_row<Op, DP>(a.out + b * a.o_sb + hq * a.o_sh + (int64_t)i * a.o_st, st.o, inv, h, a.D);
 }
 
