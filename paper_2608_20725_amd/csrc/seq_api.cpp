@@ -206,7 +206,7 @@ Sizes sizes_of(const seq_attention_t *a, bool backward)
     }
     if (backward) {
         s.stat = pad256(a->B * a->H * ((a->Lq + 63) / 64 * 64) * 8);
-        s.norms = pad256(a->B * a->H * 8);
+        s.norms = a->dt == IM2WIN_F16 ? pad256(attn_norm_bytes(a->B, a->Lq, a->Lk, a->H, a->Hkv)) : 0;
     }
     s.part = pad256(attn_part_bytes(a->dt, a->B, a->Lq, a->Lk, a->H, a->Hkv, a->D, a->R, backward));
     s.total = s.stat + s.norms + s.q_range + s.k_range + s.part;
@@ -240,7 +240,7 @@ int place(AttnArgs *r, const seq_attention_t *a, const Sizes &s, void *ws, hipSt
 {
     char *p = (char *)ws;
     r->stat = (float *)p, p += s.stat;
-    r->norms = (uint32_t *)p, p += s.norms;
+    r->norms = (float *)p, p += s.norms;
     DocRange *qr = (DocRange *)p;
     p += s.q_range;
     DocRange *kr = (DocRange *)p;

@@ -42,7 +42,7 @@ struct AttnArgs {
     char *out, *dq, *dk, *dv;
     float *lse;
     float *stat;          // backward: [B][H][2][Lq rounded up to 64] lse*log2(e) less p_shift (+inf: no pair), dout.out
-    uint32_t *norms;      // backward, fp16: bits of the largest |dout_i| and |v_j| [B][H][2]
+    float *norms;         // backward, fp16: the largest |dout_i| and |v_j| of groups of rows
     float *part;          // sums of rows that several workgroups share
     float *strip_part;    // backward: the strip's gradients of every workgroup
     const float *strip;   // its middle 2R+1 entries; heads strip_step apart
@@ -687,7 +687,8 @@ __device__ inline Work work_item(uint32_t heads, uint32_t G, uint32_t tiles, boo
     return w;
 }
 
-// Bytes of AttnArgs::part a call may use.
+// Bytes of AttnArgs::norms and part a call may use.
+int64_t attn_norm_bytes(int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv);
 int64_t attn_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv, int64_t D, int64_t R,
                         bool backward);
 // Distances that occur lie within the longer side, so only that much of a

@@ -78,13 +78,31 @@ constexpr float p_shift() { return 0.0f; }
 template <>
 constexpr float p_shift<F16Op>() { return 14.0f; }
 
+constexpr int kStatRows = 64;  // rows a workgroup of row_stats, 16 lanes each
+
+// fp16: the largest |dout_i| and |v_j| that each workgroup of row_stats met,
+// [B*Hkv][G*query tiles + key tiles].
+__host__ __device__ inline int norm_tiles(int L) { return (L + kStatRows - 1) / kStatRows; }
+__host__ __device__ inline int64_t norm_step(int G, int Lq, int Lk) { return (int64_t)G * norm_tiles(Lq) + norm_tiles(Lk); }
+
 // The power of two that dS of a head group is multiplied by.
 template <class Op>
 __device__ inline float ds_scale(const AttnArgs &a, int b, int hk)
 {
     if constexpr (sizeof(typename Op::elem) == 2 && p_shift<Op>() > 0) {
-        const uint32_t *n = a.norms + ((int64_t)b * a.Hkv + hk) * 2;
-        const float bound = 2.0f * __uint_as_float(n[0]) * __uint_as_float(n[1]);
+        const int nq = a.G * norm_tiles(a.Lq), nk = norm_tiles(a.Lk);
+        const float *const p = a.norms + ((int64_t)b * a.Hkv + hk) * (nq + nk);
+        float q = 0, v = 0;
+        for (int i = threadIdx.x & 63; i < nq; i += 64)
+            q = fmaxf(q, p[i]);
+        for (int i = threadIdx.x & 63; i < nk; i += 64)
+            v = fmaxf(v, p[nq + i]);
+#pragma unroll
+        for (int m = 32; m >= 1; m >>= 1) {
+            q = fmaxf(q, __shfl_xor(q, m));
+            v = fmaxf(v, __shfl_xor(v, m));
+        }
+        const float bound = 2.0f * q * v;
         const float e = bound > 0 ? floorf(15.0f - __log2f(bound) - 0.01f) : 0.0f;
         return exp2f(fminf(fmaxf(e, -40.0f), 40.0f));
     }
@@ -92,12 +110,6 @@ __device__ inline float ds_scale(const AttnArgs &a, int b, int hk)
 }
 
 // ---- row statistics ----
-
-__global__ __launch_bounds__(kThreads) void clear_words(uint32_t *p, int64_t n)
-{
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads)
-        p[i] = 0;
-}
 
 template <class Op>
 __device__ inline void load8(const char *p, float *f)
@@ -116,8 +128,8 @@ __device__ inline float sum16(float v)
     return v;
 }
 
-// Raises *to to the largest of v over the workgroup.
-__device__ inline void raise(uint32_t *to, float v)
+// *to = the largest of v over the workgroup.
+__device__ inline void store_max(float *to, float v)
 {
     __shared__ float w[kWaves];
 #pragma unroll
@@ -127,21 +139,41 @@ __device__ inline void raise(uint32_t *to, float v)
         w[threadIdx.x >> 6] = v;
     __syncthreads();
     if (threadIdx.x == 0)
-        atomicMax(to, __float_as_uint(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]))));  // the same in any order
+        *to = fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]));
 }
 
-constexpr int kStatRows = 64;  // rows a workgroup, 16 lanes each
-
 // {lse*log2(e) - p_shift, dout.out} and, fp16, the largest |dout| (finite ones
-// of queries that see something).
+// of queries that see something); the workgroups after those of the queries
+// take, fp16, the largest |v| of the keys there are.
 template <class Op>
 __global__ __launch_bounds__(kThreads) void row_stats(AttnArgs a)
 {
-    const uint32_t bh = blockIdx.x / a.tiles, t = blockIdx.x - bh * a.tiles;
-    const int b = bh / a.H, hq = bh - b * a.H, d = (threadIdx.x & 15) * 8;
+    const int d = (threadIdx.x & 15) * 8, tq = norm_tiles(a.Lq), tk = norm_tiles(a.Lk);
+    const uint32_t queries = (uint32_t)(a.B * a.H) * tq;
+    float most = 0;
+    if (blockIdx.x >= queries) {
+        const uint32_t id = blockIdx.x - queries, kv = id / tk;
+        const int t = id - kv * tk, b = kv / a.Hkv, hk = kv - b * a.Hkv, n = keys_of(a, b);
+#pragma unroll
+        for (int k = 0; k < kStatRows / 16; ++k) {
+            const int j = t * kStatRows + k * 16 + (threadIdx.x >> 4);
+            float f[8], sq = 0;
+            if (j < n && d < a.D && (!a.k_doc || a.k_doc[(int64_t)b * a.Lk + j] >= 0)) {
+                load8<Op>(a.v + b * a.v_sb + hk * a.v_sh + (int64_t)j * a.v_st + d * sizeof(typename Op::elem), f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    sq += f[e] * f[e];
+            }
+            sq = sum16(sq);
+            most = fmaxf(most, sq < INFINITY ? sq : 0.0f);
+        }
+        store_max(a.norms + kv * norm_step(a.G, a.Lq, a.Lk) + a.G * tq + t, sqrtf(most));
+        return;
+    }
+    const uint32_t bh = blockIdx.x / tq;
+    const int t = blockIdx.x - bh * tq, b = bh / a.H, hq = bh - b * a.H;
     const int Lp = stat_rows(a.Lq);
     float *const stat = a.stat + (int64_t)bh * 2 * Lp;
-    float most = 0;
 #pragma unroll
     for (int k = 0; k < kStatRows / 16; ++k) {
         const int i = t * kStatRows + k * 16 + (threadIdx.x >> 4);
@@ -168,30 +200,7 @@ __global__ __launch_bounds__(kThreads) void row_stats(AttnArgs a)
         }
     }
     if constexpr (p_shift<Op>() > 0)
-        raise(a.norms + ((int64_t)b * a.Hkv + hq / a.G) * 2, sqrtf(most));
-}
-
-// fp16: the largest |v_j| of each key/value head.
-template <class Op>
-__global__ __launch_bounds__(kThreads) void value_norms(AttnArgs a)
-{
-    const uint32_t bh = blockIdx.x / a.tiles, t = blockIdx.x - bh * a.tiles;
-    const int b = bh / a.Hkv, hk = bh - b * a.Hkv, d = (threadIdx.x & 15) * 8, n = keys_of(a, b);
-    float most = 0;
-#pragma unroll
-    for (int k = 0; k < kStatRows / 16; ++k) {
-        const int j = t * kStatRows + k * 16 + (threadIdx.x >> 4);
-        float f[8], sq = 0;
-        if (j < n && d < a.D && (!a.k_doc || a.k_doc[(int64_t)b * a.Lk + j] >= 0)) {
-            load8<Op>(a.v + b * a.v_sb + hk * a.v_sh + (int64_t)j * a.v_st + d * sizeof(typename Op::elem), f);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                sq += f[e] * f[e];
-        }
-        sq = sum16(sq);
-        most = fmaxf(most, sq < INFINITY ? sq : 0.0f);
-    }
-    raise(a.norms + ((int64_t)b * a.Hkv + hk) * 2 + 1, sqrtf(most));
+        store_max(a.norms + ((int64_t)b * a.Hkv + hq / a.G) * norm_step(a.G, a.Lq, a.Lk) + hq % a.G * tq + t, sqrtf(most));
 }
 
 // ---- what both kernels do with a 32 x 32 tile of scores ----
@@ -838,23 +847,29 @@ __global__ __launch_bounds__(kThreads) void dq_join(AttnArgs a)
 
 // dstrip[h][x]: the sum of `n` partial strips, which hold the `width` middle
 // entries of the `full` that a strip has (the others have no pair), 64 entries
-// a workgroup, each by four lanes that take every fourth strip.
-__global__ __launch_bounds__(kThreads) void strip_reduce(const float *__restrict__ part, float *__restrict__ dstrip,
-                                                         int32_t n, int32_t width, int32_t full)
+// a workgroup, each by 16 lanes that take every 16th strip.
+constexpr int kReducers = 16;
+__global__ __launch_bounds__(64 * kReducers) void strip_reduce(const float *__restrict__ part,
+                                                               float *__restrict__ dstrip, int32_t n, int32_t width,
+                                                               int32_t full)
 {
-    __shared__ float s[4][64];
+    __shared__ float s[kReducers][64];
     const int x = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6, h = blockIdx.y;
     const int c = x - (full - width) / 2;
     float v = 0;
     if (c >= 0 && c < width)
 #pragma unroll 4
-        for (int r = k; r < n; r += 4)
+        for (int r = k; r < n; r += kReducers)
             v += part[((int64_t)h * n + r) * width + c];
     s[k][threadIdx.x & 63] = v;
     __syncthreads();
-    if (k == 0 && x < full)
-        dstrip[(int64_t)h * full + x] =
-            (s[0][threadIdx.x] + s[1][threadIdx.x]) + (s[2][threadIdx.x] + s[3][threadIdx.x]);
+    if (k == 0 && x < full) {
+        v = 0;
+#pragma unroll
+        for (int r = 0; r < kReducers; ++r)
+            v += s[r][threadIdx.x];
+        dstrip[(int64_t)h * full + x] = v;
+    }
 }
 
 template <class Op, int DP, int FEAT>
@@ -865,18 +880,10 @@ hipError_t run(const AttnArgs &a, float *dstrip, hipStream_t st)
     const int width = 2 * a.R + 1;
     AttnArgs b = a;
     hipError_t e;
-    if constexpr (p_shift<Op>() > 0) {
-        const int64_t words = (int64_t)a.B * a.Hkv * 2;
-        if (words)
-            clear_words<<<(uint32_t)((words + kThreads - 1) / kThreads < 256 ? (words + kThreads - 1) / kThreads : 256),
-                          kThreads, 0, st>>>(a.norms, words);
-        b.tiles = (a.Lk + kStatRows - 1) / kStatRows;
-        if (a.B * b.tiles)
-            value_norms<Op><<<(uint32_t)(a.B * a.Hkv) * b.tiles, kThreads, 0, st>>>(b);
-    }
-    b.tiles = stat_rows(a.Lq) / kStatRows;
-    if (a.B * b.tiles)
-        row_stats<Op><<<(uint32_t)(a.B * a.H) * b.tiles, kThreads, 0, st>>>(b);
+    const uint32_t stat_groups = (uint32_t)(a.B * a.H) * norm_tiles(a.Lq) +
+                                 (p_shift<Op>() > 0 ? (uint32_t)(a.B * a.Hkv) * norm_tiles(a.Lk) : 0);
+    if (stat_groups)
+        row_stats<Op><<<stat_groups, kThreads, 0, st>>>(b);
     if ((e = hipGetLastError()) != hipSuccess)
         return e;
 
@@ -910,7 +917,7 @@ hipError_t run(const AttnArgs &a, float *dstrip, hipStream_t st)
             dq_join<Op><<<(uint32_t)((lanes + kThreads - 1) / kThreads), kThreads, 0, st>>>(b);
     }
     if (dstrip)
-        strip_reduce<<<dim3((uint32_t)((a.strip_step + 63) / 64), (uint32_t)a.H), kThreads, 0, st>>>(
+        strip_reduce<<<dim3((uint32_t)((a.strip_step + 63) / 64), (uint32_t)a.H), 64 * kReducers, 0, st>>>(
             b.strip_part, dstrip, a.B * b.tiles * b.splits, width, a.strip_step);
     return hipGetLastError();
 }
@@ -935,6 +942,11 @@ hipError_t run_dim(const AttnArgs &a, float *dstrip, hipStream_t st)
 }
 
 }  // namespace
+
+int64_t attn_norm_bytes(int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv)
+{
+    return B * Hkv * norm_step((int)(H / Hkv), (int)Lq, (int)Lk) * 4;
+}
 
 int64_t attn_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv, int64_t D, int64_t R,
                         bool backward)
