@@ -182,12 +182,19 @@ __global__ __launch_bounds__(64 * (Dec<Op, DP>::kNW)) void attn_decode(AttnArgs 
     }
 }
 
-// Joins the parts of each row: 32 lanes a row, four channels a lane.
+// Joins the parts of each row: 32 lanes hold its channels, four each, and
+// `groups` of 32 lanes (1 or 8) take its parts in turn.  Eight where there are
+// few rows: with one the 86 parts of four fp32 rows follow each other for
+// 40 us.
 template <class Op>
-__global__ __launch_bounds__(256) void attn_join(AttnArgs a)
+__global__ __launch_bounds__(256) void attn_join(AttnArgs a, int groups)
 {
+    typedef float v4 __attribute__((ext_vector_type(4)));
+    __shared__ v4 sv[8][32];
+    __shared__ float sl[8];
     const int rows = a.Lq * a.G, heads = a.B * a.Hkv, lane = threadIdx.x & 31, d = lane * 4;
-    const int64_t id = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);  // (sequence, key/value head, row)
+    const int group = threadIdx.x >> 5, part = group % groups;
+    const int64_t id = (int64_t)blockIdx.x * (8 / groups) + group / groups;  // (sequence, key/value head, row)
     const bool in = id < (int64_t)heads * rows;
     const int bh = in ? (int)(id / rows) : 0, row = in ? (int)(id - (int64_t)bh * rows) : 0;
     const int b = bh / a.Hkv, hk = bh - b * a.Hkv, i = row / a.G, hq = hk * a.G + row - i * a.G;
@@ -203,16 +210,27 @@ __global__ __launch_bounds__(256) void attn_join(AttnArgs a)
         m = fmaxf(m, __shfl_xor(m, x));
     const bool none = m == -INFINITY;
     const float base = none ? 0.0f : m;
-    typedef float v4 __attribute__((ext_vector_type(4)));
     v4 v = {0, 0, 0, 0};
     float l = 0;
 #pragma unroll 4
-    for (int c = 0; c < parts; ++c) {
+    for (int c = part; c < parts; c += groups) {
         const float *const q = p + c * step;
         const float f = __builtin_amdgcn_exp2f(q[a.D] - base);
         l += f * q[a.D + 1];
         if (d < a.D)
             v += *(const v4 *)(q + d) * f;
+    }
+    if (groups > 1) {
+        sv[group][lane] = v;
+        if (lane == 0)
+            sl[group] = l;
+        __syncthreads();
+        if (group)
+            return;
+        for (int k = 1; k < 8; ++k) {
+            v += sv[k][lane];
+            l += sl[k];
+        }
     }
     if (!in)
         return;
@@ -285,13 +303,15 @@ int64_t attn_decode_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_
 
 void launch_attn_join(const AttnArgs &a, int dt, hipStream_t st)
 {
-    const uint32_t grid = (uint32_t)(((int64_t)a.B * a.H * a.Lq + 7) / 8);
+    const int64_t rows = (int64_t)a.B * a.H * a.Lq;
+    const int groups = rows <= 2048 && a.splits >= 8 ? 8 : 1;
+    const uint32_t grid = (uint32_t)((rows * groups + 7) / 8);
     if (dt == IM2WIN_F32)
-        attn_join<F32Op><<<grid, 256, 0, st>>>(a);
+        attn_join<F32Op><<<grid, 256, 0, st>>>(a, groups);
     else if (dt == IM2WIN_F16)
-        attn_join<F16Op><<<grid, 256, 0, st>>>(a);
+        attn_join<F16Op><<<grid, 256, 0, st>>>(a, groups);
     else
-        attn_join<BF16Op><<<grid, 256, 0, st>>>(a);
+        attn_join<BF16Op><<<grid, 256, 0, st>>>(a, groups);
 }
 
 hipError_t launch_attn_decode(const AttnArgs &a, int dt, hipStream_t st)
