@@ -707,7 +707,7 @@ __host__ __device__ inline int64_t part_floats(int64_t D) { return D + 4; }  // 
 void launch_attn_join(const AttnArgs &a, int dt, hipStream_t st);
 
 // Few query rows: the kernel that splits the keys (seq_attn_decode.hip).
-bool attn_few_rows(int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv);
+bool attn_few_rows(int64_t Lq, int64_t H, int64_t Hkv);
 int64_t attn_decode_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv, int64_t D);
 hipError_t launch_attn_docs(const int32_t *doc, DocRange *out, int64_t B, int64_t L, hipStream_t st);
 hipError_t launch_attn_forward(const AttnArgs &a, int dt, hipStream_t st);

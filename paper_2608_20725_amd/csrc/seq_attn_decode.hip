@@ -289,11 +289,12 @@ void run_dim(const AttnArgs &a, hipStream_t st)
 
 }  // namespace
 
-bool attn_few_rows(int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv)
-{
-    (void)B, (void)Lk;
-    return Lq * (H / Hkv) <= 32;
-}
+// Up to two score tiles of rows for a key/value head.  The whole cache is read
+// once a score tile here, once a query head by attn_fwd.  Measured, here
+// against there: 32 sequences of 4096 keys, 8 heads and 8 queries each (64
+// rows) 100 us and 212, 40 fp32 rows over 2733 keys 25 and 52; beyond, 128 rows
+// over 8192 keys 50 and 32.
+bool attn_few_rows(int64_t Lq, int64_t H, int64_t Hkv) { return Lq <= 32 && Lq * (H / Hkv) <= 64; }
 
 int64_t attn_decode_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv, int64_t D)
 {

@@ -247,7 +247,7 @@ hipError_t launch_attn_docs(const int32_t *doc, DocRange *out, int64_t B, int64_
 
 int64_t attn_forward_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv, int64_t D)
 {
-    if (attn_few_rows(B, Lq, Lk, H, Hkv))
+    if (attn_few_rows(Lq, H, Hkv))
         return attn_decode_part_bytes(dt, B, Lq, Lk, H, Hkv, D);
     const int32_t splits = forward_splits(dt, B, Lq, Lk, H);
     return splits > 1 ? splits * B * H * Lq * part_floats(D) * 4 : 0;
@@ -255,7 +255,7 @@ int64_t attn_forward_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64
 
 hipError_t launch_attn_forward(const AttnArgs &a, int dt, hipStream_t st)
 {
-    if (attn_few_rows(a.B, a.Lq, a.Lk, a.H, a.Hkv))
+    if (attn_few_rows(a.Lq, a.H, a.Hkv))
         return launch_attn_decode(a, dt, st);
     return dt == IM2WIN_F32 ? run_dim<F32Op>(a, st) : dt == IM2WIN_F16 ? run_dim<F16Op>(a, st) : run_dim<BF16Op>(a, st);
 }
