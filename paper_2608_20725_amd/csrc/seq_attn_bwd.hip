@@ -207,11 +207,24 @@ __global__ __launch_bounds__(kThreads) void row_stats(AttnArgs a)
 
 // Exponents of the probabilities (base 2), without the bias: the scores of
 // the products in s less lse(r), the row statistic of register r; slope:
-// 1 - tanh^2 where scores are capped.
+// 1 - tanh^2 where scores are capped, a quarter of it in kCapped instances
+// (slope_scale has the rest).  Those round P and dS to 16 bits and give
+// nothing else, so they take tanh(u) = 1 - 2*r, r = 1/(1 + e^2u), whose error
+// of 6e-8 (times the cap) does not show, in four operations.
+template <int FEAT>
+__device__ constexpr float slope_scale() { return FEAT == kCapped ? 4.0f : 1.0f; }
 template <int FEAT, class Lse>
 __device__ inline void to_scores(f32x16_acc &s, f32x16_acc &slope, const ScoreArgs &c, Lse lse)
 {
-    if (FEAT == kAny ? c.cap : FEAT == kCapped) {
+    if constexpr (FEAT == kCapped) {
+        const float c1 = c.c1 * (2.0f * kLog2e);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const float t = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[r] * c1));
+            slope[r] = fmaf(-t, t, t);
+            s[r] = fmaf(-2.0f * c.c2, t, c.c2 - lse(r));
+        }
+    } else if (FEAT == kAny && c.cap) {
         f32x16_acc t[1] = {s};
         tanh_scores(t, c.c1);
 #pragma unroll
@@ -481,11 +494,11 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccKV)) void attn_dkdv(Att
         return;
     if (a.splits > 1) {  // sums as they are; dkdv_join adds the splits
         float *const part = a.part + (((int64_t)work.g * a.B * a.Hkv + work.kv) * a.Lk + j) * 2 * a.D;
-        store_row<F32Op, DP>((char *)part, dk, a.scale / dss, h, a.D);
+        store_row<F32Op, DP>((char *)part, dk, slope_scale<FEAT>() * a.scale / dss, h, a.D);
         store_row<F32Op, DP>((char *)(part + a.D), dv, exp2f(-p_shift<Op>()), h, a.D);
         return;
     }
-    store_row<Op, DP>(a.dk + b * a.dk_sb + hk * a.dk_sh + (int64_t)j * a.dk_st, dk, a.scale / dss, h, a.D);
+    store_row<Op, DP>(a.dk + b * a.dk_sb + hk * a.dk_sh + (int64_t)j * a.dk_st, dk, slope_scale<FEAT>() * a.scale / dss, h, a.D);
     store_row<Op, DP>(a.dv + b * a.dv_sb + hk * a.dv_sh + (int64_t)j * a.dv_st, dv, exp2f(-p_shift<Op>()), h, a.D);
 }
 
@@ -772,9 +785,9 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccQ)) void attn_dq(AttnAr
     }
     if (live && a.splits > 1)  // sums as they are; dq_join adds the splits
         store_row<F32Op, DP>((char *)(a.part + (((int64_t)split * a.B * a.H + (int64_t)b * a.H + hq) * a.Lq + i) * a.D), dq,
-                             a.scale / dss, h, a.D);
+                             slope_scale<FEAT>() * a.scale / dss, h, a.D);
     else if (live)
-        store_row<Op, DP>(a.dq + b * a.dq_sb + hq * a.dq_sh + (int64_t)i * a.dq_st, dq, a.scale / dss, h, a.D);
+        store_row<Op, DP>(a.dq + b * a.dq_sb + hq * a.dq_sh + (int64_t)i * a.dq_st, dq, slope_scale<FEAT>() * a.scale / dss, h, a.D);
     if (FEAT != kAny || !want_strip)
         return;
 #pragma unroll

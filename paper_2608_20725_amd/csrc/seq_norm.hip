@@ -96,7 +96,7 @@ __global__ __launch_bounds__((threads<LPR>())) void norm_fwd(const typename E::T
     __shared__ float red[LPR > 64 ? LPR / 32 : 1];
     constexpr int kRows = threads<LPR>() / LPR;
     const int lane = threadIdx.x % LPR;
-    const float inv = 1.0f / (float)C;
+    const float n = (float)C;
     float wv[NV][VEC], bv[NV][VEC];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -117,7 +117,7 @@ __global__ __launch_bounds__((threads<LPR>())) void norm_fwd(const typename E::T
                 s += v[i][e];
         }
         row_sum2<LPR>(s, unused, red);
-        const float mu = s * inv;
+        const float mu = s / n;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int left = C - (i * LPR + lane) * VEC;
@@ -128,7 +128,7 @@ __global__ __launch_bounds__((threads<LPR>())) void norm_fwd(const typename E::T
             }
         }
         row_sum2<LPR>(q, unused, red);
-        const float rs = 1.0f / sqrtf(q * inv + eps);
+        const float rs = 1.0f / sqrtf(q / n + eps);
         if (lane == 0) {
             mean[r] = mu;
             rstd[r] = rs;
@@ -243,19 +243,19 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_long(const typename E::T *x
                                                           int64_t rows, int32_t C, int64_t xs, float eps)
 {
     __shared__ float red[8];
-    const float inv = 1.0f / (float)C;
+    const float n = (float)C;
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         float s = 0, q = 0, unused = 0;
         for (int c = threadIdx.x; c < C; c += kThreads)
             s += E::get(x[r * xs + c]);
         row_sum2<256>(s, unused, red);
-        const float mu = s * inv;
+        const float mu = s / n;
         for (int c = threadIdx.x; c < C; c += kThreads) {
             const float d = E::get(x[r * xs + c]) - mu;
             q += d * d;
         }
         row_sum2<256>(q, unused, red);
-        const float rs = 1.0f / sqrtf(q * inv + eps);
+        const float rs = 1.0f / sqrtf(q / n + eps);
         if (threadIdx.x == 0) {
             mean[r] = mu;
             rstd[r] = rs;
