@@ -31,6 +31,7 @@ __global__ __launch_bounds__(64 * (Dec<Op, DP>::kNW)) void attn_decode(AttnArgs 
     __shared__ __align__(16) char slot0[NW * F::kSlotBytes];
     __shared__ __align__(16) char slot1[NW * F::kSlotBytes];
     __shared__ float sm[NW][32], sl[NW][32];
+    __shared__ int kdoc[NW][32];  // documents of a wave's current tile
 
     // blockIdx: (sequence, head) fastest, then row tiles, then chunks
     const int heads = a.B * a.Hkv;
@@ -80,6 +81,8 @@ __global__ __launch_bounds__(64 * (Dec<Op, DP>::kNW)) void attn_decode(AttnArgs 
         T::template dma<F::kKeys, 1>(slot + F::kTileBytes, vp + at * a.v_st, a.v_st, left, a.D, 0, lane);
     };
     auto step = [&](char *slot, char *other, int k0) {
+        if (a.q_doc && h == 0)  // no key from n on is read: Lk may end inside the tile
+            kdoc[wave][lane] = k0 + lane < n ? a.k_doc[(int64_t)b * a.Lk + k0 + lane] : -1;
         issue(other, k0 + NW * F::kKeys);
         wait_loads<F::kLoads>();
         asm volatile("" ::: "memory");
@@ -95,7 +98,7 @@ __global__ __launch_bounds__(64 * (Dec<Op, DP>::kNW)) void attn_decode(AttnArgs 
         tp.partial = k0 + F::kKeys > least || tp.docs_differ;
         tp.lim = live ? lim : INT32_MAX;
         tp.doc = doc;
-        tp.kdoc = a.k_doc + (int64_t)b * a.Lk + k0;
+        tp.kdoc = kdoc[wave];
         tp.near = tp.inner = false;
         tp.far = 0;
         if (a.R) {

@@ -367,3 +367,23 @@ def test_rows_do_not_depend_on_their_batch(dtype):
     for b in (0, 4, 8):
         one = pkg.seq_attention_forward(q[b:b + 1], k[b:b + 1], v[b:b + 1], causal=True)
         assert torch.equal(one[0][0], whole[0][b]) and torch.equal(one[1][0], whole[1][b])
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("Lk", [1, 33, 95, 417])
+def test_few_rows_documents_end_with_the_cache(dtype, Lk):
+    """Ids are taken from the keys there are: what lies behind them in memory
+    has no influence, be it the query's document."""
+    x, _ = draw(2, 1, Lk, 4, 2, 64, dtype, seed=Lk)
+    doc = torch.randint(0, 2, (2, Lk), generator=torch.Generator().manual_seed(Lk)).to(torch.int32)
+    doc[:, 0] = 1
+    q, k, v = (x[n].cuda() for n in "qkv")
+    ones = torch.ones((2, 1), dtype=torch.int32, device="cuda")
+    res = []
+    for behind in (-1, 0, 1):
+        room = torch.full((2 * Lk + 64,), behind, dtype=torch.int32, device="cuda")
+        room[:2 * Lk] = doc.flatten().cuda()
+        res.append(pkg.seq_attention_forward(q, k, v, q_doc=ones, k_doc=room[:2 * Lk].view(2, Lk)))
+    run(x, None, {"q_doc": ones.cpu(), "k_doc": doc}, backward=False)
+    for other in res[1:]:
+        assert torch.equal(res[0][0], other[0]) and torch.equal(res[0][1], other[1])
