@@ -4,7 +4,9 @@
 // A bucket is one contiguous range of distances on each side, so both
 // directions are gathers (no atomics): the strip reads its bucket's entry,
 // the table's gradient sums its bucket's range.  The bucket borders are found
-// on the host in 64 bits and travel as a kernel argument.
+// on the host in 64 bits and travel as a kernel argument.  Both are launch
+// latency: a strip of 16 heads and 257 distances takes 3 us on the GPU, the
+// gradient of 24 layers of 1601 distances and 320 buckets 5.
 #include "seq.hpp"
 
 #include <math.h>
