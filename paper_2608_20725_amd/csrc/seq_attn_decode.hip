@@ -153,7 +153,7 @@ __global__ __launch_bounds__(64 * (Dec<Op, DP>::kNW)) void attn_decode(AttnArgs 
             box[(32 * dt + reg_row(r) + 4 * h) * 33 + (lane & 31)] = st.o[dt][r] * mine;
     __syncthreads();
     const int64_t out_row = ((int64_t)b * a.H + hq) * a.Lq + i;
-    const bool none = m == -INFINITY;
+    const bool none = sum == 0.0f;  // not m == -inf: all scores may be NaN
     if (a.splits > 1) {
         float *const part = a.part + (((int64_t)chunk * heads + bh) * rows + row) * part_floats(a.D);
         if (live && wave == 0 && h == 0) {
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(64 * (Dec<Op, DP>::kNW)) void attn_decode(AttnArgs 
                 a.part[(((int64_t)chunk * heads + bh) * rows + rr) * part_floats(a.D) + d] = v;
             else
                 ((typename Op::elem *)(a.out + b * a.o_sb + hh * a.o_sh + (int64_t)ii * a.o_st))[d] =
-                    (typename Op::elem)(ms == -INFINITY ? 0.0f : v / s2);
+                    (typename Op::elem)(s2 == 0.0f ? 0.0f : v / s2);
         }
     }
 }
@@ -213,8 +213,7 @@ __global__ __launch_bounds__(256) void attn_join(AttnArgs a, int groups)
 #pragma unroll
     for (int x = 16; x >= 1; x >>= 1)
         m = fmaxf(m, __shfl_xor(m, x));
-    const bool none = m == -INFINITY;
-    const float base = none ? 0.0f : m;
+    const float base = m == -INFINITY ? 0.0f : m;
     v4 v = {0, 0, 0, 0};
     float l = 0;
 #pragma unroll 4
@@ -239,6 +238,7 @@ __global__ __launch_bounds__(256) void attn_join(AttnArgs a, int groups)
     }
     if (!in)
         return;
+    const bool none = l == 0.0f;
     const float inv = none ? 0.0f : 1.0f / l;
     if (lane == 0)
         a.lse[((int64_t)b * a.H + hq) * a.Lq + i] =

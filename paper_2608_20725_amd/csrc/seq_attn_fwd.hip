@@ -160,7 +160,9 @@ __global__ __launch_bounds__(64 * kWaves, (Fwd<Op, DP>::kOcc)) void attn_fwd(Att
         }
         return;
     }
-    const bool none = st.m == -INFINITY;
+    // no pairs: nothing was added.  The maximum does not tell: it passes over
+    // NaN, and stays -inf where all scores are NaN
+    const bool none = l == 0.0f;
     const float inv = none ? 0.0f : 1.0f / l;
     if (h == 0)
         a.lse[((int64_t)b * a.H + hq) * a.Lq + i] = none ? -INFINITY : st.lse(st.m, l);

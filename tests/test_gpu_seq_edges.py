@@ -1,0 +1,56 @@
+"""Sequence operators at the edges of their ranges: scores that are NaN, caps
+far above the scores, what padding holds, empty calls of every kernel, odd
+layouts, other streams, keys that several workgroups share."""
+import math
+
+import pytest
+import torch
+
+import paper_2608_20725_amd as pkg
+from test_gpu_seq_attention import DTYPES, draw, ids
+
+pytestmark = pytest.mark.gpu
+
+
+def nan_rows(x, lens, **opts):
+    """([B][H][Lq] rows with a NaN among their scores) by the definition."""
+    B, Lq, H, D = x["q"].shape
+    Lk, Hk = x["k"].shape[1:3]
+    i, j = torch.arange(Lq)[:, None], torch.arange(Lk)[None, :]
+    bad = torch.zeros((B, H, Lq), dtype=torch.bool)
+    for b in range(B):
+        n = int(lens[b])
+        ok = (j < n) & (j <= i + (n - Lq if opts.get("align_end") else 0))
+        for h in range(H):
+            gone = torch.isnan(x["q"][b, :, h]).any(-1)[:, None] | torch.isnan(x["k"][b, :, h * Hk // H]).any(-1)[None, :]
+            bad[b, h] = (ok & gone).any(1)
+    return bad
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("shape,end", [((2, 70, 4, 2, 64), True), ((1, 900, 4, 1, 40), True), ((100, 100, 2, 2, 64), False),
+                                       ((130, 1100, 4, 2, 96), False), ((200, 1100, 2, 1, 128), True)], ids=str)
+def test_scores_that_are_nan(shape, end, dtype):
+    """A query one of whose scores is NaN has out and lse NaN, also where all
+    of them are: it is not taken for one without pairs.  (Few rows, one chunk
+    and several; many rows, alone and with their keys split.)"""
+    Lq, Lk, H, Hk, D = shape
+    x, _ = draw(5, Lq, Lk, H, Hk, D, dtype)
+    clean = {n: t.clone() for n, t in x.items()}
+    lens = torch.tensor([Lk, Lk, Lk, 0, Lk], dtype=torch.int32)
+    x["q"][1, Lq - 1, H - 1] = math.nan
+    x["k"][2, 0, Hk - 1, 3] = math.nan     # every query of those heads sees it, the first one only it (not align_end)
+    x["k"][4] = math.nan
+    x["q"][3, 0] = math.nan                # no pair: nothing to see
+    opts = {"causal": True, "align_end": end}
+    res = []
+    for y in (clean, x):
+        res.append(pkg.seq_attention_forward(*(y[n].cuda() for n in "qkv"), kv_len=lens.cuda(), **opts))
+    bad = nan_rows(x, lens, **opts)
+    assert bad.any() and not bad[3].any()
+    (out0, lse0), (out, lse) = [(o.cpu(), l.cpu()) for o, l in res]
+    rows = bad.transpose(1, 2)
+    assert torch.equal(torch.isnan(lse), bad)
+    assert torch.isnan(out[rows]).all()
+    assert torch.equal(out[~rows], out0[~rows]) and torch.equal(lse[~bad], lse0[~bad])
+    assert (out[3] == 0).all() and (lse[3] == -math.inf).all()
