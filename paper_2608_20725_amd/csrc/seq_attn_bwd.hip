@@ -212,8 +212,12 @@ __global__ __launch_bounds__(kThreads) void row_stats(AttnArgs a)
 // the products in s less lse(r), the row statistic of register r; slope:
 // 1 - tanh^2 where scores are capped, a quarter of it in kCapped instances
 // (slope_scale has the rest).  Those round P and dS to 16 bits and give
-// nothing else, so they take tanh(u) = 1 - 2*r, r = 1/(1 + e^2u), whose error
-// of 6e-8 (times the cap) does not show, in four operations.
+// nothing else, so they take tanh(u) = 1 - 2*r, r = 1/(1 + e^2u), in four
+// operations.  Its error of 1.2e-7 whatever u is becomes one of 1.2e-7*cap in
+// the exponent, and so in P: up to kCappedMost 3.1e-5 at most, a sixteenth of
+// fp16's rounding of P (2^-11) and a 128th of bf16's.  Larger caps go to the
+// kAny instances, whose series for small u is exact to fp32.
+constexpr float kCappedMost = 256.0f;
 template <int FEAT>
 __device__ constexpr float slope_scale() { return FEAT == kCapped ? 4.0f : 1.0f; }
 template <int FEAT, class Lse>
@@ -942,7 +946,7 @@ template <class Op, int DP>
 hipError_t run_feat(const AttnArgs &a, float *dstrip, hipStream_t st)
 {
     if constexpr (!OpInfo<Op>::kIs32) {
-        if (!a.R)
+        if (!a.R && a.cap <= kCappedMost)
             return a.cap > 0 ? run<Op, DP, kCapped>(a, dstrip, st) : run<Op, DP, kPlain>(a, dstrip, st);
     }
     return run<Op, DP, kAny>(a, dstrip, st);

@@ -7,7 +7,8 @@ import pytest
 import torch
 
 import paper_2608_20725_amd as pkg
-from test_gpu_seq_attention import DTYPES, draw, ids
+from seq_ref import Attention, check
+from test_gpu_seq_attention import DTYPES, F32, draw, ids
 
 pytestmark = pytest.mark.gpu
 
@@ -54,3 +55,33 @@ def test_scores_that_are_nan(shape, end, dtype):
     assert torch.isnan(out[rows]).all()
     assert torch.equal(out[~rows], out0[~rows]) and torch.equal(lse[~bad], lse0[~bad])
     assert (out[3] == 0).all() and (lse[3] == -math.inf).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("cap", [200.0, 300.0, 1e4, 1e6])
+def test_large_caps(cap, dtype):
+    """Scores far below their cap.  There tanh(u) is its series, whose error is
+    relative to u: the reference's allowance of 4 roundings of the cap falls
+    away (but for 16 bits up to 256, where it is below a sixteenth of P's own
+    rounding), the 8 of a score cover the products with scale/cap, cap*log2(e)
+    and the series' own."""
+    for causal in (False, True):
+        x, _ = draw(2, 90, 90, 2, 2, 64, dtype, seed=int(cap))
+        opts = {"cap": cap, "causal": causal}
+        ref = Attention(x["q"], x["k"], x["v"], **opts)
+        assert float(ref.t.abs().max()) < 0.25
+        if dtype == F32 or cap > 256:
+            ref.e -= 2.0 ** -24 * 4 * cap
+        q, k, v, do = (x[n].cuda() for n in ("q", "k", "v", "dout"))
+        out, lse = pkg.seq_attention_forward(q, k, v, **opts)
+        to, tl = ref.tolerances()
+        check(out, ref.out.transpose(1, 2), to + 1e-30, "out")
+        check(lse, ref.lse, tl + 1e-30, "lse")
+        # one dout row at a time: a sum over many rows hides what one is off by
+        for rows in (slice(0, 90), slice(3, 4), slice(60, 61)):
+            x1 = torch.zeros_like(x["dout"])
+            x1[:, rows] = x["dout"][:, rows]
+            grads = pkg.seq_attention_backward(x1.cuda(), q, k, v, out, lse, **opts)
+            want, tol = ref.grads(x1, out.cpu(), lse.cpu())
+            for name, a, w, t in zip(("dq", "dk", "dv"), grads, want, tol):
+                check(a, w, t, name)
