@@ -421,9 +421,10 @@ void run_typed(const Args &a, bool bwd, void *dw, void *db)
                                                                        (T *)a.y, a.mean, a.rstd, a.rows, C, a.xs,
                                                                        a.eps);
         } else {
-            norm_bwd_long<E, W><<<(uint32_t)grid, kThreads, 0, a.st>>>((const T *)a.dy, (const T *)a.x,
-                                                                       (const U *)a.w, a.mean, a.rstd, (T *)a.y,
-                                                                       a.rows, C, a.dys, a.xs);
+            if (grid)  // without rows the sums below are still to be written, as zeros
+                norm_bwd_long<E, W><<<(uint32_t)grid, kThreads, 0, a.st>>>((const T *)a.dy, (const T *)a.x,
+                                                                           (const U *)a.w, a.mean, a.rstd, (T *)a.y,
+                                                                           a.rows, C, a.dys, a.xs);
             const dim3 g((uint32_t)((a.C + kThreads - 1) / kThreads), (uint32_t)norm_partial_rows(a.rows, a.C));
             norm_cols_long<E><<<g, kThreads, 0, a.st>>>((const T *)a.dy, (const T *)a.x, a.mean, a.rstd, a.part, a.rows,
                                                         C, a.dys, a.xs);

@@ -8,7 +8,8 @@ import torch
 
 import paper_2608_20725_amd as pkg
 from seq_ref import Attention, check
-from test_gpu_seq_attention import DTYPES, F32, draw, ids
+from test_gpu_seq_attention import BF16, DTYPES, F16, F32, draw, ids
+from test_gpu_seq_norm import test_layer_norm as layer_norm_case
 
 pytestmark = pytest.mark.gpu
 
@@ -85,3 +86,23 @@ def test_large_caps(cap, dtype):
             want, tol = ref.grads(x1, out.cpu(), lse.cpu())
             for name, a, w, t in zip(("dq", "dk", "dv"), grads, want, tol):
                 check(a, w, t, name)
+
+
+@pytest.mark.parametrize("types", [(F32, F32), (F16, F16), (F16, F32), (BF16, BF16), (BF16, F32)], ids=ids)
+@pytest.mark.parametrize("C", [40, 1025, 16384, 20000, 33001])
+def test_layer_norm_without_rows(C, types):
+    """No rows: gradients of zero, for rows that fit the registers and longer ones."""
+    dt, wdt = types
+    x = torch.zeros((0, C), dtype=dt, device="cuda")
+    w = torch.ones(C, dtype=wdt, device="cuda")
+    y, mean, rstd = pkg.seq_layer_norm_forward(x, w, w)
+    assert y.shape == (0, C)
+    dx, dw, db = pkg.seq_layer_norm_backward(x, x, w, mean, rstd)
+    assert dx.shape == (0, C) and (dw == 0).all() and (db == 0).all()
+
+
+@pytest.mark.parametrize("types", [(F32, F32), (F16, F16), (F16, F32), (BF16, BF16), (BF16, F32)], ids=ids)
+@pytest.mark.parametrize("size", [(2, 32768), (3, 32776), (5, 33001)], ids=str)
+def test_layer_norm_long_rows(size, types):
+    """The longest rows that 16-bit types hold in registers, and longer."""
+    layer_norm_case(size, types)
