@@ -457,6 +457,16 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccKV)) void attn_dkdv(Att
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 gradients(t, s, dp);
+                if (q0 + 32 * t + 32 > a.Lq) {
+                    // rows past Lq hold zeros, which times a key or value
+                    // that is infinite or NaN are not zero
+                    const int end = a.Lq - (q0 + 32 * t) - 4 * h;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        s[r] = reg_row(r) < end ? s[r] : 0.0f;
+                        dp[r] = reg_row(r) < end ? dp[r] : 0.0f;
+                    }
+                }
                 if (partial) {
                     const int lim = first == INT32_MAX ? INT32_MAX : first - (q0 + 32 * t) - 4 * h;
                     const float *const at = rows + 32 * t + 4 * h;  // + 64: delta, + 128: document
@@ -586,8 +596,11 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccQ)) void attn_dq(AttnAr
         if (doc < 0)
             lim = 0;
     }
-    // a lane without a query holds zeros and an lse of infinity: it adds
-    // nothing, masked or not
+    // A lane without a query holds zeros and an lse of infinity.  Its column
+    // of dq is not stored; of the strip's gradient, which is summed over
+    // lanes, it is left out: zero times a key or value that is infinite or NaN
+    // is not zero.
+    const bool some_dead = qt * kHeld + wave * 32 + 32 > a.Lq;
     const int most = wave_max(live ? lim : 0), least = wave_min(live ? lim : INT32_MAX);
     const int plo = wave_min(pos), phi = wave_max(pos);
     const bool seen = live && lim > 0;
@@ -735,6 +748,10 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccQ)) void attn_dq(AttnAr
                 dp[r] = ds;
             }
             if (FEAT == kAny && want_strip) {
+                if (some_dead)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        dp[r] = live ? dp[r] : 0.0f;
                 if (far) {
                     float v = 0;
 #pragma unroll

@@ -8,7 +8,7 @@ import torch
 
 import paper_2608_20725_amd as pkg
 from seq_ref import Attention, check
-from test_gpu_seq_attention import BF16, DTYPES, F16, F32, draw, ids
+from test_gpu_seq_attention import BF16, DTYPES, F16, F32, draw, ids, to_gpu
 from test_gpu_seq_norm import test_layer_norm as layer_norm_case
 
 pytestmark = pytest.mark.gpu
@@ -106,3 +106,67 @@ def test_layer_norm_without_rows(C, types):
 def test_layer_norm_long_rows(size, types):
     """The longest rows that 16-bit types hold in registers, and longer."""
     layer_norm_case(size, types)
+
+
+def forward_and_backward(x, bias, opts):
+    o = {k: to_gpu(v) for k, v in opts.items()}
+    q, k, v, do = (x[n].cuda() for n in ("q", "k", "v", "dout"))
+    out, lse = pkg.seq_attention_forward(q, k, v, bias=to_gpu(bias), **o)
+    return (out, lse) + tuple(pkg.seq_attention_backward(do, q, k, v, out, lse, bias=to_gpu(bias), **o))
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("hold", [math.nan, math.inf, -math.inf], ids=str)
+@pytest.mark.parametrize("Lq,Lk", [(100, 128), (33, 64), (70, 600), (1, 40)])
+def test_keys_behind_the_last_query(Lq, Lk, hold, dtype):
+    """Causal, more keys than queries: the keys that no query sees have no
+    influence and gradients of zero, also beside the padding of a query tile."""
+    x, bias = draw(2, Lq, Lk, 2, 1, 64, dtype, R=10)
+    res = []
+    for value in (0.0, hold):
+        y = {n: t.clone() for n, t in x.items()}
+        y["k"][:, Lq:] = value
+        y["v"][:, Lq:] = value
+        res.append(forward_and_backward(y, bias, {"causal": True}))
+    for a, b in zip(*res):
+        assert not torch.isnan(b).any() and torch.equal(a, b)
+    assert (res[1][3][:, Lq:] == 0).all() and (res[1][4][:, Lq:] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("hold", [math.nan, math.inf], ids=str)
+def test_keys_of_documents_without_queries(hold, dtype):
+    """Keys of document 0 where no query has it; the padding of a query tile has none either."""
+    B, Lq, Lk = 2, 100, 150
+    x, bias = draw(B, Lq, Lk, 2, 2, 64, dtype, R=10)
+    g = torch.Generator().manual_seed(1)
+    q_doc = torch.randint(1, 3, (B, Lq), generator=g).to(torch.int32)
+    k_doc = torch.randint(0, 3, (B, Lk), generator=g).to(torch.int32)
+    q_doc[1] = 1
+    k_doc[1] = 0
+    res = []
+    for value in (0.0, hold):
+        y = {n: t.clone() for n, t in x.items()}
+        y["k"][k_doc == 0] = value
+        y["v"][k_doc == 0] = value
+        res.append(forward_and_backward(y, bias, {"q_doc": q_doc, "k_doc": k_doc}))
+    for a, b in zip(*res):
+        assert not torch.isnan(b).any() and torch.equal(a, b)
+    gone = (k_doc == 0).cuda()
+    assert (res[1][3][gone] == 0).all() and (res[1][4][gone] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+def test_keys_of_minus_infinity(dtype):
+    """Keys whose scores are -inf for every query have probability 0: dv, dk
+    and the strip's gradient are those of keys far away, whatever the padding
+    of a query tile makes of them."""
+    x, bias = draw(1, 100, 100, 2, 2, 64, dtype, R=10)
+    x["q"] = x["q"].abs() + 0.5
+    res = []
+    for value in (-6e4, -math.inf):
+        y = {n: t.clone() for n, t in x.items()}
+        y["k"][0, 40] = value
+        res.append(forward_and_backward(y, bias, {}))
+    for n in (0, 1, 3, 4, 5):
+        assert torch.equal(res[0][n], res[1][n]), n
