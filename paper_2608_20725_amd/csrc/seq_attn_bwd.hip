@@ -82,6 +82,7 @@ template <>
 constexpr float p_shift<F16Op>() { return 14.0f; }
 
 constexpr int kStatRows = 64;  // rows a workgroup of row_stats, 16 lanes each
+static_assert(kStatRows == kDocTile, "norm_tiles counts document ranges too");
 
 // fp16: the largest |dout_i| and |v_j| that each workgroup of row_stats met,
 // [B*Hkv][G*query tiles + key tiles].
@@ -145,9 +146,37 @@ __device__ inline void store_max(float *to, float v)
         *to = fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]));
 }
 
+// Whether some query sees key j; the 16 lanes of a group ask together.  With
+// documents the queries are searched from the key's own position on, a tile of
+// them a lane, where rows of packed documents find theirs at once.
+__device__ inline bool seen_key(const AttnArgs &a, int b, int n, int j)
+{
+    const int off = first_pos(a, n);
+    const int first = a.causal && !(a.prefix && j < a.prefix[b]) ? max(j - off, 0) : 0;
+    if (j >= n || first >= a.Lq)
+        return false;
+    if (!a.k_doc)
+        return true;
+    const int doc = a.k_doc[(int64_t)b * a.Lk + j], tiles = norm_tiles(a.Lq), t0 = first / kDocTile, span = tiles - t0;
+    const DocRange *const ranges = a.q_range + (int64_t)b * tiles;
+    const int32_t *const ids = a.q_doc + (int64_t)b * a.Lq;
+    const int begin = min(max(j - off, first) / kDocTile, tiles - 1);
+    bool found = false;
+    for (int s = threadIdx.x & 15; doc >= 0 && s < span && !found; s += 16) {
+        const int t = begin + s < tiles ? begin + s : begin + s - span;
+        const DocRange r = ranges[t];
+        if (doc < r.lo || doc > r.hi)
+            continue;
+        found = !r.mixed;
+        for (int i = max(t * kDocTile, first); i < min((t + 1) * kDocTile, a.Lq) && !found; ++i)
+            found = ids[i] == doc;
+    }
+    return __ballot(found) >> (threadIdx.x & 48) & 0xffff;
+}
+
 // {lse*log2(e) - p_shift, dout.out} and, fp16, the largest |dout| (finite ones
 // of queries that see something); the workgroups after those of the queries
-// take, fp16, the largest |v| of the keys there are.
+// take, fp16, the largest |v| of the keys that a query sees.
 template <class Op>
 __global__ __launch_bounds__(kThreads) void row_stats(AttnArgs a)
 {
@@ -161,7 +190,7 @@ __global__ __launch_bounds__(kThreads) void row_stats(AttnArgs a)
         for (int k = 0; k < kStatRows / 16; ++k) {
             const int j = t * kStatRows + k * 16 + (threadIdx.x >> 4);
             float f[8], sq = 0;
-            if (j < n && d < a.D && (!a.k_doc || a.k_doc[(int64_t)b * a.Lk + j] >= 0)) {
+            if (seen_key(a, b, n, j) && d < a.D) {
                 load8<Op>(a.v + b * a.v_sb + hk * a.v_sh + (int64_t)j * a.v_st + d * sizeof(typename Op::elem), f);
 #pragma unroll
                 for (int e = 0; e < 8; ++e)

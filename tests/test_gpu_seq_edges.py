@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import paper_2608_20725_amd as pkg
-from seq_ref import Attention, check
+from seq_ref import Attention, allowed, check
 from test_gpu_seq_attention import BF16, DTYPES, F16, F32, draw, ids, to_gpu
 from test_gpu_seq_norm import test_layer_norm as layer_norm_case
 
@@ -170,3 +170,34 @@ def test_keys_of_minus_infinity(dtype):
         res.append(forward_and_backward(y, bias, {}))
     for n in (0, 1, 3, 4, 5):
         assert torch.equal(res[0][n], res[1][n]), n
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("masks", ["causal", "prefix", "align_end", "documents", "causal documents", "lengths"])
+def test_largest_numbers_in_keys_and_values_nobody_sees(masks, dtype):
+    """The type's largest number where no query looks: nothing changes, fp16's
+    scale of the gradients neither."""
+    big = torch.finfo(dtype).max
+    B, Lq, Lk = 2, 100, 230
+    g = torch.Generator().manual_seed(2)
+    j = torch.arange(Lk)[None].expand(B, Lk)
+    opts = {"causal": {"causal": True}, "prefix": {"causal": True, "prefix": torch.tensor([150, 3], dtype=torch.int32)},
+            "align_end": {"causal": True, "align_end": True, "kv_len": torch.tensor([230, 120], dtype=torch.int32)},
+            "lengths": {"kv_len": torch.tensor([130, 7], dtype=torch.int32)}}.get(masks, {"causal": masks[0] == "c"})
+    if "documents" in masks:
+        qd = torch.randint(-1, 3, (B, Lq), generator=g)     # any order; document 3 has no query
+        kd = torch.randint(-1, 4, (B, Lk), generator=g)
+        qd[1] = torch.arange(Lq) // 33 * 2                  # runs: 0, 2, 4, 6; 1, 3, 5 have no query
+        kd[1] = torch.arange(Lk) // 40
+        opts.update(q_doc=qd.to(torch.int32), k_doc=kd.to(torch.int32))
+    x, bias = draw(B, Lq, Lk, 2, 1, 64, dtype, R=10)
+    seen = allowed(B, Lq, Lk, **opts)[0].any(1)
+    assert not seen.all()
+    res = []
+    for value in (0.0, big):
+        y = {n: t.clone() for n, t in x.items()}
+        y["k"][~seen] = value
+        y["v"][~seen] = value
+        res.append(forward_and_backward(y, bias, opts))
+    for a, b in zip(*res):
+        assert not torch.isnan(b).any() and torch.equal(a, b)
