@@ -201,3 +201,24 @@ def test_largest_numbers_in_keys_and_values_nobody_sees(masks, dtype):
         res.append(forward_and_backward(y, bias, opts))
     for a, b in zip(*res):
         assert not torch.isnan(b).any() and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, F32), (BF16, BF16)], ids=ids)
+@pytest.mark.parametrize("C", [5, 100])
+def test_layer_norm_huge_constant_rows(C, types):
+    """Rows of one value near the type's largest: x - mean is 0, though
+    mean*rstd is beyond the range; lanes beyond the row add nothing."""
+    dt, wdt = types
+    x = torch.full((3, C), 2.0 ** 120, dtype=dt, device="cuda")     # sums of up to 100 are exact and finite
+    g = torch.Generator().manual_seed(C)
+    dy = torch.randn((3, C), generator=g).to(dt)
+    w = (torch.randn(C, generator=g) + 1).to(wdt)
+    y, mean, rstd = pkg.seq_layer_norm_forward(x, w.cuda(), w.cuda())
+    assert torch.equal(mean.cpu(), torch.full((3,), 2.0 ** 120)) and torch.equal(y.cpu(), w.to(dt).expand(3, C))
+    dx, dw, db = pkg.seq_layer_norm_backward(dy.cuda(), x, w.cuda(), mean, rstd)
+    G, rs = dy.double() * w.double(), rstd.double().cpu()[:, None]
+    want = rs * (G - G.mean(1, keepdim=True))
+    u = 2.0 ** -8 if dt == BF16 else 2.0 ** -24
+    check(dx, want, 2.0 ** -24 * 64 * rs * (G.abs() + G.abs().mean(1, keepdim=True)) + u * want.abs(), "dx")
+    assert (dw == 0).all()
+    check(db, dy.double().sum(0), (2.0 ** -22 + (2.0 ** -8 if wdt == BF16 else 0)) * dy.double().abs().sum(0), "db")
