@@ -2,7 +2,8 @@
 
 A thin binding over the calls of ``include/im2win_seq.h`` in ``libim2win.so``: shapes, strides and device pointers of
 PyTorch tensors and the current HIP stream.  Outputs and workspaces that are not given are allocated; there is no
-fallback.
+fallback.  With ``stream`` (a torch stream or a handle) the call is made as under ``torch.cuda.stream(stream)``: its
+inputs have to be ready there, and its results are first ready there.
 
     y, mean, rstd = seq_layer_norm_forward(x, weight, bias, eps)
     dx, dweight, dbias = seq_layer_norm_backward(dy, x, weight, mean, rstd)
@@ -58,16 +59,24 @@ def _library():
     return _lib
 
 
-def _on(stream, *tensors):
-    """The stream's handle; tensors made here for work on a stream other than
-    the current one are not reused before that work has ended."""
-    if stream is not None:
-        import torch
-        s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
-        for t in tensors:
-            if t is not None:
-                t.record_stream(s)
-    return _stream(stream)
+def _elsewhere(stream, call, *args):
+    """``call`` with ``stream`` as the current stream, so that what it allocates
+    comes from that stream's memory: a block that was freed on the caller's
+    stream may still be in use by work pending there.  The caller's tensors are
+    recorded on the call's stream and its results on the caller's, so that
+    neither is reused before the other stream's work on it has ended."""
+    import torch
+    s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+    here = torch.cuda.current_stream(s.device)
+    with torch.cuda.stream(s):
+        res = call(*args)
+    for t in args:
+        if isinstance(t, torch.Tensor):
+            t.record_stream(s)
+    for t in res if isinstance(res, tuple) else (res,):
+        if t is not None:
+            t.record_stream(here)
+    return res
 
 
 def _rows(x, what):
@@ -113,6 +122,8 @@ def seq_layer_norm_forward(x, weight, bias, eps: float = 1e-5, out=None, stream=
     """Layer norm over the last dimension.  Returns (y, mean, rstd): y dense
     like ``x`` (written to ``out`` when given, which may be a dense ``x``),
     the statistics fp32 with a value per row."""
+    if stream is not None:
+        return _elsewhere(stream, seq_layer_norm_forward, x, weight, bias, eps, out)
     import torch
     rows, C, xs = _rows(x, "x")
     wdt = _params(C, x.dtype, weight, bias)
@@ -124,12 +135,14 @@ def seq_layer_norm_forward(x, weight, bias, eps: float = 1e-5, out=None, stream=
     rstd = torch.empty_like(mean)
     _check(_library().seq_layer_norm_forward(x.data_ptr(), weight.data_ptr(), bias.data_ptr(), y.data_ptr(),
                                              mean.data_ptr(), rstd.data_ptr(), rows, C, xs, eps, _dtype_code(x.dtype),
-                                             wdt, _on(stream, y, mean, rstd)), "seq_layer_norm_forward")
+                                             wdt, _stream(None)), "seq_layer_norm_forward")
     return y, mean, rstd
 
 
 def seq_layer_norm_backward(dy, x, weight, mean, rstd, ws=None, stream=None):
     """Gradients of the layer norm: (dx, dweight, dbias)."""
+    if stream is not None:
+        return _elsewhere(stream, seq_layer_norm_backward, dy, x, weight, mean, rstd, ws)
     import torch
     rows, C, xs = _rows(x, "x")
     rows2, C2, dys = _rows(dy, "dy")
@@ -147,7 +160,7 @@ def seq_layer_norm_backward(dy, x, weight, mean, rstd, ws=None, stream=None):
     _check(_library().seq_layer_norm_backward(dy.data_ptr(), x.data_ptr(), weight.data_ptr(), mean.data_ptr(),
                                               rstd.data_ptr(), dx.data_ptr(), dw.data_ptr(), db.data_ptr(),
                                               ws.data_ptr(), _nbytes(ws), rows, C, dys, xs, _dtype_code(x.dtype), wdt,
-                                              _on(stream, dx, dw, db, ws)), "seq_layer_norm_backward")
+                                              _stream(None)), "seq_layer_norm_backward")
     return dx, dw, db
 
 
@@ -161,6 +174,8 @@ def seq_rel_bias_bucket(distance: int, buckets: int, max_distance: int, two_side
 
 def seq_rel_bias_forward(table, max_distance: int, two_sided: bool = True, out=None, stream=None):
     """The strip [H][2*max_distance + 1] (fp32) of a bucket table [buckets][H]."""
+    if stream is not None:
+        return _elsewhere(stream, seq_rel_bias_forward, table, max_distance, two_sided, out)
     import torch
     if table.dim() != 2 or not table.is_contiguous():
         raise ValueError("table must be a contiguous [buckets][H] tensor")
@@ -172,7 +187,7 @@ def seq_rel_bias_forward(table, max_distance: int, two_sided: bool = True, out=N
         raise ValueError("out must be a contiguous fp32 [H][2*max_distance + 1] tensor")
     _same_device(table, out)
     _check(_library().seq_rel_bias_forward(table.data_ptr(), out.data_ptr(), H, buckets, max_distance,
-                                           1 if two_sided else 0, _dtype_code(table.dtype), _on(stream, out)),
+                                           1 if two_sided else 0, _dtype_code(table.dtype), _stream(None)),
            "seq_rel_bias_forward")
     return out
 
@@ -181,6 +196,8 @@ def seq_rel_bias_backward(dstrip, buckets: int, two_sided: bool = True, dtype=No
     """The table's gradient [buckets][H] (of type ``dtype``, fp32 by default)
     from strips' gradients [H][2R+1], or [n][H][2R+1] of n layers that share
     the table."""
+    if stream is not None:
+        return _elsewhere(stream, seq_rel_bias_backward, dstrip, buckets, two_sided, dtype)
     import torch
     if dstrip.dim() not in (2, 3) or dstrip.dtype != torch.float32 or not dstrip.is_contiguous():
         raise ValueError("dstrip must be a contiguous fp32 [H][2R+1] or [n][H][2R+1] tensor")
@@ -191,7 +208,7 @@ def seq_rel_bias_backward(dstrip, buckets: int, two_sided: bool = True, dtype=No
     dtype = torch.float32 if dtype is None else dtype
     dtable = torch.empty((buckets, H), dtype=dtype, device=dstrip.device)
     _check(_library().seq_rel_bias_backward(dstrip.data_ptr(), dtable.data_ptr(), n, H, buckets, width // 2,
-                                            1 if two_sided else 0, _dtype_code(dtype), _on(stream, dtable)),
+                                            1 if two_sided else 0, _dtype_code(dtype), _stream(None)),
            "seq_rel_bias_backward")
     return dtable
 
@@ -299,6 +316,9 @@ def seq_attention_forward(q, k, v, scale=None, cap: float = 0.0, causal: bool = 
     kv_len    [B] int32: keys from there on do not exist
     q_doc, k_doc  [B][Lq], [B][Lk] int32: pairs need equal ids, negative ids see and are seen by nothing
     """
+    if stream is not None:
+        return _elsewhere(stream, seq_attention_forward, q, k, v, scale, cap, causal, align_end, bias, kv_len, prefix,
+                          q_doc, k_doc, out, ws)
     import torch
     device = q.device
     if out is None:
@@ -311,7 +331,7 @@ def seq_attention_forward(q, k, v, scale=None, cap: float = 0.0, causal: bool = 
     lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=device)
     ws = _attention_ws(a, 0, ws, device)
     _check(_library().seq_attention_forward(a, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
-                                            *_workspace(q, ws), _on(stream, out, lse, ws)), "seq_attention_forward")
+                                            *_workspace(q, ws), _stream(None)), "seq_attention_forward")
     return out, lse
 
 
@@ -329,6 +349,9 @@ def seq_attention_backward(dout, q, k, v, out, lse, scale=None, cap: float = 0.0
     options, from its ``out`` and ``lse``; dstrip is None without a bias.  dq,
     dk and dv are written to the tensors given, of any strides with a dense
     last dimension (columns of one packed tensor, for example)."""
+    if stream is not None:
+        return _elsewhere(stream, seq_attention_backward, dout, q, k, v, out, lse, scale, cap, causal, align_end, bias,
+                          kv_len, prefix, q_doc, k_doc, dq, dk, dv, ws)
     import torch
     _like(dout, q.shape, q.dtype, "dout")
     _like(out, q.shape, q.dtype, "out")
@@ -350,5 +373,5 @@ def seq_attention_backward(dout, q, k, v, out, lse, scale=None, cap: float = 0.0
     _check(_library().seq_attention_backward(a, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
                                              lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
                                              None if dstrip is None else dstrip.data_ptr(), *_workspace(q, ws),
-                                             _on(stream, dq, dk, dv, dstrip, ws)), "seq_attention_backward")
+                                             _stream(None)), "seq_attention_backward")
     return dq, dk, dv, dstrip

@@ -222,3 +222,83 @@ def test_layer_norm_huge_constant_rows(C, types):
     check(dx, want, 2.0 ** -24 * 64 * rs * (G.abs() + G.abs().mean(1, keepdim=True)) + u * want.abs(), "dx")
     assert (dw == 0).all()
     check(db, dy.double().sum(0), (2.0 ** -22 + (2.0 ** -8 if wdt == BF16 else 0)) * dy.double().abs().sum(0), "db")
+
+
+def busy(n=4):
+    """Some 25 ms of work on the current stream."""
+    a = torch.ones((8192, 8192), device="cuda")
+    for _ in range(n):
+        a @ a
+
+
+def stream_calls():
+    x = torch.randn((2048, 512), device="cuda")
+    w, b = torch.rand(512, device="cuda"), torch.randn(512, device="cuda")
+    y, mean, rstd = pkg.seq_layer_norm_forward(x, w, b)
+    table = torch.randn((32, 64), device="cuda")
+    ds = torch.randn((8, 64, 2049), device="cuda")
+    q = torch.randn((2, 1024, 8, 64), device="cuda").to(BF16)
+    k, v = torch.randn_like(q), torch.randn_like(q)
+    out, lse = pkg.seq_attention_forward(q, k, v)
+    return {
+        "layer norm": (pkg.seq_layer_norm_forward, (x, w, b)),
+        "layer norm backward": (pkg.seq_layer_norm_backward, (y, x, w, mean, rstd)),
+        "bias": (pkg.seq_rel_bias_forward, (table, 1024)),
+        "bias backward": (pkg.seq_rel_bias_backward, (ds, 32)),
+        "attention": (pkg.seq_attention_forward, (q, k, v)),
+        "attention backward": (pkg.seq_attention_backward, (out, q, k, v, out, lse)),
+    }
+
+
+@pytest.mark.parametrize("name", ["layer norm", "layer norm backward", "bias", "bias backward", "attention",
+                                  "attention backward"])
+@pytest.mark.parametrize("handle", [False, True], ids=["stream", "handle"])
+def test_memory_of_calls_on_another_stream(name, handle):
+    """A block freed here while work that reads it is pending is not written
+    by a call on another stream; a tensor given to such a call and freed is
+    not reused before it has been read."""
+    fn, args = stream_calls()[name]
+    want = fn(*args)
+    want = [t for t in (want if isinstance(want, tuple) else (want,)) if t is not None]
+    side = torch.cuda.Stream()
+    stream = side.cuda_stream if handle else side
+    # blocks of the results' sizes, freed while copies from them are pending
+    held = [torch.full_like(t, 7) for t in want]
+    to = [torch.empty_like(t) for t in want]
+    torch.cuda.synchronize()
+    busy()
+    for t, h in zip(to, held):
+        t.copy_(h)
+    del held, h
+    got = fn(*args, stream=stream)
+    side.synchronize()
+    torch.cuda.synchronize()
+    for t in to:
+        assert (t == 7).all()
+    got = [t for t in (got if isinstance(got, tuple) else (got,)) if t is not None]
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    # inputs freed while the call waits behind other work of its stream
+    args = tuple(t.clone() if isinstance(t, torch.Tensor) else t for t in args)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        busy()
+    got = fn(*args, stream=stream)
+    sizes = [t.shape for t in args if isinstance(t, torch.Tensor)], [t.dtype for t in args if isinstance(t, torch.Tensor)]
+    del args
+    over = [torch.full(s, math.nan, dtype=d, device="cuda") for s, d in zip(*sizes)]
+    torch.cuda.synchronize()
+    got = [t for t in (got if isinstance(got, tuple) else (got,)) if t is not None]
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
+def test_the_null_stream_by_its_handle():
+    x = torch.randn((64, 512), device="cuda")
+    w = torch.rand(512, device="cuda")
+    want = pkg.seq_layer_norm_forward(x, w, w)
+    torch.cuda.synchronize()
+    got = pkg.seq_layer_norm_forward(x, w, w, stream=0)
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
