@@ -227,7 +227,7 @@ AttnArgs make_args(const seq_attention_t *a)
     r.causal = a->causal != 0, r.align_end = a->align_end != 0;
     r.scale = a->scale, r.cap = a->cap;
     if (a->R) {
-        r.R = (int32_t)attn_range(a->R, a->Lq, a->Lk), r.strip_step = (int32_t)(2 * a->R + 1);
+        r.R = (int32_t)attn_range(a->R, a->Lq, a->Lk), r.strip_step = 2 * a->R + 1;
         r.strip = a->strip + (a->R - r.R);
     }
     r.kv_len = a->kv_len, r.prefix = a->causal ? a->prefix : nullptr;

@@ -45,14 +45,15 @@ struct AttnArgs {
     float *norms;         // backward, fp16: the largest |dout_i| and |v_j| of groups of rows
     float *part;          // sums of rows that several workgroups share
     float *strip_part;    // backward: the strip's gradients of every workgroup
-    const float *strip;   // its middle 2R+1 entries; heads strip_step apart
+    const float *strip;   // its middle 2R+1 entries
+    int64_t strip_step;   // floats between its heads
     const int32_t *kv_len, *prefix, *q_doc, *k_doc;
     const DocRange *q_range, *k_range;  // [B][ceil(L / kDocTile)]
     // byte strides
     int64_t q_sb, q_sh, k_sb, k_sh, v_sb, v_sh, o_sb, o_sh, do_sb, do_sh, dq_sb, dq_sh, dk_sb, dk_sh, dv_sb, dv_sh;
     int32_t q_st, k_st, v_st, o_st, do_st, dq_st, dk_st, dv_st;
     int32_t B, Lq, Lk, H, Hkv, G, D;
-    int32_t causal, align_end, R, strip_step;
+    int32_t causal, align_end, R;
     int32_t tiles, splits, chunk;  // held tiles of a head; workgroups that share one; decode: keys of each
     float scale, cap;
 };

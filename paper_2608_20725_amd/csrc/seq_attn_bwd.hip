@@ -913,28 +913,33 @@ __global__ __launch_bounds__(kThreads) void dq_join(AttnArgs a)
 
 // dstrip[h][x]: the sum of `n` partial strips, which hold the `width` middle
 // entries of the `full` that a strip has (the others have no pair), 64 entries
-// a workgroup, each by 16 lanes that take every 16th strip.
+// a workgroup, each by 16 lanes that take every 16th strip.  A grid has at
+// most kMaxGridY heads; its workgroups take more in turn.
 constexpr int kReducers = 16;
+constexpr int kMaxGridY = 65535;
 __global__ __launch_bounds__(64 * kReducers) void strip_reduce(const float *__restrict__ part,
                                                                float *__restrict__ dstrip, int32_t n, int32_t width,
-                                                               int32_t full)
+                                                               int32_t full, int32_t H)
 {
     __shared__ float s[kReducers][64];
-    const int x = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6, h = blockIdx.y;
+    const int x = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6;
     const int c = x - (full - width) / 2;
-    float v = 0;
-    if (c >= 0 && c < width)
+    for (int h = blockIdx.y; h < H; h += gridDim.y) {
+        float v = 0;
+        if (c >= 0 && c < width)
 #pragma unroll 4
-        for (int r = k; r < n; r += kReducers)
-            v += part[((int64_t)h * n + r) * width + c];
-    s[k][threadIdx.x & 63] = v;
-    __syncthreads();
-    if (k == 0 && x < full) {
-        v = 0;
+            for (int r = k; r < n; r += kReducers)
+                v += part[((int64_t)h * n + r) * width + c];
+        s[k][threadIdx.x & 63] = v;
+        __syncthreads();
+        if (k == 0 && x < full) {
+            v = 0;
 #pragma unroll
-        for (int r = 0; r < kReducers; ++r)
-            v += s[r][threadIdx.x];
-        dstrip[(int64_t)h * full + x] = v;
+            for (int r = 0; r < kReducers; ++r)
+                v += s[r][threadIdx.x];
+            dstrip[(int64_t)h * full + x] = v;
+        }
+        __syncthreads();
     }
 }
 
@@ -982,9 +987,11 @@ hipError_t run(const AttnArgs &a, float *dstrip, hipStream_t st)
         if (b.splits > 1)
             dq_join<Op><<<(uint32_t)((lanes + kThreads - 1) / kThreads), kThreads, 0, st>>>(b);
     }
-    if (dstrip)
-        strip_reduce<<<dim3((uint32_t)((a.strip_step + 63) / 64), (uint32_t)a.H), 64 * kReducers, 0, st>>>(
-            b.strip_part, dstrip, a.B * b.tiles * b.splits, width, a.strip_step);
+    if (dstrip) {
+        const dim3 grid((uint32_t)((a.strip_step + 63) / 64), (uint32_t)(a.H < kMaxGridY ? a.H : kMaxGridY));
+        strip_reduce<<<grid, 64 * kReducers, 0, st>>>(b.strip_part, dstrip, a.B * b.tiles * b.splits, width,
+                                                      (int32_t)a.strip_step, a.H);
+    }
     return hipGetLastError();
 }
 

@@ -302,3 +302,34 @@ def test_the_null_stream_by_its_handle():
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("Lq", [1, 33])
+def test_strip_offsets_beyond_32_bits(Lq):
+    """So many heads that the last ones' bias lies more than 2^31 floats behind
+    the first's; more heads, too, than a grid has in its second dimension."""
+    H, R, L, D = 1048100, 1024, 33, 8
+    assert (H - 20) * (2 * R + 1) > 2 ** 31
+    part = torch.arange(H - 3, H)                     # the heads that are looked at, and the first
+    part = torch.cat([torch.tensor([0, 65535, 65536]), part])
+    g = torch.Generator().manual_seed(Lq)
+    small = {n: torch.randn((1, Lq if n in ("q", "dout") else L, len(part), D), generator=g).to(F16)
+             for n in ("q", "k", "v", "dout")}
+    strip = torch.randn((len(part), 2 * R + 1), generator=g)
+    x = {n: torch.zeros((1, t.shape[1], H, D), dtype=F16, device="cuda") for n, t in small.items()}
+    for n, t in small.items():
+        x[n][:, :, part.cuda()] = t.cuda()
+    bias = torch.zeros((H, 2 * R + 1), device="cuda")
+    for i, h in enumerate(part.tolist()):
+        bias[h] = strip[i].cuda()
+    ref = Attention(small["q"], small["k"], small["v"], bias=strip)
+    out, lse = pkg.seq_attention_forward(x["q"], x["k"], x["v"], bias=bias)
+    to, tl = ref.tolerances()
+    pick = part.cuda()
+    check(out[:, :, pick], ref.out.transpose(1, 2), to + 1e-30, "out")
+    check(lse[:, pick], ref.lse, tl + 1e-30, "lse")
+    grads = pkg.seq_attention_backward(x["dout"], x["q"], x["k"], x["v"], out, lse, bias=bias)
+    want, tol = ref.grads(small["dout"], out[:, :, pick].cpu(), lse[:, pick].cpu())
+    for name, a, w, t in zip(("dq", "dk", "dv"), grads, want, tol):
+        check(a[:, :, pick], w, t, name)
+    check(torch.stack([grads[3][h] for h in part.tolist()]), want[3], tol[3], "dstrip")
