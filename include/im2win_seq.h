@@ -106,7 +106,9 @@ int64_t seq_rel_bias_bucket(int64_t d, int64_t buckets, int64_t R, int two_sided
  * elements between sequences, tokens and heads (channels dense).  Head h reads
  * key/value head h / (H / Hkv).  lse [B][H][Lq] dense fp32.
  * D a multiple of 8, 8 .. 128; H a multiple of Hkv; Lq, Lk <= 2^20;
- * B*H < 2^24; strides multiples of 16 bytes, token strides below 2^24 bytes;
+ * B*H*max(1, ceil(Lq/128)) < 2^24 (backward B*H*ceil(Lq/64) +
+ * B*Hkv*ceil(Lk/64) < 2^24), with documents B*ceil(Lq/64) and B*ceil(Lk/64)
+ * < 2^26; strides multiples of 16 bytes, token strides below 2^24 bytes;
  * pointers of 16-bit and fp32 rows 16-byte aligned.
  */
 typedef struct {

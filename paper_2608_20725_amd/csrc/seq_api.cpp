@@ -162,9 +162,16 @@ int check_dims(const seq_attention_t *a, bool backward)
         return IM2WIN_ERANGE;
     if (a->H >= (int64_t)1 << 24 || a->B >= (int64_t)1 << 24 || a->B * a->H >= (int64_t)1 << 24)
         return IM2WIN_ERANGE;
-    // workgroups of every launch, 16 tokens at the least in each
-    const int64_t longest = a->Lq > a->Lk ? a->Lq : a->Lk;
-    if (a->B * a->H * ((longest + 15) / 16) >= INT32_MAX)
+    // A grid has less than 2^32 lanes: 2^24 workgroups of 256.  (The launches
+    // with splits and the joins are small ones, and few rows make at most
+    // B*H workgroups.)
+    constexpr int64_t most = (int64_t)1 << 24;
+    const int64_t heads = a->B * a->H, longest = a->Lq > a->Lk ? a->Lq : a->Lk;
+    if (!backward && heads * ((a->Lq + kHeld - 1) / kHeld) >= most)
+        return IM2WIN_ERANGE;
+    if (backward && heads * ((a->Lq + 63) / 64) + a->B * a->Hkv * ((a->Lk + 63) / 64) >= most)
+        return IM2WIN_ERANGE;
+    if ((a->q_doc || a->k_doc) && a->B * ((longest + kDocTile - 1) / kDocTile) >= most * 4)  // one wave each
         return IM2WIN_ERANGE;
     const int64_t e = elt(a->dt);
     const Operand ops[4] = {{nullptr, a->B, a->Lq, a->H, a->D, e, a->q_stride},

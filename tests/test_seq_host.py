@@ -188,3 +188,18 @@ def test_binding_refuses_what_does_not_fit(lib):
         pkg.seq_rel_bias_forward(t(32), 128)
     with pytest.raises(ValueError):
         pkg.seq_rel_bias_backward(t(4, 8), 32)
+
+
+def test_grids_of_attention(lib):
+    """A launch has less than 2^32 lanes: what would need more is refused
+    before anything is enqueued, and only that."""
+    ws = lib.seq_attention_workspace_bytes
+    many = {"B": 1 << 11, "H": 1 << 10, "Hk": 1 << 10}
+    assert ws(pack(**many, Lq=7 * 128), 0) >= 0 and ws(pack(**many, Lq=7 * 128 + 1), 0) == ERANGE
+    assert ws(pack(**many, Lq=6 * 64, Lk=64), 1) >= 0 and ws(pack(**many, Lq=6 * 64, Lk=128), 1) == ERANGE
+    assert ws(pack(**many, Lq=8 * 64, Lk=1), 1) == ERANGE
+    # keys alone make no grid of the forward call
+    assert ws(pack(B=1 << 14, H=64, Hk=1, Lq=1, Lk=1 << 17), 0) >= 0
+    docs = {"B": 1 << 16, "H": 1, "Hk": 1, "Lq": 1}
+    assert ws(pack(**docs, Lk=1 << 15, q_doc=P, k_doc=P), 0) >= 0
+    assert ws(pack(**docs, Lk=1 << 16, q_doc=P, k_doc=P), 0) == ERANGE
