@@ -124,19 +124,35 @@ bool self_disjoint(const Operand &o)
     return true;
 }
 
-// Two operands whose extents meet may still be columns of one row (q, k and v
-// side by side in each token): the same token stride, sequences whole numbers
-// of tokens apart, and the heads' bytes of a token in different columns.
+// Bytes modulo `period` that an operand takes from its first element on: the
+// axes that step by whole periods add none.
+int64_t width(const Operand &o, int64_t period)
+{
+    const int64_t n[3] = {o.B, o.L, o.heads};
+    int64_t w = o.D;
+    for (int k = 0; k < 3; ++k)
+        if (n[k] > 1 && o.stride[k] % period)
+            w += (n[k] - 1) * o.stride[k];
+    return w * o.elt;
+}
+
+// Two operands whose extents meet may still lie side by side, as q, k and v do
+// in one tensor: there is a stride (the tokens', if they are columns of each
+// token's row; the sequences' or heads' in other orders of the dimensions)
+// modulo which their bytes are apart.
 bool side_by_side(const Operand &a, const Operand &b)
 {
-    const int64_t row = a.stride[1];
-    if (row <= 0 || b.stride[1] != row || a.stride[0] % row || b.stride[0] % row)
-        return false;
-    const int64_t bytes = row * a.elt;
-    const int64_t wa = ((a.heads - 1) * a.stride[2] + a.D) * a.elt, wb = ((b.heads - 1) * b.stride[2] + b.D) * b.elt;
+    const int64_t n[6] = {a.B, a.L, a.heads, b.B, b.L, b.heads};
     const int64_t diff = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p);
-    const int64_t off = ((diff % bytes) + bytes) % bytes;  // b's column, a's being 0
-    return off >= wa && off + wb <= bytes;
+    for (int k = 0; k < 6; ++k) {
+        const int64_t period = k < 3 ? a.stride[k] : b.stride[k - 3], bytes = period * a.elt;
+        if (n[k] <= 1 || period <= 0)
+            continue;
+        const int64_t off = ((diff % bytes) + bytes) % bytes;  // where b starts, a's start being 0
+        if (off >= width(a, period) && off + width(b, period) <= bytes)
+            return true;
+    }
+    return false;
 }
 
 bool clash(const Operand &a, const Operand &b)

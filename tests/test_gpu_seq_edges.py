@@ -333,3 +333,72 @@ def test_strip_offsets_beyond_32_bits(Lq):
     for name, a, w, t in zip(("dq", "dk", "dv"), grads, want, tol):
         check(a[:, :, pick], w, t, name)
     check(torch.stack([grads[3][h] for h in part.tolist()]), want[3], tol[3], "dstrip")
+
+
+PACKED = {  # order in memory of sequences 0, tokens 1, heads 2, parts (q, k, v) 3, channels 4
+    "parts within tokens": (0, 1, 3, 2, 4),
+    "sequences within tokens": (1, 0, 3, 2, 4),
+    "heads before tokens": (0, 3, 2, 1, 4),
+    "parts within heads": (0, 1, 2, 3, 4),
+}
+
+
+def packed_like(B, L, H, D, order, dtype):
+    """([B][L][H][D] views x 3 of one tensor whose dimensions lie in `order`, that tensor)"""
+    dims = (B, L, H, 3, D)
+    t = torch.full([dims[d] for d in order], 7, dtype=dtype, device="cuda")
+    back = [order.index(d) for d in range(5)]
+    return t.permute(back).unbind(3), t
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("layout", sorted(PACKED))
+def test_packed_layouts(layout, dtype):
+    """q, k and v in one tensor, and their gradients in another, in any order of its dimensions."""
+    B, L, H, D = 3, 70, 2, 64
+    x, bias = draw(B, L, L, H, H, D, dtype, R=7)
+    want = forward_and_backward(x, bias, {"causal": True})
+    (q, k, v), _ = packed_like(B, L, H, D, PACKED[layout], dtype)
+    for t, n in ((q, "q"), (k, "k"), (v, "v")):
+        t.copy_(x[n])
+    (dq, dk, dv), whole = packed_like(B, L, H, D, PACKED[layout], dtype)
+    out, lse = pkg.seq_attention_forward(q, k, v, bias=bias.cuda(), causal=True, out=dq)
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    assert (dk == 7).all() and (dv == 7).all()
+    out = out.clone()
+    got = pkg.seq_attention_backward(x["dout"].cuda(), q, k, v, out, lse, bias=bias.cuda(), causal=True, dq=dq, dk=dk, dv=dv)
+    for a, b in zip(got, want[2:]):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("layout", sorted(PACKED))
+def test_packed_layouts_that_meet(layout):
+    """The same layouts moved so that two outputs share bytes."""
+    B, L, H, D = 3, 20, 2, 64
+    x, _ = draw(B, L, L, H, H, D, F16)
+    q, k, v, do = (x[n].cuda() for n in ("q", "k", "v", "dout"))
+    out, lse = pkg.seq_attention_forward(q, k, v)
+    (dq, dk, dv), whole = packed_like(B, L, H, D, PACKED[layout], F16)
+    flat = torch.zeros(whole.numel() + 64, dtype=F16, device="cuda")
+    for shift in (8, 32, 56):
+        at = dk.storage_offset() + shift
+        moved = flat.as_strided(dk.shape, dk.stride(), at)
+        first = flat.as_strided(dq.shape, dq.stride(), dq.storage_offset())
+        last = flat.as_strided(dv.shape, dv.stride(), dv.storage_offset())
+        with pytest.raises(pkg.Im2winError) as e:
+            pkg.seq_attention_backward(do, q, k, v, out, lse, dq=first, dk=moved, dv=last)
+        assert e.value.status == -7
+
+
+def test_one_token_beside_the_keys():
+    """The output of a single token in a row that keys and values lie in."""
+    B, L, H, D = 1, 50, 2, 64
+    whole = torch.randn((B, L, 3, H, D), device="cuda")
+    k, v = whole[:, :, 0], whole[:, :, 1]
+    q = torch.randn((B, 1, H, D), device="cuda")
+    want, _ = pkg.seq_attention_forward(q, k.contiguous(), v.contiguous())
+    before = whole.clone()
+    out, _ = pkg.seq_attention_forward(q, k, v, out=whole[:, 7:8, 2])
+    assert torch.equal(out, want) and torch.equal(whole[:, :, :2], before[:, :, :2])
+    with pytest.raises(pkg.Im2winError):
+        pkg.seq_attention_forward(q, k, v, out=whole[:, 7:8, 1])
