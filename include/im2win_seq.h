@@ -103,7 +103,8 @@ int64_t seq_rel_bias_bucket(int64_t d, int64_t buckets, int64_t R, int two_sided
  * Left-out pairs have no influence, whatever their keys and values hold.
  *
  * q [B][Lq][H][D], k and v [B][Lk][Hkv][D], out like q: `*_stride` are the
- * elements between sequences, tokens and heads (channels dense).  Head h reads
+ * elements between sequences, tokens and heads (channels dense; not read where
+ * there is only one of them).  Head h reads
  * key/value head h / (H / Hkv).  lse [B][H][Lq] dense fp32.
  * D a multiple of 8, 8 .. 128; H a multiple of Hkv; Lq, Lk <= 2^20;
  * B*H*max(1, ceil(Lq/128)) < 2^24 (backward B*H*ceil(Lq/64) +

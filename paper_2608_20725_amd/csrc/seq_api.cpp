@@ -12,6 +12,7 @@ namespace {
 
 constexpr int64_t kMaxBytes = int64_t(1) << 62;
 constexpr int64_t kMaxLen = int64_t(1) << 20;
+constexpr int64_t kMaxReach = int64_t(1) << 44;  // elements between the first and the last of an axis: no memory is larger
 
 bool known(int dt) { return dt == IM2WIN_F32 || dt == IM2WIN_F16 || dt == IM2WIN_BF16; }
 int64_t elt(int dt) { return dt == IM2WIN_F32 ? 4 : 2; }
@@ -78,8 +79,12 @@ bool meet(const Buf &a, const Buf &b) { return a.bytes > 0 && b.bytes > 0 && ove
 struct Operand {
     const void *p;
     int64_t B, L, heads, D, elt;
-    const int64_t *stride;  // elements: sequence, token, head
+    int64_t stride[3];  // elements: sequence, token, head; 0 where there is one of them (or none): nothing steps
 
+    Operand(const void *ptr, int64_t b, int64_t l, int64_t h, int64_t d, int64_t e, const int64_t *s)
+        : p(ptr), B(b), L(l), heads(h), D(d), elt(e), stride{b > 1 ? s[0] : 0, l > 1 ? s[1] : 0, h > 1 ? s[2] : 0}
+    {
+    }
     int64_t bytes() const  // from the first element to the end of the last
     {
         if (B == 0 || L == 0)
@@ -90,10 +95,11 @@ struct Operand {
 
 int check_strides(const Operand &o)
 {
+    const int64_t n[3] = {o.B, o.L, o.heads};
     for (int k = 0; k < 3; ++k) {
         if (o.stride[k] < 0)
             return IM2WIN_EINVAL;
-        if (o.stride[k] >= kMaxBytes / 64 / (int64_t)(1 << 24))
+        if (n[k] > 1 && o.stride[k] > kMaxReach / (n[k] - 1))
             return IM2WIN_ERANGE;
     }
     if (o.stride[1] * o.elt >= (int64_t)1 << 24)
@@ -236,15 +242,25 @@ Sizes sizes_of(const seq_attention_t *a, bool backward)
     return s;
 }
 
+// An operand's strides in bytes.
+void set_strides(const Operand &o, int64_t &sequence, int32_t &token, int64_t &head)
+{
+    sequence = o.stride[0] * o.elt;
+    token = (int32_t)(o.stride[1] * o.elt);
+    head = o.stride[2] * o.elt;
+}
+
 AttnArgs make_args(const seq_attention_t *a)
 {
     AttnArgs r;
     memset(&r, 0, sizeof r);
     const int64_t e = elt(a->dt);
-    r.q_sb = a->q_stride[0] * e, r.q_st = (int32_t)(a->q_stride[1] * e), r.q_sh = a->q_stride[2] * e;
-    r.k_sb = a->k_stride[0] * e, r.k_st = (int32_t)(a->k_stride[1] * e), r.k_sh = a->k_stride[2] * e;
-    r.v_sb = a->v_stride[0] * e, r.v_st = (int32_t)(a->v_stride[1] * e), r.v_sh = a->v_stride[2] * e;
-    r.o_sb = a->out_stride[0] * e, r.o_st = (int32_t)(a->out_stride[1] * e), r.o_sh = a->out_stride[2] * e;
+    const Operand q(nullptr, a->B, a->Lq, a->H, a->D, e, a->q_stride), k(nullptr, a->B, a->Lk, a->Hkv, a->D, e, a->k_stride),
+        v(nullptr, a->B, a->Lk, a->Hkv, a->D, e, a->v_stride), o(nullptr, a->B, a->Lq, a->H, a->D, e, a->out_stride);
+    set_strides(q, r.q_sb, r.q_st, r.q_sh);
+    set_strides(k, r.k_sb, r.k_st, r.k_sh);
+    set_strides(v, r.v_sb, r.v_st, r.v_sh);
+    set_strides(o, r.o_sb, r.o_st, r.o_sh);
     r.B = (int32_t)a->B, r.Lq = (int32_t)a->Lq, r.Lk = (int32_t)a->Lk;
     r.H = (int32_t)a->H, r.Hkv = (int32_t)a->Hkv, r.G = (int32_t)(a->H / a->Hkv), r.D = (int32_t)a->D;
     r.causal = a->causal != 0, r.align_end = a->align_end != 0;
@@ -564,10 +580,10 @@ static int attention(const seq_attention_t *a, const void *dout, const void *q, 
     }
     r.o = (const char *)out, r.dout = (const char *)dout, r.lse = const_cast<float *>(lse);
     r.dq = (char *)dq, r.dk = (char *)dk, r.dv = (char *)dv;
-    r.do_sb = a->dout_stride[0] * e, r.do_st = (int32_t)(a->dout_stride[1] * e), r.do_sh = a->dout_stride[2] * e;
-    r.dq_sb = a->dq_stride[0] * e, r.dq_st = (int32_t)(a->dq_stride[1] * e), r.dq_sh = a->dq_stride[2] * e;
-    r.dk_sb = a->dk_stride[0] * e, r.dk_st = (int32_t)(a->dk_stride[1] * e), r.dk_sh = a->dk_stride[2] * e;
-    r.dv_sb = a->dv_stride[0] * e, r.dv_st = (int32_t)(a->dv_stride[1] * e), r.dv_sh = a->dv_stride[2] * e;
+    set_strides(odo, r.do_sb, r.do_st, r.do_sh);
+    set_strides(odq, r.dq_sb, r.dq_st, r.dq_sh);
+    set_strides(odk, r.dk_sb, r.dk_st, r.dk_sh);
+    set_strides(odv, r.dv_sb, r.dv_st, r.dv_sh);
     return launch_status(launch_attn_backward(r, a->dt, a->R ? dstrip : nullptr, st));
 }
 

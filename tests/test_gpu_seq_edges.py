@@ -402,3 +402,44 @@ def test_one_token_beside_the_keys():
     assert torch.equal(out, want) and torch.equal(whole[:, :, :2], before[:, :, :2])
     with pytest.raises(pkg.Im2winError):
         pkg.seq_attention_forward(q, k, v, out=whole[:, 7:8, 1])
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+def test_strides_of_dimensions_of_one(dtype):
+    """The stride of a dimension with one element is not a step: any value will do."""
+    B, H, D = 2, 2, 64
+    x, bias = draw(B, 1, 1, H, H, D, dtype, R=7)
+    want = forward_and_backward(x, bias, {})
+    far = {n: t.cuda().as_strided(t.shape, (H * D, 1 << 40, D, 1)) for n, t in x.items()}
+    new = [torch.empty((B, 1, H, D), dtype=dtype, device="cuda").as_strided((B, 1, H, D), (H * D, 12345, D, 1)) for _ in range(4)]
+    out, lse = pkg.seq_attention_forward(far["q"], far["k"], far["v"], bias=bias.cuda(), out=new[0])
+    got = pkg.seq_attention_backward(far["dout"], far["q"], far["k"], far["v"], out, lse, bias=bias.cuda(), dq=new[1],
+                                     dk=new[2], dv=new[3])
+    for a, b in zip((out, lse) + got, want):
+        assert torch.equal(a, b)
+    # one sequence, one head
+    x, bias = draw(1, 40, 70, 1, 1, D, dtype, R=7)
+    want = forward_and_backward(x, bias, {})
+    far = {n: t.cuda().as_strided(t.shape, (1 << 50, D, (1 << 45) + 3, 1)) for n, t in x.items()}
+    for a, b in zip(forward_and_backward(x, bias, {}), want):
+        assert torch.equal(a, b)
+    out, lse = pkg.seq_attention_forward(far["q"], far["k"], far["v"], bias=bias.cuda())
+    got = pkg.seq_attention_backward(far["dout"], far["q"], far["k"], far["v"], out, lse, bias=bias.cuda())
+    for a, b in zip((out, lse) + got, want):
+        assert torch.equal(a, b)
+
+
+def test_sequences_far_apart():
+    """Sequences more than 2^32 elements from each other, as in a cache of many layers."""
+    L, D, step = 40, 64, (1 << 32) + 64
+    x, _ = draw(2, L, L, 1, 1, D, F16)
+    want = forward_and_backward(x, None, {})
+    big = torch.empty(step + 2 * L * D, dtype=F16, device="cuda")
+    k = big.as_strided((2, L, 1, D), (step, D, D, 1))
+    v = big[L * D:].as_strided((2, L, 1, D), (step, D, D, 1))
+    k.copy_(x["k"])
+    v.copy_(x["v"])
+    q, do = x["q"].cuda(), x["dout"].cuda()
+    out, lse = pkg.seq_attention_forward(q, k, v)
+    for a, b in zip((out, lse) + tuple(pkg.seq_attention_backward(do, q, k, v, out, lse))[:3], want):
+        assert torch.equal(a, b)

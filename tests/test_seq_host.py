@@ -203,3 +203,14 @@ def test_grids_of_attention(lib):
     docs = {"B": 1 << 16, "H": 1, "Hk": 1, "Lq": 1}
     assert ws(pack(**docs, Lk=1 << 15, q_doc=P, k_doc=P), 0) >= 0
     assert ws(pack(**docs, Lk=1 << 16, q_doc=P, k_doc=P), 0) == ERANGE
+
+
+def test_strides_of_one_are_not_read(lib):
+    ws = lib.seq_attention_workspace_bytes
+    for far in (1 << 60, (1 << 24) + 8, -8):
+        assert ws(pack(Lq=1, q=(256, far, 64), o=(256, far, 64)), 0) >= 0
+        assert ws(pack(B=1, k=(far, 128, 64)), 0) >= 0
+        assert ws(pack(H=1, Hk=1, v=(1024, 64, far), dk=(1024, 64, far)), 1) >= 0
+    assert ws(pack(k=(1 << 40, 128, 64)), 0) >= 0
+    assert ws(pack(k=(1 << 45, 128, 64)), 0) == ERANGE
+    assert ws(pack(B=1 << 12, k=(1 << 40, 128, 64)), 0) == ERANGE
