@@ -10,10 +10,10 @@ using namespace im2win;
 
 namespace {
 
-constexpr int64_t kMaxBytes = int64_t(1) << 62;
 constexpr int64_t kMaxLen = int64_t(1) << 20;
 constexpr int64_t kMaxReach = int64_t(1) << 44;  // elements between the first and the last of an axis: no memory is larger
 
+bool too_far(int64_t n, int64_t stride) { return n > 1 && stride > kMaxReach / (n - 1); }
 bool known(int dt) { return dt == IM2WIN_F32 || dt == IM2WIN_F16 || dt == IM2WIN_BF16; }
 int64_t elt(int dt) { return dt == IM2WIN_F32 ? 4 : 2; }
 bool aligned(const void *p, int64_t a) { return ((uintptr_t)p & (uintptr_t)(a - 1)) == 0; }
@@ -99,7 +99,7 @@ int check_strides(const Operand &o)
     for (int k = 0; k < 3; ++k) {
         if (o.stride[k] < 0)
             return IM2WIN_EINVAL;
-        if (n[k] > 1 && o.stride[k] > kMaxReach / (n[k] - 1))
+        if (too_far(n[k], o.stride[k]))
             return IM2WIN_ERANGE;
     }
     if (o.stride[1] * o.elt >= (int64_t)1 << 24)
@@ -306,7 +306,7 @@ int seq_layer_norm_forward(const void *x, const void *weight, const void *bias, 
         return IM2WIN_EINVAL;
     if (!weight || !bias || (rows > 0 && (!x || !y || !mean || !rstd)))
         return IM2WIN_EINVAL;
-    if (rows > INT32_MAX || C >= (int64_t)1 << 24 || x_stride > kMaxBytes / 4 / INT32_MAX)
+    if (rows > INT32_MAX || C >= (int64_t)1 << 24 || too_far(rows, x_stride))
         return IM2WIN_ERANGE;
     const int64_t e = elt(dt), we = elt(wdt);
     if (!aligned(x, e) || !aligned(y, e) || !aligned(weight, we) || !aligned(bias, we) || !aligned(mean, 4) ||
@@ -352,8 +352,7 @@ int seq_layer_norm_backward(const void *dy, const void *x, const void *weight, c
         return IM2WIN_EINVAL;
     if (!weight || !dweight || !dbias || !ws || (rows > 0 && (!dy || !x || !mean || !rstd || !dx)))
         return IM2WIN_EINVAL;
-    if (rows > INT32_MAX || C >= (int64_t)1 << 24 || x_stride > kMaxBytes / 4 / INT32_MAX ||
-        dy_stride > kMaxBytes / 4 / INT32_MAX)
+    if (rows > INT32_MAX || C >= (int64_t)1 << 24 || too_far(rows, x_stride) || too_far(rows, dy_stride))
         return IM2WIN_ERANGE;
     const int64_t e = elt(dt), we = elt(wdt);
     if (!aligned(dy, e) || !aligned(x, e) || !aligned(dx, e) || !aligned(weight, we) || !aligned(dweight, we) ||

@@ -443,3 +443,19 @@ def test_sequences_far_apart():
     out, lse = pkg.seq_attention_forward(q, k, v)
     for a, b in zip((out, lse) + tuple(pkg.seq_attention_backward(do, q, k, v, out, lse))[:3], want):
         assert torch.equal(a, b)
+
+
+def test_layer_norm_rows_far_apart():
+    """Rows more than 2^29 elements from each other."""
+    step, C = (1 << 30) + 8, 200
+    big = torch.empty(step + 2 * C, dtype=F16, device="cuda")
+    x, dy = big.as_strided((2, C), (step, 1)), big[C:].as_strided((2, C), (step, 1))
+    g = torch.Generator().manual_seed(4)
+    for t in (x, dy):
+        t.copy_(torch.randn((2, C), generator=g))
+    w = torch.rand(C, generator=g).cuda()
+    y, mean, rstd = pkg.seq_layer_norm_forward(x, w, w)
+    want = pkg.seq_layer_norm_forward(x.contiguous(), w, w)
+    got = (y, mean, rstd) + pkg.seq_layer_norm_backward(dy, x, w, mean, rstd)
+    for a, b in zip(got, want + pkg.seq_layer_norm_backward(dy.contiguous(), x.contiguous(), w, mean, rstd)):
+        assert torch.equal(a, b)
