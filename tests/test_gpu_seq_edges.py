@@ -8,7 +8,7 @@ import torch
 
 import paper_2608_20725_amd as pkg
 from seq_ref import Attention, allowed, check
-from test_gpu_seq_attention import BF16, DTYPES, F16, F32, draw, ids, to_gpu
+from test_gpu_seq_attention import BF16, DTYPES, F16, F32, draw, ids, run, to_gpu
 from test_gpu_seq_norm import test_layer_norm as layer_norm_case
 
 pytestmark = pytest.mark.gpu
@@ -459,3 +459,40 @@ def test_layer_norm_rows_far_apart():
     got = (y, mean, rstd) + pkg.seq_layer_norm_backward(dy, x, w, mean, rstd)
     for a, b in zip(got, want + pkg.seq_layer_norm_backward(dy.contiguous(), x.contiguous(), w, mean, rstd)):
         assert torch.equal(a, b)
+
+
+MASKS = {
+    "none": {},
+    "causal cap": {"causal": True, "cap": 20.0},
+    "lengths at the end": {"causal": True, "align_end": True, "lens": True},
+    "lengths": {"lens": True},
+    "documents": {"docs": True},
+    "causal documents cap": {"causal": True, "docs": True, "cap": 20.0, "lens": True},
+    "prefix": {"causal": True, "prefix": True},
+}
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("masks", sorted(MASKS))
+@pytest.mark.parametrize("shape", [(2, 130, 700, 3, 1, 80), (3, 200, 1100, 4, 2, 64), (1, 65, 1300, 2, 2, 128),
+                                   (2, 300, 600, 2, 1, 32)], ids=str)
+def test_keys_shared_by_workgroups(shape, masks, dtype):
+    """Rows long enough, and few enough, that their keys are split over
+    workgroups and the parts joined, forward (512 keys on in fp32, 1024 in 16
+    bits) and backward (256, 512); masks under which some parts have no key,
+    with and without a bias."""
+    B, Lq, Lk, H, Hk, D = shape
+    g = torch.Generator().manual_seed(Lk + len(masks))
+    opts = dict(MASKS[masks])
+    if opts.pop("lens", False):
+        opts["kv_len"] = torch.tensor([Lk, 0, Lk // 3][:B], dtype=torch.int32)
+    if opts.pop("prefix", False):
+        opts["prefix"] = torch.tensor([Lk - 5, 0, 70][:B], dtype=torch.int32)
+    if opts.pop("docs", False):
+        kd = (torch.arange(Lk)[None] // torch.tensor([[90], [40], [333]][:B])).to(torch.int32)
+        kd[:, -20:] = -1
+        opts["q_doc"], opts["k_doc"] = kd[:, :Lq].clone(), kd
+        opts["q_doc"][0] = torch.randint(-1, 8, (Lq,), generator=g)
+    x, bias = draw(*shape, dtype, seed=Lk, R=90)
+    run(x, None, opts)
+    run(x, bias, opts)
