@@ -12,8 +12,10 @@
  * hipStream_t; NULL is the null stream) and returns without synchronising; it
  * can be captured into a HIP graph.  Buffers, workspaces among them, belong to
  * the call until that work has ended.
- * Results do not depend on launch order: no floating-point atomics, so the
- * same call on the same inputs gives the same bits.
+ * Results do not depend on launch order: every sum is taken in a fixed order
+ * (the atomics on LDS in the bias strip's gradient have an address a lane each
+ * and one wave that adds), so the same call on the same inputs gives the same
+ * bits.
  * Numerics: sums, means, softmax statistics and gradients are held in fp32;
  * fp16 and bf16 results are rounded once, to nearest even, on store.  The
  * 16-bit attention kernels also round the softmax weights P and, in the

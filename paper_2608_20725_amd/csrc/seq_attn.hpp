@@ -547,6 +547,8 @@ __device__ inline void attend(const char *tk, const char *tv, const typename Op:
         }
     st.l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
 
+    // P is rounded to 16 bits here, as operand of the matrix cores (fp32 ones
+    // run at a seventh of the rate); its sum above and the products' are fp32
     if (!tp.partial) {
 #pragma unroll
         for (int i = 0; i < 2 * SUB; ++i) {

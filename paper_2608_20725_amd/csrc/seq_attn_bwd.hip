@@ -3,7 +3,7 @@
 //   P = exp(s - lse),  dP = dout v^T,  dS = P (dP - delta),  delta = dout.out
 //   dv = P^T dout,  dk = scale dX^T q,  dq = scale dX k,  dX = dS (1 - tanh^2).
 // Two kernels, each with its own held side, so that every gradient has one
-// owner and no atomics: attn_dkdv holds 128 keys and streams the queries of
+// owner: attn_dkdv holds 128 keys and streams the queries of
 // all heads that share them (4 products a pair), attn_dq holds 128 queries
 // and streams keys (3 products, two of them the same as there).  The strip's
 // gradient is summed along the diagonals in attn_dq.  Bound by the matrix
@@ -26,7 +26,11 @@ constexpr int kThreads = 64 * kWaves;
 __host__ __device__ inline int stat_rows(int Lq) { return (Lq + 63) / 64 * 64; }
 
 // Workgroups that share the keys of one query tile in attn_dq, as in the
-// forward pass; a key costs more here, so shorter rows are worth it.
+// forward pass; a key costs more here, so shorter rows are worth it.  Measured,
+// whole backward calls, one workgroup against split: bf16, 8 heads of 128, 1024
+// tokens 81 -> 61 us; 16 heads of 64, 2048 tokens 112 -> 102 (causal 107 ->
+// 92); fp32, 4 heads of 64, 256 tokens 79 -> 67.  Not split, 256 tiles of 1024
+// keys in 16 bits: 73.3 (split 72.1; causal 73.4 and 69.6).
 int32_t dq_splits(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H)
 {
     const int64_t groups = B * H * ((Lq + kHeld - 1) / kHeld);
@@ -52,7 +56,14 @@ int64_t dq_part_floats(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int
 
 // Workgroups that share the queries of one key tile: with few key/value heads
 // and short rows there are fewer key tiles than the 256 CUs can work on, and
-// causal masks need about two of them a CU to even out.
+// causal masks need about two of them a CU to even out.  Measured, whole
+// backward calls, one workgroup against split: bf16, 8 heads of 128 over 2,
+// 2048 tokens 306 -> 118 us, 16 over 4, causal 345 -> 144; fp32, 3x6 heads of
+// 80, 1001 tokens 426 -> 353.  With 256 key tiles the second one a CU pays
+// under causal masks of long rows: 16 heads of 64, 2048 tokens 101 -> 102,
+// causal 102 -> 92, but 2x16 heads, 1024 tokens 65 -> 73, causal 71 -> 73.  Four
+// tiles each: fp16, 8 heads of 64, 512 tokens 35.8 (one each 40.5, two 35.7);
+// short fp32 rows would take fewer: 4 heads of 64, 256 tokens 67 (46, 53).
 int32_t dkdv_splits(int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv)
 {
     const int64_t groups = B * Hkv * ((Lk + kHeld - 1) / kHeld), work = (H / Hkv) * ((Lq + 63) / 64);
@@ -508,6 +519,9 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccKV)) void attn_dkdv(Att
                         dp[r] = out ? 0.0f : dp[r];
                     }
                 }
+                // rounded to 16 bits as operands of the matrix cores, whose
+                // fp32 products cost 7 times as much (154 against 1121
+                // TFLOP/s); all sums of them are fp32
                 pack16<Op>(s, p);
                 pack16<Op>(dp, ds);
                 if (partial) {
@@ -634,9 +648,10 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccQ)) void attn_dq(AttnAr
     const int plo = wave_min(pos), phi = wave_max(pos);
     const bool seen = live && lim > 0;
     const int dlo = wave_min(seen ? doc : INT32_MAX), dhi = wave_max(seen ? doc : -1);
-    // each half wave has a strip of gradients of its own: the 32 lanes that
-    // add in one instruction hold 32 different distances, so nothing is
-    // summed in an order that could change
+    // each half wave has a strip of gradients of its own, to which it adds by
+    // LDS atomics: the 32 lanes that add in one instruction hold 32 different
+    // distances, and no other wave adds, so nothing is summed in an order that
+    // could change
     float *const grad = strip + width * (1 + 2 * wave + h);
     float far_lo = 0, far_hi = 0;
     if (FEAT == kAny && a.R)

@@ -189,8 +189,10 @@ __global__ __launch_bounds__(64 * (Dec<Op, DP>::kNW)) void attn_decode(AttnArgs 
 
 // Joins the parts of each row: 32 lanes hold its channels, four each, and
 // `groups` of 32 lanes (1 or 8) take its parts in turn.  Eight where there are
-// few rows: with one the 86 parts of four fp32 rows follow each other for
-// 40 us.
+// few rows of many parts.  Measured, whole calls, one against eight: 16 rows of
+// 2000 keys 16.7 -> 10.4 us, 8 rows of 8192 keys 47 -> 23, 128 rows 55 -> 43;
+// one stays where rows are many: 8192 rows of the forward pass 41.7 (eight
+// 44.3), 18018 fp32 rows 101 (119).
 template <class Op>
 __global__ __launch_bounds__(256) void attn_join(AttnArgs a, int groups)
 {
@@ -259,7 +261,11 @@ struct Split {
 
 // Chunks of a multiple of the waves' tiles: at least 4 workgroups for each of
 // 256 CUs where the cache is long enough, so that sequences of different
-// lengths even out.
+// lengths even out.  Measured with 256, 512, 1024 and 2048 workgroups wanted:
+// one cache of 2000 keys, 16 heads of 64 over 4, fp16 10.6, 10.6, 10.4, 10.6 us;
+// 32 caches of up to 8192 keys, 32 heads of 128 over 8, bf16 138.5, 143.3,
+// 153.4, 168.8; four of them 25, 31, 43, 62: once the chunks fill the chip,
+// fewer and longer ones would be ahead.
 Split split_of(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t Hkv, int64_t G, int64_t D)
 {
     const int64_t unit = dt == IM2WIN_F32 && D > 64 ? 64 : 128;
@@ -296,9 +302,13 @@ void run_dim(const AttnArgs &a, hipStream_t st)
 
 // Up to two score tiles of rows for a key/value head.  The whole cache is read
 // once a score tile here, once a query head by attn_fwd.  Measured, here
-// against there: 32 sequences of 4096 keys, 8 heads and 8 queries each (64
-// rows) 100 us and 212, 40 fp32 rows over 2733 keys 25 and 52; beyond, 128 rows
-// over 8192 keys 50 and 32.
+// against there: 64 rows (8 queries of 8 heads) over 32 caches of 4096 keys and
+// 8 key/value heads 91 us and 204, over one key/value head 28 and 42, 40 fp32
+// rows over 2733 keys 16 and 30; beyond, 128 rows (16 queries of 8 heads) over
+// 8192 keys 21 and 17, over 8 such caches 53 and 35.  It is the number of heads
+// that costs there: single tokens of 128 heads over one key/value head, which
+// the rule leaves to attn_fwd, would take 20 us here and take 58 there, over 32
+// caches of 4096 keys 65 and 800.
 bool attn_few_rows(int64_t Lq, int64_t H, int64_t Hkv) { return Lq <= 32 && Lq * (H / Hkv) <= 64; }
 
 int64_t attn_decode_part_bytes(int dt, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t Hkv, int64_t D)

@@ -379,7 +379,14 @@ void run(const Args &a, bool bwd)
 
 // The smallest instance that holds a row of C values; false when none does.
 // Rows shorter than a wave's 64 vectors share the wave; long ones take up to
-// 16 waves before a lane holds more than two vectors.
+// 16 waves before a lane holds more than two vectors.  Between 257 and 1024
+// vectors lanes of the forward pass hold more of them than those of the
+// backward pass, which has three rows' worth of registers.  Measured, forward
+// with 256, 512 and 1024 lanes: 5673 rows of 5112 fp16 channels 38.5, 41.6,
+// 44.7 us, 20000x4096 bf16 62.7, 67.9, 60.6, 10000x8192 89, 84, 85, 5000x4096
+// fp32 26.0, 25.5, 37.4; one wave for 4096 channels 137.  Backward: 5673x5112
+// 94, 67, 57, 20000x4096 139, 159, 139, 10000x2048 fp32 53.3, 51.8, 53.2, 4
+// rows of 4096 9.9, 9.4, 9.9, but 10000x8192 bf16 221, 238, 188.
 template <class E, class W, int VEC>
 bool run_held(const Args &a, bool bwd)
 {
@@ -452,7 +459,12 @@ hipError_t run_any(const Args &a, bool bwd, int dt, int wdt, void *dw, void *db)
 int64_t norm_partial_rows(int64_t rows, int64_t C)
 {
     // enough workgroups to fill 256 CUs; a workgroup takes one row at a time,
-    // or four of the short ones, and with many rows at least 32
+    // or four of the short ones, and with many rows at least 32.  Measured with
+    // 256, 512, 1024 and 2048 workgroups: 100352x512 bf16 152, 94, 61, 74 us;
+    // 500000x64 84, 57, 52, 74; 9765x771 fp32 28.6, 25.7, 26.2, 33.8 (the rule's
+    // 306: 27.3); with 64, 128 and 256: 256x1024 bf16 12.0, 12.5, 13.2; 300x2000
+    // fp16 22, 21, 23.  Long rows would take more: 20000x4096 bf16 159 (625),
+    // 115 with 512 of them.
     const int64_t least = (rows + 31) / 32, step = C <= 1024 ? (rows + 3) / 4 : rows;
     const int64_t n = least > 256 ? least : step < 256 ? step : 256;
     return n < 1 ? 1 : n > 1024 ? 1024 : n;

@@ -3,7 +3,9 @@
 A thin binding over the calls of ``include/im2win_seq.h`` in ``libim2win.so``: shapes, strides and device pointers of
 PyTorch tensors and the current HIP stream.  Outputs and workspaces that are not given are allocated; there is no
 fallback.  With ``stream`` (a torch stream or a handle) the call is made as under ``torch.cuda.stream(stream)``: its
-inputs have to be ready there, and its results are first ready there.
+inputs have to be ready there, and its results are first ready there.  As with the convolutions, autograd does not
+record the calls: results are detached also where inputs require gradients, which the backward calls compute
+(``examples/conv_tokens.py`` wraps them in ``torch.autograd.Function``).
 
     y, mean, rstd = seq_layer_norm_forward(x, weight, bias, eps)
     dx, dweight, dbias = seq_layer_norm_backward(dy, x, weight, mean, rstd)
