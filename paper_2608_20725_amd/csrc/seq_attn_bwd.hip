@@ -820,10 +820,18 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccQ)) void attn_dq(AttnAr
                     }
                 }
             }
-            if (FEAT == kAny ? sc.cap : FEAT == kCapped)
+            if (FEAT == kAny ? sc.cap : FEAT == kCapped) {
+                if (partial) {
+                    // the slope of a left-out score may be NaN
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    dp[r] *= slope[r];
+                    for (int r = 0; r < 16; ++r)
+                        dp[r] = dp[r] == 0.0f ? 0.0f : dp[r] * slope[r];
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        dp[r] *= slope[r];
+                }
+            }
             if (!partial) {
                 pipeline<Op, false, 2, DP / 32>(cbuf, cload, [&](int i, const V8(&c)[DP / 32]) {
                     const V8 ds = pack8<Op>(dp, 8 * i);

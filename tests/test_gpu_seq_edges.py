@@ -496,3 +496,42 @@ def test_keys_shared_by_workgroups(shape, masks, dtype):
     x, bias = draw(*shape, dtype, seed=Lk, R=90)
     run(x, None, opts)
     run(x, bias, opts)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("hold", [math.nan, math.inf, -math.inf, "largest"], ids=str)
+@pytest.mark.parametrize("cap", [5.0, 1000.0])
+def test_masked_places_with_a_cap(cap, hold, dtype):
+    """What masked places hold has no influence on capped scores either: the
+    slope of a left-out score may be NaN.  Masks that cut through tiles, with
+    and without a bias."""
+    hold = torch.finfo(dtype).max if hold == "largest" else hold
+    B, Lq, Lk = 3, 100, 150
+    doc = torch.arange(Lk)[None].expand(B, Lk) // torch.tensor([[50], [9], [200]])
+    doc = torch.where(torch.arange(Lk)[None] % 7 == 3, torch.full_like(doc, -1), doc).to(torch.int32)
+    for opts in ({"causal": True, "align_end": True, "kv_len": torch.tensor([Lk, 77, 0], dtype=torch.int32)},
+                 {"causal": True}, {"q_doc": doc[:, :Lq].contiguous(), "k_doc": doc}):
+        x, bias = draw(B, Lq, Lk, 2, 1, 64, dtype, R=10)
+        ok = allowed(B, Lq, Lk, **opts)[0]
+        for strip in (None, bias):
+            res = []
+            for value in (0.0, hold):
+                y = {n: t.clone() for n, t in x.items()}
+                for n, seen in (("q", ok.any(2)), ("dout", ok.any(2)), ("k", ok.any(1)), ("v", ok.any(1))):
+                    y[n][~seen] = value
+                res.append(forward_and_backward(y, strip, {**opts, "cap": cap}))
+            for a, b in zip(*res):
+                assert a is None or (not torch.isnan(b).any() and torch.equal(a, b))
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+def test_a_key_that_is_nan_reaches_only_its_pairs(dtype):
+    """Gradients beside a NaN key, capped: NaN in the queries that see it, not in the others of its tile."""
+    L = 100
+    x, _ = draw(1, L, L, 1, 1, 64, dtype)
+    x["k"][0, 40] = math.nan
+    for cap in (0.0, 5.0, 1000.0):
+        res = forward_and_backward(x, None, {"causal": True, "cap": cap})
+        out, lse, dq = res[0].cpu(), res[1].cpu(), res[2].cpu()
+        assert torch.isfinite(out[0, :40]).all() and torch.isfinite(lse[0, 0, :40]).all() and torch.isfinite(dq[0, :40]).all()
+        assert torch.isnan(out[0, 40:]).all() and torch.isnan(lse[0, 0, 40:]).all() and torch.isnan(dq[0, 40:]).all()
