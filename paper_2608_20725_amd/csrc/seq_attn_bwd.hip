@@ -479,15 +479,16 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccKV)) void attn_dkdv(Att
                 c[0] = T::col_frag(tdo, coff, 32 * t + 16 * (i / N), i % N);
                 c[1] = T::col_frag(tq, coff, 32 * t + 16 * (i / N), i % N);
             };
+            uint32_t bad_dout = 0, bad_q = 0;  // fragments of dout and q had values that are not finite
             auto sums = [&](int t, const V8(&p)[2], const V8(&ds)[2], V8(&buf)[2][2], auto each) {
                 pipeline<Op, W::kAhead, 2 * N, 2>(
                     buf, [&](int i, V8(&c)[2]) { columns(t, i, c); },
                     [&](int i, const V8(&c)[2]) {
-                        dv[i % N] = Op::mfma(each(c[0]), p[i / N], dv[i % N]);
-                        dk[i % N] = Op::mfma(each(c[1]), ds[i / N], dk[i % N]);
+                        dv[i % N] = Op::mfma(each(c[0], bad_dout), p[i / N], dv[i % N]);
+                        dk[i % N] = Op::mfma(each(c[1], bad_q), ds[i / N], dk[i % N]);
                     });
             };
-            auto same = [](V8 c) { return c; };
+            auto same = [](V8 c, uint32_t &) { return c; };
 #pragma unroll
             for (int t = 0; t < W::kSub; ++t) {
                 f32x16_acc s, dp;
@@ -510,13 +511,12 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccKV)) void attn_dkdv(Att
                 }
                 if (partial) {
                     const int lim = first == INT32_MAX ? INT32_MAX : first - (q0 + 32 * t) - 4 * h;
-                    const float *const at = rows + 32 * t + 4 * h;  // + 64: delta, + 128: document
+                    const float *const at = rows + 32 * t + 4 * h;  // + 128: document
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const bool out =
                             reg_row(r) < lim || (docs_differ && __float_as_int(at[128 + reg_row(r)]) != doc);
-                        // a dout that is not finite reaches dv through p
-                        s[r] = out ? 0.0f : s[r] + 0.0f * at[64 + reg_row(r)];
+                        s[r] = out ? 0.0f : s[r];
                         dp[r] = out ? 0.0f : dp[r];
                     }
                 }
@@ -527,8 +527,27 @@ __global__ __launch_bounds__(kThreads, (Bwd<Op, DP>::kOccKV)) void attn_dkdv(Att
                 pack16<Op>(dp, ds);
                 if (partial) {
                     // a left-out pair's zero times infinity or NaN must stay zero
-                    uint32_t bad = 0;
-                    sums(t, p, ds, cbuf, [&](V8 c) { return finite<Op>(c, bad); });
+                    bad_dout = 0;
+                    sums(t, p, ds, cbuf, [](V8 c, uint32_t &bad) { return finite<Op>(c, bad); });
+                    if (__any(bad_dout)) {
+                        // rows of dout that are not finite reach the keys they
+                        // see (those of q do through ds, which is NaN)
+                        for (int rr = 0; rr < 32; ++rr) {
+                            if (q0 + 32 * t + rr < first ||
+                                (docs_differ && __float_as_int(rows[128 + 32 * t + rr]) != doc))
+                                continue;
+#pragma unroll
+                            for (int dt = 0; dt < N; ++dt)
+#pragma unroll
+                                for (int g4 = 0; g4 < 4; ++g4) {
+                                    float v[4];
+                                    T::four(tdo, 32 * t + rr, 32 * dt + 8 * g4 + 4 * h, v);
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e)
+                                        dv[dt][4 * g4 + e] += fabsf(v[e]) < INFINITY ? 0.0f : v[e];
+                                }
+                        }
+                    }
                 } else {
                     sums(t, p, ds, cbuf, same);
                 }

@@ -535,3 +535,26 @@ def test_a_key_that_is_nan_reaches_only_its_pairs(dtype):
         out, lse, dq = res[0].cpu(), res[1].cpu(), res[2].cpu()
         assert torch.isfinite(out[0, :40]).all() and torch.isfinite(lse[0, 0, :40]).all() and torch.isfinite(dq[0, :40]).all()
         assert torch.isnan(out[0, 40:]).all() and torch.isnan(lse[0, 0, 40:]).all() and torch.isnan(dq[0, 40:]).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("hold", [math.nan, math.inf], ids=str)
+@pytest.mark.parametrize("cap", [0.0, 5.0])
+def test_dv_takes_what_is_not_finite_from_dout_alone(cap, hold, dtype):
+    """dv = P^T dout: a value that is not finite does not reach it, a dout
+    only the channel it stands in, also in tiles with left-out pairs."""
+    L = 100
+    x, _ = draw(1, L, L, 2, 1, 64, dtype)
+    opts = {"causal": True, "cap": cap}
+    clean = forward_and_backward(x, None, opts)
+    y = {n: t.clone() for n, t in x.items()}
+    y["v"][0, 20, 0, 5] = hold
+    assert torch.equal(forward_and_backward(y, None, opts)[4], clean[4])
+    y = {n: t.clone() for n, t in x.items()}
+    y["dout"][0, 70, 1, 5] = hold
+    dv = forward_and_backward(y, None, opts)[4]
+    want = torch.zeros((1, L, 1, 64), dtype=torch.bool)
+    want[0, :71, 0, 5] = True
+    assert torch.equal(~torch.isfinite(dv.cpu()), want)
+    same = ~want.cuda()
+    assert torch.equal(dv[same], clean[4][same])
