@@ -10,7 +10,7 @@
 // cores and, with a cap or a bias, by the vector operations of both kernels'
 // scores, in attn_dq one score's after the other's (its mask is a branch for
 // each): 2x4096 causal tokens, 32 query heads of 128 over 8, cap 30, bf16:
-// 1266 us, of which attn_dkdv 800, attn_dq 507 and row_stats 27 when profiled.
+// 1280 us, of which attn_dkdv 803, attn_dq 505 and row_stats 27 when profiled.
 //
 // fp16 keeps 5 exponent bits: P is multiplied by 2^14 and dS by a power of
 // two that brings its bound 2 max|dout_i| max|v_j| to at most 2^15, so that
