@@ -3,9 +3,10 @@
  *
  * What follows a convolutional stem whose output pixels or frames are taken as
  * tokens: layer norm over the channels of each token, attention between the
- * tokens, and the learned bias by which attention sees their distance, each
- * with its gradient.  The same library and the same plain C interface as
- * im2win.h: host scalars and device pointers, status codes of im2win.h.
+ * tokens, and the learned bias or the rotation by which attention sees their
+ * distance, each with its gradient; for serving, a key/value cache in pages,
+ * also in 8 bits, and attention over it.  The same library and the same plain C
+ * interface as im2win.h: host scalars and device pointers, its status codes.
  *
  * Ownership: the caller allocates every buffer; the library allocates nothing.
  * Streams: every device call only enqueues work on `hip_stream` (a
@@ -146,6 +147,136 @@ int seq_attention_forward(const seq_attention_t *a, const void *q, const void *k
 int seq_attention_backward(const seq_attention_t *a, const void *dout, const void *q, const void *k, const void *v,
                            const void *out, const float *lse, void *dq, void *dk, void *dv, float *dstrip, void *ws,
                            int64_t ws_bytes, void *hip_stream);
+
+/*
+ * Rotary positions.  Of each head's D channels the first `rot` are turned in
+ * pairs: channels (i, i + rot/2), or (2i, 2i+1) when interleaved, i < rot/2, by
+ * the angle t = p * freq[i] of the token's position p, the others are copied:
+ *   y_a = m*(x_a*cos t - x_b*sin t),  y_b = m*(x_a*sin t + x_b*cos t),  m = amplitude.
+ * The backward call turns dy by -t (and multiplies by m): dx, the gradient.
+ *   x, y    [B][L][H][D]: `*_stride` are the elements between sequences, tokens
+ *           and heads (channels dense; not read where there is only one of
+ *           them).  y may be x itself with the same strides.
+ *   positions  with by_token [B][L], else [B] of the first tokens, the others
+ *           following; NULL: 0, 1, ..  Any int32 values; angles are reduced in
+ *           64-bit fractions of a turn, so far positions lose nothing.
+ *   freq    host memory, [rot/2] radians a position, |freq| <= 1024; copied by
+ *           the call.
+ * rot even, 2 .. min(D, 256); D <= 2^16.  Pointers need the alignment of their
+ * element type only.  A lane takes up to 16 bytes of four heads; calls of 2^32
+ * lanes and more are refused (IM2WIN_ERANGE).
+ */
+#define SEQ_ROTARY_MOST 256
+typedef struct {
+    int dt; /* im2win_dtype_t */
+    int interleaved, by_token;
+    float amplitude;
+    int64_t B, L, H, D, rot;
+    int64_t x_stride[3], y_stride[3];
+    const int32_t *positions;
+    const double *freq;
+} seq_rotary_t;
+
+int seq_rotary_forward(const seq_rotary_t *a, const void *x, void *y, void *hip_stream);
+/* x_stride is dy's, y_stride dx's. */
+int seq_rotary_backward(const seq_rotary_t *a, const void *dy, void *dx, void *hip_stream);
+
+/*
+ * Frequencies freq[i] = base^(-2i/rot), i < rot/2, for contexts `factor` times
+ * as long as the `trained` one: a pair that turns r = trained*f/(2 pi) times
+ * within the trained context keeps its frequency f from r >= high on, has
+ * f/factor up to r <= low, and between them f*(w + (1-w)/factor) with
+ * w = (r - low)/(high - low).  trained = 0: all pairs have f/factor (positions
+ * interpolated); factor = 1: all keep f.  Host only.
+ */
+int seq_rotary_frequencies(double *freq, int64_t rot, double base, double factor, double trained, double low,
+                           double high);
+
+/*
+ * A key/value cache in pages: a pool of `pages` pages of `page` tokens each and
+ * a table that names the pages of B sequences in order.  The token at position
+ * p of sequence b lies at place p % page of page table[b][p / page].  Entries
+ * outside 0 .. pages-1 name no page: tokens there are neither written nor read
+ * (they read as zeros and take no part in attention), nor are positions that
+ * the table does not reach.
+ *   k, v    [pages][page][Hkv][D] of type dt: `*_stride` are the elements
+ *           between pages, tokens and heads (channels dense; not read where
+ *           there is only one of them)
+ *   table   [B][max_pages], rows `table_stride` entries apart (>= max_pages)
+ *   k_scale, v_scale  [pages][page][Hkv] fp32, any strides; 8 bits only
+ * dt is an im2win_dtype_t or one of 8 bits, whose numbers are codes times the
+ * scale s of their token and head, with top the largest magnitude among the
+ * head's D channels:
+ *   SEQ_I8    s = top/127 in fp32, within 2^-126 and the largest number whose
+ *             127-fold is finite, code = x/s rounded to nearest even
+ *   SEQ_E4M3  s the smallest power of two >= 2^-126 with top/s <= 448, code = x/s
+ *             rounded to the nearest of 4 exponent and 3 fraction bits (bias 7,
+ *             no infinities)
+ * A head with a value that is not finite gets the scale NaN and reads as NaN;
+ * a product past the largest number of the type that is read becomes infinite.
+ * D a multiple of 8, 8 .. 128; page >= 1, max_pages*page <= 2^30, pages < 2^31;
+ * pages and dense operands 16-byte aligned with strides of multiples of 16
+ * bytes (8-bit pages: 8 bytes); table, scales and counts as their type.
+ */
+enum { SEQ_I8 = 16, SEQ_E4M3 = 17 };
+typedef struct {
+    int dt;
+    int64_t B, pages, page, max_pages, Hkv, D;
+    int64_t k_stride[3], v_stride[3], k_scale_stride[3], v_scale_stride[3];
+    int64_t table_stride;
+    void *k, *v;
+    float *k_scale, *v_scale;
+    const int32_t *table;
+} seq_cache_t;
+
+/*
+ * Writes new tokens: token t < count[b] of sequence b to position start[b] + t
+ * (count NULL: all L; start NULL: 0).  Rows from count[b] on are not read, and
+ * the pool is left as it was but for the tokens written.  The places written in one call
+ * must differ (a page shared by two sequences is not written by both): where
+ * two tokens meet, the place holds parts of either.
+ *   k, v    [B][L][Hkv][D] of type dt (that of the cache, or any beside 8-bit
+ *           pages); strides as above, of sequences, tokens and heads
+ */
+int seq_cache_write(const seq_cache_t *c, const void *k, const void *v, const int64_t *k_stride,
+                    const int64_t *v_stride, int64_t L, im2win_dtype_t dt, const int32_t *start, const int32_t *count,
+                    void *hip_stream);
+
+/*
+ * Lays sequences out densely: positions 0 .. len[b]-1 of sequence b to k and v
+ * [B][L][Hkv][D]; rows from len[b] on become zeros, positions from L on are not
+ * read.  Pages may be shared.
+ */
+int seq_cache_read(const seq_cache_t *c, void *k, void *v, const int64_t *k_stride, const int64_t *v_stride, int64_t L,
+                   im2win_dtype_t dt, const int32_t *len, void *hip_stream);
+
+/*
+ * Attention of one new token of each sequence, the last of its len[b] tokens
+ * (taken within 0 .. max_pages*page), over the cache: scores, out and lse as in
+ * seq_attention_forward with Lq = 1, align_end and position len[b] - 1, keys
+ * the tokens whose pages are there.  A sequence without any has out = 0 and
+ * lse = -inf.
+ *   q, out  [B][H][D] of type dt (that of the cache, or any beside 8-bit pages):
+ *           `*_stride` are the elements between sequences and heads
+ *   lse     [B][H] fp32
+ *   ws      seq_paged_attention_workspace_bytes(c, H, dt) bytes, 16-byte aligned
+ * H a multiple of Hkv, B*H < 2^24.  Numerics as in seq_attention_forward;
+ * 8-bit codes beside 16-bit queries are multiplied in fp16, which holds them
+ * exactly.
+ */
+typedef struct {
+    int dt; /* im2win_dtype_t */
+    float scale, cap;
+    int64_t H;
+    int64_t q_stride[2], out_stride[2];
+    int64_t R;           /* range of the bias strip; 0: no bias */
+    const float *strip;  /* [H][2R+1] fp32 */
+    const int32_t *len;  /* [B] */
+} seq_paged_attention_t;
+
+int64_t seq_paged_attention_workspace_bytes(const seq_cache_t *c, int64_t H, im2win_dtype_t dt);
+int seq_paged_attention_forward(const seq_cache_t *c, const seq_paged_attention_t *a, const void *q, void *out,
+                                float *lse, void *ws, int64_t ws_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -373,3 +373,8 @@ from .seq import *  # noqa: E402,F401,F403
 from .seq import __all__ as _seq_names  # noqa: E402
 
 __all__ += _seq_names
+
+from .seq_cache import *  # noqa: E402,F401,F403
+from .seq_cache import __all__ as _seq_cache_names  # noqa: E402
+
+__all__ += _seq_cache_names

@@ -88,7 +88,7 @@ struct Operand {
     }
 };
 
-int check_strides(const Operand &o)
+int check_strides(const Operand &o, bool any_token_stride = false)
 {
     const int64_t n[3] = {o.B, o.L, o.heads};
     for (int k = 0; k < 3; ++k) {
@@ -97,7 +97,7 @@ int check_strides(const Operand &o)
         if (too_far(n[k], o.stride[k]))
             return IM2WIN_ERANGE;
     }
-    if (o.stride[1] * o.elt >= (int64_t)1 << 24)
+    if (!any_token_stride && o.stride[1] * o.elt >= (int64_t)1 << 24)
         return IM2WIN_ERANGE;
     return IM2WIN_OK;
 }

@@ -1,0 +1,665 @@
+// Attention of one new token of each sequence over its pages.
+//
+// The work is the cache's bytes, read once.  The G = H/Hkv queries of a
+// key/value head are the columns of score tiles of the 16x16 matrix
+// instructions, up to four tiles side by side; a wave streams 32 keys at a
+// time straight from the pages into its operand registers, with no copy in LDS
+// and no barrier between the waves:
+//   scores  [key][query]: a lane's 16 bytes of a key are the operand as they lie
+//           (the order of channels within a product is free, q follows it);
+//   output  [channel][query]: the scores' registers are the operand as they lie,
+//           and a lane holds 8 channels of 8 keys, which it turns from rows of
+//           keys into rows of channels by byte permutations.
+// While a tile's scores are made the values are on their way, and while the
+// values are summed the next keys.  A sequence's keys are split evenly over
+// workgroups, whatever its table could hold, and over the four waves of each;
+// parts (maximum, sum, output) are joined in LDS and by paged_join.
+//
+// 8-bit pages go through the matrix cores as fp16, which holds every code
+// exactly; a key's scale multiplies its score, a value's the probability, over
+// the largest power of two at or above a scale seen so far.  bf16 queries over
+// them are brought to fp16 by a power of two a row: what falls below 2^-39 of
+// the row's largest channel is lost, less than fp32 sums lose.
+#include "seq_attn.hpp"
+#include "seq_cache.hpp"
+
+namespace im2win {
+namespace {
+
+constexpr int kKeys = 32;   // keys of a tile
+constexpr int kUnit = 128;  // keys of a workgroup's step: a tile a wave
+constexpr int kWavesP = 4;
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+
+// 8 bytes between rows are certain, 16 only where D is a multiple of 16.
+typedef u32x4_t u32x4_a8 __attribute__((aligned(8)));
+typedef f32x8_t f32x8_a16 __attribute__((aligned(16)));
+
+struct F32Wide {  // fp32 operands, v_mfma_f32_16x16x4_f32
+    typedef float elem;
+};
+
+// What pages of element size ES hold for a lane: 16-byte pieces of keys (the
+// lane's group takes bytes 64*c + 16*group of each), 8 channels of values.
+template <int ES>
+struct Values;
+template <>
+struct Values<4> {
+    u32x4_t w[2];
+};
+template <>
+struct Values<2> {
+    u32x4_t w[1];
+};
+template <>
+struct Values<1> {
+    u32x2_t w[1];
+};
+
+// ---- codes to fp16, exact ----
+// Two codes, bytes A and B (0 .. 3 of x, 4 .. 7 of y), as two halves of a word.
+template <class Code>
+struct Half;
+template <>
+struct Half<CodeI8> {
+    // 1024 + (code + 128) by its bits, minus 1152
+    template <int A, int B>
+    __device__ static inline uint32_t two(uint32_t y, uint32_t x)
+    {
+        const uint32_t w = __builtin_amdgcn_perm(y, x, 0x0C000C00u | (B << 16) | A);
+        const h2 less = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+        return __builtin_bit_cast(uint32_t, (h2)(__builtin_bit_cast(h2, w ^ 0x64806480u) + less));
+    }
+};
+template <>
+struct Half<CodeE4M3> {
+    template <int A, int B>
+    __device__ static inline uint32_t two(uint32_t y, uint32_t x)
+    {
+        if constexpr (A % 4 == 0 && B == A + 1)
+            return of<false>(A ? y : x);
+        else if constexpr (A % 4 == 2 && B == A + 1)
+            return of<true>(A > 3 ? y : x);
+        else
+            return of<false>(__builtin_amdgcn_perm(y, x, 0x0C0C0000u | (B << 8) | A));
+    }
+    template <bool UPPER>
+    __device__ static inline uint32_t of(uint32_t w)
+    {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, UPPER));
+    }
+};
+
+// ---- the two products ----
+// Op: F16Op, BF16Op or F32Wide; Code: CodeI8, CodeE4M3 or void (pages of Op's
+// own type).  NK pieces of 16 bytes of a key, EPC = 16/ES channels each.
+template <class Op, class Code, int DP>
+struct Math {
+    static constexpr bool kWide = __is_same(Op, F32Wide);
+    static constexpr bool kCodes = !__is_same(Code, void);
+    static constexpr int ES = kCodes ? 1 : kWide ? 4 : 2;
+    static constexpr int EPC = 16 / ES, NK = DP * ES / 64;
+    typedef Values<ES> V;
+    // a lane's channels of a query: piece by piece, EPC each
+    struct Query {
+        typename Op::elem x[NK * EPC];
+    };
+
+    __device__ static inline f32x4_acc dot(const u32x4_t (&k)[NK], const Query &q)
+    {
+        f32x4_acc s = {0, 0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < NK; ++c) {
+            if constexpr (kWide && !kCodes) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    s = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, (uint32_t)k[c][e]), q.x[4 * c + e], s, 0, 0, 0);
+            } else if constexpr (kWide) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const f32x8_t x = Code::decode(u32x2_t{k[c][2 * h], k[c][2 * h + 1]});
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        s = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], q.x[16 * c + 8 * h + e], s, 0, 0, 0);
+                }
+            } else if constexpr (!kCodes) {
+                s = Op::mfma16(__builtin_bit_cast(typename Op::v8, k[c]), eight(q, 8 * c), s);
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t x = k[c][2 * h], y = k[c][2 * h + 1];
+                    typedef Half<Code> T;
+                    const u32x4_t w = {T::template two<0, 1>(y, x), T::template two<2, 3>(y, x),
+                                       T::template two<4, 5>(y, x), T::template two<6, 7>(y, x)};
+                    s = Op::mfma16(__builtin_bit_cast(typename Op::v8, w), eight(q, 16 * c + 8 * h), s);
+                }
+            }
+        }
+        return s;
+    }
+    __device__ static inline auto eight(const Query &q, int at)
+    {
+        typename Op::v8 v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = q.x[at + e];
+        return v;
+    }
+
+    // Channel 8*(lane & 15) + j of the lane's 8 keys: rows of the operand.
+    template <int J>
+    __device__ static inline u32x4_t channel(const V (&v)[8])
+    {
+        u32x4_t w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (ES == 2) {
+                w[i] = __builtin_amdgcn_perm(v[2 * i + 1].w[0][J / 2], v[2 * i].w[0][J / 2],
+                                             J % 2 ? 0x07060302u : 0x05040100u);
+            } else {
+                w[i] = Half<Code>::template two<J % 4, 4 + J % 4>(v[2 * i + 1].w[0][J / 4], v[2 * i].w[0][J / 4]);
+            }
+        }
+        return w;
+    }
+    template <int J>
+    __device__ static inline float value(const V &v)
+    {
+        if constexpr (kCodes)
+            return Code::decode(v.w[0])[J];
+        else
+            return __builtin_bit_cast(float, (uint32_t)v.w[J / 4][J % 4]);
+    }
+
+    // o[j] += channel j of the values times the weights w[nt] of NT tiles of queries.
+    template <int NT, int J = 0>
+    __device__ static inline void sum(f32x4_acc (&o)[NT][8], const V (&v)[8], const float (&p)[NT][8],
+                                      const u32x4_t (&packed)[NT])
+    {
+        if constexpr (kWide) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float x = value<J>(v[i]);
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                    o[t][J] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, p[t][i], o[t][J], 0, 0, 0);
+            }
+        } else {
+            const auto x = __builtin_bit_cast(typename Op::v8, channel<J>(v));
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                o[t][J] = Op::mfma16(x, __builtin_bit_cast(typename Op::v8, packed[t]), o[t][J]);
+        }
+        if constexpr (J < 7)
+            sum<NT, J + 1>(o, v, p, packed);
+    }
+};
+
+// What the lanes of a wave tell each other of a tile: where its keys and values
+// lie (bytes from the head's first), and 8-bit pages' scales.
+struct Where {
+    int64_t k[kKeys], v[kKeys];
+    float ks[kKeys], vs[kKeys];
+};
+
+// Part of a row: its output sums, maximum and sum.
+__device__ inline float *part_of(const PagedArgs &a, int split, int row, int rows, int D)
+{
+    return a.part + ((int64_t)split * rows + row) * part_floats(D);
+}
+
+// Keys of a split: an even share of the sequence, in whole steps.
+__device__ inline int share_of(int n, int splits)
+{
+    return ((n + splits - 1) / splits + kUnit - 1) / kUnit * kUnit;
+}
+
+template <class E, class Op, class Code, int NT, int DP>
+__global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
+{
+    typedef Math<Op, Code, DP> M;
+    constexpr bool kHalf = __is_same(Op, F16Op);
+    // fp16 probabilities are times 2^14, so that those of long rows stay normal numbers
+    constexpr float kShift = kHalf ? 14.0f : 0.0f, kUnshift = kHalf ? 0x1p-14f : 1.0f;
+    __shared__ __align__(16) Where where[kWavesP];
+    __shared__ float box[kWavesP][16][DP + 4];
+    __shared__ float sm[kWavesP][NT][16], sl[kWavesP][NT][16];
+
+    const int heads = a.B * c.Hkv;
+    const int bh = blockIdx.x % heads, rest = blockIdx.x / heads, rt = rest % a.row_tiles, split = rest / a.row_tiles;
+    const int b = bh / c.Hkv, hk = bh - b * c.Hkv;
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = c.pages > 0 ? held_tokens(a.len[b], c.max_pages, c.page.d) : 0;
+    const int share = share_of(n, a.splits), lo = split * share, hi = min(n, lo + share);
+    if (lo >= hi && split > 0)
+        return;
+
+    // this lane's queries: column r of each tile
+    const int row0 = rt * (16 * NT);
+    float c1[NT];
+    typename M::Query q[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int row = row0 + 16 * t + r;
+        const typename E::T *const p = (const typename E::T *)(a.q + b * a.q_sb + (hk * a.G + row) * a.q_sh);
+        float x[M::NK * M::EPC];
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < M::NK; ++k)
+#pragma unroll
+            for (int e = 0; e < M::EPC; e += 4) {
+                typedef typename E::T V4 __attribute__((ext_vector_type(4)));
+                const int ch = (4 * k + g) * M::EPC + e;
+                V4 v = {};
+                if (row < a.G && ch < c.D)
+                    v = *(const V4 *)(p + ch);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[k * M::EPC + e + i] = E::get(v[i]);
+                    top = max(top, __builtin_bit_cast(uint32_t, x[k * M::EPC + e + i]) & 0x7FFFFFFFu);
+                }
+            }
+        float f = 1.0f, back = 1.0f;
+        if constexpr (M::kCodes && kHalf && __is_same(E, EltBF16)) {
+            top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+            top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+            const int e = max((int)(top >> 23) - 127, -100);  // the row's largest becomes 2^14 .. 2^15
+            f = __builtin_bit_cast(float, (uint32_t)(127 + 14 - e) << 23);
+            back = __builtin_bit_cast(float, (uint32_t)(127 - 14 + e) << 23);
+        }
+#pragma unroll
+        for (int k = 0; k < M::NK * M::EPC; ++k)
+            q[t].x[k] = (typename Op::elem)(x[k] * f);
+        c1[t] = back * (a.cap > 0 ? a.scale / a.cap : a.scale * kLog2e);
+    }
+    const float c2 = a.cap * kLog2e;
+
+    const char *const kp = c.k + hk * c.k_head, *const vp = c.v + hk * c.v_head;
+    const int32_t *const table = c.table + b * c.table_stride;
+    Where &my = where[wave];
+
+    // A lane is the owner of key (lane & 31) of each tile.
+    auto page_at = [&](int k0) {
+        const int key = k0 + (lane & 31);
+        return key < hi ? page_of(table, fdiv((uint32_t)key, c.page), c.max_pages, c.pages) : -1;
+    };
+    auto inside = [&](int k0) {
+        const uint32_t key = k0 + (lane & 31);
+        return (int)(key - fdiv(key, c.page) * c.page.d);
+    };
+    auto k_scale = [&](int id, int in) { return id < 0 ? 0.0f : *(const float *)(c.ks + hk * c.ks_head + id * c.ks_page + in * c.ks_tok); };
+    auto v_scale = [&](int id, int in) { return id < 0 ? 0.0f : *(const float *)(c.vs + hk * c.vs_head + id * c.vs_page + in * c.vs_tok); };
+    // Keys that are not there read page 0 and are left out of what follows.
+    auto tell = [&](int id, int in) {
+        if (lane < kKeys)
+            my.k[lane] = id < 0 ? 0 : id * c.k_page + in * c.k_tok;
+        else
+            my.v[lane & 31] = id < 0 ? 0 : id * c.v_page + in * c.v_tok;
+    };
+    u32x4_t kr[2][M::NK];
+    typename M::V vr[8];
+    auto load_keys = [&]() {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const char *const p = kp + my.k[16 * s + r] + 16 * g;
+#pragma unroll
+            for (int k = 0; k < M::NK; ++k) {
+                const int left = c.D * M::ES - (64 * k + 16 * g);  // a multiple of 8
+                kr[s][k] = u32x4_t{0, 0, 0, 0};
+                if (left >= 16) {
+                    kr[s][k] = *(const u32x4_a8 *)(p + 64 * k);
+                } else if (M::ES == 1 && left > 0) {
+                    const u32x2_t w = *(const u32x2_t *)(p + 64 * k);
+                    kr[s][k] = u32x4_t{w[0], w[1], 0, 0};
+                }
+            }
+        }
+    };
+    auto load_values = [&]() {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const char *const p = vp + my.v[16 * (i >> 2) + 4 * g + (i & 3)] + 8 * r * M::ES;
+            if (8 * r < c.D)
+                vr[i] = *(const typename M::V *)p;
+            else
+                vr[i] = typename M::V{};
+        }
+    };
+
+    f32x4_acc o[NT][8];
+    float m[NT], l[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        m[t] = -INFINITY, l[t] = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            o[t][j] = f32x4_acc{0, 0, 0, 0};
+    }
+    float unit = 0x1p-126f;  // 8 bits, fp16: the values' scales are over this power of two
+
+    const int first = lo + wave * kKeys;
+    int id = page_at(first), in = inside(first);
+    float ks = 0, vs = 0;
+    if (first < hi) {
+        if constexpr (M::kCodes)
+            ks = k_scale(id, in), vs = v_scale(id, in);
+        tell(id, in);
+        wave_lds_handoff();
+        load_keys();
+        load_values();
+    }
+    int id1 = page_at(first + kUnit), in1 = inside(first + kUnit);
+    for (int k0 = first; k0 < hi; k0 += kUnit) {
+        // scores of the tile; a lane's keys are 16*(i >> 2) + 4*g + (i & 3)
+        float s[NT][8];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f32x4_acc x = M::dot(kr[h], q[t]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    s[t][4 * h + i] = x[i];
+            }
+        const uint32_t there = (uint32_t)__ballot(id >= 0);  // a bit a key (lanes 0 .. 31)
+        float kscale[8], vscale[8];
+        wave_lds_handoff();
+        if constexpr (M::kCodes) {
+            my.ks[lane & 31] = ks;
+            my.vs[lane & 31] = vs;
+            wave_lds_handoff();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                kscale[i] = my.ks[16 * (i >> 2) + 4 * g + (i & 3)];
+                vscale[i] = my.vs[16 * (i >> 2) + 4 * g + (i & 3)];
+            }
+        }
+        // the next tile's keys
+        id = id1, in = in1;
+        tell(id, in);
+        wave_lds_handoff();
+        const bool more = k0 + kUnit < hi;
+        if (more) {
+            load_keys();
+            if constexpr (M::kCodes)
+                ks = k_scale(id, in), vs = v_scale(id, in);
+            id1 = page_at(k0 + 2 * kUnit), in1 = inside(k0 + 2 * kUnit);
+        }
+
+        // softmax
+        float p[NT][8], up = 1.0f, over = 1.0f;
+        if constexpr (M::kCodes && kHalf) {
+            float top = unit;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                top = fmaxf(top, vscale[i]);
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            // up to the next power of two, at most 2^126
+            const uint32_t bits = min((__builtin_bit_cast(uint32_t, top) + 0x7FFFFFu) & 0x7F800000u, 253u << 23);
+            const float now = __builtin_bit_cast(float, bits);
+            over = __builtin_bit_cast(float, (254u << 23) - bits);
+            up = unit * over;
+            unit = now;
+        }
+        u32x4_t packed[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const float *const strip = a.strip + (int64_t)min(hk * a.G + row0 + 16 * t + r, a.H - 1) * (2 * a.R + 1) + a.R;
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int at = 16 * (i >> 2) + 4 * g + (i & 3);
+                float x = s[t][i] * c1[t];
+                if constexpr (M::kCodes)
+                    x *= kscale[i];
+                if (a.cap > 0) {
+                    const float far = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * (2.0f * kLog2e)));
+                    x = c2 * (fabsf(x) < kSmallTanh ? small_tanh(x) : far);
+                }
+                if (a.R > 0)
+                    x += strip[min(max(k0 + at - (n - 1), -a.R), 0)] * kLog2e;
+                x = (there >> at) & 1 ? x : -INFINITY;
+                s[t][i] = x;
+                top = fmaxf(top, x);
+            }
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float now = fmaxf(m[t], top), base = now == -INFINITY ? 0.0f : now;
+            float f = __builtin_amdgcn_exp2f(m[t] - base);
+            m[t] = now;
+            float sum = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                p[t][i] = __builtin_amdgcn_exp2f(s[t][i] - base + kShift);
+                sum += p[t][i];
+                if constexpr (M::kCodes)
+                    p[t][i] *= kHalf ? vscale[i] * over : vscale[i];
+            }
+            l[t] = l[t] * f + sum;
+            f *= up;
+            if (__any(f != 1.0f)) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    o[t][j] *= f;
+            }
+            if constexpr (!M::kWide) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    packed[t][i] = Op::bits(p[t][2 * i]) | Op::bits(p[t][2 * i + 1]) << 16;
+            }
+        }
+        if (there != 0xFFFFFFFFu) {
+            // what was read for keys that are not there: their weights are zero,
+            // and so must be the values
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (!((there >> (16 * (i >> 2) + 4 * g + (i & 3))) & 1))
+                    vr[i] = typename M::V{};
+        }
+        M::template sum<NT>(o, vr, p, packed);
+        if (more)
+            load_values();
+    }
+
+    // join the waves
+    const float down = M::kCodes && kHalf ? unit : 1.0f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        l[t] += __shfl_xor(l[t], 16);
+        l[t] += __shfl_xor(l[t], 32);
+        if (g == 0) {
+            sm[wave][t][r] = m[t];
+            sl[wave][t][r] = l[t];
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        if (row0 + 16 * t >= a.G)  // no query from here on, for any wave
+            break;
+        __syncthreads();
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWavesP; ++w)
+            top = fmaxf(top, sm[w][t][r]);
+        const float mine = __builtin_amdgcn_exp2f(m[t] - (top == -INFINITY ? 0.0f : top)) * down;
+        // this lane's channels are 32*g .. 32*g + 31
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (32 * g < DP)
+                    box[wave][r][32 * g + 8 * i + j] = o[t][j][i] * mine;
+        __syncthreads();
+        // 16 threads a row, 8 channels each
+        const int rr = threadIdx.x >> 4, ch = (threadIdx.x & 15) * 8, row = row0 + 16 * t + rr;
+        if (row < a.G) {
+            float ms = -INFINITY, sum = 0;
+#pragma unroll
+            for (int w = 0; w < kWavesP; ++w)
+                ms = fmaxf(ms, sm[w][t][rr]);
+            const float base = ms == -INFINITY ? 0.0f : ms;
+#pragma unroll
+            for (int w = 0; w < kWavesP; ++w)
+                sum += sl[w][t][rr] * __builtin_amdgcn_exp2f(sm[w][t][rr] - base);
+            f32x8_t v = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (ch < DP)
+#pragma unroll
+                for (int w = 0; w < kWavesP; ++w)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        v[e] += box[w][rr][ch + e];
+            const int out_row = b * a.H + hk * a.G + row;
+            if (a.splits > 1) {
+                float *const part = part_of(a, split, out_row, a.B * a.H, c.D);
+                if (ch < c.D)
+                    *(f32x8_a16 *)(part + ch) = v;
+                if (ch == 0) {
+                    part[c.D] = ms;
+                    part[c.D + 1] = sum;
+                }
+            } else {
+                const bool none = sum == 0.0f;  // not ms == -inf: all scores may be NaN
+                if (ch < c.D) {
+                    typedef typename E::T V8 __attribute__((ext_vector_type(8)));
+                    V8 y;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        y[e] = E::put(none ? 0.0f : v[e] / sum);
+                    *(V8 *)(a.out + b * a.o_sb + (hk * a.G + row) * a.o_sh + ch * sizeof(typename E::T)) = y;
+                }
+                if (ch == 0)
+                    a.lse[out_row] = none ? -INFINITY : (ms + __log2f(sum * kUnshift)) * kLn2;
+            }
+        }
+    }
+}
+
+// Joins the parts of a row: 32 lanes hold its channels, four each, and `groups`
+// of them (1 or 8) take its parts in turn.
+template <class E, bool HALF>
+__global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int groups)
+{
+    typedef float v4 __attribute__((ext_vector_type(4)));
+    __shared__ v4 sv[8][32];
+    __shared__ float sl[8];
+    constexpr float kUnshift = HALF ? 0x1p-14f : 1.0f;
+    const int rows = a.B * a.H, lane = threadIdx.x & 31, d = lane * 4, group = threadIdx.x >> 5, first = group % groups;
+    const int row = blockIdx.x * (8 / groups) + group / groups, live = row < rows;
+    const int b = live ? row / a.H : 0, h = live ? row - b * a.H : 0;
+    const int n = c.pages > 0 && live ? held_tokens(a.len[b], c.max_pages, c.page.d) : 0;
+    const int share = share_of(n, a.splits), parts = n ? (n + share - 1) / share : 0;
+    float m = -INFINITY;
+    for (int k = lane; k < parts; k += 32)
+        m = fmaxf(m, part_of(a, k, row, rows, c.D)[c.D]);
+#pragma unroll
+    for (int x = 16; x >= 1; x >>= 1)
+        m = fmaxf(m, __shfl_xor(m, x));
+    const float base = m == -INFINITY ? 0.0f : m;
+    v4 v = {0, 0, 0, 0};
+    float l = 0;
+#pragma unroll 4
+    for (int k = first; k < parts; k += groups) {
+        const float *const p = part_of(a, k, row, rows, c.D);
+        const float f = __builtin_amdgcn_exp2f(p[c.D] - base);
+        l += f * p[c.D + 1];
+        if (d < c.D)
+            v += *(const v4 *)(p + d) * f;
+    }
+    if (groups > 1) {
+        sv[group][lane] = v;
+        if (lane == 0)
+            sl[group] = l;
+        __syncthreads();
+        if (group)
+            return;
+        for (int k = 1; k < 8; ++k) {
+            v += sv[k][lane];
+            l += sl[k];
+        }
+    }
+    if (!live)
+        return;
+    const bool none = l == 0.0f;
+    if (lane == 0)
+        a.lse[row] = none ? -INFINITY : (m + __log2f(l * kUnshift)) * kLn2;
+    if (d < c.D) {
+        typedef typename E::T V4 __attribute__((ext_vector_type(4)));
+        V4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            y[e] = E::put(none ? 0.0f : v[e] / l);
+        *(V4 *)(a.out + b * a.o_sb + h * a.o_sh + d * sizeof(typename E::T)) = y;
+    }
+}
+
+// Tiles of 16 queries that a workgroup takes: one, or several beside each other
+// where a key/value head has more queries than one holds (four; two in fp32,
+// whose operands take twice the registers).
+int tiles_of(int64_t G, int dt) { return G <= 16 ? 1 : dt == IM2WIN_F32 ? 2 : 4; }
+int64_t row_tiles_of(int64_t G, int dt) { return (G + 16 * tiles_of(G, dt) - 1) / (16 * tiles_of(G, dt)); }
+
+int64_t splits_of(const Pool &c, int64_t B, int64_t H, int dt)
+{
+    const int64_t row_tiles = row_tiles_of(H / c.Hkv, dt);
+    const int64_t groups = B * c.Hkv * row_tiles, most = ((int64_t)c.max_pages * c.page.d + kUnit - 1) / kUnit;
+    const int64_t want = groups > 0 ? (1024 + groups - 1) / groups : 1;
+    return want < most ? want : most > 1 ? most : 1;
+}
+
+template <class E, class Op, class Code, int NT>
+void run(const Pool &c, const PagedArgs &a, hipStream_t st)
+{
+    const uint32_t grid = (uint32_t)(a.B * c.Hkv) * a.row_tiles * a.splits;
+    if (c.D <= 64)
+        paged_attn<E, Op, Code, NT, 64><<<grid, 64 * kWavesP, 0, st>>>(c, a);
+    else
+        paged_attn<E, Op, Code, NT, 128><<<grid, 64 * kWavesP, 0, st>>>(c, a);
+    if (a.splits > 1) {
+        const int64_t rows = (int64_t)a.B * a.H;
+        const int groups = rows <= 2048 && a.splits >= 8 ? 8 : 1;
+        paged_join<E, __is_same(Op, F16Op)><<<(uint32_t)((rows * groups + 7) / 8), 256, 0, st>>>(c, a, groups);
+    }
+}
+
+template <class E, class Op, class Code>
+void run_tiles(const Pool &c, const PagedArgs &a, hipStream_t st)
+{
+    constexpr int kMany = __is_same(E, EltF32) ? 2 : 4;
+    a.G <= 16 ? run<E, Op, Code, 1>(c, a, st) : run<E, Op, Code, kMany>(c, a, st);
+}
+
+// Own: the pages' operand type where they hold E itself; Coded: of 8-bit pages.
+template <class E, class Own, class Coded>
+void run_code(const Pool &c, int ct, const PagedArgs &a, hipStream_t st)
+{
+    ct == SEQ_I8     ? run_tiles<E, Coded, CodeI8>(c, a, st)
+    : ct == SEQ_E4M3 ? run_tiles<E, Coded, CodeE4M3>(c, a, st)
+                     : run_tiles<E, Own, void>(c, a, st);
+}
+
+}  // namespace
+
+int64_t paged_part_floats(const Pool &c, int64_t B, int64_t H, int dt)
+{
+    const int64_t s = splits_of(c, B, H, dt);
+    return s > 1 ? s * B * H * part_floats(c.D) : 0;
+}
+
+hipError_t launch_paged(const Pool &c, int ct, PagedArgs a, int dt, hipStream_t st)
+{
+    a.splits = (int32_t)splits_of(c, a.B, a.H, dt);
+    a.row_tiles = (int32_t)row_tiles_of(a.G, dt);
+    if (dt == IM2WIN_F32)
+        run_code<EltF32, F32Wide, F32Wide>(c, ct, a, st);
+    else if (dt == IM2WIN_F16)
+        run_code<EltF16, F16Op, F16Op>(c, ct, a, st);
+    else
+        run_code<EltBF16, BF16Op, F16Op>(c, ct, a, st);
+    return hipGetLastError();
+}
+
+}  // namespace im2win

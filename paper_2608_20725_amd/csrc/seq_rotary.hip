@@ -1,0 +1,218 @@
+// Rotary positions: the pair (a, b) of channels at position p becomes
+// m*(a cos t - b sin t, a sin t + b cos t), t = p*freq[pair]; the gradient is
+// the same with -t.
+//
+// Angles are counted in turns, as 64-bit fractions: p*freq mod 1 is one integer
+// product whose upper bits wrap by themselves, so an angle of position 2^31 is
+// as good as one of position 1 (an fp32 product would be off by 2^-24 of
+// p*freq, 8e-3 radians at 131072) and needs no reduction beyond its octant.
+// Bound by the bytes: each value is read and written once.  A lane takes 16
+// bytes of a head's channels and of their partners, and the same channels of
+// kHeads heads of the token, so that an angle's sine and cosine (40 operations a
+// pair) are spread over them.
+#include "seq_rotary.hpp"
+
+namespace im2win {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Cosine and sine of `turn` * 2^-32 turns.  The residue of the nearest quarter
+// is at most pi/4; the first terms left out are below 2e-9 (sine) and 2e-10.
+__device__ inline void cos_sin(uint32_t turn, float &c, float &s)
+{
+    const uint32_t q = (turn + 0x20000000u) >> 30;
+    const float x = (float)(int32_t)(turn - (q << 30)) * 1.46291807926715968e-9f;  // 2 pi 2^-32
+    const float z = x * x;
+    float a = fmaf(z, 1.0f / 362880, -1.0f / 5040), b = fmaf(z, -1.0f / 3628800, 1.0f / 40320);
+    a = fmaf(z, a, 1.0f / 120), b = fmaf(z, b, -1.0f / 720);
+    a = fmaf(z, a, -1.0f / 6), b = fmaf(z, b, 1.0f / 24);
+    a = fmaf(x * z, a, x), b = fmaf(z, b, -0.5f);
+    b = fmaf(z, b, 1.0f);
+    c = q & 1 ? a : b;
+    s = q & 1 ? b : a;
+    c = (q + 1) & 2 ? -c : c;
+    s = q & 2 ? -s : s;
+}
+
+// n of N values from p on as fp32, or back; whole vectors with their element's
+// alignment, as rotated parts and strides may start anywhere.
+template <class E, int N>
+__device__ inline void load(const char *p, int n, float *f)
+{
+    typedef typename E::T T;
+    typedef T V __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    if (n >= N) {
+        const V v = *(const V *)p;
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            f[e] = E::get(v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            f[e] = e < n ? E::get(((const T *)p)[e]) : 0.0f;
+    }
+}
+template <class E, int N>
+__device__ inline void store(char *p, int n, const float *f)
+{
+    typedef typename E::T T;
+    typedef T V __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    if (n >= N) {
+        V v;
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            v[e] = E::put(f[e]);
+        *(V *)p = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (e < n)
+                ((T *)p)[e] = E::put(f[e]);
+    }
+}
+
+// Lanes: units of a head fastest, then groups of heads, then tokens.  A unit is
+// N pairs (N values and their N partners; side by side, 2N values in a row),
+// behind them, where x is not y, 2N channels that are copied.
+template <class E, bool PAIRED, int HEADS>
+__global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a, Turns f)
+{
+    typedef typename E::T T;
+    constexpr int N = PAIRED ? 8 / sizeof(T) : 16 / sizeof(T), W = PAIRED ? 2 * N : N;
+    const uint32_t id = blockIdx.x * kThreads + threadIdx.x;
+    if (id >= a.lanes)
+        return;
+    const uint32_t rest = fdiv(id, a.units), unit = id - rest * a.units.d;
+    const uint32_t token = fdiv(rest, a.groups), group = rest - token * a.groups.d;
+    const uint32_t b = fdiv(token, a.len), t = token - b * a.len.d;
+    const char *x = a.x + b * a.x_sb + t * a.x_st;
+    char *y = a.y + b * a.y_sb + t * a.y_st;
+    const int half = a.rot / 2;
+
+    if ((int)unit >= a.pair_units) {
+        const int c = a.rot + (unit - a.pair_units) * W, n = a.D - c;
+        for (int h = group; h < a.H; h += a.groups.d) {
+            // as bits: a NaN keeps its payload
+            typedef T V __attribute__((ext_vector_type(W), aligned(sizeof(T))));
+            const char *const p = x + h * a.x_sh + c * sizeof(T);
+            char *const o = y + h * a.y_sh + c * sizeof(T);
+            if (n >= W)
+                *(V *)o = *(const V *)p;
+            else
+                for (int e = 0; e < n; ++e)
+                    ((T *)o)[e] = ((const T *)p)[e];
+        }
+        return;
+    }
+    const int first = unit * N, n = half - first;  // pairs first .. first + min(n, N) - 1
+    int64_t pos = t;
+    if (a.pos)
+        pos = a.by_token ? (int64_t)a.pos[token] : (int64_t)a.pos[b] + t;
+    float c[N], s[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const uint64_t turn = (uint64_t)pos * f.turn[e < n ? first + e : 0];
+        cos_sin((uint32_t)(turn >> 32), c[e], s[e]);
+        c[e] *= a.amplitude;
+        s[e] *= a.sin_amplitude;
+    }
+    const int at = (PAIRED ? 2 * first : first) * sizeof(T), to = half * sizeof(T);
+    for (int h0 = group; h0 < a.H; h0 += HEADS * a.groups.d) {
+        float u[HEADS][N], v[HEADS][N];
+#pragma unroll
+        for (int k = 0; k < HEADS; ++k) {
+            const int h = h0 + k * a.groups.d;
+            if (h >= a.H)
+                break;
+            const char *const p = x + h * a.x_sh + at;
+            if constexpr (PAIRED) {
+                float w[W];
+                load<E, W>(p, 2 * n, w);
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    u[k][e] = w[2 * e], v[k][e] = w[2 * e + 1];
+            } else {
+                load<E, N>(p, n, u[k]);
+                load<E, N>(p + to, n, v[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < HEADS; ++k) {
+            const int h = h0 + k * a.groups.d;
+            if (h >= a.H)
+                break;
+            char *const o = y + h * a.y_sh + at;
+            float p[N], q[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                p[e] = u[k][e] * c[e] - v[k][e] * s[e];
+                q[e] = u[k][e] * s[e] + v[k][e] * c[e];
+            }
+            if constexpr (PAIRED) {
+                float w[W];
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    w[2 * e] = p[e], w[2 * e + 1] = q[e];
+                store<E, W>(o, 2 * n, w);
+            } else {
+                store<E, N>(o, n, p);
+                store<E, N>(o + to, n, q);
+            }
+        }
+    }
+}
+
+template <class E, bool PAIRED>
+void run(const RotaryArgs &a, const Turns &f, hipStream_t st)
+{
+    const uint32_t grid = (a.lanes + kThreads - 1) / kThreads;
+    const int each = (a.H + a.groups.d - 1) / a.groups.d;  // heads of a lane
+    if (each >= 4)
+        rotary<E, PAIRED, 4><<<grid, kThreads, 0, st>>>(a, f);
+    else
+        rotary<E, PAIRED, 1><<<grid, kThreads, 0, st>>>(a, f);
+}
+
+template <class E>
+void run_pairs(const RotaryArgs &a, const Turns &f, bool paired, hipStream_t st)
+{
+    paired ? run<E, true>(a, f, st) : run<E, false>(a, f, st);
+}
+
+}  // namespace
+
+bool plan_rotary(RotaryArgs &a, int64_t B, int64_t L, bool paired, bool in_place, int dt)
+{
+    const int64_t e = dt == IM2WIN_F32 ? 4 : 2, N = (paired ? 8 : 16) / e, W = paired ? 2 * N : N;
+    a.pair_units = (int32_t)((a.rot / 2 + N - 1) / N);
+    const int64_t units = a.pair_units + (in_place ? 0 : (a.D - a.rot + W - 1) / W);
+    if (B * L * units > UINT32_MAX)  // so that the products below fit
+        return false;
+    // Heads a lane: 4 where that leaves 2^17 lanes or more (512 a CU).
+    const int64_t one = B * L * units * a.H;
+    int64_t groups = a.H;
+    if (one >= (int64_t)1 << 19)
+        groups = (a.H + 3) / 4;
+    const int64_t lanes = B * L * units * groups;
+    if (lanes > UINT32_MAX - kThreads)
+        return false;
+    a.lanes = (uint32_t)lanes;
+    a.units = make_fastdiv((uint32_t)units);
+    a.groups = make_fastdiv((uint32_t)groups);
+    a.len = make_fastdiv((uint32_t)L);
+    return true;
+}
+
+hipError_t launch_rotary(const RotaryArgs &a, const Turns &f, bool paired, int dt, hipStream_t st)
+{
+    if (dt == IM2WIN_F32)
+        run_pairs<EltF32>(a, f, paired, st);
+    else if (dt == IM2WIN_F16)
+        run_pairs<EltF16>(a, f, paired, st);
+    else
+        run_pairs<EltBF16>(a, f, paired, st);
+    return hipGetLastError();
+}
+
+}  // namespace im2win

@@ -73,7 +73,7 @@ def _elsewhere(stream, call, *args):
     with torch.cuda.stream(s):
         res = call(*args)
     for t in args:
-        if isinstance(t, torch.Tensor):
+        if isinstance(t, torch.Tensor) and t.is_cuda:
             t.record_stream(s)
     for t in res if isinstance(res, tuple) else (res,):
         if t is not None:

@@ -1,0 +1,297 @@
+"""Rotary positions, a paged key/value cache and attention over it, on AMD Instinct MI355X.
+
+The same kind of binding as ``seq.py`` over the same library (``include/im2win_seq.h``): no fallback, nothing recorded by
+autograd, ``stream`` as there.  Tensors on another device than the current one make the call run on that device.
+
+    freq = seq_rotary_frequencies(rot, base=10000.0, factor=8.0, trained=4096)    # host fp64 [rot/2], kept by the caller
+    y = seq_rotary_forward(x, freq, positions)                                    # x [B][L][H][D]
+    dx = seq_rotary_backward(dy, freq, positions)
+    seq_cache_write(k, v, k_pages, v_pages, table, start, count)                  # pages [pages][page][Hkv][D]
+    k, v = seq_cache_read(k_pages, v_pages, table, length, L)                     # [B][L][Hkv][D]
+    out, lse = seq_paged_attention_forward(q, k_pages, v_pages, table, length)    # q [B][H][D]
+
+Pages hold the type of the keys, or ``torch.int8`` / ``torch.float8_e4m3fn`` codes beside fp32 scales
+[pages][page][Hkv] (``k_scale``, ``v_scale``).
+"""
+from __future__ import annotations
+
+import ctypes
+import struct
+
+from . import _check, _dtype_code, _i64, _nbytes, _stream, _vp, Im2winError
+from .seq import _elsewhere, _ints, _library as _seq_library, _like, _same_device, _strides
+
+__all__ = ["seq_rotary_frequencies", "seq_rotary_forward", "seq_rotary_backward", "seq_cache_write", "seq_cache_read",
+           "seq_paged_attention_workspace_bytes", "seq_paged_attention_forward"]
+
+_int = ctypes.c_int
+# seq_rotary_t: dt, interleaved, by_token, amplitude; B, L, H, D, rot; strides of x, y; positions, freq
+_ROTARY = struct.Struct("@3if11q2P")
+# seq_cache_t: dt; B, pages, page, max_pages, Hkv, D; strides of k, v, their scales; table's; k, v, scales, table
+_CACHE = struct.Struct("@i4x19q5P")
+# seq_paged_attention_t: dt, scale, cap; H; strides of q, out; R, strip, len
+_PAGED = struct.Struct("@i2f4x6q2P")
+_TRIPLE = struct.Struct("@3q")
+_NO_SCALES = (0, 0, 0)
+
+_lib = None
+_codes = None
+
+
+def _library():
+    global _lib
+    if _lib is None:
+        lib = _seq_library()
+        text = ctypes.c_char_p
+        lib.seq_rotary_forward.restype = lib.seq_rotary_backward.restype = _int
+        lib.seq_rotary_forward.argtypes = lib.seq_rotary_backward.argtypes = [text, _vp, _vp, _vp]
+        lib.seq_rotary_frequencies.restype = _int
+        lib.seq_rotary_frequencies.argtypes = [_vp, _i64] + [ctypes.c_double] * 5
+        lib.seq_cache_write.restype = lib.seq_cache_read.restype = _int
+        lib.seq_cache_write.argtypes = [text, _vp, _vp, text, text, _i64, _int, _vp, _vp, _vp]
+        lib.seq_cache_read.argtypes = [text, _vp, _vp, text, text, _i64, _int, _vp, _vp]
+        lib.seq_paged_attention_workspace_bytes.restype = _i64
+        lib.seq_paged_attention_workspace_bytes.argtypes = [text, _i64, _int]
+        lib.seq_paged_attention_forward.restype = _int
+        lib.seq_paged_attention_forward.argtypes = [text, text, _vp, _vp, _vp, _vp, _i64, _vp]
+        _lib = lib
+    return _lib
+
+
+def _away(t):
+    """Whether ``t`` lies on another GPU than the current one."""
+    import torch
+    at = t.get_device()
+    return at >= 0 and at != torch.cuda.current_device()
+
+
+def _over_there(t, call, *args):
+    import torch
+    with torch.cuda.device(t.device):
+        return call(*args)
+
+
+def seq_rotary_frequencies(rot: int, base: float = 10000.0, factor: float = 1.0, trained: float = 0.0, low: float = 1.0,
+                           high: float = 32.0):
+    """Frequencies [rot/2] (host, fp64) of pairs of channels: base ** (-2i/rot),
+    for contexts ``factor`` times as long as the ``trained`` one slowed down by
+    ``factor`` where a pair turns at most ``low`` times within it, kept where it
+    turns at least ``high`` times, on a straight line between; trained 0: all
+    slowed down."""
+    import torch
+    freq = torch.empty(rot // 2 if rot > 1 else 1, dtype=torch.float64)
+    _check(_library().seq_rotary_frequencies(freq.data_ptr(), rot, base, factor, trained, low, high),
+           "seq_rotary_frequencies")
+    return freq
+
+
+def _rotary(call, what, x, freq, positions, interleaved, amplitude, out):
+    import torch
+    xs = x.shape
+    st = _strides(x, "x")
+    B, L, H, D = xs
+    if freq.dim() != 1 or freq.dtype != torch.float64 or freq.is_cuda or not freq.is_contiguous():
+        raise ValueError("freq must be a contiguous fp64 [rot/2] tensor in host memory")
+    if out is None:
+        out = torch.empty(xs, dtype=x.dtype, device=x.device)
+        so = (L * H * D, H * D, D)
+    else:
+        _like(out, xs, x.dtype, "out")
+        _same_device(x, out)
+        so = _strides(out, "out")
+    pos = by_token = 0
+    if positions is not None:
+        by_token = 1 if positions.dim() == 2 else 0
+        pos = _ints("positions", positions, (B, L) if by_token else (B,), x.device)
+    a = _ROTARY.pack(_dtype_code(x.dtype), 1 if interleaved else 0, by_token, amplitude, B, L, H, D, 2 * freq.shape[0],
+                     *st, *so, pos, freq.data_ptr())
+    _check(call(a, x.data_ptr(), out.data_ptr(), _stream(None)), what)
+    return out
+
+
+def seq_rotary_forward(x, freq, positions=None, interleaved: bool = False, amplitude: float = 1.0, out=None, stream=None):
+    """Turns the pairs of the first ``2 * len(freq)`` channels of each head of
+    ``x`` [B][L][H][D] (any strides, the last dimension dense) by the angles
+    position * freq; the other channels are copied.
+
+    positions    int32 [B][L], or [B] of each sequence's first token; None: 0, 1, ..
+    interleaved  pairs are channels (2i, 2i+1), else (i, i + rot/2)
+    amplitude    factor of the turned channels
+    out          like ``x``, any strides; may be ``x``
+    """
+    if stream is not None:
+        return _elsewhere(stream, seq_rotary_forward, x, freq, positions, interleaved, amplitude, out)
+    if _away(x):
+        return _over_there(x, seq_rotary_forward, x, freq, positions, interleaved, amplitude, out)
+    return _rotary(_library().seq_rotary_forward, "seq_rotary_forward", x, freq, positions, interleaved, amplitude, out)
+
+
+def seq_rotary_backward(dy, freq, positions=None, interleaved: bool = False, amplitude: float = 1.0, out=None, stream=None):
+    """The gradient of ``seq_rotary_forward``'s input from that of its result."""
+    if stream is not None:
+        return _elsewhere(stream, seq_rotary_backward, dy, freq, positions, interleaved, amplitude, out)
+    if _away(dy):
+        return _over_there(dy, seq_rotary_backward, dy, freq, positions, interleaved, amplitude, out)
+    return _rotary(_library().seq_rotary_backward, "seq_rotary_backward", dy, freq, positions, interleaved, amplitude, out)
+
+
+def _cache_code(dtype) -> int:
+    global _codes
+    if _codes is None:
+        import torch
+        _codes = {torch.int8: 16, torch.float8_e4m3fn: 17}
+    code = _codes.get(dtype)
+    return _dtype_code(dtype) if code is None else code
+
+
+def _cache(k, v, table, k_scale, v_scale):
+    """The packed description of a cache, its element code and [page][Hkv][D]."""
+    ks = k.shape
+    sk, sv = _strides(k, "k_pages"), _strides(v, "v_pages")
+    if v.shape != ks or v.dtype != k.dtype:
+        raise ValueError("k_pages and v_pages must have one shape [pages][page][Hkv][D] and one type")
+    pages, page, Hkv, D = ks
+    code = _cache_code(k.dtype)
+    import torch
+    if table.dim() != 2 or table.dtype != torch.int32 or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("table must be an int32 [B][max_pages] tensor, dense in its last dimension")
+    B, most = table.shape
+    device = k.device
+    if v.device != device or table.device != device:
+        raise ValueError("all tensors must be on %s" % device)
+    if code < 16:
+        if k_scale is not None or v_scale is not None:
+            raise ValueError("k_scale and v_scale go with 8-bit pages")
+        s = _CACHE.pack(code, B, pages, page, most, Hkv, D, *sk, *sv, 0, 0, 0, 0, 0, 0, table.stride(0) if B > 1 else most,
+                        k.data_ptr(), v.data_ptr(), 0, 0, table.data_ptr())
+        return s, code, B, ks
+    if k_scale is None or v_scale is None:
+        raise ValueError("8-bit pages need k_scale and v_scale")
+    for t in (k_scale, v_scale):
+        if t.shape != ks[:3] or t.dtype != torch.float32:
+            raise ValueError("k_scale and v_scale must be fp32 [pages][page][Hkv]")
+        if t.device != device:
+            raise ValueError("all tensors must be on %s" % device)
+    s = _CACHE.pack(code, B, pages, page, most, Hkv, D, *sk, *sv, *k_scale.stride(), *v_scale.stride(),
+                    table.stride(0) if B > 1 else most, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                    table.data_ptr())
+    return s, code, B, ks
+
+
+def seq_cache_write(k, v, k_pages, v_pages, table, start=None, count=None, k_scale=None, v_scale=None, stream=None):
+    """Writes the tokens k, v [B][L][Hkv][D] (any strides, the last dimension
+    dense) into the pages: token t < count[b] of sequence b becomes its token
+    start[b] + t.
+
+    k_pages, v_pages  [pages][page][Hkv][D], any strides with a dense last dimension
+    table    int32 [B][max_pages]: each sequence's pages in order; entries that name no page take nothing
+    start    int32 [B], None: 0;  count  int32 [B], None: all L
+    k_scale, v_scale  fp32 [pages][page][Hkv], written with 8-bit pages
+    """
+    if stream is not None:
+        return _elsewhere(stream, seq_cache_write, k, v, k_pages, v_pages, table, start, count, k_scale, v_scale)
+    if _away(k):
+        return _over_there(k, seq_cache_write, k, v, k_pages, v_pages, table, start, count, k_scale, v_scale)
+    c, code, B, ps = _cache(k_pages, v_pages, table, k_scale, v_scale)
+    sk, sv = _strides(k, "k"), _strides(v, "v")
+    L = k.shape[1]
+    if k.shape != (B, L, ps[2], ps[3]) or v.shape != k.shape:
+        raise ValueError("k and v must be [B][L][Hkv][D], as the table and the pages have it")
+    if v.dtype != k.dtype or (code < 16 and k.dtype != k_pages.dtype):
+        raise TypeError("k and v must have one type, that of the pages unless those are 8-bit")
+    _same_device(k_pages, k, v)
+    first = 0 if start is None else _ints("start", start, (B,), k.device)
+    n = 0 if count is None else _ints("count", count, (B,), k.device)
+    _check(_library().seq_cache_write(c, k.data_ptr(), v.data_ptr(), _TRIPLE.pack(*sk), _TRIPLE.pack(*sv), L,
+                                      _dtype_code(k.dtype), first, n, _stream(None)), "seq_cache_write")
+
+
+def seq_cache_read(k_pages, v_pages, table, length, L: int, dtype=None, k_scale=None, v_scale=None, k=None, v=None,
+                   stream=None):
+    """The first length[b] tokens of each sequence as dense (k, v), each
+    [B][L][Hkv][D] of type ``dtype`` (that of the pages; fp32 for 8-bit ones),
+    written to ``k`` and ``v`` where given; rows from length[b] on are zeros."""
+    if stream is not None:
+        return _elsewhere(stream, seq_cache_read, k_pages, v_pages, table, length, L, dtype, k_scale, v_scale, k, v)
+    if _away(k_pages):
+        return _over_there(k_pages, seq_cache_read, k_pages, v_pages, table, length, L, dtype, k_scale, v_scale, k, v)
+    import torch
+    c, code, B, ps = _cache(k_pages, v_pages, table, k_scale, v_scale)
+    if dtype is None:
+        dtype = k_pages.dtype if code < 16 else torch.float32
+    if code < 16 and dtype != k_pages.dtype:
+        raise TypeError("dtype must be that of the pages unless those are 8-bit")
+    shape = (B, L, ps[2], ps[3])
+    k = torch.empty(shape, dtype=dtype, device=k_pages.device) if k is None else k
+    v = torch.empty(shape, dtype=dtype, device=k_pages.device) if v is None else v
+    _like(k, shape, dtype, "k")
+    _like(v, shape, dtype, "v")
+    _same_device(k_pages, k, v)
+    n = _ints("length", length, (B,), k_pages.device)
+    _check(_library().seq_cache_read(c, k.data_ptr(), v.data_ptr(), _TRIPLE.pack(*_strides(k, "k")),
+                                     _TRIPLE.pack(*_strides(v, "v")), L, _dtype_code(dtype), n, _stream(None)),
+           "seq_cache_read")
+    return k, v
+
+
+def _paged_ws(c, H, dt):
+    n = _library().seq_paged_attention_workspace_bytes(c, H, dt)
+    if n < 0:
+        raise Im2winError(int(n), "seq_paged_attention_workspace_bytes")
+    return int(n)
+
+
+def seq_paged_attention_workspace_bytes(q, k_pages, v_pages, table, k_scale=None, v_scale=None) -> int:
+    """Bytes of workspace of ``seq_paged_attention_forward`` with these operands."""
+    return _paged_ws(_cache(k_pages, v_pages, table, k_scale, v_scale)[0], q.shape[1], _dtype_code(q.dtype))
+
+
+def seq_paged_attention_forward(q, k_pages, v_pages, table, length, scale=None, cap: float = 0.0, bias=None, k_scale=None,
+                                v_scale=None, out=None, ws=None, stream=None):
+    """Attention of one new token of each sequence, q [B][H][D] (any strides,
+    the last dimension dense), the last of its length[b] tokens, over the pages.
+    Returns (out like q, lse [B][H] fp32); scale, cap and bias as in
+    ``seq_attention_forward``, pages and table as in ``seq_cache_write``."""
+    if stream is not None:
+        return _elsewhere(stream, seq_paged_attention_forward, q, k_pages, v_pages, table, length, scale, cap, bias,
+                          k_scale, v_scale, out, ws)
+    if _away(q):
+        return _over_there(q, seq_paged_attention_forward, q, k_pages, v_pages, table, length, scale, cap, bias, k_scale,
+                           v_scale, out, ws)
+    import torch
+    c, code, B, ps = _cache(k_pages, v_pages, table, k_scale, v_scale)
+    qs, device = q.shape, q.device
+    if len(qs) != 3 or qs[0] != B or qs[2] != ps[3]:
+        raise ValueError("q must be [B][H][D], as the table and the pages have it")
+    if code < 16 and q.dtype != k_pages.dtype:
+        raise TypeError("q must have the type of the pages unless those are 8-bit")
+    if q.stride(2) != 1 and qs[2] > 1:
+        raise ValueError("q must be dense in its last dimension")
+    H = qs[1]
+    if out is None:
+        out = torch.empty(qs, dtype=q.dtype, device=device)
+        so = (H * qs[2], qs[2])
+    else:
+        _like(out, qs, q.dtype, "out")
+        if out.stride(2) != 1 and qs[2] > 1:
+            raise ValueError("out must be dense in its last dimension")
+        so = out.stride()[:2]
+    _same_device(k_pages, q, out, ws)
+    n = _ints("length", length, (B,), device)
+    R = strip = 0
+    if bias is not None:
+        if bias.dim() != 2 or bias.shape[0] != H or bias.shape[1] % 2 == 0 or bias.shape[1] < 3 \
+                or bias.dtype != torch.float32 or not bias.is_contiguous():
+            raise ValueError("bias must be a contiguous fp32 [H][2R+1] strip")
+        _same_device(q, bias)
+        R, strip = bias.shape[1] // 2, bias.data_ptr()
+    dt = _dtype_code(q.dtype)
+    a = _PAGED.pack(dt, qs[2] ** -0.5 if scale is None else scale, cap, H, *q.stride()[:2], *so, R, strip, n)
+    lse = torch.empty((B, H), dtype=torch.float32, device=device)
+    if ws is None:
+        need = _paged_ws(c, H, dt)
+        ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    at, size = (None, 0) if ws is None else (ws.data_ptr(), _nbytes(ws))
+    _check(_library().seq_paged_attention_forward(c, a, q.data_ptr(), out.data_ptr(), lse.data_ptr(), at, size,
+                                                  _stream(None)), "seq_paged_attention_forward")
+    return out, lse
