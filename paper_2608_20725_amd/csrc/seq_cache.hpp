@@ -40,12 +40,13 @@ struct PagedArgs {
     const int32_t *len;
     const float *strip;  // [H][2R+1], or null
     int64_t q_sb, q_sh, o_sb, o_sh;  // bytes
-    int32_t B, H, G, R, splits, row_tiles;
+    int32_t B, H, G, R, row_tiles;
+    int32_t most_parts, parts;  // see Plan
     float scale, cap;
 };
 
 // Floats that the parts of one call take (0: no keys are split).
-int64_t paged_part_floats(const Pool &c, int64_t B, int64_t H, int dt);
+int64_t paged_part_floats(const Pool &c, int ct, int64_t B, int64_t H, int dt);
 hipError_t launch_paged(const Pool &c, int ct, PagedArgs a, int dt, hipStream_t st);
 
 // ---- numbers of 8 bits --------------------------------------------------------------------------------------------

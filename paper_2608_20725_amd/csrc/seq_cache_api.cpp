@@ -304,7 +304,7 @@ int64_t seq_paged_attention_workspace_bytes(const seq_cache_t *c, int64_t H, im2
     int rc;
     if ((rc = check_cache_dims(c)) || (rc = check_heads(c, H, dt)))
         return rc;
-    return pad256(paged_part_floats(make_pool(c, CacheOperands(c)), c->B, H, dt) * 4);
+    return pad256(paged_part_floats(make_pool(c, CacheOperands(c)), c->dt, c->B, H, dt) * 4);
 }
 
 int seq_paged_attention_forward(const seq_cache_t *c, const seq_paged_attention_t *a, const void *q, void *out,
@@ -358,7 +358,7 @@ int seq_paged_attention_forward(const seq_cache_t *c, const seq_paged_attention_
                 return IM2WIN_EOVERLAP;
     }
     const Pool p = make_pool(c, o);
-    const int64_t need = pad256(paged_part_floats(p, c->B, a->H, a->dt) * 4);
+    const int64_t need = pad256(paged_part_floats(p, c->dt, c->B, a->H, a->dt) * 4);
     if (need > 0 && (!ws || ws_bytes < need))
         return IM2WIN_EWORKSPACE;
     if ((rc = check_device()))

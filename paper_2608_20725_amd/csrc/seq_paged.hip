@@ -26,8 +26,6 @@
 namespace im2win {
 namespace {
 
-constexpr int kKeys = 32;   // keys of a tile
-constexpr int kUnit = 128;  // keys of a workgroup's step: a tile a wave
 constexpr int kWavesP = 4;
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
@@ -150,7 +148,7 @@ struct Math {
 
     // Channel 8*(lane & 15) + j of the lane's 8 keys: rows of the operand.
     template <int J>
-    __device__ static inline u32x4_t channel(const V (&v)[8])
+    __device__ static inline u32x4_t channel(const V *v)
     {
         u32x4_t w;
 #pragma unroll
@@ -174,68 +172,167 @@ struct Math {
     }
 
     // o[j] += channel j of the values times the weights w[nt] of NT tiles of queries.
-    template <int NT, int J = 0>
-    __device__ static inline void sum(f32x4_acc (&o)[NT][8], const V (&v)[8], const float (&p)[NT][8],
-                                      const u32x4_t (&packed)[NT])
+    template <int NT, int N, int J = 0>
+    __device__ static inline void sum(f32x4_acc (&o)[NT][8], const V (&v)[N], const float (&p)[NT][N],
+                                      const u32x4_t (&packed)[NT][N / 8])
     {
         if constexpr (kWide) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < N; ++i) {
                 const float x = value<J>(v[i]);
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
                     o[t][J] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, p[t][i], o[t][J], 0, 0, 0);
             }
         } else {
-            const auto x = __builtin_bit_cast(typename Op::v8, channel<J>(v));
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-                o[t][J] = Op::mfma16(x, __builtin_bit_cast(typename Op::v8, packed[t]), o[t][J]);
+            for (int i = 0; i < N / 8; ++i) {
+                const auto x = __builtin_bit_cast(typename Op::v8, channel<J>(v + 8 * i));
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                    o[t][J] = Op::mfma16(x, __builtin_bit_cast(typename Op::v8, packed[t][i]), o[t][J]);
+            }
         }
         if constexpr (J < 7)
-            sum<NT, J + 1>(o, v, p, packed);
+            sum<NT, N, J + 1>(o, v, p, packed);
     }
 };
 
 // What the lanes of a wave tell each other of a tile: where its keys and values
 // lie (bytes from the head's first), and 8-bit pages' scales.
+template <int KEYS>
 struct Where {
-    int64_t k[kKeys], v[kKeys];
-    float ks[kKeys], vs[kKeys];
+    int64_t k[KEYS], v[KEYS];
+    float ks[KEYS], vs[KEYS];
 };
 
-// Part of a row: its output sums, maximum and sum.
-__device__ inline float *part_of(const PagedArgs &a, int split, int row, int rows, int D)
+// ---- how the keys are split ----
+// All workgroups take about the same number of keys, whichever sequence they
+// belong to: with a share of total/kTarget keys (whole steps), a sequence of n
+// keys makes ceil(n/share) parts of equal size.  The lengths are known on the
+// GPU only, so each wave adds them up and finds its part by a scan over the
+// sequences' counts.
+struct Cut {
+    int32_t parts, piece;  // parts of a sequence, keys of each (the last has what is left)
+};
+__device__ inline Cut cut_of(int32_t n, int32_t share, int32_t unit)
 {
-    return a.part + ((int64_t)split * rows + row) * part_floats(D);
+    Cut c = {0, unit};
+    if (n > 0) {
+        const int32_t p = (n - 1) / share + 1;
+        c.piece = (int32_t)(((uint32_t)(n + p - 1) / (uint32_t)p + unit - 1) / unit * unit);
+        c.parts = (n - 1) / c.piece + 1;
+    }
+    return c;
 }
 
-// Keys of a split: an even share of the sequence, in whole steps.
-__device__ inline int share_of(int n, int splits)
+__device__ inline int32_t tokens_of(const Pool &c, const PagedArgs &a, int b)
 {
-    return ((n + splits - 1) / splits + kUnit - 1) / kUnit * kUnit;
+    return b < a.B && c.pages > 0 ? held_tokens(a.len[b], c.max_pages, c.page.d) : 0;
 }
 
-template <class E, class Op, class Code, int NT, int DP>
+__device__ inline int32_t share_of(const Pool &c, const PagedArgs &a, int32_t unit, int lane)
+{
+    int64_t total = 0;
+    for (int b = lane; b < a.B; b += 64)
+        total += tokens_of(c, a, b);
+    for (int m = 1; m < min(a.B, 64); m <<= 1)  // lanes from B on hold zeros
+        total += __shfl_xor((long long)total, m);
+    total = (int64_t)__builtin_amdgcn_readfirstlane((int)(total >> 32)) << 32 |
+            (uint32_t)__builtin_amdgcn_readfirstlane((int)total);
+    const int64_t share = total <= a.most_parts ? 1 : (total - 1) / a.most_parts + 1;
+    // no sequence is longer than 2^30
+    return ((share < 1 << 30 ? (int32_t)share : 1 << 30) + unit - 1) / unit * unit;
+}
+
+// Parts of the 64 sequences from `base` on: the lane's cut, its tokens, the
+// parts up to it and of all.
+struct Scan {
+    Cut cut;
+    int32_t n, upto, all;
+};
+__device__ inline Scan scan_parts(const Pool &c, const PagedArgs &a, int base, int32_t share, int32_t unit, int lane)
+{
+    Scan s;
+    s.n = tokens_of(c, a, base + lane);
+    s.cut = cut_of(s.n, share, unit);
+    s.upto = s.cut.parts;
+    for (int m = 1; m < min(a.B, 64); m <<= 1) {
+        const int32_t below = __shfl_up(s.upto, m);
+        s.upto += lane >= m ? below : 0;
+    }
+    s.all = __builtin_amdgcn_readlane(s.upto, min(a.B, 64) - 1);  // of fewer sequences, lanes beyond them were not added to
+    return s;
+}
+
+// Part `index` of all sequences' parts in order: keys lo .. hi - 1 of sequence
+// b of n keys.  b < 0: there is none.
+struct Part {
+    int32_t b, n, lo, hi;
+    bool alone;  // the only part of its sequence
+};
+__device__ inline Part find_part(const Pool &c, const PagedArgs &a, int32_t index, int32_t unit, int lane)
+{
+    Part p = {-1, 0, 0, 0, false};
+    const int32_t share = share_of(c, a, unit, lane);
+    for (int base = 0; base < a.B; base += 64) {
+        const Scan s = scan_parts(c, a, base, share, unit, lane);
+        if (index >= s.all) {
+            index -= s.all;
+            continue;
+        }
+        const int l = __builtin_ctzll(__ballot(s.upto > index));
+        const int32_t parts = __builtin_amdgcn_readlane(s.cut.parts, l), piece = __builtin_amdgcn_readlane(s.cut.piece, l);
+        p.b = base + l;
+        p.n = __builtin_amdgcn_readlane(s.n, l);
+        p.lo = (index - (__builtin_amdgcn_readlane(s.upto, l) - parts)) * piece;
+        p.hi = min(p.n, p.lo + piece);
+        p.alone = parts == 1;
+        break;
+    }
+    return p;
+}
+
+// Sums, maximum and sum of the exponentials of row `head` in part `index`.
+__device__ inline float *part_of(const PagedArgs &a, int64_t index, int head, int D)
+{
+    return a.part + (index * a.H + head) * part_floats(D);
+}
+
+// Keys of a wave's tile.  8-bit pages take half the registers, and twice the keys
+// keep as many bytes on their way: 48 caches of up to 16384 tokens, 64 heads of
+// 128 over 8, int8 under bf16: 362 us with tiles of 32 keys, 245 with 64.
+template <class Op, class Code, int NT>
+constexpr int keys_of_tile() { return !__is_same(Code, void) && !__is_same(Op, F32Wide) && NT == 1 ? 64 : 32; }
+
+// FULL: heads have DP channels, no more tests of where they end.
+template <class E, class Op, class Code, int NT, int DP, bool FULL>
 __global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
 {
+    constexpr int KEYS = keys_of_tile<Op, Code, NT>(), N = KEYS / 4, kUnit = kWavesP * KEYS;
+    const int D = FULL ? DP : c.D;
     typedef Math<Op, Code, DP> M;
     constexpr bool kHalf = __is_same(Op, F16Op);
     // fp16 probabilities are times 2^14, so that those of long rows stay normal numbers
     constexpr float kShift = kHalf ? 14.0f : 0.0f, kUnshift = kHalf ? 0x1p-14f : 1.0f;
-    __shared__ __align__(16) Where where[kWavesP];
+    __shared__ __align__(16) Where<KEYS> where[kWavesP];
     __shared__ float box[kWavesP][16][DP + 4];
     __shared__ float sm[kWavesP][NT][16], sl[kWavesP][NT][16];
 
-    const int heads = a.B * c.Hkv;
-    const int bh = blockIdx.x % heads, rest = blockIdx.x / heads, rt = rest % a.row_tiles, split = rest / a.row_tiles;
-    const int b = bh / c.Hkv, hk = bh - b * c.Hkv;
+    // blockIdx: heads fastest (neighbours in memory), then row tiles, then parts
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n = c.pages > 0 ? held_tokens(a.len[b], c.max_pages, c.page.d) : 0;
-    const int share = share_of(n, a.splits), lo = split * share, hi = min(n, lo + share);
-    if (lo >= hi && split > 0)
-        return;
+    const int hk = blockIdx.x % c.Hkv, rest = blockIdx.x / c.Hkv, rt = rest % a.row_tiles, index = rest / a.row_tiles;
+    Part part;
+    if (a.most_parts) {
+        part = find_part(c, a, index, kUnit, lane);
+        if (part.b < 0)
+            return;
+    } else {
+        const int n = tokens_of(c, a, index);
+        part = Part{index, n, 0, n, true};
+    }
+    const int b = part.b, n = part.n, lo = part.lo, hi = part.hi;
 
     // this lane's queries: column r of each tile
     const int row0 = rt * (16 * NT);
@@ -254,7 +351,7 @@ __global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
                 typedef typename E::T V4 __attribute__((ext_vector_type(4)));
                 const int ch = (4 * k + g) * M::EPC + e;
                 V4 v = {};
-                if (row < a.G && ch < c.D)
+                if (row < a.G && ch < D)
                     v = *(const V4 *)(p + ch);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -279,37 +376,38 @@ __global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
 
     const char *const kp = c.k + hk * c.k_head, *const vp = c.v + hk * c.v_head;
     const int32_t *const table = c.table + b * c.table_stride;
-    Where &my = where[wave];
+    Where<KEYS> &my = where[wave];
 
-    // A lane is the owner of key (lane & 31) of each tile.
+    // A lane is the owner of key lane % KEYS of each tile.
     auto page_at = [&](int k0) {
-        const int key = k0 + (lane & 31);
+        const int key = k0 + (lane & (KEYS - 1));
         return key < hi ? page_of(table, fdiv((uint32_t)key, c.page), c.max_pages, c.pages) : -1;
     };
     auto inside = [&](int k0) {
-        const uint32_t key = k0 + (lane & 31);
+        const uint32_t key = k0 + (lane & (KEYS - 1));
         return (int)(key - fdiv(key, c.page) * c.page.d);
     };
     auto k_scale = [&](int id, int in) { return id < 0 ? 0.0f : *(const float *)(c.ks + hk * c.ks_head + id * c.ks_page + in * c.ks_tok); };
     auto v_scale = [&](int id, int in) { return id < 0 ? 0.0f : *(const float *)(c.vs + hk * c.vs_head + id * c.vs_page + in * c.vs_tok); };
     // Keys that are not there read page 0 and are left out of what follows.
     auto tell = [&](int id, int in) {
-        if (lane < kKeys)
-            my.k[lane] = id < 0 ? 0 : id * c.k_page + in * c.k_tok;
-        else
-            my.v[lane & 31] = id < 0 ? 0 : id * c.v_page + in * c.v_tok;
+        if (KEYS == 64 || lane < KEYS)
+            my.k[lane & (KEYS - 1)] = id < 0 ? 0 : id * c.k_page + in * c.k_tok;
+        if (KEYS == 64 || lane >= KEYS)
+            my.v[lane & (KEYS - 1)] = id < 0 ? 0 : id * c.v_page + in * c.v_tok;
     };
-    u32x4_t kr[2][M::NK];
-    typename M::V vr[8];
+    u32x4_t kr[KEYS / 16][M::NK];
+    typename M::V vr[N];
     auto load_keys = [&]() {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
+        for (int s = 0; s < KEYS / 16; ++s) {
             const char *const p = kp + my.k[16 * s + r] + 16 * g;
 #pragma unroll
             for (int k = 0; k < M::NK; ++k) {
-                const int left = c.D * M::ES - (64 * k + 16 * g);  // a multiple of 8
-                kr[s][k] = u32x4_t{0, 0, 0, 0};
-                if (left >= 16) {
+                const int left = D * M::ES - (64 * k + 16 * g);  // a multiple of 8
+                if (!FULL)
+                    kr[s][k] = u32x4_t{0, 0, 0, 0};
+                if (FULL || left >= 16) {
                     kr[s][k] = *(const u32x4_a8 *)(p + 64 * k);
                 } else if (M::ES == 1 && left > 0) {
                     const u32x2_t w = *(const u32x2_t *)(p + 64 * k);
@@ -320,9 +418,9 @@ __global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
     };
     auto load_values = [&]() {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < N; ++i) {
             const char *const p = vp + my.v[16 * (i >> 2) + 4 * g + (i & 3)] + 8 * r * M::ES;
-            if (8 * r < c.D)
+            if (FULL && DP == 128 || 8 * r < D)
                 vr[i] = *(const typename M::V *)p;
             else
                 vr[i] = typename M::V{};
@@ -340,7 +438,7 @@ __global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
     }
     float unit = 0x1p-126f;  // 8 bits, fp16: the values' scales are over this power of two
 
-    const int first = lo + wave * kKeys;
+    const int first = lo + wave * KEYS;
     int id = page_at(first), in = inside(first);
     float ks = 0, vs = 0;
     if (first < hi) {
@@ -354,25 +452,25 @@ __global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
     int id1 = page_at(first + kUnit), in1 = inside(first + kUnit);
     for (int k0 = first; k0 < hi; k0 += kUnit) {
         // scores of the tile; a lane's keys are 16*(i >> 2) + 4*g + (i & 3)
-        float s[NT][8];
+        float s[NT][N];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < KEYS / 16; ++h) {
                 const f32x4_acc x = M::dot(kr[h], q[t]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     s[t][4 * h + i] = x[i];
             }
-        const uint32_t there = (uint32_t)__ballot(id >= 0);  // a bit a key (lanes 0 .. 31)
-        float kscale[8], vscale[8];
+        const uint64_t there = __ballot(id >= 0);  // a bit a key
+        float kscale[N], vscale[N];
         wave_lds_handoff();
         if constexpr (M::kCodes) {
-            my.ks[lane & 31] = ks;
-            my.vs[lane & 31] = vs;
+            my.ks[lane & (KEYS - 1)] = ks;
+            my.vs[lane & (KEYS - 1)] = vs;
             wave_lds_handoff();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < N; ++i) {
                 kscale[i] = my.ks[16 * (i >> 2) + 4 * g + (i & 3)];
                 vscale[i] = my.vs[16 * (i >> 2) + 4 * g + (i & 3)];
             }
@@ -390,11 +488,11 @@ __global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
         }
 
         // softmax
-        float p[NT][8], up = 1.0f, over = 1.0f;
+        float p[NT][N], up = 1.0f, over = 1.0f;
         if constexpr (M::kCodes && kHalf) {
             float top = unit;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < N; ++i)
                 top = fmaxf(top, vscale[i]);
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
@@ -405,13 +503,13 @@ __global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
             up = unit * over;
             unit = now;
         }
-        u32x4_t packed[NT];
+        u32x4_t packed[NT][N / 8];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const float *const strip = a.strip + (int64_t)min(hk * a.G + row0 + 16 * t + r, a.H - 1) * (2 * a.R + 1) + a.R;
             float top = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < N; ++i) {
                 const int at = 16 * (i >> 2) + 4 * g + (i & 3);
                 float x = s[t][i] * c1[t];
                 if constexpr (M::kCodes)
@@ -433,7 +531,7 @@ __global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
             m[t] = now;
             float sum = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < N; ++i) {
                 p[t][i] = __builtin_amdgcn_exp2f(s[t][i] - base + kShift);
                 sum += p[t][i];
                 if constexpr (M::kCodes)
@@ -448,19 +546,19 @@ __global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
             }
             if constexpr (!M::kWide) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    packed[t][i] = Op::bits(p[t][2 * i]) | Op::bits(p[t][2 * i + 1]) << 16;
+                for (int i = 0; i < N / 2; ++i)
+                    packed[t][i / 4][i % 4] = Op::bits(p[t][2 * i]) | Op::bits(p[t][2 * i + 1]) << 16;
             }
         }
-        if (there != 0xFFFFFFFFu) {
+        if ((KEYS == 64 ? ~there : (uint32_t)~there) != 0) {
             // what was read for keys that are not there: their weights are zero,
             // and so must be the values
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < N; ++i)
                 if (!((there >> (16 * (i >> 2) + 4 * g + (i & 3))) & 1))
                     vr[i] = typename M::V{};
         }
-        M::template sum<NT>(o, vr, p, packed);
+        M::template sum<NT, N>(o, vr, p, packed);
         if (more)
             load_values();
     }
@@ -512,18 +610,17 @@ __global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         v[e] += box[w][rr][ch + e];
-            const int out_row = b * a.H + hk * a.G + row;
-            if (a.splits > 1) {
-                float *const part = part_of(a, split, out_row, a.B * a.H, c.D);
-                if (ch < c.D)
-                    *(f32x8_a16 *)(part + ch) = v;
+            if (!part.alone) {
+                float *const to = part_of(a, index, hk * a.G + row, D);
+                if (ch < D)
+                    *(f32x8_a16 *)(to + ch) = v;
                 if (ch == 0) {
-                    part[c.D] = ms;
-                    part[c.D + 1] = sum;
+                    to[D] = ms;
+                    to[D + 1] = sum;
                 }
             } else {
                 const bool none = sum == 0.0f;  // not ms == -inf: all scores may be NaN
-                if (ch < c.D) {
+                if (ch < D) {
                     typedef typename E::T V8 __attribute__((ext_vector_type(8)));
                     V8 y;
 #pragma unroll
@@ -532,16 +629,16 @@ __global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
                     *(V8 *)(a.out + b * a.o_sb + (hk * a.G + row) * a.o_sh + ch * sizeof(typename E::T)) = y;
                 }
                 if (ch == 0)
-                    a.lse[out_row] = none ? -INFINITY : (ms + __log2f(sum * kUnshift)) * kLn2;
+                    a.lse[b * a.H + hk * a.G + row] = none ? -INFINITY : (ms + __log2f(sum * kUnshift)) * kLn2;
             }
         }
     }
 }
 
 // Joins the parts of a row: 32 lanes hold its channels, four each, and `groups`
-// of them (1 or 8) take its parts in turn.
+// of them (1 or 8) take its parts in turn.  Rows of one part are done already.
 template <class E, bool HALF>
-__global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int groups)
+__global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int groups, int unit)
 {
     typedef float v4 __attribute__((ext_vector_type(4)));
     __shared__ v4 sv[8][32];
@@ -550,11 +647,24 @@ __global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int group
     const int rows = a.B * a.H, lane = threadIdx.x & 31, d = lane * 4, group = threadIdx.x >> 5, first = group % groups;
     const int row = blockIdx.x * (8 / groups) + group / groups, live = row < rows;
     const int b = live ? row / a.H : 0, h = live ? row - b * a.H : 0;
-    const int n = c.pages > 0 && live ? held_tokens(a.len[b], c.max_pages, c.page.d) : 0;
-    const int share = share_of(n, a.splits), parts = n ? (n + share - 1) / share : 0;
+    // the first part of sequence b (the two rows of a wave may be of two)
+    const int wlane = threadIdx.x & 63;
+    const int32_t share = share_of(c, a, unit, wlane);
+    int64_t at = 0;
+    int parts = 0;
+    for (int base = 0; __any(base <= b); base += 64) {
+        const Scan s = scan_parts(c, a, base, share, unit, wlane);
+        const int l = b - base, upto = __shfl(s.upto, l & 63), here = __shfl(s.cut.parts, l & 63);
+        if (l >= 0 && l < 64)
+            at += upto - here, parts = here;
+        else if (l >= 64)
+            at += s.all;
+    }
+    if (groups > 1 ? parts == 1 : __all(parts == 1 || !live))  // groups > 1: one row a workgroup
+        return;
     float m = -INFINITY;
     for (int k = lane; k < parts; k += 32)
-        m = fmaxf(m, part_of(a, k, row, rows, c.D)[c.D]);
+        m = fmaxf(m, part_of(a, at + k, h, c.D)[c.D]);
 #pragma unroll
     for (int x = 16; x >= 1; x >>= 1)
         m = fmaxf(m, __shfl_xor(m, x));
@@ -563,7 +673,7 @@ __global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int group
     float l = 0;
 #pragma unroll 4
     for (int k = first; k < parts; k += groups) {
-        const float *const p = part_of(a, k, row, rows, c.D);
+        const float *const p = part_of(a, at + k, h, c.D);
         const float f = __builtin_amdgcn_exp2f(p[c.D] - base);
         l += f * p[c.D + 1];
         if (d < c.D)
@@ -581,7 +691,7 @@ __global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int group
             l += sl[k];
         }
     }
-    if (!live)
+    if (!live || parts == 1)
         return;
     const bool none = l == 0.0f;
     if (lane == 0)
@@ -600,28 +710,49 @@ __global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int group
 // where a key/value head has more queries than one holds (four; two in fp32,
 // whose operands take twice the registers).
 int tiles_of(int64_t G, int dt) { return G <= 16 ? 1 : dt == IM2WIN_F32 ? 2 : 4; }
-int64_t row_tiles_of(int64_t G, int dt) { return (G + 16 * tiles_of(G, dt) - 1) / (16 * tiles_of(G, dt)); }
 
-int64_t splits_of(const Pool &c, int64_t B, int64_t H, int dt)
+// Where no sequence can have two steps, and where there are enough of them to
+// even out by themselves, a workgroup takes a whole sequence (most_parts 0).
+struct Plan {
+    int64_t row_tiles, unit, most_parts, parts;  // parts: that the lengths can make at most
+};
+// Workgroups that share the keys, two rounds of the two that fit a CU.  Measured
+// with 512, 768, 1024, 1536 and 2048 (bf16, 8 heads of 128, H = 32): 32 caches of
+// 2048 to 8192 tokens 148, 131, 134, 133, 131 us, 32 of 8192 tokens 193, 220, 198,
+// 200, 203, four of them 26, 31, 28, 27, 33; int8, 32 of 8192: 129, 132, 130, 142,
+// 135.
+constexpr int64_t kTarget = 1024;
+Plan plan_of(const Pool &c, int ct, int64_t B, int64_t H, int dt)
 {
-    const int64_t row_tiles = row_tiles_of(H / c.Hkv, dt);
-    const int64_t groups = B * c.Hkv * row_tiles, most = ((int64_t)c.max_pages * c.page.d + kUnit - 1) / kUnit;
-    const int64_t want = groups > 0 ? (1024 + groups - 1) / groups : 1;
-    return want < most ? want : most > 1 ? most : 1;
+    Plan p;
+    const int64_t G = H / c.Hkv, tiles = tiles_of(G, dt);
+    p.row_tiles = (G + 16 * tiles - 1) / (16 * tiles);
+    p.unit = kWavesP * (ct != dt && dt != IM2WIN_F32 && tiles == 1 ? 64 : 32);
+    const int64_t heads = c.Hkv * p.row_tiles, steps = ((int64_t)c.max_pages * c.page.d + p.unit - 1) / p.unit;
+    p.most_parts = steps <= 1 || B * heads >= 16 * kTarget ? 0 : (kTarget + heads - 1) / heads;
+    p.parts = p.most_parts ? (p.most_parts + B < B * steps ? p.most_parts + B : B * steps) : B;
+    return p;
+}
+
+template <class E, class Op, class Code, int NT, int DP>
+void run_full(uint32_t grid, const Pool &c, const PagedArgs &a, hipStream_t st)
+{
+    if (c.D == DP)
+        paged_attn<E, Op, Code, NT, DP, true><<<grid, 64 * kWavesP, 0, st>>>(c, a);
+    else
+        paged_attn<E, Op, Code, NT, DP, false><<<grid, 64 * kWavesP, 0, st>>>(c, a);
 }
 
 template <class E, class Op, class Code, int NT>
 void run(const Pool &c, const PagedArgs &a, hipStream_t st)
 {
-    const uint32_t grid = (uint32_t)(a.B * c.Hkv) * a.row_tiles * a.splits;
-    if (c.D <= 64)
-        paged_attn<E, Op, Code, NT, 64><<<grid, 64 * kWavesP, 0, st>>>(c, a);
-    else
-        paged_attn<E, Op, Code, NT, 128><<<grid, 64 * kWavesP, 0, st>>>(c, a);
-    if (a.splits > 1) {
+    const uint32_t grid = (uint32_t)(a.parts * c.Hkv) * a.row_tiles;
+    c.D <= 64 ? run_full<E, Op, Code, NT, 64>(grid, c, a, st) : run_full<E, Op, Code, NT, 128>(grid, c, a, st);
+    if (a.most_parts) {
         const int64_t rows = (int64_t)a.B * a.H;
-        const int groups = rows <= 2048 && a.splits >= 8 ? 8 : 1;
-        paged_join<E, __is_same(Op, F16Op)><<<(uint32_t)((rows * groups + 7) / 8), 256, 0, st>>>(c, a, groups);
+        const int groups = rows <= 2048 ? 8 : 1;
+        paged_join<E, __is_same(Op, F16Op)><<<(uint32_t)((rows * groups + 7) / 8), 256, 0, st>>>(
+            c, a, groups, kWavesP * keys_of_tile<Op, Code, NT>());
     }
 }
 
@@ -643,16 +774,16 @@ void run_code(const Pool &c, int ct, const PagedArgs &a, hipStream_t st)
 
 }  // namespace
 
-int64_t paged_part_floats(const Pool &c, int64_t B, int64_t H, int dt)
+int64_t paged_part_floats(const Pool &c, int ct, int64_t B, int64_t H, int dt)
 {
-    const int64_t s = splits_of(c, B, H, dt);
-    return s > 1 ? s * B * H * part_floats(c.D) : 0;
+    const Plan p = plan_of(c, ct, B, H, dt);
+    return p.most_parts ? p.parts * H * part_floats(c.D) : 0;
 }
 
 hipError_t launch_paged(const Pool &c, int ct, PagedArgs a, int dt, hipStream_t st)
 {
-    a.splits = (int32_t)splits_of(c, a.B, a.H, dt);
-    a.row_tiles = (int32_t)row_tiles_of(a.G, dt);
+    const Plan p = plan_of(c, ct, a.B, a.H, dt);
+    a.most_parts = (int32_t)p.most_parts, a.parts = (int32_t)p.parts, a.row_tiles = (int32_t)p.row_tiles;
     if (dt == IM2WIN_F32)
         run_code<EltF32, F32Wide, F32Wide>(c, ct, a, st);
     else if (dt == IM2WIN_F16)
