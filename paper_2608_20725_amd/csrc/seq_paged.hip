@@ -642,7 +642,7 @@ __global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int group
 {
     typedef float v4 __attribute__((ext_vector_type(4)));
     __shared__ v4 sv[8][32];
-    __shared__ float sl[8];
+    __shared__ float sl[8], sm[8];
     constexpr float kUnshift = HALF ? 0x1p-14f : 1.0f;
     const int rows = a.B * a.H, lane = threadIdx.x & 31, d = lane * 4, group = threadIdx.x >> 5, first = group % groups;
     const int row = blockIdx.x * (8 / groups) + group / groups, live = row < rows;
@@ -662,33 +662,38 @@ __global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int group
     }
     if (groups > 1 ? parts == 1 : __all(parts == 1 || !live))  // groups > 1: one row a workgroup
         return;
-    float m = -INFINITY;
-    for (int k = lane; k < parts; k += 32)
-        m = fmaxf(m, part_of(a, at + k, h, c.D)[c.D]);
-#pragma unroll
-    for (int x = 16; x >= 1; x >>= 1)
-        m = fmaxf(m, __shfl_xor(m, x));
-    const float base = m == -INFINITY ? 0.0f : m;
+    // running maximum, sum and outputs: a part's numbers are loaded at once
+    float m = -INFINITY, l = 0;
     v4 v = {0, 0, 0, 0};
-    float l = 0;
 #pragma unroll 4
     for (int k = first; k < parts; k += groups) {
         const float *const p = part_of(a, at + k, h, c.D);
-        const float f = __builtin_amdgcn_exp2f(p[c.D] - base);
-        l += f * p[c.D + 1];
-        if (d < c.D)
-            v += *(const v4 *)(p + d) * f;
+        const float pm = p[c.D], pl = p[c.D + 1];
+        const v4 pv = d < c.D ? *(const v4 *)(p + d) : v4{0, 0, 0, 0};
+        const float top = fmaxf(m, pm), base = top == -INFINITY ? 0.0f : top;
+        const float f = __builtin_amdgcn_exp2f(m - base), g = __builtin_amdgcn_exp2f(pm - base);
+        m = top;
+        l = l * f + pl * g;
+        v = v * f + pv * g;
     }
     if (groups > 1) {
         sv[group][lane] = v;
         if (lane == 0)
-            sl[group] = l;
+            sl[group] = l, sm[group] = m;
         __syncthreads();
         if (group)
             return;
+        float top = m;
+        for (int k = 1; k < 8; ++k)
+            top = fmaxf(top, sm[k]);
+        const float base = top == -INFINITY ? 0.0f : top, f = __builtin_amdgcn_exp2f(m - base);
+        v *= f;
+        l *= f;
+        m = top;
         for (int k = 1; k < 8; ++k) {
-            v += sv[k][lane];
-            l += sl[k];
+            const float g = __builtin_amdgcn_exp2f(sm[k] - base);
+            v += sv[k][lane] * g;
+            l += sl[k] * g;
         }
     }
     if (!live || parts == 1)

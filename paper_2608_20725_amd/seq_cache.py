@@ -19,7 +19,7 @@ import ctypes
 import struct
 
 from . import _check, _dtype_code, _i64, _nbytes, _stream, _vp, Im2winError
-from .seq import _elsewhere, _ints, _library as _seq_library, _like, _same_device, _strides
+from .seq import _elsewhere, _ints, _library as _seq_library, _like, _same_device
 
 __all__ = ["seq_rotary_frequencies", "seq_rotary_forward", "seq_rotary_backward", "seq_cache_write", "seq_cache_read",
            "seq_paged_attention_workspace_bytes", "seq_paged_attention_forward"]
@@ -58,11 +58,20 @@ def _library():
     return _lib
 
 
+_current = None
+
+
 def _away(t):
     """Whether ``t`` lies on another GPU than the current one."""
-    import torch
+    global _current
     at = t.get_device()
-    return at >= 0 and at != torch.cuda.current_device()
+    if at < 0:
+        return False
+    if _current is None:
+        import torch
+        torch.cuda.current_device()  # initialises
+        _current = torch._C._cuda_getDevice  # without the checks, half a microsecond a call
+    return at != _current()
 
 
 def _over_there(t, call, *args):
@@ -86,27 +95,36 @@ def seq_rotary_frequencies(rot: int, base: float = 10000.0, factor: float = 1.0,
 
 
 def _rotary(call, what, x, freq, positions, interleaved, amplitude, out):
-    import torch
-    xs = x.shape
-    st = _strides(x, "x")
+    xs, st, device, dtype = x.shape, x.stride(), x.device, x.dtype
+    if len(xs) != 4:
+        raise ValueError("x must have four dimensions")
     B, L, H, D = xs
-    if freq.dim() != 1 or freq.dtype != torch.float64 or freq.is_cuda or not freq.is_contiguous():
+    if st[3] != 1 and D > 1:
+        raise ValueError("x must be dense in its last dimension")
+    if freq.dim() != 1 or freq.dtype != _float64() or freq.is_cuda or not freq.is_contiguous():
         raise ValueError("freq must be a contiguous fp64 [rot/2] tensor in host memory")
     if out is None:
-        out = torch.empty(xs, dtype=x.dtype, device=x.device)
-        so = (L * H * D, H * D, D)
+        import torch
+        out = torch.empty_like(x)
     else:
-        _like(out, xs, x.dtype, "out")
+        _like(out, xs, dtype, "out")
         _same_device(x, out)
-        so = _strides(out, "out")
+    so = out.stride()
+    if so[3] != 1 and D > 1:
+        raise ValueError("out must be dense in its last dimension")
     pos = by_token = 0
     if positions is not None:
         by_token = 1 if positions.dim() == 2 else 0
-        pos = _ints("positions", positions, (B, L) if by_token else (B,), x.device)
-    a = _ROTARY.pack(_dtype_code(x.dtype), 1 if interleaved else 0, by_token, amplitude, B, L, H, D, 2 * freq.shape[0],
-                     *st, *so, pos, freq.data_ptr())
+        pos = _ints("positions", positions, (B, L) if by_token else (B,), device)
+    a = _ROTARY.pack(_code(dtype), 1 if interleaved else 0, by_token, amplitude, B, L, H, D, 2 * freq.shape[0], st[0], st[1],
+                     st[2], so[0], so[1], so[2], pos, freq.data_ptr())
     _check(call(a, x.data_ptr(), out.data_ptr(), _stream(None)), what)
     return out
+
+
+def _float64():
+    import torch
+    return torch.float64
 
 
 def seq_rotary_forward(x, freq, positions=None, interleaved: bool = False, amplitude: float = 1.0, out=None, stream=None):
@@ -135,47 +153,81 @@ def seq_rotary_backward(dy, freq, positions=None, interleaved: bool = False, amp
     return _rotary(_library().seq_rotary_backward, "seq_rotary_backward", dy, freq, positions, interleaved, amplitude, out)
 
 
-def _cache_code(dtype) -> int:
+def _code(dtype) -> int:
+    """The element code of a type, 8-bit ones (16 and 17) among them."""
     global _codes
     if _codes is None:
         import torch
-        _codes = {torch.int8: 16, torch.float8_e4m3fn: 17}
+        _codes = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.int8: 16, torch.float8_e4m3fn: 17}
     code = _codes.get(dtype)
     return _dtype_code(dtype) if code is None else code
 
 
 def _cache(k, v, table, k_scale, v_scale):
-    """The packed description of a cache, its element code and [page][Hkv][D]."""
-    ks = k.shape
-    sk, sv = _strides(k, "k_pages"), _strides(v, "v_pages")
-    if v.shape != ks or v.dtype != k.dtype:
+    """The packed description of a cache, its element code, device, B and the
+    pages' shape.  (Attributes are read once and compared inline: these few
+    microseconds are most of a small call.)"""
+    ks, sk, sv, ts, st = k.shape, k.stride(), v.stride(), table.shape, table.stride()
+    dtype, device = k.dtype, k.device
+    if len(ks) != 4 or v.shape != ks or v.dtype != dtype:
         raise ValueError("k_pages and v_pages must have one shape [pages][page][Hkv][D] and one type")
     pages, page, Hkv, D = ks
-    code = _cache_code(k.dtype)
-    import torch
-    if table.dim() != 2 or table.dtype != torch.int32 or (table.shape[1] > 1 and table.stride(1) != 1):
+    if (sk[3] != 1 or sv[3] != 1) and D > 1:
+        raise ValueError("k_pages and v_pages must be dense in their last dimension")
+    if len(ts) != 2 or table.dtype != _int32() or (ts[1] > 1 and st[1] != 1):
         raise ValueError("table must be an int32 [B][max_pages] tensor, dense in its last dimension")
-    B, most = table.shape
-    device = k.device
+    B, most = ts
     if v.device != device or table.device != device:
         raise ValueError("all tensors must be on %s" % device)
+    code = _code(dtype)
     if code < 16:
         if k_scale is not None or v_scale is not None:
             raise ValueError("k_scale and v_scale go with 8-bit pages")
-        s = _CACHE.pack(code, B, pages, page, most, Hkv, D, *sk, *sv, 0, 0, 0, 0, 0, 0, table.stride(0) if B > 1 else most,
-                        k.data_ptr(), v.data_ptr(), 0, 0, table.data_ptr())
-        return s, code, B, ks
+        return _CACHE.pack(code, B, pages, page, most, Hkv, D, sk[0], sk[1], sk[2], sv[0], sv[1], sv[2], 0, 0, 0, 0, 0, 0,
+                           st[0] if B > 1 else most, k.data_ptr(), v.data_ptr(), 0, 0, table.data_ptr()), code, device, B, ks
     if k_scale is None or v_scale is None:
         raise ValueError("8-bit pages need k_scale and v_scale")
-    for t in (k_scale, v_scale):
-        if t.shape != ks[:3] or t.dtype != torch.float32:
-            raise ValueError("k_scale and v_scale must be fp32 [pages][page][Hkv]")
-        if t.device != device:
-            raise ValueError("all tensors must be on %s" % device)
-    s = _CACHE.pack(code, B, pages, page, most, Hkv, D, *sk, *sv, *k_scale.stride(), *v_scale.stride(),
-                    table.stride(0) if B > 1 else most, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
-                    table.data_ptr())
-    return s, code, B, ks
+    shape, kind = ks[:3], _float32()
+    if k_scale.shape != shape or v_scale.shape != shape or k_scale.dtype != kind or v_scale.dtype != kind:
+        raise ValueError("k_scale and v_scale must be fp32 [pages][page][Hkv]")
+    if k_scale.device != device or v_scale.device != device:
+        raise ValueError("all tensors must be on %s" % device)
+    return _CACHE.pack(code, B, pages, page, most, Hkv, D, sk[0], sk[1], sk[2], sv[0], sv[1], sv[2], *k_scale.stride(),
+                       *v_scale.stride(), st[0] if B > 1 else most, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
+                       v_scale.data_ptr(), table.data_ptr()), code, device, B, ks
+
+
+def _int32():
+    import torch
+    return torch.int32
+
+
+def _float32():
+    import torch
+    return torch.float32
+
+
+def _counts(name, t, B, device):
+    import torch
+    if t.dtype != torch.int32 or t.shape != (B,) or (B > 1 and t.stride(0) != 1):
+        raise ValueError("%s must be a contiguous int32 [%d] tensor" % (name, B))
+    if t.device != device:
+        raise ValueError("all tensors must be on %s" % device)
+    return t.data_ptr()
+
+
+def _dense(k, v, L, device, B, ps):
+    """Strides of k and v [B][L][Hkv][D], packed."""
+    shape, sk, sv = k.shape, k.stride(), v.stride()
+    if len(shape) != 4 or shape[0] != B or shape[1] != L or shape[2] != ps[2] or shape[3] != ps[3] or v.shape != shape:
+        raise ValueError("k and v must be [B][L][Hkv][D], as the table and the pages have it")
+    if v.dtype != k.dtype:
+        raise TypeError("k and v must have one type")
+    if (sk[3] != 1 or sv[3] != 1) and ps[3] > 1:
+        raise ValueError("k and v must be dense in their last dimension")
+    if k.device != device or v.device != device:
+        raise ValueError("all tensors must be on %s" % device)
+    return _TRIPLE.pack(sk[0], sk[1], sk[2]), _TRIPLE.pack(sv[0], sv[1], sv[2])
 
 
 def seq_cache_write(k, v, k_pages, v_pages, table, start=None, count=None, k_scale=None, v_scale=None, stream=None):
@@ -192,18 +244,16 @@ def seq_cache_write(k, v, k_pages, v_pages, table, start=None, count=None, k_sca
         return _elsewhere(stream, seq_cache_write, k, v, k_pages, v_pages, table, start, count, k_scale, v_scale)
     if _away(k):
         return _over_there(k, seq_cache_write, k, v, k_pages, v_pages, table, start, count, k_scale, v_scale)
-    c, code, B, ps = _cache(k_pages, v_pages, table, k_scale, v_scale)
-    sk, sv = _strides(k, "k"), _strides(v, "v")
-    L = k.shape[1]
-    if k.shape != (B, L, ps[2], ps[3]) or v.shape != k.shape:
-        raise ValueError("k and v must be [B][L][Hkv][D], as the table and the pages have it")
-    if v.dtype != k.dtype or (code < 16 and k.dtype != k_pages.dtype):
-        raise TypeError("k and v must have one type, that of the pages unless those are 8-bit")
-    _same_device(k_pages, k, v)
-    first = 0 if start is None else _ints("start", start, (B,), k.device)
-    n = 0 if count is None else _ints("count", count, (B,), k.device)
-    _check(_library().seq_cache_write(c, k.data_ptr(), v.data_ptr(), _TRIPLE.pack(*sk), _TRIPLE.pack(*sv), L,
-                                      _dtype_code(k.dtype), first, n, _stream(None)), "seq_cache_write")
+    c, code, device, B, ps = _cache(k_pages, v_pages, table, k_scale, v_scale)
+    L = k.shape[1] if k.dim() == 4 else -1
+    sk, sv = _dense(k, v, L, device, B, ps)
+    dt = _code(k.dtype)
+    if dt >= 16 or (code < 16 and dt != code):
+        raise TypeError("k and v must have the type of the pages, or a wider one than 8-bit pages")
+    first = 0 if start is None else _counts("start", start, B, device)
+    n = 0 if count is None else _counts("count", count, B, device)
+    _check(_library().seq_cache_write(c, k.data_ptr(), v.data_ptr(), sk, sv, L, dt, first, n, _stream(None)),
+           "seq_cache_write")
 
 
 def seq_cache_read(k_pages, v_pages, table, length, L: int, dtype=None, k_scale=None, v_scale=None, k=None, v=None,
@@ -215,22 +265,22 @@ def seq_cache_read(k_pages, v_pages, table, length, L: int, dtype=None, k_scale=
         return _elsewhere(stream, seq_cache_read, k_pages, v_pages, table, length, L, dtype, k_scale, v_scale, k, v)
     if _away(k_pages):
         return _over_there(k_pages, seq_cache_read, k_pages, v_pages, table, length, L, dtype, k_scale, v_scale, k, v)
-    import torch
-    c, code, B, ps = _cache(k_pages, v_pages, table, k_scale, v_scale)
+    c, code, device, B, ps = _cache(k_pages, v_pages, table, k_scale, v_scale)
     if dtype is None:
-        dtype = k_pages.dtype if code < 16 else torch.float32
-    if code < 16 and dtype != k_pages.dtype:
-        raise TypeError("dtype must be that of the pages unless those are 8-bit")
-    shape = (B, L, ps[2], ps[3])
-    k = torch.empty(shape, dtype=dtype, device=k_pages.device) if k is None else k
-    v = torch.empty(shape, dtype=dtype, device=k_pages.device) if v is None else v
-    _like(k, shape, dtype, "k")
-    _like(v, shape, dtype, "v")
-    _same_device(k_pages, k, v)
-    n = _ints("length", length, (B,), k_pages.device)
-    _check(_library().seq_cache_read(c, k.data_ptr(), v.data_ptr(), _TRIPLE.pack(*_strides(k, "k")),
-                                     _TRIPLE.pack(*_strides(v, "v")), L, _dtype_code(dtype), n, _stream(None)),
-           "seq_cache_read")
+        dtype = k_pages.dtype if code < 16 else _float32()
+    dt = _code(dtype)
+    if dt >= 16 or (code < 16 and dt != code):
+        raise TypeError("dtype must be that of the pages, or a wider one than 8-bit pages")
+    if k is None or v is None:
+        import torch
+        shape = (B, L, ps[2], ps[3])
+        k = torch.empty(shape, dtype=dtype, device=device) if k is None else k
+        v = torch.empty_like(k, memory_format=torch.contiguous_format) if v is None else v
+    sk, sv = _dense(k, v, L, device, B, ps)
+    if k.dtype != dtype:
+        raise ValueError("k and v must have the type %s" % dtype)
+    n = _counts("length", length, B, device)
+    _check(_library().seq_cache_read(c, k.data_ptr(), v.data_ptr(), sk, sv, L, dt, n, _stream(None)), "seq_cache_read")
     return k, v
 
 
@@ -243,7 +293,7 @@ def _paged_ws(c, H, dt):
 
 def seq_paged_attention_workspace_bytes(q, k_pages, v_pages, table, k_scale=None, v_scale=None) -> int:
     """Bytes of workspace of ``seq_paged_attention_forward`` with these operands."""
-    return _paged_ws(_cache(k_pages, v_pages, table, k_scale, v_scale)[0], q.shape[1], _dtype_code(q.dtype))
+    return _paged_ws(_cache(k_pages, v_pages, table, k_scale, v_scale)[0], q.shape[1], _code(q.dtype))
 
 
 def seq_paged_attention_forward(q, k_pages, v_pages, table, length, scale=None, cap: float = 0.0, bias=None, k_scale=None,
@@ -259,25 +309,26 @@ def seq_paged_attention_forward(q, k_pages, v_pages, table, length, scale=None, 
         return _over_there(q, seq_paged_attention_forward, q, k_pages, v_pages, table, length, scale, cap, bias, k_scale,
                            v_scale, out, ws)
     import torch
-    c, code, B, ps = _cache(k_pages, v_pages, table, k_scale, v_scale)
-    qs, device = q.shape, q.device
+    c, code, device, B, ps = _cache(k_pages, v_pages, table, k_scale, v_scale)
+    qs, sq, dt = q.shape, q.stride(), _code(q.dtype)
     if len(qs) != 3 or qs[0] != B or qs[2] != ps[3]:
         raise ValueError("q must be [B][H][D], as the table and the pages have it")
-    if code < 16 and q.dtype != k_pages.dtype:
-        raise TypeError("q must have the type of the pages unless those are 8-bit")
-    if q.stride(2) != 1 and qs[2] > 1:
+    if dt >= 16 or (code < 16 and dt != code):
+        raise TypeError("q must have the type of the pages, or a wider one than 8-bit pages")
+    H, D = qs[1], qs[2]
+    if sq[2] != 1 and D > 1:
         raise ValueError("q must be dense in its last dimension")
-    H = qs[1]
+    if q.device != device:
+        raise ValueError("all tensors must be on %s" % device)
     if out is None:
-        out = torch.empty(qs, dtype=q.dtype, device=device)
-        so = (H * qs[2], qs[2])
+        out = torch.empty_like(q)
     else:
         _like(out, qs, q.dtype, "out")
-        if out.stride(2) != 1 and qs[2] > 1:
-            raise ValueError("out must be dense in its last dimension")
-        so = out.stride()[:2]
-    _same_device(k_pages, q, out, ws)
-    n = _ints("length", length, (B,), device)
+        _same_device(q, out)
+    so = out.stride()
+    if so[2] != 1 and D > 1:
+        raise ValueError("out must be dense in its last dimension")
+    n = _counts("length", length, B, device)
     R = strip = 0
     if bias is not None:
         if bias.dim() != 2 or bias.shape[0] != H or bias.shape[1] % 2 == 0 or bias.shape[1] < 3 \
@@ -285,13 +336,16 @@ def seq_paged_attention_forward(q, k_pages, v_pages, table, length, scale=None, 
             raise ValueError("bias must be a contiguous fp32 [H][2R+1] strip")
         _same_device(q, bias)
         R, strip = bias.shape[1] // 2, bias.data_ptr()
-    dt = _dtype_code(q.dtype)
-    a = _PAGED.pack(dt, qs[2] ** -0.5 if scale is None else scale, cap, H, *q.stride()[:2], *so, R, strip, n)
+    a = _PAGED.pack(dt, D ** -0.5 if scale is None else scale, cap, H, sq[0], sq[1], so[0], so[1], R, strip, n)
     lse = torch.empty((B, H), dtype=torch.float32, device=device)
-    if ws is None:
-        need = _paged_ws(c, H, dt)
-        ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    at, size = (None, 0) if ws is None else (ws.data_ptr(), _nbytes(ws))
+    if ws is not None:
+        _same_device(q, ws)
+        at, size = ws.data_ptr(), _nbytes(ws)
+    else:
+        at, size = 0, _paged_ws(c, H, dt)
+        if size:
+            ws = torch.empty(size, dtype=torch.uint8, device=device)
+            at = ws.data_ptr()
     _check(_library().seq_paged_attention_forward(c, a, q.data_ptr(), out.data_ptr(), lse.data_ptr(), at, size,
                                                   _stream(None)), "seq_paged_attention_forward")
     return out, lse
