@@ -40,7 +40,7 @@ struct PagedArgs {
     const int32_t *len;
     const float *strip;  // [H][2R+1], or null
     int64_t q_sb, q_sh, o_sb, o_sh;  // bytes
-    int32_t B, H, G, R, row_tiles;
+    int32_t B, H, G, R, row_waves, row_tiles, spread;
     int32_t most_parts, parts;  // see Plan
     float scale, cap;
 };

@@ -1,25 +1,28 @@
 // Attention of one new token of each sequence over its pages.
 //
 // The work is the cache's bytes, read once.  The G = H/Hkv queries of a
-// key/value head are the columns of score tiles of the 16x16 matrix
-// instructions, up to four tiles side by side; a wave streams 32 keys at a
-// time straight from the pages into its operand registers, with no copy in LDS
-// and no barrier between the waves:
+// key/value head are columns of the 16x16 matrix instructions, 16 to a wave; a
+// wave streams tiles of 32 or 64 keys straight from the pages into its operand
+// registers, with no copy in LDS and no barrier between the waves:
 //   scores  [key][query]: a lane's 16 bytes of a key are the operand as they lie
 //           (the order of channels within a product is free, q follows it);
 //   output  [channel][query]: the scores' registers are the operand as they lie,
-//           and a lane holds 8 channels of 8 keys, which it turns from rows of
-//           keys into rows of channels by byte permutations.
+//           and a lane holds DP/16 channels of KEYS/4 keys, which it turns from
+//           rows of keys into rows of channels by byte permutations.
 // While a tile's scores are made the values are on their way, and while the
-// values are summed the next keys.  A sequence's keys are split evenly over
-// workgroups, whatever its table could hold, and over the four waves of each;
-// parts (maximum, sum, output) are joined in LDS and by paged_join.
+// values are summed the next keys.  The four waves of a workgroup take tiles in
+// turn; where a head has more than 16 queries, two or four of them take the
+// same tile for 16 queries each, so that memory still gives it once.  All keys
+// are shared evenly between the workgroups; the parts of a sequence (maximum,
+// sum, output) are joined in LDS and by paged_join.
 //
 // 8-bit pages go through the matrix cores as fp16, which holds every code
 // exactly; a key's scale multiplies its score, a value's the probability, over
-// the largest power of two at or above a scale seen so far.  bf16 queries over
-// them are brought to fp16 by a power of two a row: what falls below 2^-39 of
-// the row's largest channel is lost, less than fp32 sums lose.
+// the largest power of two at or above a scale seen so far.  bf16 and fp32
+// queries over them are brought to fp16's range by a power of two a row: what
+// falls below 2^-39 of the row's largest channel is lost, less than fp32 sums
+// lose.  fp32 ones, and their probabilities, are two fp16 numbers each, 22 bits,
+// at a quarter of the fp32 instructions' time.
 #include "seq_attn.hpp"
 #include "seq_cache.hpp"
 
@@ -35,25 +38,17 @@ typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef u32x4_t u32x4_a8 __attribute__((aligned(8)));
 typedef f32x8_t f32x8_a16 __attribute__((aligned(16)));
 
-struct F32Wide {  // fp32 operands, v_mfma_f32_16x16x4_f32
-    typedef float elem;
+template <bool B, class X, class Y>
+struct Pick {
+    typedef X T;
+};
+template <class X, class Y>
+struct Pick<false, X, Y> {
+    typedef Y T;
 };
 
-// What pages of element size ES hold for a lane: 16-byte pieces of keys (the
-// lane's group takes bytes 64*c + 16*group of each), 8 channels of values.
-template <int ES>
-struct Values;
-template <>
-struct Values<4> {
-    u32x4_t w[2];
-};
-template <>
-struct Values<2> {
-    u32x4_t w[1];
-};
-template <>
-struct Values<1> {
-    u32x2_t w[1];
+struct F32Wide {  // fp32 operands, v_mfma_f32_16x16x4_f32
+    typedef float elem;
 };
 
 // ---- codes to fp16, exact ----
@@ -91,39 +86,66 @@ struct Half<CodeE4M3> {
 };
 
 // ---- the two products ----
-// Op: F16Op, BF16Op or F32Wide; Code: CodeI8, CodeE4M3 or void (pages of Op's
-// own type).  NK pieces of 16 bytes of a key, EPC = 16/ES channels each.
-template <class Op, class Code, int DP>
+// E: type of the queries; Code: CodeI8, CodeE4M3 or void (pages of E itself); DP:
+// channels, 64 or 128, of which a head has D.
+template <class E, class Code, int DP>
 struct Math {
-    static constexpr bool kWide = __is_same(Op, F32Wide);
     static constexpr bool kCodes = !__is_same(Code, void);
+    static constexpr bool kWide = __is_same(E, EltF32) && !kCodes;  // fp32 instructions
+    static constexpr bool kHalf = kCodes || __is_same(E, EltF16);   // fp16 operands
+    static constexpr bool kRange = kCodes && !__is_same(E, EltF16); // queries brought to fp16's range
+    static constexpr int kTerms = kCodes && __is_same(E, EltF32) ? 2 : 1;  // operands a number
+    typedef typename Pick<kWide, F32Wide, typename Pick<kHalf, F16Op, BF16Op>::T>::T Op;
     static constexpr int ES = kCodes ? 1 : kWide ? 4 : 2;
-    static constexpr int EPC = 16 / ES, NK = DP * ES / 64;
-    typedef Values<ES> V;
-    // a lane's channels of a query: piece by piece, EPC each
+    static constexpr int NK = DP * ES / 64;  // pieces of 16 bytes of a key that a lane takes: bytes 64*c + 16*group
+    static constexpr int EPC = 16 / ES;      // channels of a piece
+    static constexpr int VC = DP / 16;       // channels of a value that a lane takes: VC*(lane % 16) on
+    // A tile's bytes are what a wave keeps on its way: 64 keys where they are short.
+    // 48 caches of up to 16384 tokens, 64 heads of 128 over 8, int8 under bf16: 362
+    // us with tiles of 32 keys, 245 with 64.
+    static constexpr int KEYS = DP * ES <= 128 ? 64 : 32;
+    static constexpr int N = KEYS / 4;       // keys of a lane: 16*(i >> 2) + 4*group + (i & 3)
+
+    struct __attribute__((aligned(VC * ES < 16 ? VC * ES : 16))) Value {
+        uint32_t w[VC * ES / 4];
+    };
+    // A lane's channels of a query: piece by piece, EPC each.
     struct Query {
-        typename Op::elem x[NK * EPC];
+        typename Op::elem x[kTerms][NK * EPC];
+    };
+    struct Weights {
+        float p[N];
+        u32x4_t packed[kTerms][N / 8];
     };
 
-    __device__ static inline f32x4_acc dot(const u32x4_t (&k)[NK], const Query &q)
+    __device__ static inline void set(Query &q, int at, float x)
+    {
+        q.x[0][at] = (typename Op::elem)x;
+        if constexpr (kTerms == 2)
+            q.x[1][at] = (typename Op::elem)(x - (float)q.x[0][at]);
+    }
+    __device__ static inline auto eight(const Query &q, int t, int at)
+    {
+        typename Op::v8 v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = q.x[t][at + e];
+        return v;
+    }
+    __device__ static inline f32x4_acc dot(const u32x4_t (&k)[NK], const Query &q, int bytes)
     {
         f32x4_acc s = {0, 0, 0, 0};
 #pragma unroll
         for (int c = 0; c < NK; ++c) {
-            if constexpr (kWide && !kCodes) {
+            if (64 * c >= bytes)  // behind a head's last channel
+                break;
+            if constexpr (kWide) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    s = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, (uint32_t)k[c][e]), q.x[4 * c + e], s, 0, 0, 0);
-            } else if constexpr (kWide) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const f32x8_t x = Code::decode(u32x2_t{k[c][2 * h], k[c][2 * h + 1]});
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        s = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], q.x[16 * c + 8 * h + e], s, 0, 0, 0);
-                }
+                    s = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, (uint32_t)k[c][e]), q.x[0][4 * c + e],
+                                                             s, 0, 0, 0);
             } else if constexpr (!kCodes) {
-                s = Op::mfma16(__builtin_bit_cast(typename Op::v8, k[c]), eight(q, 8 * c), s);
+                s = Op::mfma16(__builtin_bit_cast(typename Op::v8, k[c]), eight(q, 0, 8 * c), s);
             } else {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -131,70 +153,66 @@ struct Math {
                     typedef Half<Code> T;
                     const u32x4_t w = {T::template two<0, 1>(y, x), T::template two<2, 3>(y, x),
                                        T::template two<4, 5>(y, x), T::template two<6, 7>(y, x)};
-                    s = Op::mfma16(__builtin_bit_cast(typename Op::v8, w), eight(q, 16 * c + 8 * h), s);
+#pragma unroll
+                    for (int t = 0; t < kTerms; ++t)
+                        s = Op::mfma16(__builtin_bit_cast(typename Op::v8, w), eight(q, t, 16 * c + 8 * h), s);
                 }
             }
         }
         return s;
     }
-    __device__ static inline auto eight(const Query &q, int at)
-    {
-        typename Op::v8 v;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            v[e] = q.x[at + e];
-        return v;
-    }
 
-    // Channel 8*(lane & 15) + j of the lane's 8 keys: rows of the operand.
+    __device__ static inline void pack(Weights &w)
+    {
+        if constexpr (!kWide) {
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) {
+                float a = w.p[2 * i], b = w.p[2 * i + 1];
+#pragma unroll
+                for (int t = 0; t < kTerms; ++t) {
+                    const uint32_t x = Op::bits(a), y = Op::bits(b);
+                    w.packed[t][i / 4][i % 4] = x | y << 16;
+                    if constexpr (kTerms == 2) {
+                        a -= (float)__builtin_bit_cast(_Float16, (uint16_t)x);
+                        b -= (float)__builtin_bit_cast(_Float16, (uint16_t)y);
+                    }
+                }
+            }
+        }
+    }
+    // Channel VC*(lane % 16) + J of eight of the lane's keys: a row of the operand.
     template <int J>
-    __device__ static inline u32x4_t channel(const V *v)
+    __device__ static inline u32x4_t channel(const Value *v)
     {
         u32x4_t w;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if constexpr (ES == 2) {
-                w[i] = __builtin_amdgcn_perm(v[2 * i + 1].w[0][J / 2], v[2 * i].w[0][J / 2],
-                                             J % 2 ? 0x07060302u : 0x05040100u);
-            } else {
-                w[i] = Half<Code>::template two<J % 4, 4 + J % 4>(v[2 * i + 1].w[0][J / 4], v[2 * i].w[0][J / 4]);
-            }
+            if constexpr (ES == 2)
+                w[i] = __builtin_amdgcn_perm(v[2 * i + 1].w[J / 2], v[2 * i].w[J / 2], J % 2 ? 0x07060302u : 0x05040100u);
+            else
+                w[i] = Half<Code>::template two<J % 4, 4 + J % 4>(v[2 * i + 1].w[J / 4], v[2 * i].w[J / 4]);
         }
         return w;
     }
-    template <int J>
-    __device__ static inline float value(const V &v)
-    {
-        if constexpr (kCodes)
-            return Code::decode(v.w[0])[J];
-        else
-            return __builtin_bit_cast(float, (uint32_t)v.w[J / 4][J % 4]);
-    }
-
-    // o[j] += channel j of the values times the weights w[nt] of NT tiles of queries.
-    template <int NT, int N, int J = 0>
-    __device__ static inline void sum(f32x4_acc (&o)[NT][8], const V (&v)[N], const float (&p)[NT][N],
-                                      const u32x4_t (&packed)[NT][N / 8])
+    // o[j] += channel j of the values times their weights.
+    template <int J = 0>
+    __device__ static inline void sum(f32x4_acc (&o)[VC], const Value (&v)[N], const Weights &w)
     {
         if constexpr (kWide) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float x = value<J>(v[i]);
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-                    o[t][J] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, p[t][i], o[t][J], 0, 0, 0);
-            }
+            for (int i = 0; i < N; ++i)
+                o[J] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, v[i].w[J]), w.p[i], o[J], 0, 0, 0);
         } else {
 #pragma unroll
             for (int i = 0; i < N / 8; ++i) {
                 const auto x = __builtin_bit_cast(typename Op::v8, channel<J>(v + 8 * i));
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
-                    o[t][J] = Op::mfma16(x, __builtin_bit_cast(typename Op::v8, packed[t][i]), o[t][J]);
+                for (int t = 0; t < kTerms; ++t)
+                    o[J] = Op::mfma16(x, __builtin_bit_cast(typename Op::v8, w.packed[t][i]), o[J]);
             }
         }
-        if constexpr (J < 7)
-            sum<NT, N, J + 1>(o, v, p, packed);
+        if constexpr (J + 1 < VC)
+            sum<J + 1>(o, v, w);
     }
 };
 
@@ -208,8 +226,9 @@ struct Where {
 
 // ---- how the keys are split ----
 // All workgroups take about the same number of keys, whichever sequence they
-// belong to: with a share of total/kTarget keys (whole steps), a sequence of n
-// keys makes ceil(n/share) parts of equal size.  The lengths are known on the
+// belong to: with a share of total/most_parts keys (whole steps) or, where that
+// is little, twice as many, a sequence of n keys makes ceil(n/share) parts of
+// equal size.  The lengths are known on the
 // GPU only, so each wave adds them up and finds its part by a scan over the
 // sequences' counts.
 struct Cut {
@@ -240,7 +259,11 @@ __device__ inline int32_t share_of(const Pool &c, const PagedArgs &a, int32_t un
         total += __shfl_xor((long long)total, m);
     total = (int64_t)__builtin_amdgcn_readfirstlane((int)(total >> 32)) << 32 |
             (uint32_t)__builtin_amdgcn_readfirstlane((int)total);
-    const int64_t share = total <= a.most_parts ? 1 : (total - 1) / a.most_parts + 1;
+    // one round of workgroups where that leaves each a few tiles only, two else
+    const int32_t half = (a.most_parts + 1) / 2;
+    int64_t share = total <= half ? 1 : (total - 1) / half + 1;
+    if (share > 8 * a.row_waves * unit)
+        share = (total - 1) / a.most_parts + 1;
     // no sequence is longer than 2^30
     return ((share < 1 << 30 ? (int32_t)share : 1 << 30) + unit - 1) / unit * unit;
 }
@@ -299,48 +322,48 @@ __device__ inline float *part_of(const PagedArgs &a, int64_t index, int head, in
     return a.part + (index * a.H + head) * part_floats(D);
 }
 
-// Keys of a wave's tile.  8-bit pages take half the registers, and twice the keys
-// keep as many bytes on their way: 48 caches of up to 16384 tokens, 64 heads of
-// 128 over 8, int8 under bf16: 362 us with tiles of 32 keys, 245 with 64.
-template <class Op, class Code, int NT>
-constexpr int keys_of_tile() { return !__is_same(Code, void) && !__is_same(Op, F32Wide) && NT == 1 ? 64 : 32; }
-
 // FULL: heads have DP channels, no more tests of where they end.
-template <class E, class Op, class Code, int NT, int DP, bool FULL>
-__global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
+template <class E, class Code, int DP, bool FULL>
+__global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs a)
 {
-    constexpr int KEYS = keys_of_tile<Op, Code, NT>(), N = KEYS / 4, kUnit = kWavesP * KEYS;
-    const int D = FULL ? DP : c.D;
-    typedef Math<Op, Code, DP> M;
-    constexpr bool kHalf = __is_same(Op, F16Op);
+    typedef Math<E, Code, DP> M;
+    constexpr int KEYS = M::KEYS, N = M::N, VC = M::VC, ES = M::ES;
     // fp16 probabilities are times 2^14, so that those of long rows stay normal numbers
-    constexpr float kShift = kHalf ? 14.0f : 0.0f, kUnshift = kHalf ? 0x1p-14f : 1.0f;
+    constexpr float kShift = M::kHalf ? 14.0f : 0.0f, kUnshift = M::kHalf ? 0x1p-14f : 1.0f;
     __shared__ __align__(16) Where<KEYS> where[kWavesP];
     __shared__ float box[kWavesP][16][DP + 4];
-    __shared__ float sm[kWavesP][NT][16], sl[kWavesP][NT][16];
+    __shared__ float sm[kWavesP][16], sl[kWavesP][16];
+    const int D = FULL ? DP : c.D;
 
-    // blockIdx: heads fastest (neighbours in memory), then row tiles, then parts
+    // blockIdx: heads fastest, then row tiles, then parts.  Workgroups go to the 8
+    // XCDs in turn (id mod 8); where heads of a token share 128-byte lines, all
+    // heads of a part run on one (spread 8, else 1), which fetches the lines once.
+    // 32 caches of 2048 to 8192 tokens, 8 heads, 16 tokens a page, heads fastest
+    // and on one XCD: int8 of 64 channels 71 and 58 us, bf16 of 96 118 and 112; of
+    // 128 channels, where no lines are shared, bf16 136 and 139, int8 216 and 219.
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int hk = blockIdx.x % c.Hkv, rest = blockIdx.x / c.Hkv, rt = rest % a.row_tiles, index = rest / a.row_tiles;
+    const int turn = blockIdx.x / a.spread, hk = turn % c.Hkv, rest = turn / c.Hkv, rt = rest % a.row_tiles;
+    const int index = rest / a.row_tiles * a.spread + blockIdx.x % a.spread;
+    if (index >= a.parts)
+        return;
+    const int step = KEYS * (kWavesP / a.row_waves);  // keys of the workgroup's tiles
     Part part;
     if (a.most_parts) {
-        part = find_part(c, a, index, kUnit, lane);
+        part = find_part(c, a, index, step, lane);
         if (part.b < 0)
             return;
     } else {
         const int n = tokens_of(c, a, index);
         part = Part{index, n, 0, n, true};
     }
-    const int b = part.b, n = part.n, lo = part.lo, hi = part.hi;
+    const int b = part.b, n = part.n, hi = part.hi;
 
-    // this lane's queries: column r of each tile
-    const int row0 = rt * (16 * NT);
-    float c1[NT];
-    typename M::Query q[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int row = row0 + 16 * t + r;
+    // this lane's query: column r of the wave's
+    const int row0 = (rt * a.row_waves) * 16, row = row0 + wave % a.row_waves * 16 + r;
+    typename M::Query q;
+    float c1 = a.cap > 0 ? a.scale / a.cap : a.scale * kLog2e;
+    {
         const typename E::T *const p = (const typename E::T *)(a.q + b * a.q_sb + (hk * a.G + row) * a.q_sh);
         float x[M::NK * M::EPC];
         uint32_t top = 0;
@@ -359,20 +382,20 @@ __global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
                     top = max(top, __builtin_bit_cast(uint32_t, x[k * M::EPC + e + i]) & 0x7FFFFFFFu);
                 }
             }
-        float f = 1.0f, back = 1.0f;
-        if constexpr (M::kCodes && kHalf && __is_same(E, EltBF16)) {
+        float f = 1.0f;
+        if constexpr (M::kRange) {
             top = max(top, (uint32_t)__shfl_xor((int)top, 16));
             top = max(top, (uint32_t)__shfl_xor((int)top, 32));
             const int e = max((int)(top >> 23) - 127, -100);  // the row's largest becomes 2^14 .. 2^15
             f = __builtin_bit_cast(float, (uint32_t)(127 + 14 - e) << 23);
-            back = __builtin_bit_cast(float, (uint32_t)(127 - 14 + e) << 23);
+            c1 *= __builtin_bit_cast(float, (uint32_t)(127 - 14 + e) << 23);
         }
 #pragma unroll
         for (int k = 0; k < M::NK * M::EPC; ++k)
-            q[t].x[k] = (typename Op::elem)(x[k] * f);
-        c1[t] = back * (a.cap > 0 ? a.scale / a.cap : a.scale * kLog2e);
+            M::set(q, k, x[k] * f);
     }
     const float c2 = a.cap * kLog2e;
+    const float *const strip = a.strip + (int64_t)min(hk * a.G + row, a.H - 1) * (2 * a.R + 1) + a.R;
 
     const char *const kp = c.k + hk * c.k_head, *const vp = c.v + hk * c.v_head;
     const int32_t *const table = c.table + b * c.table_stride;
@@ -380,36 +403,37 @@ __global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
 
     // A lane is the owner of key lane % KEYS of each tile.
     auto page_at = [&](int k0) {
-        const int key = k0 + (lane & (KEYS - 1));
+        const int key = k0 + lane % KEYS;
         return key < hi ? page_of(table, fdiv((uint32_t)key, c.page), c.max_pages, c.pages) : -1;
     };
     auto inside = [&](int k0) {
-        const uint32_t key = k0 + (lane & (KEYS - 1));
+        const uint32_t key = k0 + lane % KEYS;
         return (int)(key - fdiv(key, c.page) * c.page.d);
     };
-    auto k_scale = [&](int id, int in) { return id < 0 ? 0.0f : *(const float *)(c.ks + hk * c.ks_head + id * c.ks_page + in * c.ks_tok); };
-    auto v_scale = [&](int id, int in) { return id < 0 ? 0.0f : *(const float *)(c.vs + hk * c.vs_head + id * c.vs_page + in * c.vs_tok); };
+    auto scale_at = [&](const char *s, int64_t page, int64_t tok, int id, int in) {
+        return id < 0 ? 0.0f : *(const float *)(s + id * page + in * tok);
+    };
     // Keys that are not there read page 0 and are left out of what follows.
     auto tell = [&](int id, int in) {
         if (KEYS == 64 || lane < KEYS)
-            my.k[lane & (KEYS - 1)] = id < 0 ? 0 : id * c.k_page + in * c.k_tok;
+            my.k[lane % KEYS] = id < 0 ? 0 : id * c.k_page + in * c.k_tok;
         if (KEYS == 64 || lane >= KEYS)
-            my.v[lane & (KEYS - 1)] = id < 0 ? 0 : id * c.v_page + in * c.v_tok;
+            my.v[lane % KEYS] = id < 0 ? 0 : id * c.v_page + in * c.v_tok;
     };
     u32x4_t kr[KEYS / 16][M::NK];
-    typename M::V vr[N];
+    typename M::Value vr[N];
     auto load_keys = [&]() {
 #pragma unroll
         for (int s = 0; s < KEYS / 16; ++s) {
             const char *const p = kp + my.k[16 * s + r] + 16 * g;
 #pragma unroll
             for (int k = 0; k < M::NK; ++k) {
-                const int left = D * M::ES - (64 * k + 16 * g);  // a multiple of 8
+                const int left = D * ES - (64 * k + 16 * g);  // a multiple of 8
                 if (!FULL)
                     kr[s][k] = u32x4_t{0, 0, 0, 0};
                 if (FULL || left >= 16) {
                     kr[s][k] = *(const u32x4_a8 *)(p + 64 * k);
-                } else if (M::ES == 1 && left > 0) {
+                } else if (ES == 1 && left > 0) {
                     const u32x2_t w = *(const u32x2_t *)(p + 64 * k);
                     kr[s][k] = u32x4_t{w[0], w[1], 0, 0};
                 }
@@ -419,55 +443,53 @@ __global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
     auto load_values = [&]() {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const char *const p = vp + my.v[16 * (i >> 2) + 4 * g + (i & 3)] + 8 * r * M::ES;
-            if (FULL && DP == 128 || 8 * r < D)
-                vr[i] = *(const typename M::V *)p;
+            const char *const p = vp + my.v[16 * (i >> 2) + 4 * g + (i & 3)] + VC * r * ES;
+            if (FULL || VC * r < D)
+                vr[i] = *(const typename M::Value *)p;
             else
-                vr[i] = typename M::V{};
+                vr[i] = typename M::Value{};
+        }
+    };
+    auto load_scales = [&](int id, int in, float &ks, float &vs) {
+        if constexpr (M::kCodes) {
+            ks = scale_at(c.ks + hk * c.ks_head, c.ks_page, c.ks_tok, id, in);
+            vs = scale_at(c.vs + hk * c.vs_head, c.vs_page, c.vs_tok, id, in);
         }
     };
 
-    f32x4_acc o[NT][8];
-    float m[NT], l[NT];
+    f32x4_acc o[VC];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        m[t] = -INFINITY, l[t] = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            o[t][j] = f32x4_acc{0, 0, 0, 0};
-    }
-    float unit = 0x1p-126f;  // 8 bits, fp16: the values' scales are over this power of two
+    for (int j = 0; j < VC; ++j)
+        o[j] = f32x4_acc{0, 0, 0, 0};
+    float m = -INFINITY, l = 0;
+    float unit = 0x1p-126f;  // 8 bits: the values' scales are over this power of two
 
-    const int first = lo + wave * KEYS;
+    const int first = part.lo + wave / a.row_waves * KEYS;
     int id = page_at(first), in = inside(first);
     float ks = 0, vs = 0;
     if (first < hi) {
-        if constexpr (M::kCodes)
-            ks = k_scale(id, in), vs = v_scale(id, in);
+        load_scales(id, in, ks, vs);
         tell(id, in);
         wave_lds_handoff();
         load_keys();
         load_values();
     }
-    int id1 = page_at(first + kUnit), in1 = inside(first + kUnit);
-    for (int k0 = first; k0 < hi; k0 += kUnit) {
-        // scores of the tile; a lane's keys are 16*(i >> 2) + 4*g + (i & 3)
-        float s[NT][N];
+    int id1 = page_at(first + step), in1 = inside(first + step);
+    for (int k0 = first; k0 < hi; k0 += step) {
+        float s[N];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int h = 0; h < KEYS / 16; ++h) {
+            const f32x4_acc x = M::dot(kr[h], q, D * ES);
 #pragma unroll
-            for (int h = 0; h < KEYS / 16; ++h) {
-                const f32x4_acc x = M::dot(kr[h], q[t]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    s[t][4 * h + i] = x[i];
-            }
+            for (int i = 0; i < 4; ++i)
+                s[4 * h + i] = x[i];
+        }
         const uint64_t there = __ballot(id >= 0);  // a bit a key
         float kscale[N], vscale[N];
         wave_lds_handoff();
         if constexpr (M::kCodes) {
-            my.ks[lane & (KEYS - 1)] = ks;
-            my.vs[lane & (KEYS - 1)] = vs;
+            my.ks[lane % KEYS] = ks;
+            my.vs[lane % KEYS] = vs;
             wave_lds_handoff();
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -479,17 +501,16 @@ __global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
         id = id1, in = in1;
         tell(id, in);
         wave_lds_handoff();
-        const bool more = k0 + kUnit < hi;
+        const bool more = k0 + step < hi;
         if (more) {
             load_keys();
-            if constexpr (M::kCodes)
-                ks = k_scale(id, in), vs = v_scale(id, in);
-            id1 = page_at(k0 + 2 * kUnit), in1 = inside(k0 + 2 * kUnit);
+            load_scales(id, in, ks, vs);
+            id1 = page_at(k0 + 2 * step), in1 = inside(k0 + 2 * step);
         }
 
         // softmax
-        float p[NT][N], up = 1.0f, over = 1.0f;
-        if constexpr (M::kCodes && kHalf) {
+        float up = 1.0f, over = 1.0f;
+        if constexpr (M::kCodes) {
             float top = unit;
 #pragma unroll
             for (int i = 0; i < N; ++i)
@@ -503,134 +524,118 @@ __global__ __launch_bounds__(64 * kWavesP) void paged_attn(Pool c, PagedArgs a)
             up = unit * over;
             unit = now;
         }
-        u32x4_t packed[NT][N / 8];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const float *const strip = a.strip + (int64_t)min(hk * a.G + row0 + 16 * t + r, a.H - 1) * (2 * a.R + 1) + a.R;
-            float top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int at = 16 * (i >> 2) + 4 * g + (i & 3);
-                float x = s[t][i] * c1[t];
-                if constexpr (M::kCodes)
-                    x *= kscale[i];
-                if (a.cap > 0) {
-                    const float far = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * (2.0f * kLog2e)));
-                    x = c2 * (fabsf(x) < kSmallTanh ? small_tanh(x) : far);
-                }
-                if (a.R > 0)
-                    x += strip[min(max(k0 + at - (n - 1), -a.R), 0)] * kLog2e;
-                x = (there >> at) & 1 ? x : -INFINITY;
-                s[t][i] = x;
-                top = fmaxf(top, x);
+        for (int i = 0; i < N; ++i) {
+            const int at = 16 * (i >> 2) + 4 * g + (i & 3);
+            float x = s[i] * c1;
+            if constexpr (M::kCodes)
+                x *= kscale[i];
+            if (a.cap > 0) {
+                const float far = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * (2.0f * kLog2e)));
+                x = c2 * (fabsf(x) < kSmallTanh ? small_tanh(x) : far);
             }
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float now = fmaxf(m[t], top), base = now == -INFINITY ? 0.0f : now;
-            float f = __builtin_amdgcn_exp2f(m[t] - base);
-            m[t] = now;
-            float sum = 0;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                p[t][i] = __builtin_amdgcn_exp2f(s[t][i] - base + kShift);
-                sum += p[t][i];
-                if constexpr (M::kCodes)
-                    p[t][i] *= kHalf ? vscale[i] * over : vscale[i];
-            }
-            l[t] = l[t] * f + sum;
-            f *= up;
-            if (__any(f != 1.0f)) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    o[t][j] *= f;
-            }
-            if constexpr (!M::kWide) {
-#pragma unroll
-                for (int i = 0; i < N / 2; ++i)
-                    packed[t][i / 4][i % 4] = Op::bits(p[t][2 * i]) | Op::bits(p[t][2 * i + 1]) << 16;
-            }
+            if (a.R > 0)
+                x += strip[min(max(k0 + at - (n - 1), -a.R), 0)] * kLog2e;
+            s[i] = x;
         }
-        if ((KEYS == 64 ? ~there : (uint32_t)~there) != 0) {
-            // what was read for keys that are not there: their weights are zero,
-            // and so must be the values
+        const bool whole = (KEYS == 64 ? ~there : (uint32_t)~there) == 0;
+        if (!whole) {
+            // keys that are not there: no score, and no value either, whatever was
+            // read in their place (their weights are zero)
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                if (!((there >> (16 * (i >> 2) + 4 * g + (i & 3))) & 1))
-                    vr[i] = typename M::V{};
+                if (!((there >> (16 * (i >> 2) + 4 * g + (i & 3))) & 1)) {
+                    s[i] = -INFINITY;
+                    vr[i] = typename M::Value{};
+                }
         }
-        M::template sum<NT, N>(o, vr, p, packed);
+        float top = s[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i)
+            top = fmaxf(top, s[i]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float now = fmaxf(m, top), base = now == -INFINITY ? 0.0f : now, less = base - kShift;
+        float f = __builtin_amdgcn_exp2f(m - base), sum = 0;
+        m = now;
+        typename M::Weights w;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            w.p[i] = __builtin_amdgcn_exp2f(s[i] - less);
+            sum += w.p[i];
+            if constexpr (M::kCodes)
+                w.p[i] *= vscale[i] * over;
+        }
+        l = l * f + sum;
+        f *= up;
+        if (__any(f != 1.0f)) {
+#pragma unroll
+            for (int j = 0; j < VC; ++j)
+                o[j] *= f;
+        }
+        M::pack(w);
+        M::sum(o, vr, w);
         if (more)
             load_values();
     }
 
-    // join the waves
-    const float down = M::kCodes && kHalf ? unit : 1.0f;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        l[t] += __shfl_xor(l[t], 16);
-        l[t] += __shfl_xor(l[t], 32);
-        if (g == 0) {
-            sm[wave][t][r] = m[t];
-            sl[wave][t][r] = l[t];
-        }
+    // join the waves of each 16 queries
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (g == 0) {
+        sm[wave][r] = m;
+        sl[wave][r] = l;
     }
+    __syncthreads();
+    float top = -INFINITY;
+    for (int w = wave % a.row_waves; w < kWavesP; w += a.row_waves)
+        top = fmaxf(top, sm[w][r]);
+    const float mine = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top)) * (M::kCodes ? unit : 1.0f);
+    // this lane's channels are 4*VC*g .. 4*VC*(g + 1) - 1
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        if (row0 + 16 * t >= a.G)  // no query from here on, for any wave
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < VC; ++j)
+            box[wave][r][4 * VC * g + VC * i + j] = o[j][i] * mine;
+    __syncthreads();
+    // 16 threads a row, 8 channels each
+    const int rr = threadIdx.x >> 4, ch = (threadIdx.x & 15) * 8;
+    for (int w0 = 0; w0 < a.row_waves; ++w0) {
+        const int rw = row0 + 16 * w0 + rr;
+        if (rw >= a.G)
             break;
-        __syncthreads();
-        float top = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < kWavesP; ++w)
-            top = fmaxf(top, sm[w][t][r]);
-        const float mine = __builtin_amdgcn_exp2f(m[t] - (top == -INFINITY ? 0.0f : top)) * down;
-        // this lane's channels are 32*g .. 32*g + 31
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (32 * g < DP)
-                    box[wave][r][32 * g + 8 * i + j] = o[t][j][i] * mine;
-        __syncthreads();
-        // 16 threads a row, 8 channels each
-        const int rr = threadIdx.x >> 4, ch = (threadIdx.x & 15) * 8, row = row0 + 16 * t + rr;
-        if (row < a.G) {
-            float ms = -INFINITY, sum = 0;
-#pragma unroll
-            for (int w = 0; w < kWavesP; ++w)
-                ms = fmaxf(ms, sm[w][t][rr]);
-            const float base = ms == -INFINITY ? 0.0f : ms;
-#pragma unroll
-            for (int w = 0; w < kWavesP; ++w)
-                sum += sl[w][t][rr] * __builtin_amdgcn_exp2f(sm[w][t][rr] - base);
-            f32x8_t v = {0, 0, 0, 0, 0, 0, 0, 0};
+        float ms = -INFINITY, sum = 0;
+        for (int w = w0; w < kWavesP; w += a.row_waves)
+            ms = fmaxf(ms, sm[w][rr]);
+        const float base = ms == -INFINITY ? 0.0f : ms;
+        f32x8_t v = {0, 0, 0, 0, 0, 0, 0, 0};
+        for (int w = w0; w < kWavesP; w += a.row_waves) {
+            sum += sl[w][rr] * __builtin_amdgcn_exp2f(sm[w][rr] - base);
             if (ch < DP)
 #pragma unroll
-                for (int w = 0; w < kWavesP; ++w)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        v[e] += box[w][rr][ch + e];
-            if (!part.alone) {
-                float *const to = part_of(a, index, hk * a.G + row, D);
-                if (ch < D)
-                    *(f32x8_a16 *)(to + ch) = v;
-                if (ch == 0) {
-                    to[D] = ms;
-                    to[D + 1] = sum;
-                }
-            } else {
-                const bool none = sum == 0.0f;  // not ms == -inf: all scores may be NaN
-                if (ch < D) {
-                    typedef typename E::T V8 __attribute__((ext_vector_type(8)));
-                    V8 y;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        y[e] = E::put(none ? 0.0f : v[e] / sum);
-                    *(V8 *)(a.out + b * a.o_sb + (hk * a.G + row) * a.o_sh + ch * sizeof(typename E::T)) = y;
-                }
-                if (ch == 0)
-                    a.lse[b * a.H + hk * a.G + row] = none ? -INFINITY : (ms + __log2f(sum * kUnshift)) * kLn2;
+                for (int e = 0; e < 8; ++e)
+                    v[e] += box[w][rr][ch + e];
+        }
+        if (!part.alone) {
+            float *const to = part_of(a, index, hk * a.G + rw, D);
+            if (ch < D)
+                *(f32x8_a16 *)(to + ch) = v;
+            if (ch == 0) {
+                to[D] = ms;
+                to[D + 1] = sum;
             }
+        } else {
+            const bool none = sum == 0.0f;  // not ms == -inf: all scores may be NaN
+            if (ch < D) {
+                typedef typename E::T V8 __attribute__((ext_vector_type(8), aligned(16)));
+                V8 y;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    y[e] = E::put(none ? 0.0f : v[e] / sum);
+                *(V8 *)(a.out + b * a.o_sb + (hk * a.G + rw) * a.o_sh + ch * sizeof(typename E::T)) = y;
+            }
+            if (ch == 0)
+                a.lse[b * a.H + hk * a.G + rw] = none ? -INFINITY : (ms + __log2f(sum * kUnshift)) * kLn2;
         }
     }
 }
@@ -711,15 +716,12 @@ __global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int group
     }
 }
 
-// Tiles of 16 queries that a workgroup takes: one, or several beside each other
-// where a key/value head has more queries than one holds (four; two in fp32,
-// whose operands take twice the registers).
-int tiles_of(int64_t G, int dt) { return G <= 16 ? 1 : dt == IM2WIN_F32 ? 2 : 4; }
-
 // Where no sequence can have two steps, and where there are enough of them to
-// even out by themselves, a workgroup takes a whole sequence (most_parts 0).
+// even out by themselves (or so many that each wave's scan would cost more), a
+// workgroup takes a whole sequence (most_parts 0).
 struct Plan {
-    int64_t row_tiles, unit, most_parts, parts;  // parts: that the lengths can make at most
+    int32_t row_waves, row_tiles, step;
+    int64_t most_parts, parts;  // parts: that the lengths can make at most
 };
 // Workgroups that share the keys, two rounds of the two that fit a CU.  Measured
 // with 512, 768, 1024, 1536 and 2048 (bf16, 8 heads of 128, H = 32): 32 caches of
@@ -730,51 +732,43 @@ constexpr int64_t kTarget = 1024;
 Plan plan_of(const Pool &c, int ct, int64_t B, int64_t H, int dt)
 {
     Plan p;
-    const int64_t G = H / c.Hkv, tiles = tiles_of(G, dt);
-    p.row_tiles = (G + 16 * tiles - 1) / (16 * tiles);
-    p.unit = kWavesP * (ct != dt && dt != IM2WIN_F32 && tiles == 1 ? 64 : 32);
-    const int64_t heads = c.Hkv * p.row_tiles, steps = ((int64_t)c.max_pages * c.page.d + p.unit - 1) / p.unit;
-    p.most_parts = steps <= 1 || B * heads >= 16 * kTarget ? 0 : (kTarget + heads - 1) / heads;
+    const int64_t G = H / c.Hkv, bytes = (c.D <= 64 ? 64 : 128) * (ct != dt ? 1 : dt == IM2WIN_F32 ? 4 : 2);
+    p.row_waves = G <= 16 ? 1 : G <= 32 ? 2 : 4;
+    p.row_tiles = (int32_t)((G + 16 * p.row_waves - 1) / (16 * p.row_waves));
+    p.step = (bytes <= 128 ? 64 : 32) * (kWavesP / p.row_waves);  // keys: see Math
+    const int64_t heads = c.Hkv * p.row_tiles, steps = ((int64_t)c.max_pages * c.page.d + p.step - 1) / p.step;
+    p.most_parts = steps <= 1 || B > 512 || B * heads >= 16 * kTarget ? 0 : (kTarget + heads - 1) / heads;
     p.parts = p.most_parts ? (p.most_parts + B < B * steps ? p.most_parts + B : B * steps) : B;
     return p;
 }
 
-template <class E, class Op, class Code, int NT, int DP>
+template <class E, class Code, int DP>
 void run_full(uint32_t grid, const Pool &c, const PagedArgs &a, hipStream_t st)
 {
     if (c.D == DP)
-        paged_attn<E, Op, Code, NT, DP, true><<<grid, 64 * kWavesP, 0, st>>>(c, a);
+        paged_attn<E, Code, DP, true><<<grid, 64 * kWavesP, 0, st>>>(c, a);
     else
-        paged_attn<E, Op, Code, NT, DP, false><<<grid, 64 * kWavesP, 0, st>>>(c, a);
+        paged_attn<E, Code, DP, false><<<grid, 64 * kWavesP, 0, st>>>(c, a);
 }
 
-template <class E, class Op, class Code, int NT>
-void run(const Pool &c, const PagedArgs &a, hipStream_t st)
+template <class E, class Code>
+void run(const Pool &c, const PagedArgs &a, int32_t step, hipStream_t st)
 {
-    const uint32_t grid = (uint32_t)(a.parts * c.Hkv) * a.row_tiles;
-    c.D <= 64 ? run_full<E, Op, Code, NT, 64>(grid, c, a, st) : run_full<E, Op, Code, NT, 128>(grid, c, a, st);
+    const uint32_t grid = (uint32_t)((a.parts + a.spread - 1) / a.spread * a.spread * c.Hkv) * a.row_tiles;
+    c.D <= 64 ? run_full<E, Code, 64>(grid, c, a, st) : run_full<E, Code, 128>(grid, c, a, st);
     if (a.most_parts) {
         const int64_t rows = (int64_t)a.B * a.H;
         const int groups = rows <= 2048 ? 8 : 1;
-        paged_join<E, __is_same(Op, F16Op)><<<(uint32_t)((rows * groups + 7) / 8), 256, 0, st>>>(
-            c, a, groups, kWavesP * keys_of_tile<Op, Code, NT>());
+        paged_join<E, Math<E, Code, 64>::kHalf><<<(uint32_t)((rows * groups + 7) / 8), 256, 0, st>>>(c, a, groups, step);
     }
 }
 
-template <class E, class Op, class Code>
-void run_tiles(const Pool &c, const PagedArgs &a, hipStream_t st)
+template <class E>
+void run_code(const Pool &c, int ct, const PagedArgs &a, int32_t step, hipStream_t st)
 {
-    constexpr int kMany = __is_same(E, EltF32) ? 2 : 4;
-    a.G <= 16 ? run<E, Op, Code, 1>(c, a, st) : run<E, Op, Code, kMany>(c, a, st);
-}
-
-// Own: the pages' operand type where they hold E itself; Coded: of 8-bit pages.
-template <class E, class Own, class Coded>
-void run_code(const Pool &c, int ct, const PagedArgs &a, hipStream_t st)
-{
-    ct == SEQ_I8     ? run_tiles<E, Coded, CodeI8>(c, a, st)
-    : ct == SEQ_E4M3 ? run_tiles<E, Coded, CodeE4M3>(c, a, st)
-                     : run_tiles<E, Own, void>(c, a, st);
+    ct == SEQ_I8     ? run<E, CodeI8>(c, a, step, st)
+    : ct == SEQ_E4M3 ? run<E, CodeE4M3>(c, a, step, st)
+                     : run<E, void>(c, a, step, st);
 }
 
 }  // namespace
@@ -788,13 +782,15 @@ int64_t paged_part_floats(const Pool &c, int ct, int64_t B, int64_t H, int dt)
 hipError_t launch_paged(const Pool &c, int ct, PagedArgs a, int dt, hipStream_t st)
 {
     const Plan p = plan_of(c, ct, a.B, a.H, dt);
-    a.most_parts = (int32_t)p.most_parts, a.parts = (int32_t)p.parts, a.row_tiles = (int32_t)p.row_tiles;
+    a.most_parts = (int32_t)p.most_parts, a.parts = (int32_t)p.parts;
+    a.row_waves = p.row_waves, a.row_tiles = p.row_tiles;
+    a.spread = c.Hkv > 1 && (c.k_head | c.v_head) % 128 != 0 ? 8 : 1;
     if (dt == IM2WIN_F32)
-        run_code<EltF32, F32Wide, F32Wide>(c, ct, a, st);
+        run_code<EltF32>(c, ct, a, p.step, st);
     else if (dt == IM2WIN_F16)
-        run_code<EltF16, F16Op, F16Op>(c, ct, a, st);
+        run_code<EltF16>(c, ct, a, p.step, st);
     else
-        run_code<EltBF16, BF16Op, F16Op>(c, ct, a, st);
+        run_code<EltBF16>(c, ct, a, p.step, st);
     return hipGetLastError();
 }
 

@@ -270,6 +270,24 @@ def test_attention_without_some_pages(types):
     assert not got[0].any() and torch.isneginf(gl[0]).all() and not got[2].any()
 
 
+@pytest.mark.parametrize("B,Hkv,wide", [(65, 1, 40), (150, 2, 24), (512, 1, 20), (513, 1, 20), (300, 64, 20)])
+@pytest.mark.parametrize("types", [(F16, F16), (BF16, I8)], ids=ids)
+def test_many_sequences(types, B, Hkv, wide):
+    """More sequences than a wave has lanes, split and not: every length from
+    nothing to the table's end, one far longer than the others."""
+    dt, ct = types
+    g = torch.Generator().manual_seed(B)
+    lens = torch.randint(0, 60, (B,), generator=g).tolist()
+    lens[B // 2], lens[0], lens[-1] = 16 * wide, 0, 33
+    c = Cache(lens, 16, Hkv, 8, dt, ct, wide=wide)
+    q = torch.randn((B, Hkv, 8), generator=g).to(dt)
+    out, lse, tol, tl = attention(q, c)
+    kp, vp, table, scales = c.device()
+    got, gl = pkg.seq_paged_attention_forward(q.cuda(), kp, vp, table, c.len.cuda(), **scales)
+    check(got, out, tol + 1e-30, "out")
+    check(gl, lse, tl + 1e-30, "lse")
+
+
 def test_no_pages_at_all():
     q = torch.randn(2, 4, 64, device="cuda")
     for shape, wide in (((0, 16, 2, 64), 3), ((4, 16, 2, 64), 0)):
