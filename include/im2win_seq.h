@@ -162,7 +162,7 @@ int seq_attention_backward(const seq_attention_t *a, const void *dout, const voi
  *           64-bit fractions of a turn, so far positions lose nothing.
  *   freq    host memory, [rot/2] radians a position, |freq| <= 1024; copied by
  *           the call.
- * rot even, 2 .. min(D, 256); D <= 2^16.  Pointers need the alignment of their
+ * rot even, 2 .. min(D, 256); D <= 2^16; H < 2^30.  Pointers need the alignment of their
  * element type only.  A lane takes up to 16 bytes of four heads; calls of 2^32
  * lanes and more are refused (IM2WIN_ERANGE).
  */

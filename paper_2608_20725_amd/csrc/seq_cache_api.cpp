@@ -41,7 +41,7 @@ int rotary(const seq_rotary_t *a, const void *x, void *y, bool backward, void *h
     const bool some = a->B > 0 && a->L > 0 && a->H > 0;
     if (some && (!x || !y))
         return IM2WIN_EINVAL;
-    if (a->rot > SEQ_ROTARY_MOST || a->D > 1 << 16 || a->B > INT32_MAX || a->L > INT32_MAX || a->H > INT32_MAX)
+    if (a->rot > SEQ_ROTARY_MOST || a->D > 1 << 16 || a->B > INT32_MAX || a->L > INT32_MAX || a->H >= 1 << 30)
         return IM2WIN_ERANGE;
     for (int64_t i = 0; i < a->rot / 2; ++i)
         if (!(fabs(a->freq[i]) <= kMaxFrequency))

@@ -345,6 +345,13 @@ def test_values_that_are_not_finite(types):
     assert torch.isnan(got[1, :4]).all() and torch.equal(gl[1], cl[1])
     for b, h in ((0, slice(0, 4)), (1, slice(4, 8)), (2, slice(0, 8))):
         assert torch.equal(got[b, h], clean[b, h]) and torch.equal(gl[b, h], cl[b, h])
+    kp, vp, table, scales = c.device()
+    q[2, 3, 7], q[0, 0, 0] = float("nan"), float("inf")
+    got, gl = pkg.seq_paged_attention_forward(q.cuda(), kp, vp, table, c.len.cuda(), **scales)
+    for b, h in ((2, 3), (0, 0)):  # scores of both signs and infinite
+        assert torch.isnan(got[b, h]).all() and torch.isnan(gl[b, h])
+        got[b, h], gl[b, h] = clean[b, h], cl[b, h]
+    assert torch.equal(got, clean) and torch.equal(gl, cl)
 
 
 @pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16), (F16, I8), (F16, E4M3)], ids=ids)

@@ -80,7 +80,7 @@ def test_rotary_refusals(lib, backward):
               {"f": float("nan")}, {"f": float("inf")}, {"xs": (-1, 64, 16)}, {"ys": (192, 64, -16)}):
         assert f(**k) == EINVAL, k
     for k in ({"D": 258, "rot": 258}, {"D": (1 << 16) + 2}, {"f": 1025.0}, {"f": -1025.0}, {"B": 1 << 31}, {"L": 1 << 31},
-              {"H": 1 << 31}, {"B": 1 << 20, "L": 1 << 20}, {"xs": (1 << 60, 64, 16)},
+              {"H": 1 << 30, "L": 1, "D": 2, "rot": 2}, {"B": 1 << 20, "L": 1 << 20}, {"xs": (1 << 60, 64, 16)},
               {"B": 1, "L": 1 << 30, "D": 64, "rot": 64}, {"B": 1 << 16, "L": 1 << 15, "H": (1 << 31) - 1, "xs": (0, 0, 0)}):
         assert f(**k) == ERANGE, k
     assert f(x=P + 1) == EALIGN and f(y=2 * P + 1) == EALIGN and f(pos=3 * P + 2) == EALIGN
