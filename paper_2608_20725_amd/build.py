@@ -1,4 +1,5 @@
-"""Builds libim2win.so (the C-ABI library and its gfx950 kernels) in-tree.
+"""Builds libim2win.so (the C-ABI library and its gfx950 kernels) and _seq_cache.so
+(the Python binding of the cache's calls) in-tree.
 
 Every HIP source is compiled for gfx950 only, with packed fp32 VALU
 instructions disabled (``-packed-fp32-ops``): the fp32 path uses plain
@@ -18,6 +19,10 @@ SOURCES = ["api.cpp", "plan.cpp", "chunked.cpp", "transform.hip", "conv_fp32.hip
            "seq_api.cpp", "seq_norm.hip", "seq_bias.hip", "seq_attn_fwd.hip", "seq_attn_decode.hip",
            "seq_attn_bwd.hip", "seq_cache_api.cpp", "seq_rotary.hip", "seq_cache.hip", "seq_paged.hip"]
 
+# The Python binding of the small serving calls: host code against torch's headers.
+BINDING = os.path.join(HERE, "_seq_cache.so")
+BINDING_SOURCE = "py_cache.cpp"
+
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "-x", "hip", "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -35,6 +40,26 @@ def _run(cmd):
     return p.returncode, noise
 
 
+def _binding_commands(obj, out):
+    """Compile and link commands of the binding."""
+    import importlib.util
+    import sysconfig
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    cxx = os.environ.get("CXX", "g++")
+    rocm = os.path.dirname(os.path.dirname(os.path.realpath(HIPCC)))
+    headers = [sysconfig.get_paths()["include"], os.path.join(rocm, "include"), os.path.join(torch, "include"),
+               os.path.join(torch, "include", "torch", "csrc", "api", "include")]
+    # HIP's and torch's headers ask which platform they are compiled for
+    compile_cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+                   "-I", os.path.join(ROOT, "include")]
+    for h in headers:
+        compile_cmd += ["-isystem", h]
+    compile_cmd += ["-c", os.path.join(CSRC, BINDING_SOURCE), "-o", obj]
+    link_cmd = [cxx, "-shared", obj, "-L", HERE, "-l:libim2win.so", "-Wl,-rpath,$ORIGIN", "-L", os.path.join(torch, "lib"),
+                "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip", "-o", out]
+    return compile_cmd, link_cmd
+
+
 def build(verbose: bool = False) -> str:
     """Compiles every source to an object (in parallel), then links them."""
     from concurrent.futures import ThreadPoolExecutor
@@ -45,6 +70,11 @@ def build(verbose: bool = False) -> str:
     for s in SOURCES:
         obj = os.path.join(objdir, os.path.splitext(s)[0] + ".o")
         jobs.append((obj, [HIPCC] + compile_flags + ["-c", os.path.join(CSRC, s), "-o", obj]))
+    binding_obj = os.path.join(objdir, os.path.splitext(BINDING_SOURCE)[0] + ".o")
+    binding_tmp = BINDING + ".tmp%d" % os.getpid()
+    binding_compile, binding_link = _binding_commands(binding_obj, binding_tmp)
+    objects = [j[0] for j in jobs]
+    jobs.append((binding_obj, binding_compile))
     workers = max(1, min(len(jobs), os.cpu_count() or 1, 16))
     with ThreadPoolExecutor(workers) as ex:
         results = list(ex.map(lambda j: _run(j[1]), jobs))
@@ -58,7 +88,7 @@ def build(verbose: bool = False) -> str:
     if failed:
         raise RuntimeError("hipcc failed building libim2win.so")
     tmp = LIB + ".tmp%d" % os.getpid()
-    cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC"] + [j[0] for j in jobs] + ["-o", tmp]
+    cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC"] + objects + ["-o", tmp]
     if verbose:
         print(" ".join(cmd), flush=True)
     rc, noise = _run(cmd)
@@ -66,6 +96,13 @@ def build(verbose: bool = False) -> str:
         sys.stderr.write("\n".join(noise) + "\n")
         raise RuntimeError("linking libim2win.so failed")
     os.replace(tmp, LIB)
+    if verbose:
+        print(" ".join(binding_link), flush=True)
+    rc, noise = _run(binding_link)
+    if rc != 0:
+        sys.stderr.write("\n".join(noise) + "\n")
+        raise RuntimeError("linking _seq_cache.so failed")
+    os.replace(binding_tmp, BINDING)
     return LIB
 
 

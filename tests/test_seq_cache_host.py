@@ -2,15 +2,14 @@
 structs' sizes, refusals of the C interface and of the binding, frequencies,
 and the walk through a page table.  No call here reaches a GPU."""
 import ctypes
-import math
 import os
+import struct
 import subprocess
 
 import pytest
 import torch
 
 import paper_2608_20725_amd as pkg
-from paper_2608_20725_amd import seq_cache
 from seq_cache_ref import frequencies
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -18,12 +17,29 @@ EINVAL, EALIGN, ERANGE, EWORKSPACE, EOVERLAP, EBUFFER = -1, -2, -3, -6, -7, -8
 P = 1 << 40  # an aligned address nothing is read from
 
 
+# seq_rotary_t: dt, interleaved, by_token, amplitude; B, L, H, D, rot; strides of x, y; positions, freq
+ROTARY = struct.Struct("@3if11q2P")
+# seq_cache_t: dt; B, pages, page, max_pages, Hkv, D; strides of k, v, their scales; table's; k, v, scales, table
+CACHE = struct.Struct("@i4x19q5P")
+# seq_paged_attention_t: dt, scale, cap; H; strides of q, out; R, strip, len
+PAGED = struct.Struct("@i2f4x6q2P")
+TRIPLE = struct.Struct("@3q")
+
+
 @pytest.fixture(scope="module")
 def lib():
     if not os.path.exists(pkg.library_path()):
         from paper_2608_20725_amd import build
         build.build()
-    return seq_cache._library()
+    lib = ctypes.CDLL(pkg.library_path())
+    text, i64, vp, int_ = ctypes.c_char_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int
+    lib.seq_rotary_forward.argtypes = lib.seq_rotary_backward.argtypes = [text, vp, vp, vp]
+    lib.seq_cache_write.argtypes = [text, vp, vp, text, text, i64, int_, vp, vp, vp]
+    lib.seq_cache_read.argtypes = [text, vp, vp, text, text, i64, int_, vp, vp]
+    lib.seq_paged_attention_workspace_bytes.restype = i64
+    lib.seq_paged_attention_workspace_bytes.argtypes = [text, i64, int_]
+    lib.seq_paged_attention_forward.argtypes = [text, text, vp, vp, vp, vp, i64, vp]
+    return lib
 
 
 def test_descriptions_have_the_structs_layout(tmp_path):
@@ -37,9 +53,9 @@ def test_descriptions_have_the_structs_layout(tmp_path):
     subprocess.run(["gcc", "-I", os.path.join(ROOT, "include"), str(src), "-o", exe], check=True)
     rot, b, freq, cache, stride, table, paged, length = map(
         int, subprocess.run([exe], capture_output=True, text=True, check=True).stdout.split())
-    r = seq_cache._ROTARY.pack(0, 0, 0, 0.0, 71, *([0] * 10), 0, 72)
-    c = seq_cache._CACHE.pack(0, *([0] * 18), 73, 0, 0, 0, 0, 74)
-    a = seq_cache._PAGED.pack(0, 0.0, 0.0, *([0] * 6), 0, 75)
+    r = ROTARY.pack(0, 0, 0, 0.0, 71, *([0] * 10), 0, 72)
+    c = CACHE.pack(0, *([0] * 18), 73, 0, 0, 0, 0, 74)
+    a = PAGED.pack(0, 0.0, 0.0, *([0] * 6), 0, 75)
     assert (len(r), len(c), len(a)) == (rot, cache, paged)
     at = lambda s, o: int.from_bytes(s[o:o + 8], "little")
     assert (at(r, b), at(r, freq), at(c, stride), at(c, table), at(a, length)) == (71, 72, 73, 74, 75)
@@ -67,7 +83,7 @@ def rotary(lib, x=P, y=2 * P, dt=1, B=2, L=3, H=4, D=16, rot=16, xs=None, ys=Non
            backward=False):
     dense = (L * H * D, H * D, D)
     host = (ctypes.c_double * 256)(*([f] * 256))
-    a = seq_cache._ROTARY.pack(dt, 0, 0, amplitude, B, L, H, D, rot, *(xs or dense), *(ys or dense), pos,
+    a = ROTARY.pack(dt, 0, 0, amplitude, B, L, H, D, rot, *(xs or dense), *(ys or dense), pos,
                                ctypes.addressof(host) if freq else 0)
     return (lib.seq_rotary_backward if backward else lib.seq_rotary_forward)(a, x, y, None)
 
@@ -93,7 +109,7 @@ def test_rotary_refusals(lib, backward):
 def cache(dt=1, B=2, pages=8, page=16, most=4, Hkv=2, D=64, ks=None, vs=None, kss=(0, 0, 0), vss=(0, 0, 0), ts=None, k=P,
           v=2 * P, k_scale=0, v_scale=0, table=3 * P):
     dense = (page * Hkv * D, Hkv * D, D)
-    return seq_cache._CACHE.pack(dt, B, pages, page, most, Hkv, D, *(ks or dense), *(vs or dense), *kss, *vss,
+    return CACHE.pack(dt, B, pages, page, most, Hkv, D, *(ks or dense), *(vs or dense), *kss, *vss,
                                  most if ts is None else ts, k or 0, v or 0, k_scale, v_scale, table or 0)
 
 
@@ -111,7 +127,7 @@ BAD_CACHE = [
 
 def copies(lib, c, k=4 * P, v=5 * P, ks=(8 * 128, 128, 64), vs=(8 * 128, 128, 64), L=8, dt=1, start=6 * P, count=7 * P,
            read=False):
-    t = seq_cache._TRIPLE
+    t = TRIPLE
     ks, vs = (None if s is None else t.pack(*s) for s in (ks, vs))
     if read:
         return lib.seq_cache_read(c, k, v, ks, vs, L, dt, count, None)
@@ -120,7 +136,7 @@ def copies(lib, c, k=4 * P, v=5 * P, ks=(8 * 128, 128, 64), vs=(8 * 128, 128, 64
 
 def attends(lib, c, dt=1, scale=0.1, cap=0.0, H=4, qs=(256, 64), os=(256, 64), R=0, strip=0, length=6 * P, q=4 * P,
             out=5 * P, lse=7 * P, ws=None, size=0):
-    a = seq_cache._PAGED.pack(dt, scale, cap, H, *qs, *os, R, strip, length or 0)
+    a = PAGED.pack(dt, scale, cap, H, *qs, *os, R, strip, length or 0)
     return lib.seq_paged_attention_forward(c, a, q, out, lse, ws, size, None)
 
 
@@ -174,7 +190,7 @@ def test_paged_attention_refusals(lib):
     assert ws(cache(most=4096), 4, 1) >= 2 * 2 * 4 * 68 * 4  # split: 4 rows of 64 sums each
 
 
-def test_binding_refusals():
+def test_binding_refusals(lib):
     k = torch.zeros(2, 3, 2, 64)
     pages, table, length = torch.zeros(4, 16, 2, 64), torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
     codes, scale = torch.zeros(4, 16, 2, 64, dtype=torch.int8), torch.zeros(4, 16, 2)
@@ -214,6 +230,22 @@ def test_binding_refusals():
             a(q, pages, pages, table, length, bias=bad)
     with pytest.raises(TypeError):
         a(q.half(), pages, pages, table, length)
+    for bad in ((None, pages, pages, table, length), (q, pages, pages, table, 3)):
+        with pytest.raises(TypeError):
+            a(*bad)
+    for bad in ((q, pages, pages, table, None), (q.double(), pages, pages, table, length)):
+        with pytest.raises(ValueError):
+            a(*bad)
+    with pytest.raises(TypeError):
+        pkg.seq_cache_read(pages, pages, table, length, 2.5)
+    with pytest.raises(ValueError):
+        pkg.seq_cache_read(pages, pages, table, length, -1)
+    # host memory is refused by its address
+    for call in (lambda: a(q, pages, pages, table, length), lambda: w(k, k, pages, pages.clone(), table),
+                 lambda: pkg.seq_cache_read(pages, pages, table, length, 8), lambda: pkg.seq_rotary_forward(k, freq)):
+        with pytest.raises(pkg.Im2winError) as e:
+            call()
+        assert e.value.status in (EBUFFER, -4) and "seq_" in str(e.value)
 
 
 def test_walk_through_a_table(tmp_path):
