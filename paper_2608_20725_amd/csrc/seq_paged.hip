@@ -87,8 +87,8 @@ struct Half<CodeE4M3> {
 
 // ---- the two products ----
 // E: type of the queries; Code: CodeI8, CodeE4M3 or void (pages of E itself); DP:
-// channels, 64 or 128, of which a head has D.
-template <class E, class Code, int DP>
+// channels, 64 or 128, of which a head has D; SMALL: tiles of 32 keys.
+template <class E, class Code, int DP, bool SMALL>
 struct Math {
     static constexpr bool kCodes = !__is_same(Code, void);
     static constexpr bool kWide = __is_same(E, EltF32) && !kCodes;  // fp32 instructions
@@ -102,8 +102,10 @@ struct Math {
     static constexpr int VC = DP / 16;       // channels of a value that a lane takes: VC*(lane % 16) on
     // A tile's bytes are what a wave keeps on its way: 64 keys where they are short.
     // 48 caches of up to 16384 tokens, 64 heads of 128 over 8, int8 under bf16: 362
-    // us with tiles of 32 keys, 245 with 64.
-    static constexpr int KEYS = DP * ES <= 128 ? 64 : 32;
+    // us with tiles of 32 keys, 245 with 64.  Where a tile a wave is all there is to
+    // do, 32 are done sooner: one cache of 2000, 16 heads of 64 over 4, fp16: 7.9 us
+    // with 64, 6.6 with 32.
+    static constexpr int KEYS = DP * ES <= 128 && !SMALL ? 64 : 32;
     static constexpr int N = KEYS / 4;       // keys of a lane: 16*(i >> 2) + 4*group + (i & 3)
 
     struct __attribute__((aligned(VC * ES < 16 ? VC * ES : 16))) Value {
@@ -323,10 +325,10 @@ __device__ inline float *part_of(const PagedArgs &a, int64_t index, int head, in
 }
 
 // FULL: heads have DP channels, no more tests of where they end.
-template <class E, class Code, int DP, bool FULL>
+template <class E, class Code, int DP, bool FULL, bool SMALL>
 __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs a)
 {
-    typedef Math<E, Code, DP> M;
+    typedef Math<E, Code, DP, SMALL> M;
     constexpr int KEYS = M::KEYS, N = M::N, VC = M::VC, ES = M::ES;
     // fp16 probabilities are times 2^14, so that those of long rows stay normal numbers
     constexpr float kShift = M::kHalf ? 14.0f : 0.0f, kUnshift = M::kHalf ? 0x1p-14f : 1.0f;
@@ -457,6 +459,22 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
         }
     };
 
+    // The bias of a tile's scores, loaded before its values: loads end in the order
+    // they start, so that scores do not wait for the values or for later keys.
+    // 32 caches of 2048 to 8192 tokens, 8 heads of 128, bf16: 157 us where scores
+    // load it, 137 here.  fp32 queries over 64 keys of 8-bit pages have no registers
+    // for that: they load it after the products, before the next keys (int8: 125
+    // us, 112 here with spills, 102 so).
+    constexpr bool kEarly = !(M::kTerms == 2 && DP == 128 && KEYS == 64);
+    float near[N];
+    auto load_bias = [&](int k0) {
+        if (a.R > 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                near[i] = strip[min(max(k0 + 16 * (i >> 2) + 4 * g + (i & 3) - (n - 1), -a.R), 0)];
+        }
+    };
+
     f32x4_acc o[VC];
 #pragma unroll
     for (int j = 0; j < VC; ++j)
@@ -472,6 +490,8 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
         tell(id, in);
         wave_lds_handoff();
         load_keys();
+        if (kEarly)
+            load_bias(first);
         load_values();
     }
     int id1 = page_at(first + step), in1 = inside(first + step);
@@ -497,6 +517,8 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
                 vscale[i] = my.vs[16 * (i >> 2) + 4 * g + (i & 3)];
             }
         }
+        if (!kEarly)
+            load_bias(k0);
         // the next tile's keys
         id = id1, in = in1;
         tell(id, in);
@@ -526,7 +548,6 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int at = 16 * (i >> 2) + 4 * g + (i & 3);
             float x = s[i] * c1;
             if constexpr (M::kCodes)
                 x *= kscale[i];
@@ -535,7 +556,7 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
                 x = c2 * (fabsf(x) < kSmallTanh ? small_tanh(x) : far);
             }
             if (a.R > 0)
-                x += strip[min(max(k0 + at - (n - 1), -a.R), 0)] * kLog2e;
+                x += near[i] * kLog2e;
             s[i] = x;
         }
         const bool whole = (KEYS == 64 ? ~there : (uint32_t)~there) == 0;
@@ -575,8 +596,11 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
         }
         M::pack(w);
         M::sum(o, vr, w);
-        if (more)
+        if (more) {
+            if (kEarly)
+                load_bias(k0 + step);
             load_values();
+        }
     }
 
     // join the waves of each 16 queries
@@ -721,6 +745,7 @@ __global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int group
 // workgroup takes a whole sequence (most_parts 0).
 struct Plan {
     int32_t row_waves, row_tiles, step;
+    bool small;
     int64_t most_parts, parts;  // parts: that the lengths can make at most
 };
 // Workgroups that share the keys, two rounds of the two that fit a CU.  Measured
@@ -735,40 +760,53 @@ Plan plan_of(const Pool &c, int ct, int64_t B, int64_t H, int dt)
     const int64_t G = H / c.Hkv, bytes = (c.D <= 64 ? 64 : 128) * (ct != dt ? 1 : dt == IM2WIN_F32 ? 4 : 2);
     p.row_waves = G <= 16 ? 1 : G <= 32 ? 2 : 4;
     p.row_tiles = (int32_t)((G + 16 * p.row_waves - 1) / (16 * p.row_waves));
-    p.step = (bytes <= 128 ? 64 : 32) * (kWavesP / p.row_waves);  // keys: see Math
-    const int64_t heads = c.Hkv * p.row_tiles, steps = ((int64_t)c.max_pages * c.page.d + p.step - 1) / p.step;
+    const int64_t heads = c.Hkv * p.row_tiles, most = (int64_t)c.max_pages * c.page.d;
+    const int32_t waves = kWavesP / p.row_waves;
+    p.small = bytes <= 128 && B * heads <= kTarget / 2 && (most + 32 * waves - 1) / (32 * waves) * B * heads <= kTarget / 2;
+    p.step = (bytes <= 128 && !p.small ? 64 : 32) * waves;  // keys: see Math
+    const int64_t steps = (most + p.step - 1) / p.step;
     p.most_parts = steps <= 1 || B > 512 || B * heads >= 16 * kTarget ? 0 : (kTarget + heads - 1) / heads;
     p.parts = p.most_parts ? (p.most_parts + B < B * steps ? p.most_parts + B : B * steps) : B;
     return p;
 }
 
-template <class E, class Code, int DP>
+template <class E, class Code, int DP, bool SMALL>
 void run_full(uint32_t grid, const Pool &c, const PagedArgs &a, hipStream_t st)
 {
     if (c.D == DP)
-        paged_attn<E, Code, DP, true><<<grid, 64 * kWavesP, 0, st>>>(c, a);
+        paged_attn<E, Code, DP, true, SMALL><<<grid, 64 * kWavesP, 0, st>>>(c, a);
     else
-        paged_attn<E, Code, DP, false><<<grid, 64 * kWavesP, 0, st>>>(c, a);
+        paged_attn<E, Code, DP, false, SMALL><<<grid, 64 * kWavesP, 0, st>>>(c, a);
+}
+
+template <class E, class Code, int DP>
+void run_small(bool small, uint32_t grid, const Pool &c, const PagedArgs &a, hipStream_t st)
+{
+    if constexpr (Math<E, Code, DP, false>::KEYS == 64)
+        if (small)
+            return run_full<E, Code, DP, true>(grid, c, a, st);
+    run_full<E, Code, DP, false>(grid, c, a, st);
 }
 
 template <class E, class Code>
-void run(const Pool &c, const PagedArgs &a, int32_t step, hipStream_t st)
+void run(const Plan &p, const Pool &c, const PagedArgs &a, hipStream_t st)
 {
     const uint32_t grid = (uint32_t)((a.parts + a.spread - 1) / a.spread * a.spread * c.Hkv) * a.row_tiles;
-    c.D <= 64 ? run_full<E, Code, 64>(grid, c, a, st) : run_full<E, Code, 128>(grid, c, a, st);
+    c.D <= 64 ? run_small<E, Code, 64>(p.small, grid, c, a, st) : run_small<E, Code, 128>(p.small, grid, c, a, st);
     if (a.most_parts) {
         const int64_t rows = (int64_t)a.B * a.H;
         const int groups = rows <= 2048 ? 8 : 1;
-        paged_join<E, Math<E, Code, 64>::kHalf><<<(uint32_t)((rows * groups + 7) / 8), 256, 0, st>>>(c, a, groups, step);
+        paged_join<E, Math<E, Code, 64, false>::kHalf><<<(uint32_t)((rows * groups + 7) / 8), 256, 0, st>>>(c, a, groups,
+                                                                                                        p.step);
     }
 }
 
 template <class E>
-void run_code(const Pool &c, int ct, const PagedArgs &a, int32_t step, hipStream_t st)
+void run_code(const Plan &p, const Pool &c, int ct, const PagedArgs &a, hipStream_t st)
 {
-    ct == SEQ_I8     ? run<E, CodeI8>(c, a, step, st)
-    : ct == SEQ_E4M3 ? run<E, CodeE4M3>(c, a, step, st)
-                     : run<E, void>(c, a, step, st);
+    ct == SEQ_I8     ? run<E, CodeI8>(p, c, a, st)
+    : ct == SEQ_E4M3 ? run<E, CodeE4M3>(p, c, a, st)
+                     : run<E, void>(p, c, a, st);
 }
 
 }  // namespace
@@ -786,11 +824,11 @@ hipError_t launch_paged(const Pool &c, int ct, PagedArgs a, int dt, hipStream_t 
     a.row_waves = p.row_waves, a.row_tiles = p.row_tiles;
     a.spread = c.Hkv > 1 && (c.k_head | c.v_head) % 128 != 0 ? 8 : 1;
     if (dt == IM2WIN_F32)
-        run_code<EltF32>(c, ct, a, p.step, st);
+        run_code<EltF32>(p, c, ct, a, st);
     else if (dt == IM2WIN_F16)
-        run_code<EltF16>(c, ct, a, p.step, st);
+        run_code<EltF16>(p, c, ct, a, st);
     else
-        run_code<EltBF16>(c, ct, a, p.step, st);
+        run_code<EltBF16>(p, c, ct, a, st);
     return hipGetLastError();
 }
 
