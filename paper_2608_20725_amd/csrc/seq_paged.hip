@@ -740,9 +740,14 @@ __global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int group
     }
 }
 
-// Where no sequence can have two steps, and where there are enough of them to
-// even out by themselves (or so many that each wave's scan would cost more), a
-// workgroup takes a whole sequence (most_parts 0).
+// Where no sequence can have more than a few steps, a workgroup takes a whole one
+// (most_parts 0): a step more takes less than the join's launch.  One sequence of
+// 256, 384, 512 and 768 tokens (steps of 128), split and whole, in a graph: 16
+// heads of 64 over 4, fp16 10.2, 10.3, 10.3, 10.4 and 6.3, 7.8, 9.2, 11.8 us; 32 of
+// 128 over 8, bf16 11.1, 11.2, 11.2, 11.2 and 7.5, 9.3, 10.9, 14.2; four of 8 heads of
+// 80, fp32 13.9, 14.1, 14.1, 14.2 and 12.0, 15.8, 19.7, 28.6.  So too where there are
+// enough sequences to even out by themselves, or so many that each wave's scan
+// would cost more.
 struct Plan {
     int32_t row_waves, row_tiles, step;
     bool small;
@@ -765,7 +770,8 @@ Plan plan_of(const Pool &c, int ct, int64_t B, int64_t H, int dt)
     p.small = bytes <= 128 && B * heads <= kTarget / 2 && (most + 32 * waves - 1) / (32 * waves) * B * heads <= kTarget / 2;
     p.step = (bytes <= 128 && !p.small ? 64 : 32) * waves;  // keys: see Math
     const int64_t steps = (most + p.step - 1) / p.step;
-    p.most_parts = steps <= 1 || B > 512 || B * heads >= 16 * kTarget ? 0 : (kTarget + heads - 1) / heads;
+    const int64_t few = ct == IM2WIN_F32 ? 2 : 4;
+    p.most_parts = steps <= few || B > 512 || B * heads >= 16 * kTarget ? 0 : (kTarget + heads - 1) / heads;
     p.parts = p.most_parts ? (p.most_parts + B < B * steps ? p.most_parts + B : B * steps) : B;
     return p;
 }
