@@ -85,9 +85,13 @@ struct Half<CodeE4M3> {
     }
 };
 
+// Keys of a tile, of `bytes` each in a page: two sizes, but for 16 bits and 128
+// channels, whose products take 32 keys at once.
+constexpr int tile_keys(int64_t bytes, bool small) { return bytes <= 128 ? (small ? 32 : 64) : bytes > 256 && small ? 16 : 32; }
+
 // ---- the two products ----
 // E: type of the queries; Code: CodeI8, CodeE4M3 or void (pages of E itself); DP:
-// channels, 64 or 128, of which a head has D; SMALL: tiles of 32 keys.
+// channels, 64 or 128, of which a head has D; SMALL: the smaller tiles.
 template <class E, class Code, int DP, bool SMALL>
 struct Math {
     static constexpr bool kCodes = !__is_same(Code, void);
@@ -105,7 +109,7 @@ struct Math {
     // us with tiles of 32 keys, 245 with 64.  Where a tile a wave is all there is to
     // do, 32 are done sooner: one cache of 2000, 16 heads of 64 over 4, fp16: 7.9 us
     // with 64, 6.6 with 32.
-    static constexpr int KEYS = DP * ES <= 128 && !SMALL ? 64 : 32;
+    static constexpr int KEYS = tile_keys(DP * ES, SMALL);
     static constexpr int N = KEYS / 4;       // keys of a lane: 16*(i >> 2) + 4*group + (i & 3)
 
     struct __attribute__((aligned(VC * ES < 16 ? VC * ES : 16))) Value {
@@ -117,7 +121,7 @@ struct Math {
     };
     struct Weights {
         float p[N];
-        u32x4_t packed[kTerms][N / 8];
+        u32x4_t packed[kTerms][N > 8 ? N / 8 : 1];
     };
 
     __device__ static inline void set(Query &q, int at, float x)
@@ -363,39 +367,6 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
 
     // this lane's query: column r of the wave's
     const int row0 = (rt * a.row_waves) * 16, row = row0 + wave % a.row_waves * 16 + r;
-    typename M::Query q;
-    float c1 = a.cap > 0 ? a.scale / a.cap : a.scale * kLog2e;
-    {
-        const typename E::T *const p = (const typename E::T *)(a.q + b * a.q_sb + (hk * a.G + row) * a.q_sh);
-        float x[M::NK * M::EPC];
-        uint32_t top = 0;
-#pragma unroll
-        for (int k = 0; k < M::NK; ++k)
-#pragma unroll
-            for (int e = 0; e < M::EPC; e += 4) {
-                typedef typename E::T V4 __attribute__((ext_vector_type(4)));
-                const int ch = (4 * k + g) * M::EPC + e;
-                V4 v = {};
-                if (row < a.G && ch < D)
-                    v = *(const V4 *)(p + ch);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x[k * M::EPC + e + i] = E::get(v[i]);
-                    top = max(top, __builtin_bit_cast(uint32_t, x[k * M::EPC + e + i]) & 0x7FFFFFFFu);
-                }
-            }
-        float f = 1.0f;
-        if constexpr (M::kRange) {
-            top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-            top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-            const int e = max((int)(top >> 23) - 127, -100);  // the row's largest becomes 2^14 .. 2^15
-            f = __builtin_bit_cast(float, (uint32_t)(127 + 14 - e) << 23);
-            c1 *= __builtin_bit_cast(float, (uint32_t)(127 - 14 + e) << 23);
-        }
-#pragma unroll
-        for (int k = 0; k < M::NK * M::EPC; ++k)
-            M::set(q, k, x[k] * f);
-    }
     const float c2 = a.cap * kLog2e;
     const float *const strip = a.strip + (int64_t)min(hk * a.G + row, a.H - 1) * (2 * a.R + 1) + a.R;
 
@@ -419,7 +390,7 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
     auto tell = [&](int id, int in) {
         if (KEYS == 64 || lane < KEYS)
             my.k[lane % KEYS] = id < 0 ? 0 : id * c.k_page + in * c.k_tok;
-        if (KEYS == 64 || lane >= KEYS)
+        if (KEYS == 64 || lane >= 64 - KEYS)
             my.v[lane % KEYS] = id < 0 ? 0 : id * c.v_page + in * c.v_tok;
     };
     u32x4_t kr[KEYS / 16][M::NK];
@@ -462,10 +433,10 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
     // The bias of a tile's scores, loaded before its values: loads end in the order
     // they start, so that scores do not wait for the values or for later keys.
     // 32 caches of 2048 to 8192 tokens, 8 heads of 128, bf16: 157 us where scores
-    // load it, 137 here.  fp32 queries over 64 keys of 8-bit pages have no registers
-    // for that: they load it after the products, before the next keys (int8: 125
-    // us, 112 here with spills, 102 so).
-    constexpr bool kEarly = !(M::kTerms == 2 && DP == 128 && KEYS == 64);
+    // load it, 137 here.  fp32 queries of 128 channels over 64 keys of 8-bit pages or
+    // 32 of their own type have no registers for that: they load it after the
+    // products, before the next keys (int8: 125 us, 112 here with spills, 102 so).
+    constexpr bool kEarly = !(__is_same(E, EltF32) && DP == 128 && KEYS == (M::kCodes ? 64 : 32));
     float near[N];
     auto load_bias = [&](int k0) {
         if (a.R > 0) {
@@ -482,8 +453,50 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
     float m = -INFINITY, l = 0;
     float unit = 0x1p-126f;  // 8 bits: the values' scales are over this power of two
 
+    // The first loads start in the order in which they are needed last: pages'
+    // numbers, the query (made into operands while keys and values come), keys.
     const int first = part.lo + wave / a.row_waves * KEYS;
     int id = page_at(first), in = inside(first);
+    int id1 = page_at(first + step), in1 = inside(first + step);
+    typedef typename E::T V4 __attribute__((ext_vector_type(4)));
+    V4 raw[M::NK * M::EPC / 4];
+    {
+        const typename E::T *const p = (const typename E::T *)(a.q + b * a.q_sb + (hk * a.G + row) * a.q_sh);
+#pragma unroll
+        for (int k = 0; k < M::NK * M::EPC / 4; ++k) {
+            const int ch = (4 * (4 * k / M::EPC) + g) * M::EPC + 4 * k % M::EPC;
+            raw[k] = V4{};
+            if (row < a.G && ch < D)
+                raw[k] = *(const V4 *)(p + ch);
+        }
+    }
+    typename M::Query q;
+    float c1 = a.cap > 0 ? a.scale / a.cap : a.scale * kLog2e;
+    auto make_query = [&]() {
+        float x[M::NK * M::EPC];
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < M::NK * M::EPC; ++k) {
+            x[k] = E::get(raw[k / 4][k % 4]);
+            top = max(top, __builtin_bit_cast(uint32_t, x[k]) & 0x7FFFFFFFu);
+        }
+        float f = 1.0f;
+        if constexpr (M::kRange) {
+            top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+            top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+            const int e = max((int)(top >> 23) - 127, -100);  // the row's largest becomes 2^14 .. 2^15
+            f = __builtin_bit_cast(float, (uint32_t)(127 + 14 - e) << 23);
+            c1 *= __builtin_bit_cast(float, (uint32_t)(127 - 14 + e) << 23);
+        }
+#pragma unroll
+        for (int k = 0; k < M::NK * M::EPC; ++k)
+            M::set(q, k, x[k] * f);
+    };
+    // Of 8-bit pages the query is made at once: its conversion takes the registers
+    // that the tile's would be waiting in (48 caches of up to
+    // 16384 tokens, int8 under bf16: 215 us, 221 the other way).
+    if (M::kCodes)
+        make_query();
     float ks = 0, vs = 0;
     if (first < hi) {
         load_scales(id, in, ks, vs);
@@ -494,7 +507,8 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
             load_bias(first);
         load_values();
     }
-    int id1 = page_at(first + step), in1 = inside(first + step);
+    if (!M::kCodes)
+        make_query();
     for (int k0 = first; k0 < hi; k0 += step) {
         float s[N];
 #pragma unroll
@@ -767,8 +781,9 @@ Plan plan_of(const Pool &c, int ct, int64_t B, int64_t H, int dt)
     p.row_tiles = (int32_t)((G + 16 * p.row_waves - 1) / (16 * p.row_waves));
     const int64_t heads = c.Hkv * p.row_tiles, most = (int64_t)c.max_pages * c.page.d;
     const int32_t waves = kWavesP / p.row_waves;
-    p.small = bytes <= 128 && B * heads <= kTarget / 2 && (most + 32 * waves - 1) / (32 * waves) * B * heads <= kTarget / 2;
-    p.step = (bytes <= 128 && !p.small ? 64 : 32) * waves;  // keys: see Math
+    const int32_t least = tile_keys(bytes, true) * waves;
+    p.small = B * heads <= kTarget / 2 && (most + least - 1) / least * B * heads <= kTarget / 2;
+    p.step = tile_keys(bytes, p.small) * waves;
     const int64_t steps = (most + p.step - 1) / p.step;
     const int64_t few = ct == IM2WIN_F32 ? 2 : 4;
     p.most_parts = steps <= few || B > 512 || B * heads >= 16 * kTarget ? 0 : (kTarget + heads - 1) / heads;
@@ -788,7 +803,7 @@ void run_full(uint32_t grid, const Pool &c, const PagedArgs &a, hipStream_t st)
 template <class E, class Code, int DP>
 void run_small(bool small, uint32_t grid, const Pool &c, const PagedArgs &a, hipStream_t st)
 {
-    if constexpr (Math<E, Code, DP, false>::KEYS == 64)
+    if constexpr (Math<E, Code, DP, false>::KEYS != Math<E, Code, DP, true>::KEYS)
         if (small)
             return run_full<E, Code, DP, true>(grid, c, a, st);
     run_full<E, Code, DP, false>(grid, c, a, st);
