@@ -7,9 +7,11 @@
 // as good as one of position 1 (an fp32 product would be off by 2^-24 of
 // p*freq, 8e-3 radians at 131072) and needs no reduction beyond its octant.
 // Bound by the bytes: each value is read and written once.  A lane takes 16
-// bytes of a head's channels and of their partners, and the same channels of
-// kHeads heads of the token, so that an angle's sine and cosine (40 operations a
-// pair) are spread over them.
+// bytes of a head's channels and of their partners, and the same channels of up
+// to four heads of the token, so that an angle's sine and cosine (30 operations a
+// pair) are spread over them; all of it is loaded before the angles are made.
+// Backward, 8 rows of 4096 tokens, 40 heads of 128, bf16: 129 us, 5.2 TB/s (144
+// with the angles first).
 #include "seq_rotary.hpp"
 
 namespace im2win {
@@ -35,42 +37,34 @@ __device__ inline void cos_sin(uint32_t turn, float &c, float &s)
     s = q & 2 ? -s : s;
 }
 
-// n of N values from p on as fp32, or back; whole vectors with their element's
-// alignment, as rotated parts and strides may start anywhere.
-template <class E, int N>
-__device__ inline void load(const char *p, int n, float *f)
-{
-    typedef typename E::T T;
+// N values from p on, n of them there, as they lie in memory; whole vectors with
+// their element's alignment, as rotated parts and strides may start anywhere.
+template <class T, int N>
+struct Run {
     typedef T V __attribute__((ext_vector_type(N), aligned(sizeof(T))));
-    if (n >= N) {
-        const V v = *(const V *)p;
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            f[e] = E::get(v[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            f[e] = e < n ? E::get(((const T *)p)[e]) : 0.0f;
-    }
-}
-template <class E, int N>
-__device__ inline void store(char *p, int n, const float *f)
-{
-    typedef typename E::T T;
-    typedef T V __attribute__((ext_vector_type(N), aligned(sizeof(T))));
-    if (n >= N) {
-        V v;
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            v[e] = E::put(f[e]);
-        *(V *)p = v;
-    } else {
+    __device__ static inline V load(const char *p, int n)
+    {
+        if (n >= N)
+            return *(const V *)p;
+        V v = {};
 #pragma unroll
         for (int e = 0; e < N; ++e)
             if (e < n)
-                ((T *)p)[e] = E::put(f[e]);
+                v[e] = ((const T *)p)[e];
+        return v;
     }
-}
+    __device__ static inline void store(char *p, int n, const V &v)
+    {
+        if (n >= N) {
+            *(V *)p = v;
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (e < n)
+                ((T *)p)[e] = v[e];
+    }
+};
 
 // Lanes: units of a head fastest, then groups of heads, then tokens.  A unit is
 // N pairs (N values and their N partners; side by side, 2N values in a row),
@@ -106,6 +100,25 @@ __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a, Turns f)
         return;
     }
     const int first = unit * N, n = half - first;  // pairs first .. first + min(n, N) - 1
+    const int at = (PAIRED ? 2 * first : first) * sizeof(T), to = half * sizeof(T);
+    // this lane's heads: group, group + groups, ..
+    typedef Run<T, N> R;
+    typedef Run<T, W> RW;
+    typename R::V u[HEADS], v[HEADS];  // the pairs' two sides; side by side, all of them in w
+    typename RW::V w[HEADS];
+#pragma unroll
+    for (int k = 0; k < HEADS; ++k) {
+        const int h = group + k * a.groups.d;
+        if (h >= a.H)
+            break;
+        const char *const p = x + h * a.x_sh + at;
+        if constexpr (PAIRED) {
+            w[k] = RW::load(p, 2 * n);
+        } else {
+            u[k] = R::load(p, n);
+            v[k] = R::load(p + to, n);
+        }
+    }
     int64_t pos = t;
     if (a.pos)
         pos = a.by_token ? (int64_t)a.pos[token] : (int64_t)a.pos[b] + t;
@@ -117,48 +130,27 @@ __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a, Turns f)
         c[e] *= a.amplitude;
         s[e] *= a.sin_amplitude;
     }
-    const int at = (PAIRED ? 2 * first : first) * sizeof(T), to = half * sizeof(T);
-    for (int h0 = group; h0 < a.H; h0 += HEADS * a.groups.d) {
-        float u[HEADS][N], v[HEADS][N];
 #pragma unroll
-        for (int k = 0; k < HEADS; ++k) {
-            const int h = h0 + k * a.groups.d;
-            if (h >= a.H)
-                break;
-            const char *const p = x + h * a.x_sh + at;
-            if constexpr (PAIRED) {
-                float w[W];
-                load<E, W>(p, 2 * n, w);
+    for (int k = 0; k < HEADS; ++k) {
+        const int h = group + k * a.groups.d;
+        if (h >= a.H)
+            break;
+        char *const o = y + h * a.y_sh + at;
 #pragma unroll
-                for (int e = 0; e < N; ++e)
-                    u[k][e] = w[2 * e], v[k][e] = w[2 * e + 1];
-            } else {
-                load<E, N>(p, n, u[k]);
-                load<E, N>(p + to, n, v[k]);
-            }
+        for (int e = 0; e < N; ++e) {
+            const float p = E::get(PAIRED ? w[k][PAIRED ? 2 * e : 0] : u[k][e]);
+            const float q = E::get(PAIRED ? w[k][PAIRED ? 2 * e + 1 : 0] : v[k][e]);
+            const T yp = E::put(p * c[e] - q * s[e]), yq = E::put(p * s[e] + q * c[e]);
+            if constexpr (PAIRED)
+                w[k][2 * e] = yp, w[k][2 * e + 1] = yq;
+            else
+                u[k][e] = yp, v[k][e] = yq;
         }
-#pragma unroll
-        for (int k = 0; k < HEADS; ++k) {
-            const int h = h0 + k * a.groups.d;
-            if (h >= a.H)
-                break;
-            char *const o = y + h * a.y_sh + at;
-            float p[N], q[N];
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                p[e] = u[k][e] * c[e] - v[k][e] * s[e];
-                q[e] = u[k][e] * s[e] + v[k][e] * c[e];
-            }
-            if constexpr (PAIRED) {
-                float w[W];
-#pragma unroll
-                for (int e = 0; e < N; ++e)
-                    w[2 * e] = p[e], w[2 * e + 1] = q[e];
-                store<E, W>(o, 2 * n, w);
-            } else {
-                store<E, N>(o, n, p);
-                store<E, N>(o + to, n, q);
-            }
+        if constexpr (PAIRED) {
+            RW::store(o, 2 * n, w[k]);
+        } else {
+            R::store(o, n, u[k]);
+            R::store(o + to, n, v[k]);
         }
     }
 }
@@ -167,8 +159,7 @@ template <class E, bool PAIRED>
 void run(const RotaryArgs &a, const Turns &f, hipStream_t st)
 {
     const uint32_t grid = (a.lanes + kThreads - 1) / kThreads;
-    const int each = (a.H + a.groups.d - 1) / a.groups.d;  // heads of a lane
-    if (each >= 4)
+    if ((uint32_t)a.H > a.groups.d)  // up to 4 heads a lane
         rotary<E, PAIRED, 4><<<grid, kThreads, 0, st>>>(a, f);
     else
         rotary<E, PAIRED, 1><<<grid, kThreads, 0, st>>>(a, f);
@@ -189,7 +180,8 @@ bool plan_rotary(RotaryArgs &a, int64_t B, int64_t L, bool paired, bool in_place
     const int64_t units = a.pair_units + (in_place ? 0 : (a.D - a.rot + W - 1) / W);
     if (B * L * units > UINT32_MAX)  // so that the products below fit
         return false;
-    // Heads a lane: 4 where that leaves 2^17 lanes or more (512 a CU).
+    // Heads a lane: 4 where that leaves 2^17 lanes or more (512 a CU), else one, for
+    // the least time of a lane.
     const int64_t one = B * L * units * a.H;
     int64_t groups = a.H;
     if (one >= (int64_t)1 << 19)
