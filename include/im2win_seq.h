@@ -261,8 +261,10 @@ int seq_cache_read(const seq_cache_t *c, void *k, void *v, const int64_t *k_stri
  *   lse     [B][H] fp32
  *   ws      seq_paged_attention_workspace_bytes(c, H, dt) bytes, 16-byte aligned
  * H a multiple of Hkv, B*H < 2^24.  Numerics as in seq_attention_forward;
- * 8-bit codes beside 16-bit queries are multiplied in fp16, which holds them
- * exactly.
+ * 8-bit codes are multiplied in fp16, which holds them exactly (fp32 queries
+ * and weights as two fp16 terms).  The keys of all sequences are shared evenly
+ * between workgroups, so a sequence's sums are split, and rounded, by the lengths
+ * of the others too; the same call gives the same bits.
  */
 typedef struct {
     int dt; /* im2win_dtype_t */

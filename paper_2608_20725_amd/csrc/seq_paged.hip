@@ -234,9 +234,8 @@ struct Where {
 // All workgroups take about the same number of keys, whichever sequence they
 // belong to: with a share of total/most_parts keys (whole steps) or, where that
 // is little, twice as many, a sequence of n keys makes ceil(n/share) parts of
-// equal size.  The lengths are known on the
-// GPU only, so each wave adds them up and finds its part by a scan over the
-// sequences' counts.
+// equal size.  The lengths are known on the GPU only, so each wave adds them up
+// and finds its part by a scan over the sequences' counts.
 struct Cut {
     int32_t parts, piece;  // parts of a sequence, keys of each (the last has what is left)
 };
@@ -493,8 +492,8 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
             M::set(q, k, x[k] * f);
     };
     // Of 8-bit pages the query is made at once: its conversion takes the registers
-    // that the tile's would be waiting in (48 caches of up to
-    // 16384 tokens, int8 under bf16: 215 us, 221 the other way).
+    // that the tile's would be waiting in (48 caches of up to 16384 tokens, int8
+    // under bf16: 215 us, 221 the other way).
     if (M::kCodes)
         make_query();
     float ks = 0, vs = 0;

@@ -230,20 +230,26 @@ def test_attention(types, case):
         check(gl, lse, tl + 1e-30, "lse %d" % k)
 
 
+@pytest.mark.parametrize("D,G", [(64, 3), (128, 4), (72, 17), (128, 40), (40, 1)])
 @pytest.mark.parametrize("types", PAIRS, ids=ids)
-def test_a_table_far_longer_than_its_sequences(types):
-    """Few keys and many parts wanted: parts without keys, and one sequence
-    beside empty ones."""
+def test_a_table_far_longer_than_its_sequences(types, D, G):
+    """Few keys and many parts wanted: parts without keys, one sequence beside
+    empty ones; and the larger tiles, which a table of this width chooses."""
     dt, ct = types
-    lens = [3, 0, 400, 129]
-    c = Cache(lens, 16, 2, 64, dt, ct, wide=2000)
-    q = torch.randn((4, 6, 64), generator=torch.Generator().manual_seed(1)).to(dt)
-    out, lse, tol, tl = attention(q, c)
-    kp, vp, table, scales = c.device()
-    got, gl = pkg.seq_paged_attention_forward(q.cuda(), kp, vp, table, c.len.cuda(), **scales)
-    check(got, out, tol + 1e-30, "out")
-    check(gl, lse, tl + 1e-30, "lse")
-    assert not got[1].any() and torch.isneginf(gl[1]).all()
+    lens = [3, 0, 400, 129, 1301]
+    g = torch.Generator().manual_seed(1)
+    for heads_first in (False, True):
+        c = Cache(lens, 16, 2, D, dt, ct, wide=2000, heads_first=heads_first)
+        q = torch.randn((5, 2 * G, D), generator=g).to(dt)
+        bias = torch.randn((2 * G, 2 * 60 + 1), generator=g) if heads_first else None
+        cap = 25.0 if heads_first else 0.0
+        out, lse, tol, tl = attention(q, c, bias=bias, cap=cap)
+        kp, vp, table, scales = c.device()
+        got, gl = pkg.seq_paged_attention_forward(q.cuda(), kp, vp, table, c.len.cuda(), cap=cap,
+                                                  bias=None if bias is None else bias.cuda(), **scales)
+        check(got, out, tol + 1e-30, "out")
+        check(gl, lse, tl + 1e-30, "lse")
+        assert not got[1].any() and torch.isneginf(gl[1]).all()
 
 
 @pytest.mark.parametrize("types", PAIRS, ids=ids)
