@@ -68,12 +68,12 @@ struct Run {
 
 // Lanes: units of a head fastest, then groups of heads, then tokens.  A unit is
 // N pairs (N values and their N partners; side by side, 2N values in a row),
-// behind them, where x is not y, 2N channels that are copied.
-template <class E, bool PAIRED, int HEADS>
-__global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a, Turns f)
+// behind them, where x is not y, as many channels that are copied.
+template <class E, bool PAIRED, int N, int HEADS, int PAIRS>
+__global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a, TurnsOf<PAIRS> f)
 {
     typedef typename E::T T;
-    constexpr int N = PAIRED ? 8 / sizeof(T) : 16 / sizeof(T), W = PAIRED ? 2 * N : N;
+    constexpr int W = PAIRED ? 2 * N : N;
     const uint32_t id = blockIdx.x * kThreads + threadIdx.x;
     if (id >= a.lanes)
         return;
@@ -155,36 +155,53 @@ __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a, Turns f)
     }
 }
 
+// Pairs of a unit: 16 bytes of a side (of both, side by side).
 template <class E, bool PAIRED>
-void run(const RotaryArgs &a, const Turns &f, hipStream_t st)
+constexpr int kPairs = (PAIRED ? 8 : 16) / sizeof(typename E::T);
+// Pairs of a unit in small calls, see plan_rotary.
+constexpr int kFew = 2;
+
+template <class E, bool PAIRED, int PAIRS>
+void run(const RotaryArgs &a, const TurnsOf<PAIRS> &f, hipStream_t st)
 {
     const uint32_t grid = (a.lanes + kThreads - 1) / kThreads;
     if ((uint32_t)a.H > a.groups.d)  // up to 4 heads a lane
-        rotary<E, PAIRED, 4><<<grid, kThreads, 0, st>>>(a, f);
+        rotary<E, PAIRED, kPairs<E, PAIRED>, 4><<<grid, kThreads, 0, st>>>(a, f);
+    else if (a.few)
+        rotary<E, PAIRED, kFew, 1><<<grid, kThreads, 0, st>>>(a, f);
     else
-        rotary<E, PAIRED, 1><<<grid, kThreads, 0, st>>>(a, f);
+        rotary<E, PAIRED, kPairs<E, PAIRED>, 1><<<grid, kThreads, 0, st>>>(a, f);
 }
 
 template <class E>
 void run_pairs(const RotaryArgs &a, const Turns &f, bool paired, hipStream_t st)
 {
-    paired ? run<E, true>(a, f, st) : run<E, false>(a, f, st);
+    if (a.rot / 2 > kUsualPairs)
+        return paired ? run<E, true>(a, f, st) : run<E, false>(a, f, st);
+    TurnsOf<kUsualPairs> g;
+    for (int i = 0; i < kUsualPairs; ++i)
+        g.turn[i] = f.turn[i];
+    paired ? run<E, true>(a, g, st) : run<E, false>(a, g, st);
 }
 
 }  // namespace
 
 bool plan_rotary(RotaryArgs &a, int64_t B, int64_t L, bool paired, bool in_place, int dt)
 {
-    const int64_t e = dt == IM2WIN_F32 ? 4 : 2, N = (paired ? 8 : 16) / e, W = paired ? 2 * N : N;
+    const int64_t e = dt == IM2WIN_F32 ? 4 : 2;
+    // Where two pairs a lane make 2^17 lanes at most (512 a CU), the time is one
+    // lane's: 4 tokens of 40 heads of 128, bf16: 3.8 us with eight pairs, 3.0 with two.
+    const int64_t units_few = (a.rot / 2 + kFew - 1) / kFew;
+    a.few = B * L <= 1 << 17 && B * L * a.H <= 1 << 17 && B * L * a.H * units_few <= 1 << 17;
+    const int64_t N = a.few ? kFew : (paired ? 8 : 16) / e, W = paired ? 2 * N : N;
     a.pair_units = (int32_t)((a.rot / 2 + N - 1) / N);
     const int64_t units = a.pair_units + (in_place ? 0 : (a.D - a.rot + W - 1) / W);
     if (B * L * units > UINT32_MAX)  // so that the products below fit
         return false;
-    // Heads a lane: 4 where that leaves 2^17 lanes or more (512 a CU), else one, for
-    // the least time of a lane.
+    // Heads a lane: 4 where that leaves 2^17 lanes or more, else one.
     const int64_t one = B * L * units * a.H;
     int64_t groups = a.H;
-    if (one >= (int64_t)1 << 19)
+    if (one >= (int64_t)1 << 19 && !a.few)
         groups = (a.H + 3) / 4;
     const int64_t lanes = B * L * units * groups;
     if (lanes > UINT32_MAX - kThreads)
