@@ -53,22 +53,42 @@ struct Run {
                 v[e] = ((const T *)p)[e];
         return v;
     }
-    __device__ static inline void store(char *p, int n, const V &v)
+    // Values from..n-1.
+    __device__ static inline void store(char *p, int from, int n, const V &v)
     {
-        if (n >= N) {
+        if (from == 0 && n >= N) {
             *(V *)p = v;
             return;
         }
 #pragma unroll
         for (int e = 0; e < N; ++e)
-            if (e < n)
+            if (e >= from && e < n)
                 ((T *)p)[e] = v[e];
     }
 };
 
+// Copies n of fewer than W values: vectors of W/2, W/4, .. 1, as n's bits say.
+template <class T, int W>
+__device__ inline void copy_few(char *o, const char *p, int n)
+{
+    if constexpr (W > 1) {
+        constexpr int H = W / 2;
+        if (n & H) {
+            typedef T V __attribute__((ext_vector_type(H), aligned(sizeof(T))));
+            *(V *)o = *(const V *)p;
+            o += H * sizeof(T), p += H * sizeof(T);
+        }
+        copy_few<T, H>(o, p, n);
+    }
+}
+
 // Lanes: units of a head fastest, then groups of heads, then tokens.  A unit is
 // N pairs (N values and their N partners; side by side, 2N values in a row),
-// behind them, where x is not y, as many channels that are copied.
+// behind them, where x is not y, W channels that are copied.  Where N does not
+// divide the pairs, the last unit is moved back to end with them: the pairs it
+// shares with the one before come out alike, so that both may store them,
+// unless x is y, where it stores its own only (the others may be turned
+// already).  So too the last unit of the copied channels.
 template <class E, bool PAIRED, int N, int HEADS, int PAIRS>
 __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a, TurnsOf<PAIRS> f)
 {
@@ -83,29 +103,43 @@ __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a, TurnsOf<PAIRS> 
     const char *x = a.x + b * a.x_sb + t * a.x_st;
     char *y = a.y + b * a.y_sb + t * a.y_st;
     const int half = a.rot / 2;
-
-    if ((int)unit >= a.pair_units) {
-        const int c = a.rot + (unit - a.pair_units) * W, n = a.D - c;
-        for (int h = group; h < a.H; h += a.groups.d) {
-            // as bits: a NaN keeps its payload
-            typedef T V __attribute__((ext_vector_type(W), aligned(sizeof(T))));
-            const char *const p = x + h * a.x_sh + c * sizeof(T);
-            char *const o = y + h * a.y_sh + c * sizeof(T);
-            if (n >= W)
-                *(V *)o = *(const V *)p;
-            else
-                for (int e = 0; e < n; ++e)
-                    ((T *)o)[e] = ((const T *)p)[e];
-        }
-        return;
-    }
-    const int first = unit * N, n = half - first;  // pairs first .. first + min(n, N) - 1
-    const int at = (PAIRED ? 2 * first : first) * sizeof(T), to = half * sizeof(T);
-    // this lane's heads: group, group + groups, ..
     typedef Run<T, N> R;
     typedef Run<T, W> RW;
     typename R::V u[HEADS], v[HEADS];  // the pairs' two sides; side by side, all of them in w
     typename RW::V w[HEADS];
+
+    // this lane's heads: group, group + groups, ..
+    if ((int)unit >= a.pair_units) {
+        int c = a.rot + (unit - a.pair_units) * W;
+        const int n = a.D - c;
+        const bool all = a.D - a.rot >= W;
+        c = all ? min(c, a.D - W) : c;
+        x += c * sizeof(T);
+        y += c * sizeof(T);
+        if (all) {
+#pragma unroll
+            for (int k = 0; k < HEADS; ++k) {
+                const int h = group + k * a.groups.d;
+                if (h >= a.H)
+                    break;
+                w[k] = *(const typename RW::V *)(x + h * a.x_sh);  // as bits: a NaN keeps its payload
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < HEADS; ++k) {
+            const int h = group + k * a.groups.d;
+            if (h >= a.H)
+                break;
+            if (all)
+                *(typename RW::V *)(y + h * a.y_sh) = w[k];
+            else
+                copy_few<T, W>(y + h * a.y_sh, x + h * a.x_sh, n);
+        }
+        return;
+    }
+    const int own = unit * N;  // its pairs are own .. own + N - 1, as far as there are
+    const int first = half >= N ? min(own, half - N) : own, n = half - first;
+    const int at = (PAIRED ? 2 * first : first) * sizeof(T), to = half * sizeof(T);
 #pragma unroll
     for (int k = 0; k < HEADS; ++k) {
         const int h = group + k * a.groups.d;
@@ -130,6 +164,7 @@ __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a, TurnsOf<PAIRS> 
         c[e] *= a.amplitude;
         s[e] *= a.sin_amplitude;
     }
+    const int skip = a.in_place ? own - first : 0;  // pairs that the unit before stores
 #pragma unroll
     for (int k = 0; k < HEADS; ++k) {
         const int h = group + k * a.groups.d;
@@ -147,10 +182,10 @@ __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a, TurnsOf<PAIRS> 
                 u[k][e] = yp, v[k][e] = yq;
         }
         if constexpr (PAIRED) {
-            RW::store(o, 2 * n, w[k]);
+            RW::store(o, 2 * skip, 2 * n, w[k]);
         } else {
-            R::store(o, n, u[k]);
-            R::store(o + to, n, v[k]);
+            R::store(o, skip, n, u[k]);
+            R::store(o + to, skip, n, v[k]);
         }
     }
 }
@@ -158,17 +193,20 @@ __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a, TurnsOf<PAIRS> 
 // Pairs of a unit: 16 bytes of a side (of both, side by side).
 template <class E, bool PAIRED>
 constexpr int kPairs = (PAIRED ? 8 : 16) / sizeof(typename E::T);
-// Pairs of a unit in small calls, see plan_rotary.
+// Pairs of a unit in small calls and of few pairs, see plan_rotary.
 constexpr int kFew = 2;
 
 template <class E, bool PAIRED, int PAIRS>
 void run(const RotaryArgs &a, const TurnsOf<PAIRS> &f, hipStream_t st)
 {
     const uint32_t grid = (a.lanes + kThreads - 1) / kThreads;
-    if ((uint32_t)a.H > a.groups.d)  // up to 4 heads a lane
-        rotary<E, PAIRED, kPairs<E, PAIRED>, 4><<<grid, kThreads, 0, st>>>(a, f);
+    const bool heads = (uint32_t)a.H > a.groups.d;  // up to 4 a lane
+    if (a.few && heads)
+        rotary<E, PAIRED, kFew, 4><<<grid, kThreads, 0, st>>>(a, f);
     else if (a.few)
         rotary<E, PAIRED, kFew, 1><<<grid, kThreads, 0, st>>>(a, f);
+    else if (heads)
+        rotary<E, PAIRED, kPairs<E, PAIRED>, 4><<<grid, kThreads, 0, st>>>(a, f);
     else
         rotary<E, PAIRED, kPairs<E, PAIRED>, 1><<<grid, kThreads, 0, st>>>(a, f);
 }
@@ -191,9 +229,11 @@ bool plan_rotary(RotaryArgs &a, int64_t B, int64_t L, bool paired, bool in_place
     const int64_t e = dt == IM2WIN_F32 ? 4 : 2;
     // Where two pairs a lane make 2^17 lanes at most (512 a CU), the time is one
     // lane's: 4 tokens of 40 heads of 128, bf16: 3.8 us with eight pairs, 3.0 with two.
-    const int64_t units_few = (a.rot / 2 + kFew - 1) / kFew;
-    a.few = B * L <= 1 << 17 && B * L * a.H <= 1 << 17 && B * L * a.H * units_few <= 1 << 17;
-    const int64_t N = a.few ? kFew : (paired ? 8 : 16) / e, W = paired ? 2 * N : N;
+    // Two also where there are fewer than a larger unit has.
+    const int64_t units_few = (a.rot / 2 + kFew - 1) / kFew, full = (paired ? 8 : 16) / e;
+    const bool small = B * L <= 1 << 17 && B * L * a.H <= 1 << 17 && B * L * a.H * units_few <= 1 << 17;
+    a.few = small || a.rot / 2 < full;
+    const int64_t N = a.few ? kFew : full, W = paired ? 2 * N : N;
     a.pair_units = (int32_t)((a.rot / 2 + N - 1) / N);
     const int64_t units = a.pair_units + (in_place ? 0 : (a.D - a.rot + W - 1) / W);
     if (B * L * units > UINT32_MAX)  // so that the products below fit
@@ -201,11 +241,12 @@ bool plan_rotary(RotaryArgs &a, int64_t B, int64_t L, bool paired, bool in_place
     // Heads a lane: 4 where that leaves 2^17 lanes or more, else one.
     const int64_t one = B * L * units * a.H;
     int64_t groups = a.H;
-    if (one >= (int64_t)1 << 19 && !a.few)
+    if (one >= (int64_t)1 << 19)
         groups = (a.H + 3) / 4;
     const int64_t lanes = B * L * units * groups;
     if (lanes > UINT32_MAX - kThreads)
         return false;
+    a.in_place = in_place;
     a.lanes = (uint32_t)lanes;
     a.units = make_fastdiv((uint32_t)units);
     a.groups = make_fastdiv((uint32_t)groups);

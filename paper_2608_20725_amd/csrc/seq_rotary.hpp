@@ -23,7 +23,7 @@ struct RotaryArgs {
     int64_t x_sb, x_st, x_sh, y_sb, y_st, y_sh;  // bytes between sequences, tokens, heads
     FastDiv units, groups, len;                // units of a head, groups of heads, tokens of a sequence
     uint32_t lanes;
-    int32_t H, D, rot, pair_units, by_token, few;
+    int32_t H, D, rot, pair_units, by_token, few, in_place;
     float amplitude, sin_amplitude;
 };
 

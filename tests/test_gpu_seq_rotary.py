@@ -97,6 +97,27 @@ def test_strides_and_in_place(dtype, interleaved):
     check(pkg.seq_rotary_forward(many, freq, pos.cuda(), interleaved), w1, t1 + 1e-30, "expanded")
 
 
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("interleaved", [False, True], ids=["half", "pairs"])
+@pytest.mark.parametrize("shape", [(2, 1500, 12, 60, 50), (2, 1500, 12, 128, 38), (3, 3000, 5, 24, 14), (2, 31, 3, 24, 14),
+                                   (1, 20000, 8, 40, 2), (2, 9000, 8, 26, 26), (1, 3, 2, 10, 6)], ids=lambda s: "x".join(map(str, s)))
+def test_in_place_where_units_overlap(shape, dtype, interleaved):
+    """Pairs that no unit divides: the last unit takes pairs of the one before
+    again, which in place may be turned already.  The same bits both ways."""
+    B, L, H, D, rot = shape
+    x, pos = inputs(B, L, H, D, dtype, far=77)
+    freq = pkg.seq_rotary_frequencies(rot)
+    xd, pd = x.cuda(), pos.cuda()
+    want = pkg.seq_rotary_forward(xd, freq, pd, interleaved)
+    ref, tol = rotary(x[:, :40], freq.tolist(), pos[:, :40], interleaved)
+    bare = tol == 0
+    check(want[:, :40], ref, torch.where(bare, torch.ones_like(tol), tol), "rotary")
+    for _ in range(3):
+        again = xd.clone()
+        pkg.seq_rotary_forward(again, freq, pd, interleaved, out=again)
+        assert torch.equal(again, want)
+
+
 def test_gradient_against_differences():
     """sum(dy * y(x + h d)) - sum(dy * y(x - h d)) over 2h against sum(dx * d):
     the map is linear, so the difference is exact but for rounding (fp32, sums
