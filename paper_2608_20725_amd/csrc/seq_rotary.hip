@@ -175,7 +175,12 @@ __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a, TurnsOf<PAIRS> 
         for (int e = 0; e < N; ++e) {
             const float p = E::get(PAIRED ? w[k][PAIRED ? 2 * e : 0] : u[k][e]);
             const float q = E::get(PAIRED ? w[k][PAIRED ? 2 * e + 1 : 0] : v[k][e]);
-            const T yp = E::put(p * c[e] - q * s[e]), yq = E::put(p * s[e] + q * c[e]);
+            // Rounded to fp32, then to T, wherever in a vector the pair stands: the
+            // compiler may neither fuse the products its own way nor make a mixed
+            // fp16 instruction of the sum and its conversion.
+            float fp = fmaf(p, c[e], -(q * s[e])), fq = fmaf(p, s[e], q * c[e]);
+            asm("" : "+v"(fp), "+v"(fq));
+            const T yp = E::put(fp), yq = E::put(fq);
             if constexpr (PAIRED)
                 w[k][2 * e] = yp, w[k][2 * e + 1] = yq;
             else
