@@ -42,6 +42,7 @@ struct PagedArgs {
     int64_t q_sb, q_sh, o_sb, o_sh;  // bytes
     int32_t B, H, G, R, row_waves, row_tiles, spread;
     int32_t most_parts, parts;  // see Plan
+    FastDiv most, half;         // by most_parts and half as many
     float scale, cap;
 };
 

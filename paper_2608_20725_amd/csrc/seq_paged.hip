@@ -239,13 +239,15 @@ struct Where {
 struct Cut {
     int32_t parts, piece;  // parts of a sequence, keys of each (the last has what is left)
 };
+// x up to a multiple of a step, a power of two.
+__device__ inline uint32_t up_to(uint32_t x, int32_t unit) { return (x + unit - 1) & ~(uint32_t)(unit - 1); }
 __device__ inline Cut cut_of(int32_t n, int32_t share, int32_t unit)
 {
     Cut c = {0, unit};
     if (n > 0) {
-        const int32_t p = (n - 1) / share + 1;
-        c.piece = (int32_t)(((uint32_t)(n + p - 1) / (uint32_t)p + unit - 1) / unit * unit);
-        c.parts = (n - 1) / c.piece + 1;
+        const uint32_t p = (uint32_t)(n - 1) / (uint32_t)share + 1;
+        c.piece = (int32_t)up_to((n + p - 1) / p, unit);
+        c.parts = (int32_t)((uint32_t)(n - 1) / (uint32_t)c.piece + 1);
     }
     return c;
 }
@@ -265,12 +267,16 @@ __device__ inline int32_t share_of(const Pool &c, const PagedArgs &a, int32_t un
     total = (int64_t)__builtin_amdgcn_readfirstlane((int)(total >> 32)) << 32 |
             (uint32_t)__builtin_amdgcn_readfirstlane((int)total);
     // one round of workgroups where that leaves each a few tiles only, two else
-    const int32_t half = (a.most_parts + 1) / 2;
-    int64_t share = total <= half ? 1 : (total - 1) / half + 1;
+    auto of = [&](const FastDiv &parts) {  // ceil(total / parts), at least 1
+        if (total <= (int64_t)parts.d)
+            return (int64_t)1;
+        return total <= (int64_t)UINT32_MAX ? (int64_t)fdiv((uint32_t)(total - 1), parts) + 1 : (total - 1) / parts.d + 1;
+    };
+    int64_t share = of(a.half);
     if (share > 8 * a.row_waves * unit)
-        share = (total - 1) / a.most_parts + 1;
+        share = of(a.most);
     // no sequence is longer than 2^30
-    return ((share < 1 << 30 ? (int32_t)share : 1 << 30) + unit - 1) / unit * unit;
+    return (int32_t)up_to(share < 1 << 30 ? (uint32_t)share : 1u << 30, unit);
 }
 
 // Parts of the 64 sequences from `base` on: the lane's cut, its tokens, the
@@ -296,12 +302,11 @@ __device__ inline Scan scan_parts(const Pool &c, const PagedArgs &a, int base, i
 // Part `index` of all sequences' parts in order: keys lo .. hi - 1 of sequence
 // b of n keys.  b < 0: there is none.
 struct Part {
-    int32_t b, n, lo, hi;
-    bool alone;  // the only part of its sequence
+    int32_t b, n, lo, hi, parts;  // parts of the sequence
 };
 __device__ inline Part find_part(const Pool &c, const PagedArgs &a, int32_t index, int32_t unit, int lane)
 {
-    Part p = {-1, 0, 0, 0, false};
+    Part p = {-1, 0, 0, 0, 0};
     const int32_t share = share_of(c, a, unit, lane);
     for (int base = 0; base < a.B; base += 64) {
         const Scan s = scan_parts(c, a, base, share, unit, lane);
@@ -315,16 +320,22 @@ __device__ inline Part find_part(const Pool &c, const PagedArgs &a, int32_t inde
         p.n = __builtin_amdgcn_readlane(s.n, l);
         p.lo = (index - (__builtin_amdgcn_readlane(s.upto, l) - parts)) * piece;
         p.hi = min(p.n, p.lo + piece);
-        p.alone = parts == 1;
+        p.parts = parts;
         break;
     }
     return p;
 }
 
-// Sums, maximum and sum of the exponentials of row `head` in part `index`.
+// The workspace: for each sequence its first part and their number (written by
+// the first part's workgroup, for the join), then the parts: sums, maximum and
+// sum of the exponentials of row `head` in part `index`.
+struct FirstPart {
+    int32_t index, parts;
+};
+__host__ __device__ inline int64_t first_part_floats(int64_t B) { return (2 * B + 3) / 4 * 4; }
 __device__ inline float *part_of(const PagedArgs &a, int64_t index, int head, int D)
 {
-    return a.part + (index * a.H + head) * part_floats(D);
+    return a.part + first_part_floats(a.B) + (index * a.H + head) * part_floats(D);
 }
 
 // FULL: heads have DP channels, no more tests of where they end.
@@ -360,9 +371,11 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
             return;
     } else {
         const int n = tokens_of(c, a, index);
-        part = Part{index, n, 0, n, true};
+        part = Part{index, n, 0, n, 1};
     }
     const int b = part.b, n = part.n, hi = part.hi;
+    if (a.most_parts && part.lo == 0 && hk == 0 && rt == 0 && threadIdx.x == 0)
+        ((FirstPart *)a.part)[b] = FirstPart{index, part.parts};
 
     // this lane's query: column r of the wave's
     const int row0 = (rt * a.row_waves) * 16, row = row0 + wave % a.row_waves * 16 + r;
@@ -653,7 +666,7 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
                 for (int e = 0; e < 8; ++e)
                     v[e] += box[w][rr][ch + e];
         }
-        if (!part.alone) {
+        if (part.parts > 1) {
             float *const to = part_of(a, index, hk * a.G + rw, D);
             if (ch < D)
                 *(f32x8_a16 *)(to + ch) = v;
@@ -680,7 +693,7 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
 // Joins the parts of a row: 32 lanes hold its channels, four each, and `groups`
 // of them (1 or 8) take its parts in turn.  Rows of one part are done already.
 template <class E, bool HALF>
-__global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int groups, int unit)
+__global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int groups)
 {
     typedef float v4 __attribute__((ext_vector_type(4)));
     __shared__ v4 sv[8][32];
@@ -689,19 +702,9 @@ __global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int group
     const int rows = a.B * a.H, lane = threadIdx.x & 31, d = lane * 4, group = threadIdx.x >> 5, first = group % groups;
     const int row = blockIdx.x * (8 / groups) + group / groups, live = row < rows;
     const int b = live ? row / a.H : 0, h = live ? row - b * a.H : 0;
-    // the first part of sequence b (the two rows of a wave may be of two)
-    const int wlane = threadIdx.x & 63;
-    const int32_t share = share_of(c, a, unit, wlane);
-    int64_t at = 0;
-    int parts = 0;
-    for (int base = 0; __any(base <= b); base += 64) {
-        const Scan s = scan_parts(c, a, base, share, unit, wlane);
-        const int l = b - base, upto = __shfl(s.upto, l & 63), here = __shfl(s.cut.parts, l & 63);
-        if (l >= 0 && l < 64)
-            at += upto - here, parts = here;
-        else if (l >= 64)
-            at += s.all;
-    }
+    const FirstPart of = ((const FirstPart *)a.part)[b];  // nobody writes it for a sequence without tokens
+    const int64_t at = of.index;
+    const int parts = live && tokens_of(c, a, b) > 0 ? of.parts : 0;
     if (groups > 1 ? parts == 1 : __all(parts == 1 || !live))  // groups > 1: one row a workgroup
         return;
     // running maximum, sum and outputs: a part's numbers are loaded at once
@@ -816,8 +819,7 @@ void run(const Plan &p, const Pool &c, const PagedArgs &a, hipStream_t st)
     if (a.most_parts) {
         const int64_t rows = (int64_t)a.B * a.H;
         const int groups = rows <= 2048 ? 8 : 1;
-        paged_join<E, Math<E, Code, 64, false>::kHalf><<<(uint32_t)((rows * groups + 7) / 8), 256, 0, st>>>(c, a, groups,
-                                                                                                        p.step);
+        paged_join<E, Math<E, Code, 64, false>::kHalf><<<(uint32_t)((rows * groups + 7) / 8), 256, 0, st>>>(c, a, groups);
     }
 }
 
@@ -834,13 +836,15 @@ void run_code(const Plan &p, const Pool &c, int ct, const PagedArgs &a, hipStrea
 int64_t paged_part_floats(const Pool &c, int ct, int64_t B, int64_t H, int dt)
 {
     const Plan p = plan_of(c, ct, B, H, dt);
-    return p.most_parts ? p.parts * H * part_floats(c.D) : 0;
+    return p.most_parts ? first_part_floats(B) + p.parts * H * part_floats(c.D) : 0;
 }
 
 hipError_t launch_paged(const Pool &c, int ct, PagedArgs a, int dt, hipStream_t st)
 {
     const Plan p = plan_of(c, ct, a.B, a.H, dt);
     a.most_parts = (int32_t)p.most_parts, a.parts = (int32_t)p.parts;
+    a.most = make_fastdiv(p.most_parts ? (uint32_t)p.most_parts : 1);
+    a.half = make_fastdiv((a.most.d + 1) / 2);
     a.row_waves = p.row_waves, a.row_tiles = p.row_tiles;
     a.spread = c.Hkv > 1 && (c.k_head | c.v_head) % 128 != 0 ? 8 : 1;
     if (dt == IM2WIN_F32)
