@@ -138,11 +138,13 @@ struct Math {
             v[e] = q.x[t][at + e];
         return v;
     }
+    // Of the pieces FROM .. TO - 1.
+    template <int FROM = 0, int TO = NK>
     __device__ static inline f32x4_acc dot(const u32x4_t (&k)[NK], const Query &q, int bytes)
     {
         f32x4_acc s = {0, 0, 0, 0};
 #pragma unroll
-        for (int c = 0; c < NK; ++c) {
+        for (int c = FROM; c < TO; ++c) {
             if (64 * c >= bytes)  // behind a head's last channel
                 break;
             if constexpr (kWide) {
@@ -224,10 +226,10 @@ struct Math {
 
 // What the lanes of a wave tell each other of a tile: where its keys and values
 // lie (bytes from the head's first), and 8-bit pages' scales.
-template <int KEYS>
+template <int KEYS, int HEADS>
 struct Where {
     int64_t k[KEYS], v[KEYS];
-    float ks[KEYS], vs[KEYS];
+    float ks[HEADS][KEYS], vs[HEADS][KEYS];
 };
 
 // ---- how the keys are split ----
@@ -339,17 +341,26 @@ __device__ inline float *part_of(const PagedArgs &a, int64_t index, int head, in
 }
 
 // FULL: heads have DP channels, no more tests of where they end.
-template <class E, class Code, int DP, bool FULL, bool SMALL>
+// PAIR: two key/value heads of 64 channels that lie side by side are taken as one of
+// 128 with the queries of both, at most 16.  A query is zero in the other head's
+// channels and keeps the products of its own, so that nothing passes from head to
+// head.  A tile's bytes are doubled for the same scores, whose columns were idle:
+// 32 caches of 2048 to 8192 tokens, 8 heads, alone and in pairs: fp16 78 and 67 us;
+// 64 of 4096 to 16384, 4 heads, int8 under bf16 106 and 90.  fp32 queries have no
+// registers for it.
+template <class E, class Code, int DP, bool FULL, bool SMALL, bool PAIR>
 __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs a)
 {
     typedef Math<E, Code, DP, SMALL> M;
     constexpr int KEYS = M::KEYS, N = M::N, VC = M::VC, ES = M::ES;
     // fp16 probabilities are times 2^14, so that those of long rows stay normal numbers
     constexpr float kShift = M::kHalf ? 14.0f : 0.0f, kUnshift = M::kHalf ? 0x1p-14f : 1.0f;
-    __shared__ __align__(16) Where<KEYS> where[kWavesP];
+    constexpr int HEADS = PAIR ? 2 : 1;
+    static_assert(!PAIR || (DP == 128 && FULL && !M::kWide));
+    __shared__ __align__(16) Where<KEYS, HEADS> where[kWavesP];
     __shared__ float box[kWavesP][16][DP + 4];
     __shared__ float sm[kWavesP][16], sl[kWavesP][16];
-    const int D = FULL ? DP : c.D;
+    const int D = FULL ? DP : c.D, one = D / HEADS;  // channels of the tile, of a head
 
     // blockIdx: heads fastest, then row tiles, then parts.  Workgroups go to the 8
     // XCDs in turn (id mod 8); where heads of a token share 128-byte lines, all
@@ -384,7 +395,8 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
 
     const char *const kp = c.k + hk * c.k_head, *const vp = c.v + hk * c.v_head;
     const int32_t *const table = c.table + b * c.table_stride;
-    Where<KEYS> &my = where[wave];
+    Where<KEYS, HEADS> &my = where[wave];
+    const bool second = PAIR && r >= a.G / 2;  // this lane's query is the second head's
 
     // A lane is the owner of key lane % KEYS of each tile.
     auto page_at = [&](int k0) {
@@ -435,10 +447,13 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
                 vr[i] = typename M::Value{};
         }
     };
-    auto load_scales = [&](int id, int in, float &ks, float &vs) {
+    auto load_scales = [&](int id, int in, float (&ks)[HEADS], float (&vs)[HEADS]) {
         if constexpr (M::kCodes) {
-            ks = scale_at(c.ks + hk * c.ks_head, c.ks_page, c.ks_tok, id, in);
-            vs = scale_at(c.vs + hk * c.vs_head, c.vs_page, c.vs_tok, id, in);
+#pragma unroll
+            for (int h = 0; h < HEADS; ++h) {
+                ks[h] = scale_at(c.ks + (HEADS * hk + h) * c.ks_head, c.ks_page, c.ks_tok, id, in);
+                vs[h] = scale_at(c.vs + (HEADS * hk + h) * c.vs_head, c.vs_page, c.vs_tok, id, in);
+            }
         }
     };
 
@@ -478,8 +493,8 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
         for (int k = 0; k < M::NK * M::EPC / 4; ++k) {
             const int ch = (4 * (4 * k / M::EPC) + g) * M::EPC + 4 * k % M::EPC;
             raw[k] = V4{};
-            if (row < a.G && ch < D)
-                raw[k] = *(const V4 *)(p + ch);
+            if (row < a.G && ch < D && (!PAIR || second == (ch >= one)))
+                raw[k] = *(const V4 *)(p + (PAIR ? ch % one : ch));
         }
     }
     typename M::Query q;
@@ -509,7 +524,7 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
     // under bf16: 215 us, 221 the other way).
     if (M::kCodes)
         make_query();
-    float ks = 0, vs = 0;
+    float ks[HEADS] = {}, vs[HEADS] = {};
     if (first < hi) {
         load_scales(id, in, ks, vs);
         tell(id, in);
@@ -525,22 +540,33 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
         float s[N];
 #pragma unroll
         for (int h = 0; h < KEYS / 16; ++h) {
-            const f32x4_acc x = M::dot(kr[h], q, D * ES);
+            if constexpr (PAIR) {
+                const f32x4_acc x = M::template dot<0, M::NK / 2>(kr[h], q, D * ES);
+                const f32x4_acc y = M::template dot<M::NK / 2>(kr[h], q, D * ES);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                s[4 * h + i] = x[i];
+                for (int i = 0; i < 4; ++i)
+                    s[4 * h + i] = second ? y[i] : x[i];
+            } else {
+                const f32x4_acc x = M::dot(kr[h], q, D * ES);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    s[4 * h + i] = x[i];
+            }
         }
         const uint64_t there = __ballot(id >= 0);  // a bit a key
         float kscale[N], vscale[N];
         wave_lds_handoff();
         if constexpr (M::kCodes) {
-            my.ks[lane % KEYS] = ks;
-            my.vs[lane % KEYS] = vs;
+#pragma unroll
+            for (int h = 0; h < HEADS; ++h) {
+                my.ks[h][lane % KEYS] = ks[h];
+                my.vs[h][lane % KEYS] = vs[h];
+            }
             wave_lds_handoff();
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                kscale[i] = my.ks[16 * (i >> 2) + 4 * g + (i & 3)];
-                vscale[i] = my.vs[16 * (i >> 2) + 4 * g + (i & 3)];
+                kscale[i] = my.ks[second][16 * (i >> 2) + 4 * g + (i & 3)];
+                vscale[i] = my.vs[second][16 * (i >> 2) + 4 * g + (i & 3)];
             }
         }
         if (!kEarly)
@@ -654,6 +680,7 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
         const int rw = row0 + 16 * w0 + rr;
         if (rw >= a.G)
             break;
+        const int to_ch = PAIR && rw >= a.G / 2 ? ch - one : ch;  // of its head
         float ms = -INFINITY, sum = 0;
         for (int w = w0; w < kWavesP; w += a.row_waves)
             ms = fmaxf(ms, sm[w][rr]);
@@ -667,24 +694,24 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
                     v[e] += box[w][rr][ch + e];
         }
         if (part.parts > 1) {
-            float *const to = part_of(a, index, hk * a.G + rw, D);
-            if (ch < D)
-                *(f32x8_a16 *)(to + ch) = v;
-            if (ch == 0) {
-                to[D] = ms;
-                to[D + 1] = sum;
+            float *const to = part_of(a, index, hk * a.G + rw, one);
+            if (to_ch >= 0 && to_ch < one)
+                *(f32x8_a16 *)(to + to_ch) = v;
+            if (to_ch == 0) {
+                to[one] = ms;
+                to[one + 1] = sum;
             }
         } else {
             const bool none = sum == 0.0f;  // not ms == -inf: all scores may be NaN
-            if (ch < D) {
+            if (to_ch >= 0 && to_ch < one) {
                 typedef typename E::T V8 __attribute__((ext_vector_type(8), aligned(16)));
                 V8 y;
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     y[e] = E::put(none ? 0.0f : v[e] / sum);
-                *(V8 *)(a.out + b * a.o_sb + (hk * a.G + rw) * a.o_sh + ch * sizeof(typename E::T)) = y;
+                *(V8 *)(a.out + b * a.o_sb + (hk * a.G + rw) * a.o_sh + to_ch * sizeof(typename E::T)) = y;
             }
-            if (ch == 0)
+            if (to_ch == 0)
                 a.lse[b * a.H + hk * a.G + rw] = none ? -INFINITY : (ms + __log2f(sum * kUnshift)) * kLn2;
         }
     }
@@ -766,7 +793,7 @@ __global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int group
 // would cost more.
 struct Plan {
     int32_t row_waves, row_tiles, step;
-    bool small;
+    bool small, pair;
     int64_t most_parts, parts;  // parts: that the lengths can make at most
 };
 // Workgroups that share the keys, two rounds of the two that fit a CU.  Measured
@@ -775,31 +802,55 @@ struct Plan {
 // 200, 203, four of them 26, 31, 28, 27, 33; int8, 32 of 8192: 129, 132, 130, 142,
 // 135.
 constexpr int64_t kTarget = 1024;
-Plan plan_of(const Pool &c, int ct, int64_t B, int64_t H, int dt)
+// pair: heads may be taken by two (see paged_attn).
+Plan plan_of(const Pool &c, int ct, int64_t B, int64_t H, int dt, bool pair)
 {
     Plan p;
-    const int64_t G = H / c.Hkv, bytes = (c.D <= 64 ? 64 : 128) * (ct != dt ? 1 : dt == IM2WIN_F32 ? 4 : 2);
+    p.pair = pair;
+    const int64_t Hkv = pair ? c.Hkv / 2 : c.Hkv, G = H / Hkv;
+    const int64_t bytes = (c.D <= 64 && !pair ? 64 : 128) * (ct != dt ? 1 : dt == IM2WIN_F32 ? 4 : 2);
     p.row_waves = G <= 16 ? 1 : G <= 32 ? 2 : 4;
     p.row_tiles = (int32_t)((G + 16 * p.row_waves - 1) / (16 * p.row_waves));
-    const int64_t heads = c.Hkv * p.row_tiles, most = (int64_t)c.max_pages * c.page.d;
+    const int64_t heads = Hkv * p.row_tiles, most = (int64_t)c.max_pages * c.page.d;
     const int32_t waves = kWavesP / p.row_waves;
     const int32_t least = tile_keys(bytes, true) * waves;
     p.small = B * heads <= kTarget / 2 && (most + least - 1) / least * B * heads <= kTarget / 2;
     p.step = tile_keys(bytes, p.small) * waves;
+    if (p.small && pair)  // enough workgroups first
+        return plan_of(c, ct, B, H, dt, false);
     const int64_t steps = (most + p.step - 1) / p.step;
     const int64_t few = ct == IM2WIN_F32 ? 2 : 4;
     p.most_parts = steps <= few || B > 512 || B * heads >= 16 * kTarget ? 0 : (kTarget + heads - 1) / heads;
     p.parts = p.most_parts ? (p.most_parts + B < B * steps ? p.most_parts + B : B * steps) : B;
     return p;
 }
+// Whether pairs of heads can be taken as one, wherever they lie.
+bool pairs(const Pool &c, int64_t H, int dt)
+{
+    return c.D == 64 && c.Hkv % 2 == 0 && H / c.Hkv <= 8 && dt != IM2WIN_F32;
+}
+
+int32_t spread_of(const Pool &c) { return c.Hkv > 1 && (c.k_head | c.v_head) % 128 != 0 ? 8 : 1; }
+uint32_t grid_of(const Pool &c, const PagedArgs &a)
+{
+    return (uint32_t)((a.parts + a.spread - 1) / a.spread * a.spread * c.Hkv) * a.row_tiles;
+}
 
 template <class E, class Code, int DP, bool SMALL>
 void run_full(uint32_t grid, const Pool &c, const PagedArgs &a, hipStream_t st)
 {
     if (c.D == DP)
-        paged_attn<E, Code, DP, true, SMALL><<<grid, 64 * kWavesP, 0, st>>>(c, a);
+        paged_attn<E, Code, DP, true, SMALL, false><<<grid, 64 * kWavesP, 0, st>>>(c, a);
     else
-        paged_attn<E, Code, DP, false, SMALL><<<grid, 64 * kWavesP, 0, st>>>(c, a);
+        paged_attn<E, Code, DP, false, SMALL, false><<<grid, 64 * kWavesP, 0, st>>>(c, a);
+}
+template <class E, class Code>
+void run_pair(Pool c, PagedArgs a, hipStream_t st)
+{
+    c.Hkv /= 2, c.D *= 2, a.G *= 2;
+    c.k_head *= 2, c.v_head *= 2;
+    a.spread = spread_of(c);
+    paged_attn<E, Code, 128, true, false, true><<<grid_of(c, a), 64 * kWavesP, 0, st>>>(c, a);
 }
 
 template <class E, class Code, int DP>
@@ -812,10 +863,17 @@ void run_small(bool small, uint32_t grid, const Pool &c, const PagedArgs &a, hip
 }
 
 template <class E, class Code>
-void run(const Plan &p, const Pool &c, const PagedArgs &a, hipStream_t st)
+void run(const Plan &p, const Pool &c, PagedArgs a, hipStream_t st)
 {
-    const uint32_t grid = (uint32_t)((a.parts + a.spread - 1) / a.spread * a.spread * c.Hkv) * a.row_tiles;
-    c.D <= 64 ? run_small<E, Code, 64>(p.small, grid, c, a, st) : run_small<E, Code, 128>(p.small, grid, c, a, st);
+    if constexpr (!__is_same(E, EltF32)) {
+        if (p.pair)
+            run_pair<E, Code>(c, a, st);
+    }
+    if (!p.pair) {
+        a.spread = spread_of(c);
+        const uint32_t grid = grid_of(c, a);
+        c.D <= 64 ? run_small<E, Code, 64>(p.small, grid, c, a, st) : run_small<E, Code, 128>(p.small, grid, c, a, st);
+    }
     if (a.most_parts) {
         const int64_t rows = (int64_t)a.B * a.H;
         const int groups = rows <= 2048 ? 8 : 1;
@@ -835,18 +893,24 @@ void run_code(const Plan &p, const Pool &c, int ct, const PagedArgs &a, hipStrea
 
 int64_t paged_part_floats(const Pool &c, int ct, int64_t B, int64_t H, int dt)
 {
-    const Plan p = plan_of(c, ct, B, H, dt);
-    return p.most_parts ? first_part_floats(B) + p.parts * H * part_floats(c.D) : 0;
+    // for either order in which heads may lie
+    int64_t parts = 0;
+    for (int pair = 0; pair <= (int)pairs(c, H, dt); ++pair) {
+        const Plan p = plan_of(c, ct, B, H, dt, pair);
+        if (p.most_parts && p.parts > parts)
+            parts = p.parts;
+    }
+    return parts ? first_part_floats(B) + parts * H * part_floats(c.D) : 0;
 }
 
 hipError_t launch_paged(const Pool &c, int ct, PagedArgs a, int dt, hipStream_t st)
 {
-    const Plan p = plan_of(c, ct, a.B, a.H, dt);
+    const int64_t bytes = c.D * (ct != dt ? 1 : 2);  // of a 16-bit or 8-bit head
+    const Plan p = plan_of(c, ct, a.B, a.H, dt, pairs(c, a.H, dt) && c.k_head == bytes && c.v_head == bytes);
     a.most_parts = (int32_t)p.most_parts, a.parts = (int32_t)p.parts;
     a.most = make_fastdiv(p.most_parts ? (uint32_t)p.most_parts : 1);
     a.half = make_fastdiv((a.most.d + 1) / 2);
     a.row_waves = p.row_waves, a.row_tiles = p.row_tiles;
-    a.spread = c.Hkv > 1 && (c.k_head | c.v_head) % 128 != 0 ? 8 : 1;
     if (dt == IM2WIN_F32)
         run_code<EltF32>(p, c, ct, a, st);
     else if (dt == IM2WIN_F16)

@@ -360,6 +360,57 @@ def test_values_that_are_not_finite(types):
     assert torch.equal(got, clean) and torch.equal(gl, cl)
 
 
+@pytest.mark.parametrize("G", [1, 5, 8])
+@pytest.mark.parametrize("types", PAIRS, ids=ids)
+def test_heads_of_64_channels_side_by_side(types, G):
+    """Two heads that lie next to each other, also where one of them is not
+    finite, in a split sequence, a short one, an empty one and many whole ones."""
+    dt, ct = types
+    for lens, wide in (([2100, 70, 0, 1], 2000), ([40, 300, 0, 7] * 140, 20)):
+        say("side by side", types, G, len(lens))
+        c = Cache(lens, 16, 4, 64, dt, ct, wide=wide)
+        q = torch.randn((len(lens), 4 * G, 64), generator=torch.Generator().manual_seed(4)).to(dt)
+        bias = torch.randn((4 * G, 81), generator=torch.Generator().manual_seed(5))
+        out, lse, tol, tl = attention(q, c, bias=bias, cap=15.0)
+        kp, vp, table, scales = c.device()
+
+        def run():
+            return pkg.seq_paged_attention_forward(q.cuda(), kp, vp, table, c.len.cuda(), cap=15.0, bias=bias.cuda(), **scales)
+        got, gl = run()
+        check(got, out, tol + 1e-30, "out")
+        check(gl, lse, tl + 1e-30, "lse")
+        # head 1's keys and head 2's values of a token of sequences 0 and 1
+        if ct == I8:
+            kbad, vbad = scales["k_scale"], scales["v_scale"]
+        else:
+            kbad, vbad = kp, vp
+        for b, pos in ((0, 33), (1, 69 if len(lens) == 4 else 290)):
+            at = (int(c.table[b, pos // 16]), pos % 16)
+            nan = torch.full((1,), float("nan"), device="cuda").to(kbad.dtype)
+            kbad[at + (1,)] = nan.expand(kbad[at + (1,)].shape) if kbad.dim() == 4 else nan[0]
+            vbad[at + (2,)] = nan.expand(vbad[at + (2,)].shape) if vbad.dim() == 4 else nan[0]
+        bad, bl = run()
+        for b in range(2):
+            if lens[b] > (33, 69 if len(lens) == 4 else 290)[b]:
+                assert torch.isnan(bad[b, G:3 * G]).all() and torch.isnan(bl[b, G:2 * G]).all()
+                assert torch.equal(bl[b, 2 * G:3 * G], gl[b, 2 * G:3 * G])
+                bad[b, G:3 * G], bl[b, G:2 * G] = got[b, G:3 * G], gl[b, G:2 * G]
+        assert torch.equal(bad, got) and torch.equal(bl, gl)
+
+
+@pytest.mark.parametrize("types,Hkv", [((BF16, BF16), 16), ((F16, I8), 32), ((F32, F32), 8)], ids=["bf16", "f16-i8", "f32"])
+def test_sequences_that_end_within_their_shares(types, Hkv):
+    """Lengths that make a half more parts than the first estimate."""
+    dt, ct = types
+    c = Cache([800] * 25 + [799], 64, Hkv, 64, dt, ct)
+    q = torch.randn((26, Hkv, 64), generator=torch.Generator().manual_seed(6)).to(dt)
+    out, lse, tol, tl = attention(q, c)
+    kp, vp, table, scales = c.device()
+    got, gl = pkg.seq_paged_attention_forward(q.cuda(), kp, vp, table, c.len.cuda(), **scales)
+    check(got, out, tol + 1e-30, "out")
+    check(gl, lse, tl + 1e-30, "lse")
+
+
 @pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16), (F16, I8), (F16, E4M3)], ids=ids)
 def test_strides_of_queries_results_tables_and_pages(types):
     dt, ct = types
