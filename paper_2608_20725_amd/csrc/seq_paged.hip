@@ -363,11 +363,13 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
     const int D = FULL ? DP : c.D, one = D / HEADS;  // channels of the tile, of a head
 
     // blockIdx: heads fastest, then row tiles, then parts.  Workgroups go to the 8
-    // XCDs in turn (id mod 8); where heads of a token share 128-byte lines, all
-    // heads of a part run on one (spread 8, else 1), which fetches the lines once.
-    // 32 caches of 2048 to 8192 tokens, 8 heads, 16 tokens a page, heads fastest
-    // and on one XCD: int8 of 64 channels 71 and 58 us, bf16 of 96 118 and 112; of
-    // 128 channels, where no lines are shared, bf16 136 and 139, int8 216 and 219.
+    // XCDs in turn (id mod 8); all heads of a part run on one (spread 8, else 1)
+    // where they share lines, which it then fetches once: keys that do not lie on
+    // 128-byte lines, and the scales of several heads beside keys of few bytes.
+    // 32 caches of 2048 to 8192 tokens, 8 heads, 16 tokens a page, heads fastest and
+    // on one XCD: bf16 of 96 channels 118 and 112 us, int8 of 128 92 and 87; of 256
+    // bytes or more bf16 of 128 139 and 140, fp32 of 64 (16 caches of 4096, 12 heads)
+    // 45 and 59.
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int turn = blockIdx.x / a.spread, hk = turn % c.Hkv, rest = turn / c.Hkv, rt = rest % a.row_tiles;
@@ -830,7 +832,10 @@ bool pairs(const Pool &c, int64_t H, int dt)
     return c.D == 64 && c.Hkv % 2 == 0 && H / c.Hkv <= 8 && dt != IM2WIN_F32;
 }
 
-int32_t spread_of(const Pool &c) { return c.Hkv > 1 && (c.k_head | c.v_head) % 128 != 0 ? 8 : 1; }
+int32_t spread_of(const Pool &c)
+{
+    return c.Hkv > 1 && ((c.k_head | c.v_head) % 128 != 0 || c.k_head < 256 || c.v_head < 256) ? 8 : 1;
+}
 uint32_t grid_of(const Pool &c, const PagedArgs &a)
 {
     return (uint32_t)((a.parts + a.spread - 1) / a.spread * a.spread * c.Hkv) * a.row_tiles;
