@@ -365,13 +365,14 @@ __device__ inline float *part_of(const PagedArgs &a, int64_t index, int head, in
 }
 
 // FULL: heads have DP channels, no more tests of where they end.
-// PAIR: two key/value heads of 64 channels that lie side by side are taken as one of
-// 128 with the queries of both, at most 16.  A query is zero in the other head's
-// channels and keeps the products of its own, so that nothing passes from head to
-// head.  A tile's bytes are doubled for the same scores, whose columns were idle:
-// 32 caches of 2048 to 8192 tokens, 8 heads, alone and in pairs: fp16 78 and 67 us;
-// 64 of 4096 to 16384, 4 heads, int8 under bf16 106 and 90.  fp32 queries have no
-// registers for it.
+// PAIR: two key/value heads that lie side by side are taken as one of DP channels
+// with the queries of both, at most 16.  A query keeps the products with its own
+// head's pieces of the keys, so that nothing passes from head to head.  A tile's
+// bytes are doubled for the same scores, whose columns were idle: 32 caches of 2048
+// to 8192 tokens, 8 heads, alone and in pairs: fp16 of 64 channels 78 and 67 us, of
+// 32 54 and 39; 34 of up to 13781, 4 heads of 32, fp32 111 and 83; 64 of up to
+// 16384, 4 heads of 64, int8 under bf16 106 and 90.  fp32 queries of two heads of 64
+// have no registers for it, 8-bit heads of 32 no piece each.
 template <class E, class Code, int DP, bool FULL, bool SMALL, bool PAIR>
 __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs a)
 {
@@ -380,7 +381,7 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
     // fp16 probabilities are times 2^14, so that those of long rows stay normal numbers
     constexpr float kShift = M::kHalf ? 14.0f : 0.0f, kUnshift = M::kHalf ? 0x1p-14f : 1.0f;
     constexpr int HEADS = PAIR ? 2 : 1;
-    static_assert(!PAIR || (DP == 128 && FULL && !M::kWide));
+    static_assert(!PAIR || (FULL && DP * ES >= 128));  // whole pieces a head
     __shared__ __align__(16) Where<KEYS, HEADS> where[kWavesP];
     __shared__ float box[kWavesP][16][DP + 4];
     __shared__ float sm[kWavesP][16], sl[kWavesP][16];
@@ -834,7 +835,7 @@ Plan plan_of(const Pool &c, int ct, int64_t B, int64_t H, int dt, bool pair)
     Plan p;
     p.pair = pair;
     const int64_t Hkv = pair ? c.Hkv / 2 : c.Hkv, G = H / Hkv;
-    const int64_t bytes = (c.D <= 64 && !pair ? 64 : 128) * (ct != dt ? 1 : dt == IM2WIN_F32 ? 4 : 2);
+    const int64_t bytes = (c.D * (pair ? 2 : 1) <= 64 ? 64 : 128) * (ct != dt ? 1 : dt == IM2WIN_F32 ? 4 : 2);
     p.row_waves = G <= 16 ? 1 : G <= 32 ? 2 : 4;
     p.row_tiles = (int32_t)((G + 16 * p.row_waves - 1) / (16 * p.row_waves));
     const int64_t heads = Hkv * p.row_tiles, most = (int64_t)c.max_pages * c.page.d;
@@ -851,9 +852,9 @@ Plan plan_of(const Pool &c, int ct, int64_t B, int64_t H, int dt, bool pair)
     return p;
 }
 // Whether pairs of heads can be taken as one, wherever they lie.
-bool pairs(const Pool &c, int64_t H, int dt)
+bool pairs(const Pool &c, int ct, int64_t H, int dt)
 {
-    return c.D == 64 && c.Hkv % 2 == 0 && H / c.Hkv <= 8 && dt != IM2WIN_F32;
+    return (c.D == 64 ? dt != IM2WIN_F32 : c.D == 32 && ct == dt) && c.Hkv % 2 == 0 && H / c.Hkv <= 8;
 }
 
 int32_t spread_of(const Pool &c)
@@ -873,13 +874,13 @@ void run_full(uint32_t grid, const Pool &c, const PagedArgs &a, hipStream_t st)
     else
         paged_attn<E, Code, DP, false, SMALL, false><<<grid, 64 * kWavesP, 0, st>>>(c, a);
 }
-template <class E, class Code>
+template <class E, class Code, int DP>
 void run_pair(Pool c, PagedArgs a, hipStream_t st)
 {
     c.Hkv /= 2, c.D *= 2, a.G *= 2;
     c.k_head *= 2, c.v_head *= 2;
     a.spread = spread_of(c);
-    paged_attn<E, Code, 128, true, false, true><<<grid_of(c, a), 64 * kWavesP, 0, st>>>(c, a);
+    paged_attn<E, Code, DP, true, false, true><<<grid_of(c, a), 64 * kWavesP, 0, st>>>(c, a);
 }
 
 template <class E, class Code, int DP>
@@ -894,10 +895,12 @@ void run_small(bool small, uint32_t grid, const Pool &c, const PagedArgs &a, hip
 template <class E, class Code>
 void run(const Plan &p, const Pool &c, PagedArgs a, hipStream_t st)
 {
-    if constexpr (!__is_same(E, EltF32)) {
-        if (p.pair)
-            run_pair<E, Code>(c, a, st);
-    }
+    if constexpr (!__is_same(E, EltF32))
+        if (p.pair && c.D == 64)
+            run_pair<E, Code, 128>(c, a, st);
+    if constexpr (__is_same(Code, void))
+        if (p.pair && c.D == 32)
+            run_pair<E, Code, 64>(c, a, st);
     if (!p.pair) {
         a.spread = spread_of(c);
         const uint32_t grid = grid_of(c, a);
@@ -924,7 +927,7 @@ int64_t paged_part_floats(const Pool &c, int ct, int64_t B, int64_t H, int dt)
 {
     // for either order in which heads may lie
     int64_t parts = 0;
-    for (int pair = 0; pair <= (int)pairs(c, H, dt); ++pair) {
+    for (int pair = 0; pair <= (int)pairs(c, ct, H, dt); ++pair) {
         const Plan p = plan_of(c, ct, B, H, dt, pair);
         if (p.most_parts && p.parts > parts)
             parts = p.parts;
@@ -934,8 +937,8 @@ int64_t paged_part_floats(const Pool &c, int ct, int64_t B, int64_t H, int dt)
 
 hipError_t launch_paged(const Pool &c, int ct, PagedArgs a, int dt, hipStream_t st)
 {
-    const int64_t bytes = c.D * (ct != dt ? 1 : 2);  // of a 16-bit or 8-bit head
-    const Plan p = plan_of(c, ct, a.B, a.H, dt, pairs(c, a.H, dt) && c.k_head == bytes && c.v_head == bytes);
+    const int64_t bytes = c.D * (ct != dt ? 1 : dt == IM2WIN_F32 ? 4 : 2);  // of a head
+    const Plan p = plan_of(c, ct, a.B, a.H, dt, pairs(c, ct, a.H, dt) && c.k_head == bytes && c.v_head == bytes);
     a.most_parts = (int32_t)p.most_parts, a.parts = (int32_t)p.parts;
     a.most = make_fastdiv(p.most_parts ? (uint32_t)p.most_parts : 1);
     a.half = make_fastdiv((a.most.d + 1) / 2);

@@ -360,16 +360,16 @@ def test_values_that_are_not_finite(types):
     assert torch.equal(got, clean) and torch.equal(gl, cl)
 
 
-@pytest.mark.parametrize("G", [1, 5, 8])
+@pytest.mark.parametrize("D,G", [(64, 1), (64, 5), (64, 8), (32, 1), (32, 8)])
 @pytest.mark.parametrize("types", PAIRS, ids=ids)
-def test_heads_of_64_channels_side_by_side(types, G):
+def test_short_heads_side_by_side(types, D, G):
     """Two heads that lie next to each other, also where one of them is not
     finite, in a split sequence, a short one, an empty one and many whole ones."""
     dt, ct = types
     for lens, wide in (([2100, 70, 0, 1], 2000), ([40, 300, 0, 7] * 140, 20)):
-        say("side by side", types, G, len(lens))
-        c = Cache(lens, 16, 4, 64, dt, ct, wide=wide)
-        q = torch.randn((len(lens), 4 * G, 64), generator=torch.Generator().manual_seed(4)).to(dt)
+        say("side by side", types, D, G, len(lens))
+        c = Cache(lens, 16, 4, D, dt, ct, wide=wide)
+        q = torch.randn((len(lens), 4 * G, D), generator=torch.Generator().manual_seed(4)).to(dt)
         bias = torch.randn((4 * G, 81), generator=torch.Generator().manual_seed(5))
         out, lse, tol, tl = attention(q, c, bias=bias, cap=15.0)
         kp, vp, table, scales = c.device()
