@@ -9,9 +9,10 @@
 // Bound by the bytes: each value is read and written once.  A lane takes 16
 // bytes of a head's channels and of their partners, and the same channels of up
 // to four heads of the token, so that an angle's sine and cosine (30 operations a
-// pair) are spread over them; all of it is loaded before the angles are made.
-// Backward, 8 rows of 4096 tokens, 40 heads of 128, bf16: 129 us, 5.2 TB/s (144
-// with the angles first).
+// pair) are spread over them; all of it is loaded before the angles are made and
+// stored when all of it is turned.  Backward, 8 rows of 4096 tokens, 40 heads of
+// 128, bf16: 121 us, 5.5 TB/s (15 more with the angles first, 10 where each head is
+// stored before the next is turned).
 #include "seq_rotary.hpp"
 
 namespace im2win {
@@ -37,14 +38,14 @@ __device__ inline void cos_sin(uint32_t turn, float &c, float &s)
     s = q & 2 ? -s : s;
 }
 
-// N values from p on, n of them there, as they lie in memory; whole vectors with
-// their element's alignment, as rotated parts and strides may start anywhere.
-template <class T, int N>
+// N values from p on as they lie in memory, vectors with their element's alignment,
+// as rotated parts and strides may start anywhere.  PART: fewer, n, may be there.
+template <class T, int N, bool PART>
 struct Run {
     typedef T V __attribute__((ext_vector_type(N), aligned(sizeof(T))));
     __device__ static inline V load(const char *p, int n)
     {
-        if (n >= N)
+        if (!PART || n >= N)
             return *(const V *)p;
         V v = {};
 #pragma unroll
@@ -56,13 +57,13 @@ struct Run {
     // Values from..n-1.
     __device__ static inline void store(char *p, int from, int n, const V &v)
     {
-        if (from == 0 && n >= N) {
+        if (from == 0 && (!PART || n >= N)) {
             *(V *)p = v;
             return;
         }
 #pragma unroll
         for (int e = 0; e < N; ++e)
-            if (e >= from && e < n)
+            if (e >= from && (!PART || e < n))
                 ((T *)p)[e] = v[e];
     }
 };
@@ -82,14 +83,25 @@ __device__ inline void copy_few(char *o, const char *p, int n)
     }
 }
 
+// Pairs of a unit: 16 bytes of a side (of both, side by side).
+template <class E, bool PAIRED>
+constexpr int kPairs = (PAIRED ? 8 : 16) / sizeof(typename E::T);
+// Pairs of a unit in small calls and of few pairs, see plan_rotary.
+constexpr int kFew = 2;
+
 // Lanes: units of a head fastest, then groups of heads, then tokens.  A unit is
 // N pairs (N values and their N partners; side by side, 2N values in a row),
-// behind them, where x is not y, W channels that are copied.  Where N does not
-// divide the pairs, the last unit is moved back to end with them: the pairs it
-// shares with the one before come out alike, so that both may store them,
-// unless x is y, where it stores its own only (the others may be turned
+// behind them, where x is not y (COPIES), 16 bytes of channels that are copied.
+// Where N does not divide the pairs, the last unit is moved back to end with them:
+// the pairs it shares with the one before come out alike, so that both may store
+// them, unless x is y, where it stores its own only (the others may be turned
 // already).  So too the last unit of the copied channels.
-template <class E, bool PAIRED, int N, int HEADS, int PAIRS>
+// Turned and copied channels share lines of 128 bytes, and are loaded and stored by
+// one instruction where both are 16 bytes, so that no line is written in two
+// pieces: 15 rows of 2404 tokens, 40 heads of 64, bf16, 16 channels turned, 66 us
+// so, 116 where a wave's copies go before its pairs, 101 where they are loaded with
+// them and stored before.
+template <class E, bool PAIRED, int N, int HEADS, bool COPIES, int PAIRS>
 __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a, TurnsOf<PAIRS> f)
 {
     typedef typename E::T T;
@@ -103,117 +115,132 @@ __global__ __launch_bounds__(kThreads) void rotary(RotaryArgs a, TurnsOf<PAIRS> 
     const char *x = a.x + b * a.x_sb + t * a.x_st;
     char *y = a.y + b * a.y_sb + t * a.y_st;
     const int half = a.rot / 2;
-    typedef Run<T, N> R;
-    typedef Run<T, W> RW;
-    typename R::V u[HEADS], v[HEADS];  // the pairs' two sides; side by side, all of them in w
-    typename RW::V w[HEADS];
+    constexpr int CW = 16 / sizeof(T);  // copied channels of a lane
+    constexpr bool ONE = W == CW;       // loaded and stored as pairs are
+    constexpr bool PART = N == kFew;    // larger units are for as many pairs or more
+    typedef Run<T, N, PART> R;
+    typedef Run<T, W, PART> RW;
+    typedef Run<T, CW, false> RC;
+    typename RW::V w[HEADS];  // the pairs (as ONE, also copied channels, whose bits stay), or their first side and in v the second
+    typename R::V v[HEADS];
+    typename RC::V copied[HEADS];
 
     // this lane's heads: group, group + groups, ..
-    if ((int)unit >= a.pair_units) {
-        int c = a.rot + (unit - a.pair_units) * W;
-        const int n = a.D - c;
-        const bool all = a.D - a.rot >= W;
-        c = all ? min(c, a.D - W) : c;
-        x += c * sizeof(T);
-        y += c * sizeof(T);
-        if (all) {
+    int copies = COPIES && (int)unit >= a.pair_units;
+    const int own = unit * N;  // its pairs are own .. own + N - 1, as far as there are
+    const int first = half >= N ? min(own, half - N) : own, n = half - first;
+    int at = PAIRED ? 2 * first : first, values = PAIRED ? 2 * n : n;
+    const int to = half * sizeof(T);
+    if (copies) {
+        at = a.rot + (unit - a.pair_units) * CW;
+        values = a.D - at;
+        if (a.D - a.rot < CW) {
 #pragma unroll
             for (int k = 0; k < HEADS; ++k) {
                 const int h = group + k * a.groups.d;
                 if (h >= a.H)
                     break;
-                w[k] = *(const typename RW::V *)(x + h * a.x_sh);  // as bits: a NaN keeps its payload
+                copy_few<T, CW>(y + h * a.y_sh + at * sizeof(T), x + h * a.x_sh + at * sizeof(T), values);
             }
+            return;
         }
-#pragma unroll
-        for (int k = 0; k < HEADS; ++k) {
-            const int h = group + k * a.groups.d;
-            if (h >= a.H)
-                break;
-            if (all)
-                *(typename RW::V *)(y + h * a.y_sh) = w[k];
-            else
-                copy_few<T, W>(y + h * a.y_sh, x + h * a.x_sh, n);
-        }
-        return;
+        at = min(at, a.D - CW);
+        values = CW;
     }
-    const int own = unit * N;  // its pairs are own .. own + N - 1, as far as there are
-    const int first = half >= N ? min(own, half - N) : own, n = half - first;
-    const int at = (PAIRED ? 2 * first : first) * sizeof(T), to = half * sizeof(T);
-#pragma unroll
-    for (int k = 0; k < HEADS; ++k) {
-        const int h = group + k * a.groups.d;
-        if (h >= a.H)
-            break;
-        const char *const p = x + h * a.x_sh + at;
-        if constexpr (PAIRED) {
-            w[k] = RW::load(p, 2 * n);
-        } else {
-            u[k] = R::load(p, n);
-            v[k] = R::load(p + to, n);
-        }
-    }
+    x += at * sizeof(T);
+    y += at * sizeof(T);
+    // first, so that the angles need not wait for the rest
     int64_t pos = t;
     if (a.pos)
         pos = a.by_token ? (int64_t)a.pos[token] : (int64_t)a.pos[b] + t;
-    float c[N], s[N];
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-        const uint64_t turn = (uint64_t)pos * f.turn[e < n ? first + e : 0];
-        cos_sin((uint32_t)(turn >> 32), c[e], s[e]);
-        c[e] *= a.amplitude;
-        s[e] *= a.sin_amplitude;
-    }
-    const int skip = a.in_place ? own - first : 0;  // pairs that the unit before stores
 #pragma unroll
     for (int k = 0; k < HEADS; ++k) {
         const int h = group + k * a.groups.d;
         if (h >= a.H)
             break;
-        char *const o = y + h * a.y_sh + at;
+        const char *const p = x + h * a.x_sh;
+        if (!ONE && copies)
+            copied[k] = *(const typename RC::V *)p;
+        else
+            w[k] = RW::load(p, values);
+        if (!PAIRED && !copies)
+            v[k] = R::load(p + to, n);
+    }
+    if constexpr (COPIES)
+        asm("" : "+v"(copies));  // or the compiler makes two paths of it, one behind the other
+    float c[N], s[N];
+    if (!copies) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const float p = E::get(PAIRED ? w[k][PAIRED ? 2 * e : 0] : u[k][e]);
-            const float q = E::get(PAIRED ? w[k][PAIRED ? 2 * e + 1 : 0] : v[k][e]);
-            // Rounded to fp32, then to T, wherever in a vector the pair stands: the
-            // compiler may neither fuse the products its own way nor make a mixed
-            // fp16 instruction of the sum and its conversion.
-            float fp = fmaf(p, c[e], -(q * s[e])), fq = fmaf(p, s[e], q * c[e]);
-            asm("" : "+v"(fp), "+v"(fq));
-            const T yp = E::put(fp), yq = E::put(fq);
-            if constexpr (PAIRED)
-                w[k][2 * e] = yp, w[k][2 * e + 1] = yq;
-            else
-                u[k][e] = yp, v[k][e] = yq;
+            const uint64_t turn = (uint64_t)pos * f.turn[e < n ? first + e : 0];
+            cos_sin((uint32_t)(turn >> 32), c[e], s[e]);
+            c[e] *= a.amplitude;
+            s[e] *= a.sin_amplitude;
         }
-        if constexpr (PAIRED) {
-            RW::store(o, 2 * skip, 2 * n, w[k]);
+    }
+    const int skip = a.in_place && !copies ? own - first : 0;  // pairs that the unit before stores
+#pragma unroll
+    for (int k = 0; k < HEADS; ++k) {
+        const int h = group + k * a.groups.d;
+        if (h >= a.H)
+            break;
+        if (!copies) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float p = E::get(w[k][PAIRED ? 2 * e : e]);
+                const float q = E::get(PAIRED ? w[k][PAIRED ? 2 * e + 1 : 0] : v[k][e]);
+                // Rounded to fp32, then to T, wherever in a vector the pair stands: the
+                // compiler may neither fuse the products its own way nor make a mixed
+                // fp16 instruction of the sum and its conversion.
+                float fp = fmaf(p, c[e], -(q * s[e])), fq = fmaf(p, s[e], q * c[e]);
+                asm("" : "+v"(fp), "+v"(fq));
+                w[k][PAIRED ? 2 * e : e] = E::put(fp);
+                if constexpr (PAIRED)
+                    w[k][2 * e + 1] = E::put(fq);
+                else
+                    v[k][e] = E::put(fq);
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < HEADS; ++k) {
+        const int h = group + k * a.groups.d;
+        if (h >= a.H)
+            break;
+        char *const o = y + h * a.y_sh;
+        if (!ONE && copies) {
+            *(typename RC::V *)o = copied[k];
+        } else if (!PART && skip == 0) {
+            *(typename RW::V *)o = w[k];
+            if (!PAIRED && !copies)
+                *(typename R::V *)(o + to) = v[k];
         } else {
-            R::store(o, skip, n, u[k]);
-            R::store(o + to, skip, n, v[k]);
+            RW::store(o, PAIRED ? 2 * skip : skip, values, w[k]);
+            if (!PAIRED && !copies)
+                R::store(o + to, skip, n, v[k]);
         }
     }
 }
 
-// Pairs of a unit: 16 bytes of a side (of both, side by side).
-template <class E, bool PAIRED>
-constexpr int kPairs = (PAIRED ? 8 : 16) / sizeof(typename E::T);
-// Pairs of a unit in small calls and of few pairs, see plan_rotary.
-constexpr int kFew = 2;
-
-template <class E, bool PAIRED, int PAIRS>
-void run(const RotaryArgs &a, const TurnsOf<PAIRS> &f, hipStream_t st)
+template <class E, bool PAIRED, bool COPIES, int PAIRS>
+void run_copies(const RotaryArgs &a, const TurnsOf<PAIRS> &f, hipStream_t st)
 {
     const uint32_t grid = (a.lanes + kThreads - 1) / kThreads;
     const bool heads = (uint32_t)a.H > a.groups.d;  // up to 4 a lane
     if (a.few && heads)
-        rotary<E, PAIRED, kFew, 4><<<grid, kThreads, 0, st>>>(a, f);
+        rotary<E, PAIRED, kFew, 4, COPIES><<<grid, kThreads, 0, st>>>(a, f);
     else if (a.few)
-        rotary<E, PAIRED, kFew, 1><<<grid, kThreads, 0, st>>>(a, f);
+        rotary<E, PAIRED, kFew, 1, COPIES><<<grid, kThreads, 0, st>>>(a, f);
     else if (heads)
-        rotary<E, PAIRED, kPairs<E, PAIRED>, 4><<<grid, kThreads, 0, st>>>(a, f);
+        rotary<E, PAIRED, kPairs<E, PAIRED>, 4, COPIES><<<grid, kThreads, 0, st>>>(a, f);
     else
-        rotary<E, PAIRED, kPairs<E, PAIRED>, 1><<<grid, kThreads, 0, st>>>(a, f);
+        rotary<E, PAIRED, kPairs<E, PAIRED>, 1, COPIES><<<grid, kThreads, 0, st>>>(a, f);
+}
+
+template <class E, bool PAIRED, int PAIRS>
+void run(const RotaryArgs &a, const TurnsOf<PAIRS> &f, hipStream_t st)
+{
+    (int)a.units.d > a.pair_units ? run_copies<E, PAIRED, true>(a, f, st) : run_copies<E, PAIRED, false>(a, f, st);
 }
 
 template <class E>
@@ -238,7 +265,7 @@ bool plan_rotary(RotaryArgs &a, int64_t B, int64_t L, bool paired, bool in_place
     const int64_t units_few = (a.rot / 2 + kFew - 1) / kFew, full = (paired ? 8 : 16) / e;
     const bool small = B * L <= 1 << 17 && B * L * a.H <= 1 << 17 && B * L * a.H * units_few <= 1 << 17;
     a.few = small || a.rot / 2 < full;
-    const int64_t N = a.few ? kFew : full, W = paired ? 2 * N : N;
+    const int64_t N = a.few ? kFew : full, W = 16 / e;
     a.pair_units = (int32_t)((a.rot / 2 + N - 1) / N);
     const int64_t units = a.pair_units + (in_place ? 0 : (a.D - a.rot + W - 1) / W);
     if (B * L * units > UINT32_MAX)  // so that the products below fit

@@ -118,6 +118,29 @@ def test_in_place_where_units_overlap(shape, dtype, interleaved):
         assert torch.equal(again, want)
 
 
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("interleaved", [False, True], ids=["half", "pairs"])
+@pytest.mark.parametrize("D,rot", [(64, 2), (64, 6), (64, 20), (64, 60), (72, 32), (80, 80), (30, 22)])
+def test_long_calls_are_short_ones_in_a_row(D, rot, dtype, interleaved):
+    """Bit for bit, though lanes take more pairs and heads; copied channels as they are."""
+    B, L, H = 2, 2100, 27
+    x, pos = inputs(B, L, H, D, dtype, seed=3, far=9000)
+    freq = pkg.seq_rotary_frequencies(rot)
+    xd, pd = x.cuda(), pos.cuda()
+    xd[:, ::7, :, rot:] = float("nan")
+    got = pkg.seq_rotary_forward(xd, freq, pd, interleaved)
+    for at in (0, 1000, 2095):
+        few = slice(at, at + 5)
+        want = pkg.seq_rotary_forward(xd[:, few], freq, pd[:, few].contiguous(), interleaved)
+        assert torch.equal(got[:, few, :, :rot], want[..., :rot])
+    bits = {4: torch.int32, 2: torch.int16}[x.element_size()]
+    assert torch.equal(got[..., rot:].contiguous().view(bits), xd[..., rot:].contiguous().view(bits))
+    ref, tol = rotary(x[:, 1000:1040], freq.tolist(), pos[:, 1000:1040], interleaved)
+    check(got[:, 1000:1040, :, :rot], ref[..., :rot], tol[..., :rot], "rotary")
+    pkg.seq_rotary_forward(xd, freq, pd, interleaved, out=xd)
+    assert torch.equal(xd[..., :rot], got[..., :rot])
+
+
 def test_gradient_against_differences():
     """sum(dy * y(x + h d)) - sum(dy * y(x - h d)) over 2h against sum(dx * d):
     the map is linear, so the difference is exact but for rounding (fp32, sums
