@@ -401,6 +401,8 @@ PyObject *paged_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
     at::Tensor lse = empty({c.c.B, a.H}, at::kFloat, c.device);
     if (args[11] != Py_None) {
         ws = tensor(args[11], "ws");
+        if (!ws.is_contiguous())  // its bytes are numbered from the first
+            refuse(PyExc_ValueError, "ws must be contiguous");
         on_device(ws, c.device);
     } else {
         const int64_t need = seq_paged_attention_workspace_bytes(&c.c, a.H, (im2win_dtype_t)a.dt);

@@ -240,6 +240,9 @@ def test_binding_refusals(lib):
         pkg.seq_cache_read(pages, pages, table, length, 2.5)
     with pytest.raises(ValueError):
         pkg.seq_cache_read(pages, pages, table, length, -1)
+    for ws in (torch.zeros(1).expand(1 << 20), torch.zeros(1 << 10)[::2]):
+        with pytest.raises(ValueError):
+            a(q, pages, pages, table, length, ws=ws)
     # host memory is refused by its address
     for call in (lambda: a(q, pages, pages, table, length), lambda: w(k, k, pages, pages.clone(), table),
                  lambda: pkg.seq_cache_read(pages, pages, table, length, 8), lambda: pkg.seq_rotary_forward(k, freq)):
