@@ -353,8 +353,9 @@ __device__ inline Part find_part(const Pool &c, const PagedArgs &a, int32_t inde
 }
 
 // The workspace: for each sequence its first part and their number (written by
-// the first part's workgroup, for the join), then the parts: sums, maximum and
-// sum of the exponentials of row `head` in part `index`.
+// the first part's workgroup, for the join), then the parts: sums, maximum, sum of
+// the exponentials and, of 8 bits, what 1 in the sums stands for, of row `head` in
+// part `index`.
 struct FirstPart {
     int32_t index, parts;
 };
@@ -363,6 +364,20 @@ __device__ inline float *part_of(const PagedArgs &a, int64_t index, int head, in
 {
     return a.part + first_part_floats(a.B) + (index * a.H + head) * part_floats(D);
 }
+
+// Sums of 8-bit values are kept as numbers times a power of two, the unit, up to the
+// last step, after the division by the sum of the weights: a result that the type
+// holds is reached, however many keys and however large scales led to it.  The least
+// unit is that which 2^14 can be divided by; smaller scales' weights are subnormal.
+constexpr float kLeastUnit = 0x1p-112f;
+// The power of two at or above x, from kLeastUnit to 2^126.
+__device__ inline float power_up_to(float x)
+{
+    const uint32_t bits = (__builtin_bit_cast(uint32_t, fmaxf(x, kLeastUnit)) + 0x7FFFFFu) & 0x7F800000u;
+    return __builtin_bit_cast(float, min(bits, 253u << 23));
+}
+// Of a power of two from 2^-126 to 2^126.
+__device__ inline float inverse(float x) { return __builtin_bit_cast(float, (254u << 23) - __builtin_bit_cast(uint32_t, x)); }
 
 // FULL: heads have DP channels, no more tests of where they end.
 // PAIR: two key/value heads that lie side by side are taken as one of DP channels
@@ -379,12 +394,13 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
     typedef Math<E, Code, DP, SMALL> M;
     constexpr int KEYS = M::KEYS, N = M::N, VC = M::VC, ES = M::ES;
     // fp16 probabilities are times 2^14, so that those of long rows stay normal numbers
-    constexpr float kShift = M::kHalf ? 14.0f : 0.0f, kUnshift = M::kHalf ? 0x1p-14f : 1.0f;
+    // (over 8-bit pages the unit of their products with the scales carries it)
+    constexpr float kShift = M::kHalf && !M::kCodes ? 14.0f : 0.0f, kUnshift = M::kHalf && !M::kCodes ? 0x1p-14f : 1.0f;
     constexpr int HEADS = PAIR ? 2 : 1;
     static_assert(!PAIR || (FULL && DP * ES >= 128));  // whole pieces a head
     __shared__ __align__(16) Where<KEYS, HEADS> where[kWavesP];
     __shared__ float box[kWavesP][16][DP + 4];
-    __shared__ float sm[kWavesP][16], sl[kWavesP][16];
+    __shared__ float sm[kWavesP][16], sl[kWavesP][16], su[kWavesP][16];
     const int D = FULL ? DP : c.D, one = D / HEADS;  // channels of the tile, of a head
 
     // blockIdx: heads fastest, then row tiles, then parts.  Workgroups go to the 8
@@ -505,7 +521,7 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
     for (int j = 0; j < VC; ++j)
         o[j] = f32x4_acc{0, 0, 0, 0};
     float m = -INFINITY, l = 0;
-    float unit = 0x1p-126f;  // 8 bits: the values' scales are over this power of two
+    float unit = kLeastUnit;  // 8 bits: what 2^14 in the outputs stands for, a power of two
 
     // The first loads start in the order in which they are needed last: pages'
     // numbers, the query (made into operands while keys and values come), keys.
@@ -618,11 +634,9 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
                 top = fmaxf(top, vscale[i]);
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            // up to the next power of two, at most 2^126
-            const uint32_t bits = min((__builtin_bit_cast(uint32_t, top) + 0x7FFFFFu) & 0x7F800000u, 253u << 23);
-            const float now = __builtin_bit_cast(float, bits);
-            over = __builtin_bit_cast(float, (254u << 23) - bits);
-            up = unit * over;
+            const float now = power_up_to(top);
+            over = 0x1p14f * inverse(now);
+            up = unit * inverse(now);
             unit = now;
         }
 #pragma unroll
@@ -688,12 +702,24 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
     if (g == 0) {
         sm[wave][r] = m;
         sl[wave][r] = l;
+        if constexpr (M::kCodes)
+            su[wave][r] = unit;
     }
     __syncthreads();
+    // 8 bits: the unit of a row's sum over the waves w0, w0 + row_waves, ..
+    auto common = [&](int w0, int r, float top) {
+        const float base = top == -INFINITY ? 0.0f : top;
+        float u = 0;
+        for (int w = w0; w < kWavesP; w += a.row_waves)
+            u = fmaxf(u, su[w][r] * __builtin_amdgcn_exp2f(sm[w][r] - base));
+        return power_up_to(u);
+    };
     float top = -INFINITY;
     for (int w = wave % a.row_waves; w < kWavesP; w += a.row_waves)
         top = fmaxf(top, sm[w][r]);
-    const float mine = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top)) * (M::kCodes ? unit : 1.0f);
+    float mine = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
+    if constexpr (M::kCodes)
+        mine *= unit * inverse(common(wave % a.row_waves, r, top));
     // this lane's channels are 4*VC*g .. 4*VC*(g + 1) - 1
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -720,6 +746,7 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
                 for (int e = 0; e < 8; ++e)
                     v[e] += box[w][rr][ch + e];
         }
+        const float value = M::kCodes ? common(w0, rr, ms) * 0x1p-14f : 1.0f;  // of 1 in v
         if (part.parts > 1) {
             float *const to = part_of(a, index, hk * a.G + rw, one);
             if (to_ch >= 0 && to_ch < one)
@@ -727,6 +754,7 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
             if (to_ch == 0) {
                 to[one] = ms;
                 to[one + 1] = sum;
+                to[one + 2] = value;
             }
         } else {
             const bool none = sum == 0.0f;  // not ms == -inf: all scores may be NaN
@@ -735,7 +763,7 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
                 V8 y;
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    y[e] = E::put(none ? 0.0f : v[e] / sum);
+                    y[e] = E::put(none ? 0.0f : v[e] / sum * value);
                 *(V8 *)(a.out + b * a.o_sb + (hk * a.G + rw) * a.o_sh + to_ch * sizeof(typename E::T)) = y;
             }
             if (to_ch == 0)
@@ -746,13 +774,14 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
 
 // Joins the parts of a row: 32 lanes hold its channels, four each, and `groups`
 // of them (1 or 8) take its parts in turn.  Rows of one part are done already.
-template <class E, bool HALF>
+// SHIFTED: weights are times 2^14; UNITS: sums are times a unit (8 bits).
+template <class E, bool SHIFTED, bool UNITS>
 __global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int groups)
 {
     typedef float v4 __attribute__((ext_vector_type(4)));
     __shared__ v4 sv[8][32];
-    __shared__ float sl[8], sm[8];
-    constexpr float kUnshift = HALF ? 0x1p-14f : 1.0f;
+    __shared__ float sl[8], sm[8], su[8];
+    constexpr float kUnshift = SHIFTED ? 0x1p-14f : 1.0f;
     const int rows = a.B * a.H, lane = threadIdx.x & 31, d = lane * 4, group = threadIdx.x >> 5, first = group % groups;
     const int row = blockIdx.x * (8 / groups) + group / groups, live = row < rows;
     const int b = live ? row / a.H : 0, h = live ? row - b * a.H : 0;
@@ -761,38 +790,49 @@ __global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int group
     const int parts = live && tokens_of(c, a, b) > 0 ? of.parts : 0;
     if (groups > 1 ? parts == 1 : __all(parts == 1 || !live))  // groups > 1: one row a workgroup
         return;
-    // running maximum, sum and outputs: a part's numbers are loaded at once
-    float m = -INFINITY, l = 0;
+    // running maximum, sum, outputs and their unit: a part's numbers are loaded at once
+    float m = -INFINITY, l = 0, unit = UNITS ? 0x1p-126f : 1.0f;
     v4 v = {0, 0, 0, 0};
+    // the unit of two sums, of which the factors f and g become those to it
+    auto meet = [&](float &f, float &g, float other) {
+        if constexpr (UNITS) {
+            f *= unit, g *= other;
+            unit = power_up_to(fmaxf(f, g));
+            f *= inverse(unit), g *= inverse(unit);
+        }
+    };
 #pragma unroll 4
     for (int k = first; k < parts; k += groups) {
         const float *const p = part_of(a, at + k, h, c.D);
-        const float pm = p[c.D], pl = p[c.D + 1];
+        const float pm = p[c.D], pl = p[c.D + 1], pu = UNITS ? p[c.D + 2] : 1.0f;
         const v4 pv = d < c.D ? *(const v4 *)(p + d) : v4{0, 0, 0, 0};
         const float top = fmaxf(m, pm), base = top == -INFINITY ? 0.0f : top;
-        const float f = __builtin_amdgcn_exp2f(m - base), g = __builtin_amdgcn_exp2f(pm - base);
+        float f = __builtin_amdgcn_exp2f(m - base), g = __builtin_amdgcn_exp2f(pm - base);
         m = top;
         l = l * f + pl * g;
+        meet(f, g, pu);
         v = v * f + pv * g;
     }
     if (groups > 1) {
         sv[group][lane] = v;
         if (lane == 0)
-            sl[group] = l, sm[group] = m;
+            sl[group] = l, sm[group] = m, su[group] = unit;
         __syncthreads();
         if (group)
             return;
         float top = m;
         for (int k = 1; k < 8; ++k)
             top = fmaxf(top, sm[k]);
-        const float base = top == -INFINITY ? 0.0f : top, f = __builtin_amdgcn_exp2f(m - base);
-        v *= f;
+        const float base = top == -INFINITY ? 0.0f : top;
+        float f = __builtin_amdgcn_exp2f(m - base);
         l *= f;
         m = top;
         for (int k = 1; k < 8; ++k) {
-            const float g = __builtin_amdgcn_exp2f(sm[k] - base);
-            v += sv[k][lane] * g;
+            float g = __builtin_amdgcn_exp2f(sm[k] - base);
             l += sl[k] * g;
+            meet(f, g, su[k]);
+            v = v * f + sv[k][lane] * g;
+            f = 1.0f;
         }
     }
     if (!live || parts == 1)
@@ -805,7 +845,7 @@ __global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int group
         V4 y;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            y[e] = E::put(none ? 0.0f : v[e] / l);
+            y[e] = E::put(none ? 0.0f : v[e] / l * unit);
         *(V4 *)(a.out + b * a.o_sb + h * a.o_sh + d * sizeof(typename E::T)) = y;
     }
 }
@@ -909,7 +949,8 @@ void run(const Plan &p, const Pool &c, PagedArgs a, hipStream_t st)
     if (a.most_parts) {
         const int64_t rows = (int64_t)a.B * a.H;
         const int groups = rows <= 2048 ? 8 : 1;
-        paged_join<E, Math<E, Code, 64, false>::kHalf><<<(uint32_t)((rows * groups + 7) / 8), 256, 0, st>>>(c, a, groups);
+        typedef Math<E, Code, 64, false> M;
+        paged_join<E, M::kHalf && !M::kCodes, M::kCodes><<<(uint32_t)((rows * groups + 7) / 8), 256, 0, st>>>(c, a, groups);
     }
 }
 

@@ -1,0 +1,56 @@
+"""Attention over 8-bit pages whose numbers come near the ends of the type's range."""
+import pytest
+import torch
+
+import paper_2608_20725_amd as pkg
+from gpu_util import say
+from seq_cache_ref import E4M3, Cache, attention
+from seq_ref import check
+
+pytestmark = pytest.mark.gpu
+
+F32, F16, BF16, I8 = torch.float32, torch.float16, torch.bfloat16, torch.int8
+NAMES = {F32: "f32", F16: "f16", BF16: "bf16", I8: "i8", E4M3: "e4m3"}
+WIDE_OVER_CODES = [(F32, I8), (BF16, I8), (F32, E4M3), (BF16, E4M3)]
+ids = lambda v: "-".join(NAMES[t] for t in v) if isinstance(v[0], torch.dtype) else None
+
+
+def scaled(c, name, factor):
+    """The cache's keys or values times ``factor`` [B][longest][Hkv] or a number, by their scales."""
+    s = getattr(c, name + "_codes")
+    old = getattr(c, name).abs().amax(-1) / s.abs().amax(-1).clamp(min=1)
+    new = (old * factor).float()
+    setattr(c, name, s * new.double()[..., None])
+    setattr(c, name + "_top", float(new.max()))
+    c._fill(getattr(c, name + "_scale"), new)
+
+
+def attend(q, c, **opts):
+    kp, vp, table, scales = c.device()
+    need = pkg.seq_paged_attention_workspace_bytes(q.cuda(), kp, vp, table, **scales)
+    out, lse = pkg.seq_paged_attention_forward(q.cuda(), kp, vp, table, c.len.cuda(), **scales, **opts)
+    return out, lse, need > 0
+
+
+# Lengths, table, key/value heads, queries each, channels; whether the keys are split.
+SHAPES = [([1], None, 1, 1, 64, False), ([1, 700, 0, 5000], None, 2, 4, 64, True), ([3000], 2000, 1, 5, 128, True),
+          ([40, 300, 1] * 50, 20, 2, 2, 128, False), ([900, 33], 500, 2, 17, 72, True), ([2500, 3], None, 1, 40, 64, True),
+          ([300, 12], 20, 3, 3, 32, False)]
+
+
+@pytest.mark.parametrize("e", [108, 112, 116, 120, 123])
+@pytest.mark.parametrize("types", WIDE_OVER_CODES, ids=ids)
+def test_values_near_the_largest_number(types, e):
+    """Every result is a mean of values, so it is within the type's range where they are (up to 2^(e + 3.2))."""
+    dt, ct = types
+    for k, (lens, wide, Hkv, G, D, split) in enumerate(SHAPES):
+        say("large values", types, e, k)
+        c = Cache(lens, 16, Hkv, D, dt, ct, wide=wide, seed=k)
+        scaled(c, "v", 2.0 ** e)
+        q = (torch.randn((len(lens), Hkv * G, D), generator=torch.Generator().manual_seed(k)) * 2.0 ** -4).to(dt)
+        out, lse, tol, tl = attention(q, c)
+        assert torch.isfinite(out).all() and float(out.abs().max()) < 2.0 ** 127
+        got, gl, parts = attend(q, c)
+        assert parts == split
+        check(got, out, tol + 1e-30, "out %d" % k)
+        check(gl, lse, tl + 1e-30, "lse %d" % k)
