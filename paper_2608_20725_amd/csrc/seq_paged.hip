@@ -18,7 +18,8 @@
 //
 // 8-bit pages go through the matrix cores as fp16, which holds every code
 // exactly; a key's scale multiplies its score, a value's the probability, over
-// the largest power of two at or above a scale seen so far.  bf16 and fp32
+// the power of two at or above the largest such product so far (not the largest
+// scale: a value that is not looked at would take the others' bits).  bf16 and fp32
 // queries over them are brought to fp16's range by a power of two a row: what
 // falls below 2^-39 of the row's largest channel is lost, less than fp32 sums
 // lose.  fp32 ones, and their probabilities, are two fp16 numbers each, 22 bits,
@@ -626,19 +627,6 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
         }
 
         // softmax
-        float up = 1.0f, over = 1.0f;
-        if constexpr (M::kCodes) {
-            float top = unit;
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                top = fmaxf(top, vscale[i]);
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float now = power_up_to(top);
-            over = 0x1p14f * inverse(now);
-            up = unit * inverse(now);
-            unit = now;
-        }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float x = s[i] * c1;
@@ -678,10 +666,25 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
             w.p[i] = __builtin_amdgcn_exp2f(s[i] - less);
             sum += w.p[i];
             if constexpr (M::kCodes)
-                w.p[i] *= vscale[i] * over;
+                w.p[i] *= vscale[i];
         }
         l = l * f + sum;
-        f *= up;
+        if constexpr (M::kCodes) {
+            // the weights' unit: at or above the largest of them, and of those before
+            float most = 0;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                most = fmaxf(most, fabsf(w.p[i]));
+            most = fmaxf(most, __shfl_xor(most, 16));
+            most = fmaxf(most, __shfl_xor(most, 32));
+            f *= unit;
+            unit = power_up_to(fmaxf(f, most));
+            const float inv = inverse(unit);
+            f *= inv;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                w.p[i] *= 0x1p14f * inv;
+        }
         if (__any(f != 1.0f)) {
 #pragma unroll
             for (int j = 0; j < VC; ++j)

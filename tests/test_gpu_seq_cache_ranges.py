@@ -54,3 +54,37 @@ def test_values_near_the_largest_number(types, e):
         assert parts == split
         check(got, out, tol + 1e-30, "out %d" % k)
         check(gl, lse, tl + 1e-30, "lse %d" % k)
+
+
+@pytest.mark.parametrize("r", [30, 45, 100, 200])
+@pytest.mark.parametrize("types", WIDE_OVER_CODES + [(F16, I8), (F16, E4M3)], ids=ids)
+def test_large_values_that_are_not_looked_at(types, r):
+    """A token whose weight is nothing, with a value 2^r times the others', takes no bit of theirs: in its tile, in
+    one before and in one behind, in its part of split keys and in whole sequences."""
+    dt, ct = types
+    least = -90 if r == 200 and dt != F16 else 0  # the others' size
+    r = min(r, 110) if dt == F16 else r
+    for k, (lens, wide, at) in enumerate((([2], None, 0), ([700, 300], None, 0), ([700, 300], None, 299), ([260] * 40, 20, 130),
+                                          ([6000, 3000], 500, 2900))):
+        say("not looked at", types, r, k)
+        D = 64 if k % 2 else 128
+        c = Cache(lens, 16, 2, D, dt, ct, wide=wide, seed=k)
+        f = torch.full(c.v.shape[:3], 2.0 ** least, dtype=torch.float64)
+        f[:, at] *= 2.0 ** r
+        scaled(c, "v", f)
+        q = torch.randn((len(lens), 4, D), generator=torch.Generator().manual_seed(k)).to(dt)
+        # the bias of its distance puts its score 400 below the others'
+        n, R = min(lens), 1000
+        c.len = torch.full_like(c.len, n)
+        bias = torch.zeros(4, 2 * R + 1)
+        bias[:, R - (n - 1 - at)] = -400.0
+        _, lse, _, tl = attention(q, c, bias=bias)
+        # and the bound is that of the others
+        there = torch.ones(c.v.shape[:2], dtype=torch.bool)
+        there[:, at] = False
+        c.v_codes[:, at], c.v[:, at] = 0, 0
+        c.v_top *= 2.0 ** -r
+        near, _, tol, _ = attention(q, c, there, bias=bias)
+        got, gl, _ = attend(q, c, bias=bias.cuda())
+        check(got, near, tol + 1e-40, "out %d" % k)
+        check(gl, lse, tl + 1e-30, "lse %d" % k)
