@@ -629,9 +629,8 @@ __global__ __launch_bounds__(64 * kWavesP, 2) void paged_attn(Pool c, PagedArgs 
         // softmax
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            float x = s[i] * c1;
-            if constexpr (M::kCodes)
-                x *= kscale[i];
+            // the factors first: a query of 2^120 and a key of 2^-120 may have a score of 1
+            float x = s[i] * (M::kCodes ? c1 * kscale[i] : c1);
             if (a.cap > 0) {
                 const float far = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * (2.0f * kLog2e)));
                 x = c2 * (fabsf(x) < kSmallTanh ? small_tanh(x) : far);

@@ -88,3 +88,21 @@ def test_large_values_that_are_not_looked_at(types, r):
         got, gl, _ = attend(q, c, bias=bias.cuda())
         check(got, near, tol + 1e-40, "out %d" % k)
         check(gl, lse, tl + 1e-30, "lse %d" % k)
+
+
+@pytest.mark.parametrize("e,size", [(-110, 0.5), (-60, 0.5), (60, 0.5), (100, 0.5), (118, 64.0)])
+@pytest.mark.parametrize("types", WIDE_OVER_CODES, ids=ids)
+def test_large_queries_of_small_keys(types, e, size):
+    """Queries of 2^e over keys of 2^-e, all of one sign: ordinary scores."""
+    dt, ct = types
+    for k, (lens, wide, Hkv, G, D, split) in enumerate(SHAPES):
+        say("large queries", types, e, k)
+        c = Cache(lens, 16, Hkv, D, dt, ct, wide=wide, seed=k)
+        c.k, c.k_codes = c.k.abs(), c.k_codes.abs()
+        c._fill(c.k_pages, c.k_codes.to(ct))
+        scaled(c, "k", 2.0 ** -e)
+        q = (torch.randn((len(lens), Hkv * G, D), generator=torch.Generator().manual_seed(k)).abs() * 2.0 ** e).to(dt)
+        out, lse, tol, tl = attention(q, c, scale=size / D)
+        got, gl, _ = attend(q, c, scale=size / D)
+        check(got, out, tol + 1e-30, "out %d" % k)
+        check(gl, lse, tl + 1e-30, "lse %d" % k)
