@@ -146,8 +146,14 @@ struct Cache {
     at::ScalarType type;
 };
 
-Cache cache(PyObject *k_pages, PyObject *v_pages, PyObject *table_, PyObject *k_scale, PyObject *v_scale)
+// Memory that a call writes, asked for before that which it reads: a lazy copy gets
+// its own first, and what shares its storage moves with it.
+void *written(const at::Tensor &t) { return t.mutable_data_ptr(); }
+
+// write: the call writes the pages and scales.
+Cache cache(PyObject *k_pages, PyObject *v_pages, PyObject *table_, PyObject *k_scale, PyObject *v_scale, bool write)
 {
+    const auto memory = [write](const at::Tensor &t) { return write ? written(t) : const_cast<void *>(t.const_data_ptr()); };
     const at::Tensor &k = tensor(k_pages, "k_pages"), &v = tensor(v_pages, "v_pages"), &table = tensor(table_, "table");
     Cache r;
     r.device = k.device(), r.type = k.scalar_type();
@@ -166,7 +172,7 @@ Cache cache(PyObject *k_pages, PyObject *v_pages, PyObject *table_, PyObject *k_
     c.table_stride = c.B > 1 ? table.stride(0) : c.max_pages;
     strides3(k, c.k_stride);
     strides3(v, c.v_stride);
-    c.k = const_cast<void *>(k.const_data_ptr()), c.v = const_cast<void *>(v.const_data_ptr());
+    c.k = memory(k), c.v = memory(v);
     c.table = (const int32_t *)table.const_data_ptr();
     c.k_scale = c.v_scale = nullptr;
     for (int i = 0; i < 3; ++i)
@@ -186,8 +192,7 @@ Cache cache(PyObject *k_pages, PyObject *v_pages, PyObject *table_, PyObject *k_
     on_device(vs, r.device);
     strides3(ks, c.k_scale_stride);
     strides3(vs, c.v_scale_stride);
-    c.k_scale = (float *)const_cast<void *>(ks.const_data_ptr());
-    c.v_scale = (float *)const_cast<void *>(vs.const_data_ptr());
+    c.k_scale = (float *)memory(ks), c.v_scale = (float *)memory(vs);
     return r;
 }
 
@@ -266,8 +271,8 @@ PyObject *rotary(PyObject *, PyObject *const *args, Py_ssize_t n)
     strides3(x, a.x_stride);
     strides3(out, a.y_stride);
     a.freq = (const double *)freq.const_data_ptr();
+    void *const to = written(out);
     const void *const from = x.const_data_ptr();
-    void *const to = const_cast<void *>(out.const_data_ptr());
     check(without_gil([&] { return (backward ? seq_rotary_backward : seq_rotary_forward)(&a, from, to, place.stream); }),
           backward ? "seq_rotary_backward" : "seq_rotary_forward");
     return THPVariable_Wrap(std::move(out));
@@ -279,7 +284,7 @@ PyObject *cache_write(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     expect(n, 9);
-    const Cache c = cache(args[2], args[3], args[4], args[7], args[8]);
+    const Cache c = cache(args[2], args[3], args[4], args[7], args[8], true);
     const at::Tensor &k = tensor(args[0], "k"), &v = tensor(args[1], "v");
     const int64_t L = k.dim() == 4 ? k.size(1) : 0;
     dense(c, k, v, L);
@@ -303,7 +308,7 @@ PyObject *cache_read(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     expect(n, 10);
-    const Cache c = cache(args[0], args[1], args[2], args[6], args[7]);
+    const Cache c = cache(args[0], args[1], args[2], args[6], args[7], false);
     const int64_t L = PyLong_AsLongLong(args[4]);
     if (L == -1 && PyErr_Occurred())
         throw python_error();
@@ -335,7 +340,7 @@ PyObject *cache_read(PyObject *, PyObject *const *args, Py_ssize_t n)
     int64_t ks[3], vs[3];
     strides3(out[0], ks);
     strides3(out[1], vs);
-    void *const kp = const_cast<void *>(out[0].const_data_ptr()), *const vp = const_cast<void *>(out[1].const_data_ptr());
+    void *const kp = written(out[0]), *const vp = written(out[1]);
     check(without_gil([&] { return seq_cache_read(&c.c, kp, vp, ks, vs, L, (im2win_dtype_t)dt, len, place.stream); }),
           "seq_cache_read");
     PyObject *const pair = PyTuple_New(2);
@@ -352,7 +357,7 @@ PyObject *paged_workspace_bytes(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     expect(n, 6);
-    const Cache c = cache(args[1], args[2], args[3], args[4], args[5]);
+    const Cache c = cache(args[1], args[2], args[3], args[4], args[5], false);
     const at::Tensor &q = tensor(args[0], "q");
     if (q.dim() != 3)
         refuse(PyExc_ValueError, "q must be [B][H][D], as the table and the pages have it");
@@ -367,7 +372,7 @@ PyObject *paged_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     expect(n, 12);
-    const Cache c = cache(args[1], args[2], args[3], args[8], args[9]);
+    const Cache c = cache(args[1], args[2], args[3], args[8], args[9], false);
     const at::Tensor &q = tensor(args[0], "q");
     if (q.dim() != 3 || q.size(0) != c.c.B || q.size(2) != c.c.D)
         refuse(PyExc_ValueError, "q must be [B][H][D], as the table and the pages have it");
@@ -412,10 +417,10 @@ PyObject *paged_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
     }
     a.q_stride[0] = q.stride(0), a.q_stride[1] = q.stride(1);
     a.out_stride[0] = out.stride(0), a.out_stride[1] = out.stride(1);
+    void *const op = written(out);
+    float *const lp = (float *)written(lse);
+    void *const wp = ws.defined() ? written(ws) : nullptr;
     const void *const qp = q.const_data_ptr();
-    void *const op = const_cast<void *>(out.const_data_ptr());
-    float *const lp = (float *)const_cast<void *>(lse.const_data_ptr());
-    void *const wp = ws.defined() ? const_cast<void *>(ws.const_data_ptr()) : nullptr;
     const int64_t size = ws.defined() ? (int64_t)ws.nbytes() : 0;
     check(without_gil([&] { return seq_paged_attention_forward(&c.c, &a, qp, op, lp, wp, size, place.stream); }),
           "seq_paged_attention_forward");
