@@ -1,5 +1,7 @@
-"""Builds libim2win.so (the C-ABI library and its gfx950 kernels) and _seq_cache.so
-(the Python binding of the cache's calls) in-tree.
+"""Builds libim2win.so (the C-ABI library and its gfx950 kernels) and, where torch
+is installed, _seq_cache.so (the Python binding of the cache's calls) in-tree.
+
+    python -m paper_2608_20725_amd.build [--library]     # --library: without the binding
 
 Every HIP source is compiled for gfx950 only, with packed fp32 VALU
 instructions disabled (``-packed-fp32-ops``): the fp32 path uses plain
@@ -7,9 +9,13 @@ v_fma_f32 / v_fmac_f32.
 """
 from __future__ import annotations
 
+import importlib.util
 import os
+import shutil
 import subprocess
 import sys
+import sysconfig
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -40,11 +46,14 @@ def _run(cmd):
     return p.returncode, noise
 
 
-def _binding_commands(obj, out):
-    """Compile and link commands of the binding."""
-    import importlib.util
-    import sysconfig
-    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+def _torch_folder():
+    """torch's package folder, or None."""
+    spec = importlib.util.find_spec("torch")
+    return list(spec.submodule_search_locations)[0] if spec and spec.submodule_search_locations else None
+
+
+def _binding_commands(torch, obj, libdir, out):
+    """Compile and link commands of the binding, against torch's package folder and the library in ``libdir``."""
     cxx = os.environ.get("CXX", "g++")
     rocm = os.path.dirname(os.path.dirname(os.path.realpath(HIPCC)))
     headers = [sysconfig.get_paths()["include"], os.path.join(rocm, "include"), os.path.join(torch, "include"),
@@ -55,56 +64,66 @@ def _binding_commands(obj, out):
     for h in headers:
         compile_cmd += ["-isystem", h]
     compile_cmd += ["-c", os.path.join(CSRC, BINDING_SOURCE), "-o", obj]
-    link_cmd = [cxx, "-shared", obj, "-L", HERE, "-l:libim2win.so", "-Wl,-rpath,$ORIGIN", "-L", os.path.join(torch, "lib"),
+    link_cmd = [cxx, "-shared", obj, "-L", libdir, "-l:libim2win.so", "-Wl,-rpath,$ORIGIN", "-L", os.path.join(torch, "lib"),
                 "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip", "-o", out]
     return compile_cmd, link_cmd
 
 
-def build(verbose: bool = False) -> str:
-    """Compiles every source to an object (in parallel), then links them."""
-    from concurrent.futures import ThreadPoolExecutor
-    objdir = os.path.join(ROOT, "_build", "obj")
-    os.makedirs(objdir, exist_ok=True)
-    compile_flags = [f for f in FLAGS if f != "-shared"]
-    jobs = []
-    for s in SOURCES:
-        obj = os.path.join(objdir, os.path.splitext(s)[0] + ".o")
-        jobs.append((obj, [HIPCC] + compile_flags + ["-c", os.path.join(CSRC, s), "-o", obj]))
-    binding_obj = os.path.join(objdir, os.path.splitext(BINDING_SOURCE)[0] + ".o")
-    binding_tmp = BINDING + ".tmp%d" % os.getpid()
-    binding_compile, binding_link = _binding_commands(binding_obj, binding_tmp)
-    objects = [j[0] for j in jobs]
-    jobs.append((binding_obj, binding_compile))
-    workers = max(1, min(len(jobs), os.cpu_count() or 1, 16))
-    with ThreadPoolExecutor(workers) as ex:
-        results = list(ex.map(lambda j: _run(j[1]), jobs))
-    failed = False
-    for (obj, cmd), (rc, noise) in zip(jobs, results):
-        if verbose:
-            print(" ".join(cmd), flush=True)
-        if noise and (verbose or rc != 0):
-            sys.stderr.write("\n".join(noise) + "\n")
-        failed |= rc != 0
-    if failed:
-        raise RuntimeError("hipcc failed building libim2win.so")
-    tmp = LIB + ".tmp%d" % os.getpid()
-    cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC"] + objects + ["-o", tmp]
+def _result(cmd, result, verbose, what):
+    """Prints a command and what it said; a failed one raises."""
+    rc, noise = result
     if verbose:
         print(" ".join(cmd), flush=True)
-    rc, noise = _run(cmd)
-    if rc != 0:
+    if noise and (verbose or rc != 0):
         sys.stderr.write("\n".join(noise) + "\n")
-        raise RuntimeError("linking libim2win.so failed")
-    os.replace(tmp, LIB)
-    if verbose:
-        print(" ".join(binding_link), flush=True)
-    rc, noise = _run(binding_link)
     if rc != 0:
-        sys.stderr.write("\n".join(noise) + "\n")
-        raise RuntimeError("linking _seq_cache.so failed")
-    os.replace(binding_tmp, BINDING)
+        raise RuntimeError(what)
+
+
+def build(verbose: bool = False, binding: bool = True) -> str:
+    """Compiles every source to an object (in parallel), then links them.
+
+    ``binding`` False, or no torch: the library alone, without anything of torch.
+    A binding of another library is not left beside it: both are replaced when
+    both are linked, and where only the library is built an old binding goes."""
+    from concurrent.futures import ThreadPoolExecutor
+    torch = _torch_folder() if binding else None
+    if binding and torch is None:
+        print("torch is not installed: libim2win.so is built without _seq_cache.so", flush=True)
+    objdir = os.path.join(ROOT, "_build", "obj")
+    os.makedirs(objdir, exist_ok=True)
+    link = tempfile.mkdtemp(prefix="link", dir=os.path.join(ROOT, "_build"))
+    try:
+        lib, module = os.path.join(link, os.path.basename(LIB)), os.path.join(link, os.path.basename(BINDING))
+        compile_flags = [f for f in FLAGS if f != "-shared"]
+        objects = [os.path.join(objdir, os.path.splitext(s)[0] + ".o") for s in SOURCES]
+        jobs = [[HIPCC] + compile_flags + ["-c", os.path.join(CSRC, s), "-o", obj] for s, obj in zip(SOURCES, objects)]
+        what = ["hipcc failed building libim2win.so"] * len(jobs)
+        if torch:
+            binding_compile, binding_link = _binding_commands(
+                torch, os.path.join(objdir, os.path.splitext(BINDING_SOURCE)[0] + ".o"), link, module)
+            jobs.append(binding_compile)
+            what.append("compiling _seq_cache.so, the binding to torch, failed; build(binding=False) (--library) builds "
+                        "libim2win.so alone")
+        workers = max(1, min(len(jobs), os.cpu_count() or 1, 16))
+        with ThreadPoolExecutor(workers) as ex:
+            results = list(ex.map(_run, jobs))
+        for cmd, result, text in zip(jobs, results, what):
+            _result(cmd, result, verbose, text)
+        cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC"] + objects + ["-o", lib]
+        _result(cmd, _run(cmd), verbose, "linking libim2win.so failed")
+        if torch:
+            _result(binding_link, _run(binding_link), verbose, "linking _seq_cache.so, the binding to torch, failed; "
+                    "build(binding=False) (--library) builds libim2win.so alone")
+        elif os.path.exists(BINDING):
+            os.remove(BINDING)
+        os.replace(lib, LIB)
+        if torch:
+            os.replace(module, BINDING)
+    finally:
+        shutil.rmtree(link, ignore_errors=True)
     return LIB
 
 
 if __name__ == "__main__":
-    print(build(verbose=True))
+    print(build(verbose=True, binding="--library" not in sys.argv[1:]))
