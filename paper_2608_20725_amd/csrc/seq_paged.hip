@@ -899,13 +899,14 @@ bool pairs(const Pool &c, int ct, int64_t H, int dt)
     return (c.D == 64 ? dt != IM2WIN_F32 : c.D == 32 && ct == dt) && c.Hkv % 2 == 0 && H / c.Hkv <= 8;
 }
 
-int32_t spread_of(const Pool &c)
+// Sets a.spread (see paged_attn) and gives the grid.  Parts are rounded up to the 8
+// XCDs where that leaves less than 2^32 lanes; B*H < 2^24 alone does.
+uint32_t spread_grid(const Pool &c, PagedArgs &a)
 {
-    return c.Hkv > 1 && ((c.k_head | c.v_head) % 128 != 0 || c.k_head < 256 || c.v_head < 256) ? 8 : 1;
-}
-uint32_t grid_of(const Pool &c, const PagedArgs &a)
-{
-    return (uint32_t)((a.parts + a.spread - 1) / a.spread * a.spread * c.Hkv) * a.row_tiles;
+    const int64_t heads = (int64_t)c.Hkv * a.row_tiles, even = (a.parts + 7) / 8 * 8 * heads;
+    const bool share = c.Hkv > 1 && ((c.k_head | c.v_head) % 128 != 0 || c.k_head < 256 || c.v_head < 256);
+    a.spread = share && even < (int64_t)1 << 24 ? 8 : 1;
+    return (uint32_t)(a.spread == 8 ? even : a.parts * heads);
 }
 
 template <class E, class Code, int DP, bool SMALL>
@@ -921,8 +922,8 @@ void run_pair(Pool c, PagedArgs a, hipStream_t st)
 {
     c.Hkv /= 2, c.D *= 2, a.G *= 2;
     c.k_head *= 2, c.v_head *= 2;
-    a.spread = spread_of(c);
-    paged_attn<E, Code, DP, true, false, true><<<grid_of(c, a), 64 * kWavesP, 0, st>>>(c, a);
+    const uint32_t grid = spread_grid(c, a);
+    paged_attn<E, Code, DP, true, false, true><<<grid, 64 * kWavesP, 0, st>>>(c, a);
 }
 
 template <class E, class Code, int DP>
@@ -944,8 +945,7 @@ void run(const Plan &p, const Pool &c, PagedArgs a, hipStream_t st)
         if (p.pair && c.D == 32)
             run_pair<E, Code, 64>(c, a, st);
     if (!p.pair) {
-        a.spread = spread_of(c);
-        const uint32_t grid = grid_of(c, a);
+        const uint32_t grid = spread_grid(c, a);
         c.D <= 64 ? run_small<E, Code, 64>(p.small, grid, c, a, st) : run_small<E, Code, 128>(p.small, grid, c, a, st);
     }
     if (a.most_parts) {

@@ -106,3 +106,27 @@ def test_large_queries_of_small_keys(types, e, size):
         got, gl, _ = attend(q, c, scale=size / D)
         check(got, out, tol + 1e-30, "out %d" % k)
         check(gl, lse, tl + 1e-30, "lse %d" % k)
+
+
+@pytest.mark.parametrize("B", [1, 7])
+@pytest.mark.parametrize("ct", [F16, I8], ids=["f16", "i8"])
+def test_as_many_heads_as_are_taken(ct, B):
+    """Parts rounded up to the XCDs would pass 2^32 lanes here: 2^21 heads a sequence, the most with B*H < 2^24."""
+    H, g = 1 << 21, torch.Generator("cuda").manual_seed(B)
+    codes = lambda: torch.randint(-127, 128, (B, 1, H, 8), generator=g, device="cuda", dtype=torch.int8)
+    k, v = codes(), codes()
+    scales = {}
+    if ct == F16:
+        k, v = k.to(F16) / 64, v.to(F16) / 64
+    else:
+        scales = {"k_scale": torch.full((B, 1, H), 2.0 ** -6, device="cuda"), "v_scale": torch.full((B, 1, H), 2.0 ** -6, device="cuda")}
+    q = torch.randint(-8, 9, (B, H, 8), generator=g, device="cuda").to(F16)
+    table = torch.arange(B, dtype=torch.int32, device="cuda")[:, None]
+    n = torch.ones(B, dtype=torch.int32, device="cuda")
+    out, lse = pkg.seq_paged_attention_forward(q, k, v, table, n, scale=0.25, **scales)
+    values = lambda t: (t.float() * (2.0 ** -6 if ct == I8 else 1.0))[:, 0]
+    # one key: its value, and its score (multiples of 2^-8 below 2^9, exact in fp32) times log2(e), plus and less 14 of
+    # the weights' 2^14, and times ln(2): four roundings of values up to |1.45 score| + 14
+    assert torch.equal(out, values(v).to(F16))
+    score = (q.float() * values(k)).sum(-1) * 0.25
+    assert ((lse - score).abs() <= 2.0 ** -21 * (2 * score.abs() + 14)).all()
