@@ -23,7 +23,8 @@
 // queries over them are brought to fp16's range by a power of two a row: what
 // falls below 2^-39 of the row's largest channel is lost, less than fp32 sums
 // lose.  fp32 ones, and their probabilities, are two fp16 numbers each, 22 bits,
-// at a quarter of the fp32 instructions' time.
+// at a quarter of the fp32 instructions' time; probabilities over 16-bit pages are
+// two numbers of the pages' type.
 #include "seq_attn.hpp"
 #include "seq_cache.hpp"
 
@@ -99,7 +100,15 @@ struct Math {
     static constexpr bool kWide = __is_same(E, EltF32) && !kCodes;  // fp32 instructions
     static constexpr bool kHalf = kCodes || __is_same(E, EltF16);   // fp16 operands
     static constexpr bool kRange = kCodes && !__is_same(E, EltF16); // queries brought to fp16's range
-    static constexpr int kTerms = kCodes && __is_same(E, EltF32) ? 2 : 1;  // operands a number
+    static constexpr int kTerms = kCodes && __is_same(E, EltF32) ? 2 : 1;  // operands a query's number
+    // Operands a weight.  In one, 16 bits wide, a weight is off by as much as a 16-bit
+    // result; a second, for what the first leaves, takes no time that is seen, as the
+    // matrix cores wait for memory: 32 caches of up to 8192, 8 heads, one and two: bf16 of
+    // 128 channels 131 and 131 us, of 64 65 and 65, of 96 103 and 104; 64 heads over one 44
+    // and 45.  Over 8-bit pages, where a value's code is off by 2^-8 of its head's largest,
+    // 16-bit queries stay with one, 2^-11: 64 channels 44 and 46 us, 48 caches of up to
+    // 16384 214 and 217.
+    static constexpr int kWeightTerms = kWide ? 1 : kCodes ? kTerms : 2;
     typedef typename Pick<kWide, F32Wide, typename Pick<kHalf, F16Op, BF16Op>::T>::T Op;
     static constexpr int ES = kCodes ? 1 : kWide ? 4 : 2;
     static constexpr int NK = DP * ES / 64;  // pieces of 16 bytes of a key that a lane takes: bytes 64*c + 16*group
@@ -122,7 +131,7 @@ struct Math {
     };
     struct Weights {
         float p[N];
-        u32x4_t packed[kTerms][N > 8 ? N / 8 : 1];
+        u32x4_t packed[kWeightTerms][N > 8 ? N / 8 : 1];
     };
 
     __device__ static inline void set(Query &q, int at, float x)
@@ -178,12 +187,12 @@ struct Math {
             for (int i = 0; i < N / 2; ++i) {
                 float a = w.p[2 * i], b = w.p[2 * i + 1];
 #pragma unroll
-                for (int t = 0; t < kTerms; ++t) {
+                for (int t = 0; t < kWeightTerms; ++t) {
                     const uint32_t x = Op::bits(a), y = Op::bits(b);
                     w.packed[t][i / 4][i % 4] = x | y << 16;
-                    if constexpr (kTerms == 2) {
-                        a -= (float)__builtin_bit_cast(_Float16, (uint16_t)x);
-                        b -= (float)__builtin_bit_cast(_Float16, (uint16_t)y);
+                    if constexpr (kWeightTerms == 2) {
+                        a -= (float)__builtin_bit_cast(typename Op::elem, (uint16_t)x);
+                        b -= (float)__builtin_bit_cast(typename Op::elem, (uint16_t)y);
                     }
                 }
             }
@@ -216,7 +225,7 @@ struct Math {
             for (int i = 0; i < N / 8; ++i) {
                 const auto x = __builtin_bit_cast(typename Op::v8, channel<J>(v + 8 * i));
 #pragma unroll
-                for (int t = 0; t < kTerms; ++t)
+                for (int t = 0; t < kWeightTerms; ++t)
                     o[J] = Op::mfma16(x, __builtin_bit_cast(typename Op::v8, w.packed[t][i]), o[J]);
             }
         }
