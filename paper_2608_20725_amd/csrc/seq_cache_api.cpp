@@ -210,11 +210,13 @@ int copy(const seq_cache_t *c, const void *k, const void *v, const int64_t *k_st
     if (write) {
         if (!self_disjoint(o.k) || !self_disjoint(o.v) || clash(o.k, o.v))
             return IM2WIN_EOVERLAP;
-        if (coded(c->dt) && (!self_disjoint(o.ks) || !self_disjoint(o.vs) || clash(o.ks, o.vs)))
+        // scales may lie beside the codes, in the same pages
+        if (coded(c->dt) && (!self_disjoint(o.ks) || !self_disjoint(o.vs) || clash(o.ks, o.vs) || clash(o.k, o.ks) ||
+                             clash(o.k, o.vs) || clash(o.v, o.ks) || clash(o.v, o.vs)))
             return IM2WIN_EOVERLAP;
         const int outs[4] = {0, 1, 3, 4};
         for (const int i : outs) {
-            if (meet(own[i], own[2]) || (i < 3 && (meet(own[i], own[3]) || meet(own[i], own[4]))))
+            if (meet(own[i], own[2]))
                 return IM2WIN_EOVERLAP;
             for (const Buf &d : dense)
                 if (meet(own[i], d))

@@ -125,14 +125,14 @@ bool self_disjoint(const Operand &o)
     return true;
 }
 
-// Bytes modulo `period` that an operand takes from its first element on: the
-// axes that step by whole periods add none.
+// Bytes modulo `period` bytes that an operand takes from its first element on:
+// the axes that step by whole periods add none.
 int64_t width(const Operand &o, int64_t period)
 {
     const int64_t n[3] = {o.B, o.L, o.heads};
     int64_t w = o.D;
     for (int k = 0; k < 3; ++k)
-        if (n[k] > 1 && o.stride[k] % period)
+        if (n[k] > 1 && o.stride[k] * o.elt % period)
             w += (n[k] - 1) * o.stride[k];
     return w * o.elt;
 }
@@ -146,11 +146,11 @@ bool side_by_side(const Operand &a, const Operand &b)
     const int64_t n[6] = {a.B, a.L, a.heads, b.B, b.L, b.heads};
     const int64_t diff = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p);
     for (int k = 0; k < 6; ++k) {
-        const int64_t period = k < 3 ? a.stride[k] : b.stride[k - 3], bytes = period * a.elt;
+        const int64_t period = k < 3 ? a.stride[k] * a.elt : b.stride[k - 3] * b.elt;
         if (n[k] <= 1 || period <= 0)
             continue;
-        const int64_t off = ((diff % bytes) + bytes) % bytes;  // where b starts, a's start being 0
-        if (off >= width(a, period) && off + width(b, period) <= bytes)
+        const int64_t off = ((diff % period) + period) % period;  // where b starts, a's start being 0
+        if (off >= width(a, period) && off + width(b, period) <= period)
             return true;
     }
     return false;
