@@ -203,7 +203,8 @@ int seq_rotary_frequencies(double *freq, int64_t rot, double base, double factor
  *           between pages, tokens and heads (channels dense; not read where
  *           there is only one of them)
  *   table   [B][max_pages], rows `table_stride` entries apart (>= max_pages)
- *   k_scale, v_scale  [pages][page][Hkv] fp32, any strides; 8 bits only
+ *   k_scale, v_scale  [pages][page][Hkv] fp32, any strides, beside the codes too;
+ *           8 bits only
  * dt is an im2win_dtype_t or one of 8 bits, whose numbers are codes times the
  * scale s of their token and head, with top the largest magnitude among the
  * head's D channels:
@@ -260,11 +261,18 @@ int seq_cache_read(const seq_cache_t *c, void *k, void *v, const int64_t *k_stri
  *           `*_stride` are the elements between sequences and heads
  *   lse     [B][H] fp32
  *   ws      seq_paged_attention_workspace_bytes(c, H, dt) bytes, 16-byte aligned
- * H a multiple of Hkv, B*H < 2^24.  Numerics as in seq_attention_forward;
- * 8-bit codes are multiplied in fp16, which holds them exactly (fp32 queries
- * and weights as two fp16 terms).  The keys of all sequences are shared evenly
- * between workgroups, so a sequence's sums are split, and rounded, by the lengths
- * of the others too; the same call gives the same bits.
+ * H a multiple of Hkv, B*H < 2^24.  Scores, sums and statistics are fp32.
+ * Weights over 16-bit pages are two terms of the pages' type; over 32- and 16-bit
+ * pages sums of exp(s - largest) times values are divided last, and are infinite
+ * past fp32's range.  8-bit codes are multiplied in fp16, which holds them exactly;
+ * weights times scales are one fp16 number (two with fp32 queries) over a power of
+ * two that follows the largest, so that what falls below 2^-39 of it is lost and
+ * every mean of values that the type holds is reached.  bf16 and fp32 queries
+ * over 8-bit pages are brought to fp16's range by a power of two a row (largest
+ * channel 2^-100 or more; below, bits are lost).
+ * The keys of all sequences are shared evenly between workgroups, so a sequence's
+ * sums are split, and rounded, by the lengths of the others too; the same call
+ * gives the same bits.
  */
 typedef struct {
     int dt; /* im2win_dtype_t */

@@ -866,19 +866,26 @@ __global__ __launch_bounds__(256) void paged_join(Pool c, PagedArgs a, int group
 // 256, 384, 512 and 768 tokens (steps of 128), split and whole, in a graph: 16
 // heads of 64 over 4, fp16 10.2, 10.3, 10.3, 10.4 and 6.3, 7.8, 9.2, 11.8 us; 32 of
 // 128 over 8, bf16 11.1, 11.2, 11.2, 11.2 and 7.5, 9.3, 10.9, 14.2; four of 8 heads of
-// 80, fp32 13.9, 14.1, 14.1, 14.2 and 12.0, 15.8, 19.7, 28.6.  So too where there are
-// enough sequences to even out by themselves, or so many that each wave's scan
-// would cost more.
+// 80, fp32 13.9, 14.1, 14.1, 14.2 and 12.0, 15.8, 19.7, 28.6.  So too from 513
+// sequences or 16384 pairs of a sequence and a tile of heads on: each wave's scan over
+// the lengths grows with them, and lengths that differ little even out.  One long
+// sequence among short ones does not, and is slower whole.  Split and whole, in a
+// graph, bf16: 1024 sequences of 1024 tokens, 8 heads over 1 159 and 100 us, 32 over 8
+// 885 and 756; of 512 to 2048 202 and 136, 1030 and 958; of 256, one of 16384 90 and
+// 253, 435 and 482; 512 sequences of 64 heads of 64 channels 1506 and 1464, 1885 and
+// 1846, 713 and 681.  Below, 512 sequences: 70 and 44, 419 and 380; 86 and 68, 506 and
+// 490; 59 and 242, 195 and 389.
 struct Plan {
     int32_t row_waves, row_tiles, step;
     bool small, pair;
     int64_t most_parts, parts;  // parts: that the lengths can make at most
 };
 // Workgroups that share the keys, two rounds of the two that fit a CU.  Measured
-// with 512, 768, 1024, 1536 and 2048 (bf16, 8 heads of 128, H = 32): 32 caches of
-// 2048 to 8192 tokens 148, 131, 134, 133, 131 us, 32 of 8192 tokens 193, 220, 198,
-// 200, 203, four of them 26, 31, 28, 27, 33; int8, 32 of 8192: 129, 132, 130, 142,
-// 135.
+// with 512, 768, 1024, 1536 and 2048 (bf16, 32 heads over 8, of 128): 32 caches of
+// 2048 to 8192 tokens 140, 153, 135, 134, 139 us, 32 of 8192 tokens 199, 227, 202,
+// 206, 206, 4 of 2048 to 8192 22, 25, 23, 27, 27, 16 of 1024 to 4096 39, 38, 36, 42,
+// 41; 48 of 4096 to 16384, 64 heads over 8, 445, 441, 386, 380, 385; heads of 64, 32 of
+// 2048 to 8192, 69, 77, 75, 78, 76.
 constexpr int64_t kTarget = 1024;
 // pair: heads may be taken by two (see paged_attn).
 Plan plan_of(const Pool &c, int ct, int64_t B, int64_t H, int dt, bool pair)
@@ -894,7 +901,9 @@ Plan plan_of(const Pool &c, int ct, int64_t B, int64_t H, int dt, bool pair)
     const int32_t least = tile_keys(bytes, true) * waves;
     p.small = B * heads <= kTarget / 2 && (most + least - 1) / least * B * heads <= kTarget / 2;
     p.step = tile_keys(bytes, p.small) * waves;
-    if (p.small && pair)  // enough workgroups first
+    // Enough workgroups first: 2000 tokens, 16 heads of 64 over 4, fp16, 9.9 us alone
+    // and 10.7 in pairs; 4096, 32 over 8, bf16, 9.8 and 10.5; 2000, 32 over 32, 11.0 and 10.8.
+    if (p.small && pair)
         return plan_of(c, ct, B, H, dt, false);
     const int64_t steps = (most + p.step - 1) / p.step;
     const int64_t few = ct == IM2WIN_F32 ? 2 : 4;
@@ -959,6 +968,8 @@ void run(const Plan &p, const Pool &c, PagedArgs a, hipStream_t st)
     }
     if (a.most_parts) {
         const int64_t rows = (int64_t)a.B * a.H;
+        // one row a workgroup and eight: 256 rows of 128 channels 22.8 and 23.6 us, 512 of
+        // 64 23.7 and 24.7, 2048 of 128 140 and 140, 8192 512 and 510
         const int groups = rows <= 2048 ? 8 : 1;
         typedef Math<E, Code, 64, false> M;
         paged_join<E, M::kHalf && !M::kCodes, M::kCodes><<<(uint32_t)((rows * groups + 7) / 8), 256, 0, st>>>(c, a, groups);
